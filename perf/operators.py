@@ -317,7 +317,7 @@ def _run_own(st):
         qb.qzo_qk_norm_rope(st["qkv"], st["q_heads"], st["kv_heads"], st["out"], q_gain=st["q_gain"], k_gain=st["k_gain"], eps=NORM_EPS,
                             theta=st["theta"], positions=st["positions"], cache=cache, slots=st["slots"])
         return [st["out"]] if c is None else [st["out"], c["k"], c["v"]]
-    qb.qzo_paged_attention(st["q"], cache, st["tables"], st["lengths"], st["out"], st["scale"], starts=st["starts"], max_new=st["new"])
+    qb.qzo_paged_attention(st["q"], cache, st["tables"], st["lengths"], st["out"], st["scale"], starts=st["starts"])
     return [st["out"]]
 
 

@@ -331,6 +331,95 @@ qzo_status qzo_apply_update_channel(void* c_dev, uint32_t n_rows, uint32_t row_b
 qzo_status qzo_apply_update(void* s_dev, uint32_t n_rows, uint32_t G, uint32_t row_base,
                             uint64_t seed, float eta, float d_clipped, uint32_t scale_fp16, void* stream);
 
+/*
+ * Answering with a trained model: a paged cache of keys and values.  The cache is a pool of blocks of `block` tokens each;
+ * a sequence holds the blocks that its row of the block tables names, position p of it lies in block table[p / block],
+ * at slot table[p / block] * block + p % block of the pool.  k_dev and v_dev: [n_blocks, kv_heads, block, head_dim], in
+ * bf16 (type 0) or e4m3 (type 1: one sign, four exponent and three mantissa bits, largest 448, as the OCP standard has it);
+ * a stored e4m3 value times its key head's entry of the fp32 [kv_heads] scales (nullable: 1; positive) is the value.
+ * block is 16, 32, 64, 128 or 256, head_dim 64 or 128, n_blocks * block below 2^31; the pools may exceed 2^32 bytes.
+ */
+typedef struct {
+  uint32_t struct_size;            /* sizeof(qzo_cache) */
+  uint32_t type;                   /* 0: bf16, 1: e4m3 */
+  uint32_t n_blocks, block, kv_heads, head_dim;
+  void *k_dev, *v_dev;
+  const float *k_scale_dev, *v_scale_dev;     /* e4m3 only; null with bf16 */
+} qzo_cache;
+
+/* Device memory, 16 bytes: what qzo_cache_plan reads (n_free) and leaves. */
+typedef struct {
+  int32_t n_free;                  /* blocks on the free list */
+  int32_t n_tokens;                /* tokens that the call's sequences add */
+  int32_t status;                  /* QZO_OK, or why nothing was planned (below) */
+  int32_t n_taken;                 /* blocks taken off the free list */
+} qzo_cache_state;
+
+/*
+ * Block tables and slots of the tokens that n_seq sequences add, from lengths that only the device knows.  Sequence i has
+ * cached_dev[i] tokens in the cache and adds added_dev[i]; a negative added_dev[i] ends it.  int32 throughout.
+ *   free_dev [n_blocks], a stack of free block ids of which before_dev->n_free are valid.  First the blocks of the sequences
+ *     that end are put on it (sequence by sequence, in table order), then the others take the blocks that they need for
+ *     cached + added tokens off its top, sequence by sequence, and enter them in their rows of tables_dev
+ *     [n_seq, max_blocks] behind those that they hold.  Nothing else of the tables is written.
+ *   lengths_dev [n_seq]: cached + added, 0 where a sequence ends (may be cached_dev).
+ *   starts_dev [n_seq + 1]: tokens added by the sequences before; the new tokens are listed sequence by sequence.
+ *   slots_dev, positions_dev [max_tokens]: slot and position of every new token; -1 and 0 behind the last one.
+ *   after_dev (may be before_dev): the new state.
+ * A plan is made as a whole or not at all: where status is not QZO_OK, lengths are cached_dev's, starts 0, slots -1,
+ * positions 0, n_tokens and n_taken 0, the free list and the tables as they were.  QZO_ERR_WORKSPACE: not enough free
+ * blocks; QZO_ERR_SHAPE: a row of the tables is too short for its sequence, or max_tokens too small; QZO_ERR_ARG: a negative
+ * length, an n_free outside 0 .. n_blocks, more blocks given back than the pool has.
+ * Block ids in the tables and on the list are the caller's (0 .. n_blocks - 1); this call copies them without a look, the
+ * calls that use them treat others as absent.  Otherwise the buffers must not overlap.  n_seq 1 .. 8192, max_blocks and
+ * max_tokens at least 1, n_seq * max_blocks below 2^31; buffers 16-byte aligned.
+ */
+qzo_status qzo_cache_plan(const int32_t* cached_dev, const int32_t* added_dev, uint32_t n_seq, uint32_t block,
+                          uint32_t n_blocks, uint32_t max_blocks, uint32_t max_tokens, int32_t* tables_dev, int32_t* free_dev,
+                          const qzo_cache_state* before_dev, int32_t* lengths_dev, int32_t* starts_dev, int32_t* slots_dev,
+                          int32_t* positions_dev, qzo_cache_state* after_dev, void* stream);
+
+/*
+ * Heads of q and k normed and rotated, and with a cache k and v written to their slots, in one pass.  Row t of qkv_dev
+ * (bf16, rows ld_qkv elements apart) holds q_heads heads of q, kv_heads of k, kv_heads of v, of head_dim features each:
+ *   y = R(p) (x / sqrt(mean(x^2) + eps) * gain)
+ * RMSNorm over the head with q_gain_dev / k_gain_dev (bf16 [head_dim]; null: that one is not normed), then features i and
+ * i + head_dim/2 turned by the angle p * rope_theta^(-2i/head_dim) (rope_theta 0: not rotated), fp32 throughout (the angle in
+ * double) with one rounding at the end.  p: positions_dev[t], or t % seq where positions_dev is null.
+ *   cache null: out_dev (bf16, rows ld_out elements apart) receives the heads of q, then those of k; it may be qkv_dev with
+ *     ld_out = ld_qkv (in place; v is not touched).  slots_dev must be null.
+ *   cache given: out_dev receives the heads of q; k and v of the row go to slot slots_dev[t] of the cache (in e4m3: divided by
+ *     their scale, cut off at +-448, rounded to nearest even).  A row whose slot is negative or beyond the pool is skipped, its
+ *     out row included.  The slots of a call must differ from one another.
+ * head_dim 64 or 128 (of the cache, too); ld_qkv and ld_out multiples of 8, at least the row's heads; eps positive or 0.
+ */
+qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tokens, uint32_t q_heads, uint32_t kv_heads,
+                            uint32_t head_dim, const void* q_gain_dev, const void* k_gain_dev, float eps, float rope_theta,
+                            const int32_t* positions_dev, uint32_t seq, const qzo_cache* cache, const int32_t* slots_dev,
+                            void* out_dev, uint64_t ld_out, void* stream);
+
+/*
+ * Attention of the newest tokens of n_seq sequences over the cache, which holds their own keys and values already.
+ * q_dev bf16, n_rows rows ld_q elements apart, q_heads heads of the cache's head_dim; query heads h * q_heads / kv_heads ..
+ * share key head h.  lengths_dev [n_seq]: tokens in the cache, the new ones included.  starts_dev [n_seq + 1]: rows
+ * starts[i] .. starts[i+1] - 1 are the newest tokens of sequence i, in order (starts[0] = 0, ascending); null: row i is
+ * the one new token of sequence i.  A row sees the positions of its sequence up to its own:
+ *   out[row, h] = sum_k p_k v_k / sum_k p_k,  p_k = exp(scale * q . k - max),  out_dev bf16, rows ld_out elements apart.
+ * One pass over the cache with the running maximum and sum (fp32; p rounded to bf16 as it meets v), the sequences cut into
+ * pieces that fill the chip and joined in order: the same call gives the same bits.  A row that sees nothing (length 0)
+ * is set to zero; rows behind the last sequence's and not named by starts stay as they are.  Keys that a row does not see
+ * reach its output in no way, NaN and infinities among them; nor do positions whose block id lies outside the pool (they
+ * count as unseen), or positions beyond max_blocks * block.  A score of -infinity counts as unseen.
+ * scratch_dev: qzo_paged_attention_scratch_bytes bytes, 256-byte aligned, contents undefined before and after; calls that may overlap
+ * (another stream, another captured graph) need scratch of their own.  n_seq 1 .. 8192, q_heads a multiple of kv_heads,
+ * scale finite, ld_q and ld_out multiples of 8 and at least q_heads * head_dim.
+ */
+qzo_status qzo_paged_attention_scratch_bytes(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim, uint64_t* out);
+qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows, uint32_t n_seq, uint32_t q_heads,
+                               const qzo_cache* cache, const int32_t* tables_dev, uint32_t max_blocks,
+                               const int32_t* lengths_dev, const int32_t* starts_dev, float scale, void* out_dev,
+                               uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream);
+
 /* RTN quantizer of Eq. 3 with the k=4 absmax scale: w_dev fp32 [N,K] ->
  * q_dev packed int4 [N,K/2], s_dev bf16 [N,K/group].  Model construction, not
  * part of the timed step. */

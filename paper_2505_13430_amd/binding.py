@@ -29,6 +29,7 @@ EXPORTS = [
     "qzo_int4_expand", "qzo_int4_scratch_bytes", "qzo_int4_gemm_expanded", "qzo_model_set_int4_path",
     "qzo_nf4_expand", "qzo_nf4_scratch_bytes", "qzo_nf4_gemm",
     "qzo_codebook_scratch_bytes", "qzo_codebook_gemm", "qzo_apply_update_channel",
+    "qzo_cache_plan", "qzo_qk_norm_rope", "qzo_paged_attention_scratch_bytes", "qzo_paged_attention",
     "qzo_debug_philox", "qzo_debug_normal_pairs", "qzo_debug_normals", "qzo_debug_dequant", "qzo_debug_dequant_zp",
     "qzo_debug_forward", "qzo_debug_bf16_gemm", "qzo_debug_reduce_norm", "qzo_debug_fused_linear", "qzo_debug_attention_slices",
     "qzo_debug_attention_linear",
@@ -56,6 +57,12 @@ class qzo_buf(C.Structure):
     _fields_ = [("ptr_dev", C.c_void_p), ("bytes", C.c_uint64)]
 
 
+class qzo_cache(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_uint32), ("n_blocks", C.c_uint32), ("block", C.c_uint32),
+                ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p),
+                ("k_scale_dev", C.c_void_p), ("v_scale_dev", C.c_void_p)]
+
+
 def lib():
     global _lib
     if _lib is None:
@@ -66,6 +73,11 @@ def lib():
         _lib.qzo_last_error.restype = C.c_char_p
         for name in EXPORTS[:-1]:
             getattr(_lib, name).restype = C.c_int
+        # called once or more per layer and token: arguments converted by declared types
+        u32, u64, p, f = C.c_uint32, C.c_uint64, C.c_void_p, C.c_float
+        _lib.qzo_cache_plan.argtypes = [p, p, u32, u32, u32, u32, u32] + [p] * 9
+        _lib.qzo_qk_norm_rope.argtypes = [p, u64, u32, u32, u32, u32, p, p, f, f, p, u32, p, p, p, u64, p]
+        _lib.qzo_paged_attention.argtypes = [p, u64, u32, u32, u32, p, p, u32, p, p, f, p, u64, p, u64, p]
     return _lib
 
 
@@ -460,3 +472,106 @@ def qzo_apply_update_channel(c, row_base, seed, eta, d_clipped, stream=None):
     _check(lib().qzo_apply_update_channel(_ptr(c), C.c_uint32(c.numel()), C.c_uint32(row_base),
                                           C.c_uint64(seed), C.c_float(eta), C.c_float(d_clipped),
                                           _stream(stream)))
+
+
+def _rows(t):
+    """Address and row stride of a matrix whose rows are contiguous."""
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "rows of a matrix must be contiguous"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _typed(t, dtype):
+    """Address of a contiguous tensor of that type; None: null."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype, f"a contiguous CUDA tensor of {dtype} is needed"
+    return t.data_ptr()
+
+
+def _here(stream, *tensors):
+    """The call's stream; its tensors live on the device that is current."""
+    at = torch.cuda.current_device()
+    assert all(t is None or t.get_device() == at for t in tensors), "tensors must be on the current device"
+    return torch.cuda.current_stream() if stream is None else stream
+
+
+def make_cache(k, v, k_scale=None, v_scale=None) -> qzo_cache:
+    """k, v: bf16 or float8_e4m3fn [n_blocks, kv_heads, block, head_dim]; e4m3: fp32 scales [kv_heads].  Holds its tensors."""
+    assert k.dtype in (torch.bfloat16, torch.float8_e4m3fn) and k.shape == v.shape and k.dim() == 4
+    assert all(s is None or s.numel() == k.shape[1] for s in (k_scale, v_scale))
+    c = qzo_cache(C.sizeof(qzo_cache), int(k.dtype != torch.bfloat16), k.shape[0], k.shape[2], k.shape[1], k.shape[3], _typed(k, k.dtype),
+                  _typed(v, k.dtype), _typed(k_scale, torch.float32), _typed(v_scale, torch.float32))
+    c.tensors = (k, v, k_scale, v_scale)
+    return c
+
+
+def qzo_cache_plan(cached, added, block, tables, free, before, lengths, starts, slots, positions, after, stream=None):
+    """int32 tensors; tables [n_seq, max_blocks], free [n_blocks], slots and positions [max_tokens], before and after: a
+    qzo_cache_state of four int32 (free blocks, tokens, status, blocks taken)."""
+    i32, (n, most) = torch.int32, tables.shape
+    assert cached.numel() == added.numel() == lengths.numel() == n and starts.numel() == n + 1 and slots.numel() == positions.numel()
+    assert before.numel() == after.numel() == 4
+    _check(lib().qzo_cache_plan(_typed(cached, i32), _typed(added, i32), n, block, free.numel(), most, slots.numel(), _typed(tables, i32),
+                                _typed(free, i32), _typed(before, i32), _typed(lengths, i32), _typed(starts, i32), _typed(slots, i32),
+                                _typed(positions, i32), _typed(after, i32), _here(stream, cached, tables, slots).cuda_stream))
+
+
+def qzo_qk_norm_rope(qkv, q_heads, kv_heads, out, q_gain=None, k_gain=None, eps=1e-6, theta=10000.0, positions=None, seq=0, cache=None,
+                     slots=None, stream=None):
+    """qkv bf16 [tokens, (q_heads + 2 kv_heads) head_dim]; out bf16 [tokens, the heads of q (and of k without a cache)], it may be
+    a column range of qkv's own rows from the first on (in place).  Rows may be strided."""
+    x, ldx = _rows(qkv)
+    y, ldy = _rows(out)
+    T, heads = qkv.shape[0], q_heads + 2 * kv_heads
+    dh = qkv.shape[1] // heads
+    assert qkv.dtype == out.dtype == torch.bfloat16 and qkv.shape[1] == heads * dh
+    assert out.shape[0] == T and out.shape[1] >= (q_heads + (0 if cache is not None else kv_heads)) * dh
+    assert all(g is None or g.numel() == dh for g in (q_gain, k_gain)) and all(i is None or i.numel() >= T for i in (positions, slots))
+    if T == 0:
+        return                                  # an empty tensor has no address
+    _check(lib().qzo_qk_norm_rope(x, ldx, T, q_heads, kv_heads, dh, _typed(q_gain, torch.bfloat16), _typed(k_gain, torch.bfloat16), eps, theta,
+                                  _typed(positions, torch.int32), seq, None if cache is None else C.addressof(cache),
+                                  _typed(slots, torch.int32), y, ldy, _here(stream, qkv, out, q_gain, k_gain, positions, slots).cuda_stream))
+
+
+def qzo_paged_attention_scratch_bytes(n_rows, n_seq, q_heads, head_dim) -> int:
+    out = C.c_uint64(0)
+    _check(lib().qzo_paged_attention_scratch_bytes(C.c_uint32(n_rows), C.c_uint32(n_seq), C.c_uint32(q_heads), C.c_uint32(head_dim),
+                                                   C.byref(out)))
+    return out.value
+
+
+_stream_scratch = {}
+
+
+def _scratch_of_stream(device, stream, nbytes):
+    """Scratch of the calls on one stream, which do not overlap.  A captured graph keeps the address it was captured with and may
+    be replayed on any stream beside any other: it is given scratch of its own."""
+    assert not torch.cuda.is_current_stream_capturing(), "a captured call needs scratch of its own: pass scratch"
+    t = _stream_scratch.get((device, stream.cuda_stream))
+    if t is None or t.numel() < nbytes:
+        with torch.cuda.stream(stream):        # what is outgrown is used again on this stream only
+            t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+        _stream_scratch[device, stream.cuda_stream] = t
+    return t
+
+
+def qzo_paged_attention(q, cache, tables, lengths, out, scale, starts=None, scratch="auto", stream=None):
+    """q, out bf16 [rows, q_heads head_dim], rows may be strided; tables int32 [n_seq, max_blocks], lengths int32 [n_seq], starts
+    int32 [n_seq + 1] or None: a row per sequence."""
+    x, ldx = _rows(q)
+    y, ldy = _rows(out)
+    n, most = tables.shape
+    dh = cache.head_dim
+    heads = q.shape[1] // dh
+    assert q.dtype == out.dtype == torch.bfloat16 and q.shape == out.shape and heads * dh == q.shape[1]
+    assert lengths.numel() == n and (starts is None or starts.numel() == n + 1)
+    if q.shape[0] == 0:
+        return
+    st = _here(stream, q, out, tables, lengths, starts)
+    if isinstance(scratch, str):
+        need = qzo_paged_attention_scratch_bytes(q.shape[0], n, heads, dh)
+        scratch = _scratch_of_stream(q.device, st, need) if need else None
+    _check(lib().qzo_paged_attention(x, ldx, q.shape[0], n, heads, C.addressof(cache), _typed(tables, torch.int32), most,
+                                     _typed(lengths, torch.int32), _typed(starts, torch.int32), scale, y, ldy,
+                                     None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel() * scratch.element_size(), st.cuda_stream))

@@ -1601,4 +1601,127 @@ qzo_status qzo_debug_dequant_zp(const void* q_dev, const void* s_dev, const void
   return QZO_OK;
 }
 
+// ---- answering: the paged cache ----
+static qzo_status cache_check(const qzo_cache* c) {
+  if (c->struct_size != sizeof(qzo_cache)) return fail(QZO_ERR_ARG, "cache.struct_size does not match this library");
+  if (c->type > 1) return fail(QZO_ERR_UNSUPPORTED, "cache.type must be 0 (bf16) or 1 (e4m3)");
+  if (!c->k_dev || !c->v_dev) return fail(QZO_ERR_ARG, "a pool of the cache is null");
+  if (!aligned16(c->k_dev) || !aligned16(c->v_dev) || !aligned16(c->k_scale_dev) || !aligned16(c->v_scale_dev))
+    return fail(QZO_ERR_ALIGN, "a pool or a scale of the cache is not 16-byte aligned");
+  if (c->type == 0 && (c->k_scale_dev || c->v_scale_dev)) return fail(QZO_ERR_ARG, "a bf16 cache has no scales");
+  if (c->block < 16 || c->block > 256 || (c->block & (c->block - 1))) return fail(QZO_ERR_SHAPE, "cache.block must be 16, 32, 64, 128 or 256");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(QZO_ERR_SHAPE, "cache.head_dim must be 64 or 128");
+  if (!c->n_blocks || (uint64_t)c->n_blocks * c->block >= (1ull << 31)) return fail(QZO_ERR_SHAPE, "n_blocks * block must be 1 .. 2^31 - 1");
+  if (!c->kv_heads || c->kv_heads > 65535) return fail(QZO_ERR_SHAPE, "kv_heads must be 1 .. 65535");
+  return QZO_OK;
+}
+
+qzo_status qzo_cache_plan(const int32_t* cached_dev, const int32_t* added_dev, uint32_t n_seq, uint32_t block,
+                          uint32_t n_blocks, uint32_t max_blocks, uint32_t max_tokens, int32_t* tables_dev, int32_t* free_dev,
+                          const qzo_cache_state* before_dev, int32_t* lengths_dev, int32_t* starts_dev, int32_t* slots_dev,
+                          int32_t* positions_dev, qzo_cache_state* after_dev, void* stream) {
+  const void* all[] = {cached_dev, added_dev, tables_dev, free_dev, before_dev, lengths_dev, starts_dev, slots_dev, positions_dev, after_dev};
+  for (const void* p : all)
+    if (!p) return fail(QZO_ERR_ARG, "null device pointer");
+  for (const void* p : all)
+    if (!aligned16(p)) return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  if (block < 16 || block > 256 || (block & (block - 1))) return fail(QZO_ERR_SHAPE, "block must be 16, 32, 64, 128 or 256");
+  if (!n_blocks || (uint64_t)n_blocks * block >= (1ull << 31)) return fail(QZO_ERR_SHAPE, "n_blocks * block must be 1 .. 2^31 - 1");
+  if (!n_seq || n_seq > CACHE_MAX_SEQ) return fail(QZO_ERR_SHAPE, "n_seq must be 1 .. 8192");
+  if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31)) return fail(QZO_ERR_SHAPE, "n_seq * max_blocks must be 1 .. 2^31 - 1");
+  if (!max_tokens || max_tokens >= (1u << 31)) return fail(QZO_ERR_SHAPE, "max_tokens must be 1 .. 2^31 - 1");
+  CachePlanArgs a = {cached_dev, added_dev, n_seq, (uint32_t)__builtin_ctz(block), n_blocks, max_blocks, max_tokens, tables_dev, free_dev,
+                     before_dev, lengths_dev, starts_dev, slots_dev, positions_dev, after_dev};
+  QZO_HIP(launch_cache_plan(a, (hipStream_t)stream));
+  return QZO_OK;
+}
+
+qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tokens, uint32_t q_heads, uint32_t kv_heads,
+                            uint32_t head_dim, const void* q_gain_dev, const void* k_gain_dev, float eps, float rope_theta,
+                            const int32_t* positions_dev, uint32_t seq, const qzo_cache* cache, const int32_t* slots_dev,
+                            void* out_dev, uint64_t ld_out, void* stream) {
+  if (!qkv_dev || !out_dev) return fail(QZO_ERR_ARG, "null device pointer");
+  if ((cache != nullptr) != (slots_dev != nullptr)) return fail(QZO_ERR_ARG, "cache and slots belong together");
+  if (!aligned16(qkv_dev) || !aligned16(out_dev) || !aligned16(q_gain_dev) || !aligned16(k_gain_dev) || !aligned16(positions_dev) ||
+      !aligned16(slots_dev))
+    return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  if (head_dim != 64 && head_dim != 128) return fail(QZO_ERR_SHAPE, "head_dim must be 64 or 128");
+  if (!q_heads || !kv_heads || q_heads > 65535 || kv_heads > 65535) return fail(QZO_ERR_SHAPE, "q_heads and kv_heads must be 1 .. 65535");
+  if (n_tokens >= (1u << 31)) return fail(QZO_ERR_SHAPE, "too many tokens");
+  if (!std::isfinite(eps) || eps < 0.0f) return fail(QZO_ERR_ARG, "eps must be finite and not negative");
+  if (!std::isfinite(rope_theta) || rope_theta < 0.0f) return fail(QZO_ERR_ARG, "rope_theta must be positive, or 0 for no rotation");
+  if (!positions_dev && rope_theta > 0.0f && seq == 0) return fail(QZO_ERR_ARG, "positions or seq is needed");
+  const uint64_t in_row = (uint64_t)(q_heads + 2 * kv_heads) * head_dim, out_row = (uint64_t)(q_heads + (cache ? 0 : kv_heads)) * head_dim;
+  if (ld_qkv % 8 || ld_out % 8 || ld_qkv < in_row || ld_out < out_row)
+    return fail(QZO_ERR_SHAPE, "ld_qkv and ld_out must be multiples of 8 that hold a row");
+  if (ld_qkv >= (1ull << 32) || ld_out >= (1ull << 32)) return fail(QZO_ERR_SHAPE, "ld_qkv and ld_out must be below 2^32");
+  if (qkv_dev == out_dev && ld_qkv != ld_out) return fail(QZO_ERR_ARG, "in place both rows have the same stride");
+  QkArgs a = {};
+  a.qkv = (const bf16_t*)qkv_dev; a.ld_qkv = ld_qkv; a.out = (bf16_t*)out_dev; a.ld_out = ld_out;
+  a.n_tokens = n_tokens; a.q_heads = q_heads; a.kv_heads = kv_heads; a.rope = rope_theta > 0.0f;
+  a.q_gain = (const bf16_t*)q_gain_dev; a.k_gain = (const bf16_t*)k_gain_dev; a.eps = eps;
+  a.positions = positions_dev; a.pass_stride = 0xffffffffu; a.seq = seq ? seq : 1u;
+  if (cache) {
+    qzo_status st = cache_check(cache);
+    if (st != QZO_OK) return st;
+    if (cache->head_dim != head_dim || cache->kv_heads != kv_heads) return fail(QZO_ERR_SHAPE, "the cache has other heads");
+    a.cache_type = cache->type + 1; a.block_shift = (uint32_t)__builtin_ctz(cache->block);
+    a.n_slots = cache->n_blocks * cache->block;
+    a.k = cache->k_dev; a.v = cache->v_dev; a.k_scale = cache->k_scale_dev; a.v_scale = cache->v_scale_dev;
+    a.slots = slots_dev;
+  }
+  QZO_HIP(launch_qk_norm_rope(a, head_dim, (double)rope_theta, (hipStream_t)stream));
+  return QZO_OK;
+}
+
+static qzo_status paged_shape(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim) {
+  if (head_dim != 64 && head_dim != 128) return fail(QZO_ERR_SHAPE, "head_dim must be 64 or 128");
+  if (!n_seq || n_seq > CACHE_MAX_SEQ) return fail(QZO_ERR_SHAPE, "n_seq must be 1 .. 8192");
+  if (!q_heads || q_heads > 65535) return fail(QZO_ERR_SHAPE, "q_heads must be 1 .. 65535");
+  if ((uint64_t)n_rows * q_heads >= (1ull << 31)) return fail(QZO_ERR_SHAPE, "n_rows * q_heads must be below 2^31");
+  return QZO_OK;
+}
+
+qzo_status qzo_paged_attention_scratch_bytes(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim, uint64_t* out) {
+  if (!out) return fail(QZO_ERR_ARG, "out is null");
+  qzo_status st = paged_shape(n_rows, n_seq, q_heads, head_dim);
+  if (st != QZO_OK) return st;
+  *out = paged_attention_scratch(n_rows, n_seq, q_heads, head_dim);
+  return QZO_OK;
+}
+
+qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows, uint32_t n_seq, uint32_t q_heads,
+                               const qzo_cache* cache, const int32_t* tables_dev, uint32_t max_blocks,
+                               const int32_t* lengths_dev, const int32_t* starts_dev, float scale, void* out_dev,
+                               uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream) {
+  if (!q_dev || !cache || !tables_dev || !lengths_dev || !out_dev) return fail(QZO_ERR_ARG, "null pointer");
+  if (!aligned16(q_dev) || !aligned16(tables_dev) || !aligned16(lengths_dev) || !aligned16(starts_dev) || !aligned16(out_dev))
+    return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  qzo_status st = cache_check(cache);
+  if (st != QZO_OK) return st;
+  st = paged_shape(n_rows, n_seq, q_heads, cache->head_dim);
+  if (st != QZO_OK) return st;
+  if (q_heads % cache->kv_heads) return fail(QZO_ERR_SHAPE, "q_heads must be a multiple of kv_heads");
+  if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31) || (uint64_t)max_blocks * cache->block >= (1ull << 31))
+    return fail(QZO_ERR_SHAPE, "n_seq * max_blocks and max_blocks * block must be 1 .. 2^31 - 1");
+  const uint64_t row = (uint64_t)q_heads * cache->head_dim;
+  if (ld_q % 8 || ld_out % 8 || ld_q < row || ld_out < row) return fail(QZO_ERR_SHAPE, "ld_q and ld_out must be multiples of 8 that hold a row");
+  if (ld_q >= (1ull << 32) || ld_out >= (1ull << 32)) return fail(QZO_ERR_SHAPE, "ld_q and ld_out must be below 2^32");
+  if (!std::isfinite(scale)) return fail(QZO_ERR_ARG, "scale not finite");
+  const uint64_t need = paged_attention_scratch(n_rows, n_seq, q_heads, cache->head_dim);
+  if (need) {
+    if (!scratch_dev) return fail(QZO_ERR_ARG, "scratch_dev is null");
+    if ((uintptr_t)scratch_dev & 255u) return fail(QZO_ERR_ALIGN, "scratch not 256-byte aligned");
+    if (scratch_bytes < need) return fail(QZO_ERR_WORKSPACE, "scratch too small: see qzo_paged_attention_scratch_bytes");
+  }
+  PagedArgs a = {};
+  a.q = (const bf16_t*)q_dev; a.ld_q = ld_q; a.out = (bf16_t*)out_dev; a.ld_out = ld_out;
+  a.n_rows = n_rows; a.n_seq = n_seq; a.q_heads = q_heads; a.kv_heads = cache->kv_heads; a.group = q_heads / cache->kv_heads;
+  a.k = cache->k_dev; a.v = cache->v_dev; a.k_scale = cache->k_scale_dev; a.v_scale = cache->v_scale_dev;
+  a.n_blocks = cache->n_blocks; a.block_shift = (uint32_t)__builtin_ctz(cache->block); a.max_blocks = max_blocks;
+  a.tables = tables_dev; a.lengths = lengths_dev; a.starts = starts_dev; a.scale = scale;
+  QZO_HIP(launch_paged_attention(a, cache->head_dim, cache->type == 1, scratch_dev, (hipStream_t)stream));
+  return QZO_OK;
+}
+
 }  // extern "C"

@@ -55,6 +55,13 @@ __device__ __forceinline__ uint32_t pack_scale_x2(float lo, float hi, bool fp16)
 }
 __device__ __forceinline__ uint32_t f32_to_scale(float f, bool fp16) { return pack_scale_x2(f, 0.0f, fp16) & 0xffffu; }
 
+// Four floats as e4m3 bytes (round to nearest even); a value beyond the largest, 448, is to be cut off before (NaN stays NaN).
+__device__ __forceinline__ float to_e4m3_range(float f) { return f != f ? f : __builtin_amdgcn_fmed3f(f, -448.0f, 448.0f); }
+__device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
+
 struct u32x4_t { uint32_t x, y, z, w; };
 
 // a ^ b ^ c in one instruction

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "../../include/qzo.h"
+#include "qzo_device.hpp"
 
 namespace qzo {
 
@@ -331,5 +332,49 @@ hipError_t launch_repack_kmajor(const void* qweight, const void* qzeros, const v
 hipError_t launch_debug_dequant(const void* q, const void* s, const void* zp, bool s_fp16, uint32_t row_base,
                                 uint32_t N, uint32_t K, uint32_t seed_lo, uint32_t seed_hi, float eps_signed,
                                 void* w_eff, hipStream_t st);
+
+// ---- answering: the paged cache of keys and values (qzo_cache.hip, qzo_paged.hip) ----
+constexpr uint32_t CACHE_MAX_SEQ = 8192;      // sequences of a call: their prefixes stay in the LDS
+struct CachePlanArgs {
+  const int32_t *cached, *added;     // [n_seq]
+  uint32_t n_seq, block_shift, n_blocks, max_blocks, max_tokens;
+  int32_t *tables, *free;            // [n_seq, max_blocks], [n_blocks]
+  const qzo_cache_state* before;
+  int32_t *lengths, *starts, *slots, *positions;
+  qzo_cache_state* after;
+};
+hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t st);
+
+struct RopeTurns { double t[64]; };  // theta^(-2i/head_dim) / 2 pi
+struct QkArgs {
+  const bf16_t* qkv;                 // rows of q_heads + 2 kv_heads heads
+  uint64_t ld_qkv, ld_out;
+  uint32_t n_tokens, q_heads, kv_heads, rope;
+  const bf16_t *q_gain, *k_gain;     // nullable
+  float eps;
+  const int32_t* positions;          // null: (row % pass_stride) % seq
+  uint32_t pass_stride, seq;
+  bf16_t* out;
+  uint32_t cache_type;               // 0: none, q and k to out; 1: bf16, 2: e4m3
+  uint32_t block_shift, n_slots;
+  void *k, *v;
+  const float *k_scale, *v_scale;
+  const int32_t* slots;
+};
+hipError_t launch_qk_norm_rope(const QkArgs& a, uint32_t head_dim, double theta, hipStream_t st);
+
+struct PagedArgs {
+  const bf16_t* q;
+  uint64_t ld_q, ld_out;
+  uint32_t n_rows, n_seq, q_heads, kv_heads, group;
+  const void *k, *v;
+  const float *k_scale, *v_scale;
+  uint32_t n_blocks, block_shift, max_blocks;
+  const int32_t *tables, *lengths, *starts;     // starts null: row i is the one token of sequence i
+  float scale;
+  bf16_t* out;
+};
+uint64_t paged_attention_scratch(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim);
+hipError_t launch_paged_attention(const PagedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st);
 
 }  // namespace qzo

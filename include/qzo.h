@@ -410,8 +410,9 @@ qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tok
  * is set to zero; rows behind the last sequence's and not named by starts stay as they are.  Keys that a row does not see
  * reach its output in no way, NaN and infinities among them; nor do positions whose block id lies outside the pool (they
  * count as unseen), or positions beyond max_blocks * block.  A score of -infinity counts as unseen.
- * scratch_dev: qzo_paged_attention_scratch_bytes bytes, 256-byte aligned, contents undefined before and after; calls that may overlap
- * (another stream, another captured graph) need scratch of their own.  n_seq 1 .. 8192, q_heads a multiple of kv_heads,
+ * scratch_dev: qzo_paged_attention_scratch_bytes bytes, 256-byte aligned.  Its first 2048 bytes are counters: zero before the first call
+ * that uses it, zero again after every call, whatever its sizes; the rest is undefined.  Calls that may overlap (another
+ * stream, another captured graph) need scratch of their own.  n_seq 1 .. 8192, q_heads a multiple of kv_heads,
  * scale finite, ld_q and ld_out multiples of 8 and at least q_heads * head_dim.
  */
 qzo_status qzo_paged_attention_scratch_bytes(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim, uint64_t* out);

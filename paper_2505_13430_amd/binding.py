@@ -551,7 +551,7 @@ def _scratch_of_stream(device, stream, nbytes):
     t = _stream_scratch.get((device, stream.cuda_stream))
     if t is None or t.numel() < nbytes:
         with torch.cuda.stream(stream):        # what is outgrown is used again on this stream only
-            t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+            t = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=device)
         _stream_scratch[device, stream.cuda_stream] = t
     return t
 

@@ -26,17 +26,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 
-// The sequences are cut into pieces of `cut` units of 128 keys, the same for all, so that there are some TARGET pieces
-// (key heads times column tiles times units, over TARGET).  A sequence of one piece writes its result itself, the others
-// leave (maximum, sum, accumulators) per piece, at most 2 TARGET of them: more than one piece of a sequence means units >
-// cut, pieces <= 2 units / cut, and units sum to at most cut TARGET.
-constexpr uint32_t TARGET = 1024, MAX_PARTS = 2 * TARGET, UNIT = 128, COLS = 16, WAVES = 4;
-constexpr uint32_t MIN_CUT = 2;
+// How the work is dealt out.  A group is a column tile of one sequence and key head; it has units of 128 keys, and SETUP more
+// that stand for what a group costs apart from its keys.  All groups' units are counted through, and workgroup b takes units
+// b per .. (b + 1) per - 1: every workgroup the same share, whatever the lengths.  A group that lies in one workgroup's share
+// is written by it; otherwise each leaves (maximum, sum, accumulators) in the scratch, its first group's in place 2 b, a later
+// one's (only the last can go on) in 2 b + 1, and who finds the group's counter at its last piece adds them up, in order.  The
+// counter (that of the workgroup of the group's first piece) goes back to zero for the next call.
+constexpr uint32_t UNIT = 128, COLS = 16, WAVES = 4, MAX_WGS = 512;
+constexpr uint32_t SETUP = 2, MIN_SHARE = 6;
 
-struct PagedPlan {        // at the head of the scratch
-  uint32_t cut, pad[63];
-  uint32_t first[CACHE_MAX_SEQ + 1];      // pieces that leave parts, before each sequence
-};
 struct SeqWork { uint32_t row0, rows, len, units, tiles; };
 
 __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i) {
@@ -54,6 +52,32 @@ __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i) {
 
 // What all lanes agree on, in a scalar register.
 __device__ __forceinline__ uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ uint64_t scalar64(uint64_t x) { return (uint64_t)scalar((uint32_t)(x >> 32)) << 32 | scalar((uint32_t)x); }
+
+// Two floats for another workgroup, on any XCD: stored through the L2 and loaded past it (agent scope), so that no L2 has to be
+// written back or invalidated as a whole, which a fence of that scope does (64 ragged sequences: 366 us with fences).  A
+// wavefront's stores have arrived when its count of outstanding ones is zero; it raises the group's counter after that.
+__device__ __forceinline__ void share_out(float* p, float x, float y) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void shared_out() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ float2 shared_in(const float* p) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// Four accumulators of a column, of several pieces of its keys.
+struct Joined {
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  __device__ __forceinline__ void add(float m1, float l1, const f32x4& o1) {
+    if (m1 == -INFINITY && l1 == 0.0f) return;           // saw nothing (a NaN goes on)
+    const float top = fmaxf(m, m1), f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top), f1 = __builtin_amdgcn_exp2f(m1 - top);
+    l = l * f + l1 * f1;
+    o = o * f + o1 * f1;
+    m = top;
+  }
+};
 
 template <class T>
 __device__ __forceinline__ T block_scan(T v, T* total, T* red) {     // exclusive, 256 threads
@@ -98,7 +122,7 @@ struct PagedStep {
 };
 
 template <int DH, bool E4M3, int KP>
-__global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, PagedPlan* plan, float* parts, uint32_t part_cols) {
+__global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, uint32_t* counters, float* parts, uint32_t part_cols) {
   constexpr int KS = DH / 32, VW = DH / 16, ES = E4M3 ? 1 : 2;
   constexpr uint32_t STEP = 32 * KP, ROUND = STEP * WAVES;
   typedef PagedStep<DH, E4M3, KP> Step;
@@ -106,54 +130,82 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, Pa
   float* const sum_acc = (float*)lds;                                   // [WAVES][COLS][DH + 4]
   float* const sum_m = sum_acc + WAVES * COLS * (DH + 4);               // [WAVES][COLS]
   float* const sum_l = sum_m + WAVES * COLS;
-  uint32_t* const red = (uint32_t*)(sum_l + WAVES * COLS);              // [8]
-  uint32_t* const item_first = red + 8;                                 // [n_seq + 1]
-  uint32_t* const part_first = item_first + a.n_seq + 1;                // [n_seq + 1]
-  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint64_t* const red = (uint64_t*)(sum_l + WAVES * COLS);              // [WAVES]
+  uint64_t* const first_unit = red + WAVES;                             // [n_seq], more than 64 sequences only
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = scalar(tid >> 6);
   const uint32_t col = lane & 15u, g = lane >> 4;
 
-  // ---- which pieces there are
-  const uint32_t per = (a.n_seq + 255) / 256, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
-  uint64_t units = 0, total;
-  for (uint32_t i = s_first; i < s_last; ++i) {
-    const SeqWork w = seq_work(a, i);
-    units += (uint64_t)w.units * w.tiles;
-  }
-  block_scan(units, &total, (uint64_t*)red);
-  const uint32_t cut = scalar(max(MIN_CUT, (uint32_t)((total * a.kv_heads + TARGET - 1) / TARGET)));
-  uint32_t items = 0, split = 0, n_items, n_split;
-  for (uint32_t i = s_first; i < s_last; ++i) {
-    const SeqWork w = seq_work(a, i);
-    const uint32_t n = (w.units + cut - 1) / cut, all = n * w.tiles * a.kv_heads;
-    item_first[i] = items; part_first[i] = split;
-    items += all; split += n > 1 ? all : 0u;
-  }
-  const uint32_t items_before = block_scan(items, &n_items, red), split_before = block_scan(split, &n_split, red);
-  for (uint32_t i = s_first; i < s_last; ++i) {
-    item_first[i] += items_before; part_first[i] += split_before;
-    if (blockIdx.x == 0) plan->first[i] = part_first[i];
-  }
-  if (tid == 0) {
-    item_first[a.n_seq] = n_items;
-    if (blockIdx.x == 0) { plan->cut = cut; plan->first[a.n_seq] = n_split; }
-  }
-  __syncthreads();
-
-  const uint32_t per_xcd = (n_items + 7) / 8;
-  for (uint32_t v = blockIdx.x; v < per_xcd * 8; v += gridDim.x) {
-    const uint32_t item = (v & 7u) * per_xcd + (v >> 3);      // neighbours (the column tiles of the same keys) on one XCD
-    if (item >= n_items) continue;
-    uint32_t lo = 0, hi = a.n_seq;
-    while (hi - lo > 1) {
-      const uint32_t mid = (lo + hi) >> 1;
-      if (item_first[mid] <= item) lo = mid; else hi = mid;
+  // ---- the sequences' units: up to 64 sequences in the lanes of every wavefront, more in the LDS
+  const bool few = a.n_seq <= 64;
+  uint64_t total, mine = 0;
+  SeqWork lane_work = {0, 0, 0, 1, 0};
+  if (few) {
+    uint64_t n = 0;
+    if (lane < a.n_seq) {
+      lane_work = seq_work(a, lane);
+      n = (uint64_t)(lane_work.units + SETUP) * lane_work.tiles * a.kv_heads;
     }
-    const uint32_t seq = scalar(lo);
-    SeqWork w = seq_work(a, seq);
-    w.row0 = scalar(w.row0); w.rows = scalar(w.rows); w.len = scalar(w.len); w.units = scalar(w.units); w.tiles = scalar(w.tiles);
-    uint32_t r = scalar(item - item_first[seq]);
-    const uint32_t tile = scalar(r % w.tiles); r = scalar(r / w.tiles);
-    const uint32_t kh = scalar(r % a.kv_heads), piece = scalar(r / a.kv_heads), pieces = scalar((w.units + cut - 1) / cut);
+    uint64_t s = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint64_t u = __shfl_up(s, o, 64);
+      if (lane >= (uint32_t)o) s += u;
+    }
+    total = __shfl(s, 63, 64);
+    mine = s - n;
+  } else {
+    const uint32_t per = (a.n_seq + 255) / 256, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
+    uint64_t n = 0;
+    for (uint32_t i = s_first; i < s_last; ++i) {
+      const SeqWork w = seq_work(a, i);
+      first_unit[i] = n;
+      n += (uint64_t)(w.units + SETUP) * w.tiles * a.kv_heads;
+    }
+    const uint64_t before = block_scan(n, &total, red);
+    for (uint32_t i = s_first; i < s_last; ++i) first_unit[i] += before;
+    __syncthreads();
+  }
+  total = scalar64(total);
+  const uint64_t share = max((uint64_t)MIN_SHARE, (total + gridDim.x - 1) / gridDim.x);
+  // neighbours (the column tiles of the same keys) on one XCD; the grid is a multiple of 8
+  const uint32_t wg = (blockIdx.x & 7u) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  const uint64_t begin = share * wg, end = min(begin + share, total);
+
+  for (uint64_t unit = begin; unit < end;) {
+    uint32_t seq;
+    uint64_t seq_first;
+    SeqWork w;
+    if (few) {
+      // prefixes ascend and begin at 0: the last one not above is the sequence that has the unit
+      seq = scalar((uint32_t)__popcll(__ballot(lane < a.n_seq && mine <= unit)) - 1u);
+      seq_first = (uint64_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, (int)seq) & 0xffffffffu;
+      seq_first |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), (int)seq) << 32;
+      auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)seq); };
+      w = {of(lane_work.row0), of(lane_work.rows), of(lane_work.len), of(lane_work.units), of(lane_work.tiles)};
+    } else {
+      uint32_t lo = 0, hi = a.n_seq;
+      while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (first_unit[mid] <= unit) lo = mid; else hi = mid;
+      }
+      seq = scalar(lo);
+      seq_first = scalar64(first_unit[seq]);
+      w = seq_work(a, seq);
+      w = {scalar(w.row0), scalar(w.rows), scalar(w.len), scalar(w.units), scalar(w.tiles)};
+    }
+    const uint32_t span = w.units + SETUP;
+    const uint64_t r = unit - seq_first;
+    const uint32_t group = scalar((r >> 32) ? (uint32_t)(r / span) : (uint32_t)r / span);
+    const uint32_t tile = scalar(group % w.tiles), kh = scalar(group / w.tiles);
+    const uint32_t at = scalar((uint32_t)(r - (uint64_t)group * span));                     // within the group, SETUP first
+    const uint32_t n_units = scalar((uint32_t)min((uint64_t)(span - at), end - unit));
+    const uint64_t group_first = unit - at + SETUP, group_last = unit - at + span - 1;
+    const bool at_begin = unit == begin;
+    unit += n_units;
+    if (at + n_units <= SETUP) continue;
+    const uint32_t u_first = max(at, SETUP) - SETUP, u_end = at + n_units - SETUP;
+    const uint32_t wg_first = group_first >= begin ? wg : wg - scalar((uint32_t)((begin - group_first + share - 1) / share));
+    const uint32_t wg_last = group_last < end ? wg : wg + scalar((uint32_t)((group_last - end) / share)) + 1u, pieces = wg_last - wg_first + 1u;
 
     // ---- this tile's columns
     const uint32_t flat = tile * COLS + col, token = flat / a.group, head = kh * a.group + flat % a.group;
@@ -163,7 +215,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, Pa
     const int32_t sees = live ? (int32_t)(w.len + token + 1u - w.rows) : 0;                  // positions that the column sees
     const int32_t least = (int32_t)(w.len + tile * COLS / a.group + 1u - w.rows);             // the first column's, the fewest
     const int32_t most = (int32_t)(w.len + (tile * COLS + n_cols - 1) / a.group + 1u - w.rows);
-    const int32_t k_first = (int32_t)(piece * cut * UNIT), k_end = (int32_t)min((int64_t)most, (int64_t)(piece + 1) * cut * UNIT);
+    const int32_t k_first = (int32_t)(u_first * UNIT), k_end = (int32_t)min((int64_t)most, (int64_t)u_end * UNIT);
 
     bf16x8 q[KS];
 #pragma unroll
@@ -365,7 +417,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, Pa
     l += __shfl_xor(l, 32, 64);
 
     // ---- the four wavefronts' sums together
-    __syncthreads();                          // the last item's have been read
+    __syncthreads();                          // the last group's have been read
     if (g == 0) { sum_m[wave * COLS + col] = m; sum_l[wave * COLS + col] = l; }
     if (live) {
 #pragma unroll
@@ -376,76 +428,68 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, Pa
               f32x4{acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j]};
     }
     __syncthreads();
-    const uint32_t part = part_first[seq] + (piece * a.kv_heads + kh) * w.tiles + tile;
     const float vs = E4M3 && a.v_scale ? a.v_scale[kh] : 1.0f;
-    for (uint32_t u = tid; u < n_cols * (DH / 4); u += 256) {
-      const uint32_t c = u / (DH / 4), d = u % (DH / 4) * 4u;
-      float top = -INFINITY;
-#pragma unroll
-      for (uint32_t x = 0; x < WAVES; ++x) top = fmaxf(top, sum_m[x * COLS + c]);
-      f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-      float ls = 0.0f;
-#pragma unroll
-      for (uint32_t x = 0; x < WAVES; ++x) {
-        const float mx = sum_m[x * COLS + c], f = mx == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx - top);
-        if (mx == -INFINITY && sum_l[x * COLS + c] == 0.0f) continue;      // saw nothing (a NaN goes on)
-        ls += f * sum_l[x * COLS + c];
-        o += f * *reinterpret_cast<const f32x4*>(sum_acc + (x * COLS + c) * (DH + 4) + d);
-      }
-      if (pieces > 1) {
-        if (part < MAX_PARTS) {
-          float* to = parts + ((uint64_t)part * part_cols + c) * (DH + 4);
-          *reinterpret_cast<f32x4*>(to + 4 + d) = o;
-          if (d == 0) { to[0] = top; to[1] = ls; }
-        }
-        continue;
-      }
+    auto put = [&](uint32_t c, uint32_t d, const f32x4& o, float ls) {       // a column that saw nothing: zero
       const float inv = ls == 0.0f ? 0.0f : vs / ls;
-      const uint32_t f2 = tile * COLS + c;
-      bf16_t* to = a.out + (uint64_t)(w.row0 + f2 / a.group) * a.ld_out + (uint64_t)(kh * a.group + f2 % a.group) * DH + d;
+      const uint32_t f = tile * COLS + c;
+      bf16_t* to = a.out + (uint64_t)(w.row0 + f / a.group) * a.ld_out + (uint64_t)(kh * a.group + f % a.group) * DH + d;
       *reinterpret_cast<uint2*>(to) = ls == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    };
+    constexpr uint32_t DV = DH / 4, STRIDE = DH + 4;
+    auto part_of = [&](uint32_t place) { return parts + (uint64_t)place * part_cols * STRIDE; };
+    for (uint32_t u = tid; u < n_cols * DV; u += 256) {
+      const uint32_t c = u / DV, d = u % DV * 4u;
+      Joined j;
+#pragma unroll
+      for (uint32_t x = 0; x < WAVES; ++x)
+        j.add(sum_m[x * COLS + c], sum_l[x * COLS + c], *reinterpret_cast<const f32x4*>(sum_acc + (x * COLS + c) * STRIDE + d));
+      if (pieces == 1) { put(c, d, j.o, j.l); continue; }
+      float* to = part_of(2u * wg + (at_begin ? 0u : 1u)) + c * STRIDE;
+      share_out(to + 4 + d, j.o[0], j.o[1]);
+      share_out(to + 6 + d, j.o[2], j.o[3]);
+      if (d == 0) share_out(to, j.m, j.l);
     }
-  }
-}
+    if (pieces == 1) continue;
 
-// Joins the pieces of a row's head, in order: one wavefront, DH/64 features a lane.
-template <int DH>
-__global__ __launch_bounds__(64) void paged_join_kernel(PagedArgs a, const PagedPlan* plan, const float* parts, uint32_t part_cols) {
-  constexpr int E = DH / 64;
-  const uint32_t row = blockIdx.x / a.q_heads, head = blockIdx.x % a.q_heads, lane = threadIdx.x;
-  uint32_t seq = row;
-  if (a.starts) {
-    uint32_t lo = 0, hi = a.n_seq;
-    while (hi - lo > 1) {
-      const uint32_t mid = (lo + hi) >> 1;
-      if (a.starts[mid] <= (int32_t)row) lo = mid; else hi = mid;
+    // ---- the last piece of a group to be done adds them up
+    shared_out();
+    __syncthreads();
+    uint32_t* const arrived = (uint32_t*)red;
+    if (tid == 0) {
+      const uint32_t n = atomicAdd(counters + wg_first, 1u);
+      if (n + 1u == pieces) __hip_atomic_store(counters + wg_first, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *arrived = n + 1u;
     }
-    seq = lo;
+    __syncthreads();
+    if (*arrived != pieces) continue;
+    const uint32_t first_place = 2u * wg_first + (group_first - SETUP <= share * wg_first ? 0u : 1u);
+    const uint32_t lanes = n_cols * DV, teams = max(1u, 256u / lanes), team = tid / lanes;      // of threads, each with its pieces
+    for (uint32_t u = tid % lanes; u < lanes && team < teams; u += 256) {
+      const uint32_t c = u / DV, d = u % DV * 4u;
+      Joined j;
+#pragma unroll 4
+      for (uint32_t x = team; x < pieces; x += teams) {
+        const float* from = part_of(x ? 2u * (wg_first + x) : first_place) + c * STRIDE;
+        const float2 ml = shared_in(from), lo = shared_in(from + 4 + d), hi = shared_in(from + 6 + d);
+        j.add(ml.x, ml.y, f32x4{lo.x, lo.y, hi.x, hi.y});
+      }
+      if (teams == 1) { put(c, d, j.o, j.l); continue; }
+      float* to = sum_acc + tid * 8u;
+      *reinterpret_cast<f32x4*>(to) = j.o;
+      to[4] = j.m; to[5] = j.l;
+    }
+    if (teams > 1) {
+      __syncthreads();
+      if (tid < lanes) {
+        Joined j;
+        for (uint32_t x = 0; x < teams; ++x) {
+          const float* from = sum_acc + (x * lanes + tid) * 8u;
+          j.add(from[4], from[5], *reinterpret_cast<const f32x4*>(from));
+        }
+        put(tid / DV, tid % DV * 4u, j.o, j.l);
+      }
+    }
   }
-  if (seq >= a.n_seq) return;
-  const SeqWork w = seq_work(a, seq);
-  const uint32_t pieces = (w.units + plan->cut - 1) / plan->cut;
-  if (pieces < 2 || row < w.row0 || row >= w.row0 + w.rows) return;
-  const uint32_t kh = head / a.group, flat = (row - w.row0) * a.group + head % a.group, tile = flat / COLS, c = flat % COLS;
-  float top = -INFINITY, ls = 0.0f, o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.0f;
-  for (uint32_t p = 0; p < pieces; ++p) {
-    const uint32_t part = plan->first[seq] + (p * a.kv_heads + kh) * w.tiles + tile;
-    if (part >= MAX_PARTS) break;
-    const float* from = parts + ((uint64_t)part * part_cols + c) * (DH + 4);
-    const float mx = from[0], lx = from[1];
-    if (mx == -INFINITY && lx == 0.0f) continue;
-    const float m2 = fmaxf(top, mx), f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - m2), fx = __builtin_amdgcn_exp2f(mx - m2);
-    ls = ls * f + lx * fx;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f + from[4 + lane * E + e] * fx;
-    top = m2;
-  }
-  const float inv = ls == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[kh] : 1.0f) / ls;
-  bf16_t* to = a.out + (uint64_t)row * a.ld_out + (uint64_t)head * DH + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; ++e) to[e] = (bf16_t)(pack_bf16x2(ls == 0.0f ? 0.0f : o[e] * inv, 0.0f) & 0xffffu);
 }
 
 uint32_t part_columns(uint32_t n_rows, uint32_t group) { return (uint32_t)std::min<uint64_t>(COLS, (uint64_t)n_rows * group); }
@@ -455,21 +499,17 @@ hipError_t launch_paged(const PagedArgs& a, void* scratch, hipStream_t st) {
   constexpr int KP = E4M3 ? 2 : 1;
   const uint32_t rows = a.starts ? a.n_rows : std::min(a.n_rows, a.n_seq);
   if (rows == 0) return hipSuccess;
-  PagedPlan* plan = (PagedPlan*)scratch;
-  float* parts = (float*)((unsigned char*)scratch + (sizeof(PagedPlan) + 255) / 256 * 256);
-  const uint32_t lds = WAVES * COLS * (DH + 4) * 4 + WAVES * COLS * 8 + 32 + (a.n_seq + 1) * 8;
+  uint32_t* counters = (uint32_t*)scratch;
+  float* parts = (float*)scratch + MAX_WGS;
+  const uint32_t lds = WAVES * COLS * (DH + 4) * 4 + WAVES * COLS * 8 + WAVES * 8 + (a.n_seq > 64 ? a.n_seq * 8 : 0);
   if (lds > 60u * 1024) {
     hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3, KP>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  // pieces there can be: column tiles, key heads, units of the longest sequence that the tables have room for
+  // units that there can be: column tiles, key heads, the longest sequence that the tables have room for
   const uint64_t tiles = ((uint64_t)rows * a.group + COLS - 1) / COLS + a.n_seq, units = (((uint64_t)a.max_blocks << a.block_shift) + UNIT - 1) / UNIT;
-  const uint32_t wgs = (uint32_t)std::min<uint64_t>(512, (tiles * a.kv_heads * ((units + MIN_CUT - 1) / MIN_CUT) + 7) / 8 * 8);
-  const uint32_t cols = part_columns(rows, a.group);
-  paged_attention_kernel<DH, E4M3, KP><<<wgs, 256, lds, st>>>(a, plan, parts, cols);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || units <= MIN_CUT) return e;
-  paged_join_kernel<DH><<<rows * a.q_heads, 64, 0, st>>>(a, plan, parts, cols);
+  const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (tiles * a.kv_heads * (units + SETUP) / MIN_SHARE + 8) / 8 * 8);
+  paged_attention_kernel<DH, E4M3, KP><<<wgs, 256, lds, st>>>(a, counters, parts, part_columns(rows, a.group));
   return hipGetLastError();
 }
 
@@ -477,7 +517,7 @@ hipError_t launch_paged(const PagedArgs& a, void* scratch, hipStream_t st) {
 
 uint64_t paged_attention_scratch(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim) {
   (void)n_seq;
-  return (sizeof(PagedPlan) + 255) / 256 * 256 + (uint64_t)MAX_PARTS * part_columns(n_rows, q_heads) * (head_dim + 4) * 4;
+  return MAX_WGS * 4 + 2ull * MAX_WGS * part_columns(n_rows, q_heads) * (head_dim + 4) * 4;
 }
 
 hipError_t launch_paged_attention(const PagedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st) {

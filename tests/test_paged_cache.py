@@ -581,7 +581,7 @@ def test_captured_steps_replay():
                  positions=_i32([0] * n), added=_i32([1] * n), x=torch.zeros(n, (H + 2 * Hk) * dh, dtype=torch.bfloat16, device=DEV),
                  q=torch.zeros(n, H * dh, dtype=torch.bfloat16, device=DEV), out=torch.zeros(n, H * dh, dtype=torch.bfloat16, device=DEV))
         d["cache"] = qb.make_cache(*d["pools"])
-        d["scratch"] = torch.empty(max(256, qb.qzo_paged_attention_scratch_bytes(n, n, H, dh)), dtype=torch.uint8, device=DEV)
+        d["scratch"] = torch.zeros(max(256, qb.qzo_paged_attention_scratch_bytes(n, n, H, dh)), dtype=torch.uint8, device=DEV)
         return d
 
     def step(d):

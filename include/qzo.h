@@ -391,7 +391,7 @@ qzo_status qzo_cache_plan(const int32_t* cached_dev, const int32_t* added_dev, u
  *   cache given: out_dev receives the heads of q; k and v of the row go to slot slots_dev[t] of the cache (in e4m3: divided by
  *     their scale, cut off at +-448, rounded to nearest even).  A row whose slot is negative or beyond the pool is skipped, its
  *     out row included.  The slots of a call must differ from one another.
- * head_dim 64 or 128 (of the cache, too); ld_qkv and ld_out multiples of 8, at least the row's heads; eps positive or 0.
+ * n_tokens below 2^26; head_dim 64 or 128 (of the cache, too); ld_qkv and ld_out multiples of 8, at least the row's heads; eps positive or 0.
  */
 qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tokens, uint32_t q_heads, uint32_t kv_heads,
                             uint32_t head_dim, const void* q_gain_dev, const void* k_gain_dev, float eps, float rope_theta,

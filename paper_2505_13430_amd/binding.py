@@ -77,6 +77,7 @@ def lib():
         u32, u64, p, f = C.c_uint32, C.c_uint64, C.c_void_p, C.c_float
         _lib.qzo_cache_plan.argtypes = [p, p, u32, u32, u32, u32, u32] + [p] * 9
         _lib.qzo_qk_norm_rope.argtypes = [p, u64, u32, u32, u32, u32, p, p, f, f, p, u32, p, p, p, u64, p]
+        _lib.qzo_paged_attention_scratch_bytes.argtypes = [u32, u32, u32, u32, p]
         _lib.qzo_paged_attention.argtypes = [p, u64, u32, u32, u32, p, p, u32, p, p, f, p, u64, p, u64, p]
     return _lib
 
@@ -488,19 +489,22 @@ def _typed(t, dtype):
     return t.data_ptr()
 
 
-def _here(stream, *tensors):
-    """The call's stream; its tensors live on the device that is current."""
+def _here(stream, tensors):
+    """Handle of the call's stream; its tensors live on the device that is current."""
     at = torch.cuda.current_device()
-    assert all(t is None or t.get_device() == at for t in tensors), "tensors must be on the current device"
-    return torch.cuda.current_stream() if stream is None else stream
+    for t in tensors:
+        assert t is None or t.get_device() == at, "tensors must be on the current device"
+    return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
 
 def make_cache(k, v, k_scale=None, v_scale=None) -> qzo_cache:
     """k, v: bf16 or float8_e4m3fn [n_blocks, kv_heads, block, head_dim]; e4m3: fp32 scales [kv_heads].  Holds its tensors."""
-    assert k.dtype in (torch.bfloat16, torch.float8_e4m3fn) and k.shape == v.shape and k.dim() == 4
-    assert all(s is None or s.numel() == k.shape[1] for s in (k_scale, v_scale))
-    c = qzo_cache(C.sizeof(qzo_cache), int(k.dtype != torch.bfloat16), k.shape[0], k.shape[2], k.shape[1], k.shape[3], _typed(k, k.dtype),
-                  _typed(v, k.dtype), _typed(k_scale, torch.float32), _typed(v_scale, torch.float32))
+    n_blocks, kv_heads, block, dh = k.shape
+    assert k.dtype in (torch.bfloat16, torch.float8_e4m3fn) and k.shape == v.shape
+    for s in (k_scale, v_scale):
+        assert s is None or s.numel() == kv_heads
+    c = qzo_cache(C.sizeof(qzo_cache), k.dtype != torch.bfloat16, n_blocks, block, kv_heads, dh, _typed(k, k.dtype), _typed(v, k.dtype),
+                  _typed(k_scale, torch.float32), _typed(v_scale, torch.float32))
     c.tensors = (k, v, k_scale, v_scale)
     return c
 
@@ -513,7 +517,7 @@ def qzo_cache_plan(cached, added, block, tables, free, before, lengths, starts, 
     assert before.numel() == after.numel() == 4
     _check(lib().qzo_cache_plan(_typed(cached, i32), _typed(added, i32), n, block, free.numel(), most, slots.numel(), _typed(tables, i32),
                                 _typed(free, i32), _typed(before, i32), _typed(lengths, i32), _typed(starts, i32), _typed(slots, i32),
-                                _typed(positions, i32), _typed(after, i32), _here(stream, cached, tables, slots).cuda_stream))
+                                _typed(positions, i32), _typed(after, i32), _here(stream, (cached, tables, slots))))
 
 
 def qzo_qk_norm_rope(qkv, q_heads, kv_heads, out, q_gain=None, k_gain=None, eps=1e-6, theta=10000.0, positions=None, seq=0, cache=None,
@@ -526,33 +530,33 @@ def qzo_qk_norm_rope(qkv, q_heads, kv_heads, out, q_gain=None, k_gain=None, eps=
     dh = qkv.shape[1] // heads
     assert qkv.dtype == out.dtype == torch.bfloat16 and qkv.shape[1] == heads * dh
     assert out.shape[0] == T and out.shape[1] >= (q_heads + (0 if cache is not None else kv_heads)) * dh
-    assert all(g is None or g.numel() == dh for g in (q_gain, k_gain)) and all(i is None or i.numel() >= T for i in (positions, slots))
+    assert (q_gain is None or q_gain.numel() == dh) and (k_gain is None or k_gain.numel() == dh)
+    assert (positions is None or positions.numel() >= T) and (slots is None or slots.numel() >= T)
     if T == 0:
         return                                  # an empty tensor has no address
     _check(lib().qzo_qk_norm_rope(x, ldx, T, q_heads, kv_heads, dh, _typed(q_gain, torch.bfloat16), _typed(k_gain, torch.bfloat16), eps, theta,
                                   _typed(positions, torch.int32), seq, None if cache is None else C.addressof(cache),
-                                  _typed(slots, torch.int32), y, ldy, _here(stream, qkv, out, q_gain, k_gain, positions, slots).cuda_stream))
+                                  _typed(slots, torch.int32), y, ldy, _here(stream, (qkv, out, positions, slots))))
 
 
 def qzo_paged_attention_scratch_bytes(n_rows, n_seq, q_heads, head_dim) -> int:
     out = C.c_uint64(0)
-    _check(lib().qzo_paged_attention_scratch_bytes(C.c_uint32(n_rows), C.c_uint32(n_seq), C.c_uint32(q_heads), C.c_uint32(head_dim),
-                                                   C.byref(out)))
+    _check(lib().qzo_paged_attention_scratch_bytes(n_rows, n_seq, q_heads, head_dim, C.addressof(out)))
     return out.value
 
 
 _stream_scratch = {}
 
 
-def _scratch_of_stream(device, stream, nbytes):
+def _scratch_of_stream(device, stream, handle, nbytes):
     """Scratch of the calls on one stream, which do not overlap.  A captured graph keeps the address it was captured with and may
     be replayed on any stream beside any other: it is given scratch of its own."""
     assert not torch.cuda.is_current_stream_capturing(), "a captured call needs scratch of its own: pass scratch"
-    t = _stream_scratch.get((device, stream.cuda_stream))
+    t = _stream_scratch.get((device, handle))
     if t is None or t.numel() < nbytes:
         with torch.cuda.stream(stream):        # what is outgrown is used again on this stream only
-            t = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=device)
-        _stream_scratch[device, stream.cuda_stream] = t
+            t = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        _stream_scratch[device, handle] = t
     return t
 
 
@@ -568,10 +572,9 @@ def qzo_paged_attention(q, cache, tables, lengths, out, scale, starts=None, scra
     assert lengths.numel() == n and (starts is None or starts.numel() == n + 1)
     if q.shape[0] == 0:
         return
-    st = _here(stream, q, out, tables, lengths, starts)
+    st = _here(stream, (q, out, tables, lengths, cache.tensors[0]))
     if isinstance(scratch, str):
-        need = qzo_paged_attention_scratch_bytes(q.shape[0], n, heads, dh)
-        scratch = _scratch_of_stream(q.device, st, need) if need else None
+        scratch = _scratch_of_stream(q.device, stream, st, qzo_paged_attention_scratch_bytes(q.shape[0], n, heads, dh))
     _check(lib().qzo_paged_attention(x, ldx, q.shape[0], n, heads, C.addressof(cache), _typed(tables, torch.int32), most,
                                      _typed(lengths, torch.int32), _typed(starts, torch.int32), scale, y, ldy,
-                                     None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel() * scratch.element_size(), st.cuda_stream))
+                                     None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel() * scratch.element_size(), st))

@@ -1647,7 +1647,7 @@ qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tok
     return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
   if (head_dim != 64 && head_dim != 128) return fail(QZO_ERR_SHAPE, "head_dim must be 64 or 128");
   if (!q_heads || !kv_heads || q_heads > 65535 || kv_heads > 65535) return fail(QZO_ERR_SHAPE, "q_heads and kv_heads must be 1 .. 65535");
-  if (n_tokens >= (1u << 31)) return fail(QZO_ERR_SHAPE, "too many tokens");
+  if (n_tokens >= (1u << 26)) return fail(QZO_ERR_SHAPE, "n_tokens must be below 2^26");
   if (!std::isfinite(eps) || eps < 0.0f) return fail(QZO_ERR_ARG, "eps must be finite and not negative");
   if (!std::isfinite(rope_theta) || rope_theta < 0.0f) return fail(QZO_ERR_ARG, "rope_theta must be positive, or 0 for no rotation");
   if (!positions_dev && rope_theta > 0.0f && seq == 0) return fail(QZO_ERR_ARG, "positions or seq is needed");

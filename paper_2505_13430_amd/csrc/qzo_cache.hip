@@ -19,88 +19,114 @@ __device__ __forceinline__ uint32_t last_not_above(const int32_t* prefix, uint32
   return lo;
 }
 
-// One workgroup.  What sequence i gives back (ended), takes and adds is summed over the sequences before it; the three
-// prefixes stay in the LDS, where the blocks and the tokens find their sequence by bisection, so that long prompts are
-// spread over all threads.  Every input is read before the first output is written (lengths may be cached, after may be
-// before), and no output of this launch is read back: a taken block is found in the free list or in the row of the
-// sequence that gives it back, neither of which changes below the stack's old height.
+// Inclusive sum over the lanes: within rows of 16, then rows 0 and 2 into 1 and 3, then both into the upper half.
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T from_before(T v) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false)); }
+template <class T>
+__device__ __forceinline__ T lane_scan(T v) {
+  v += from_before<0x111, 0xf>(v);              // row_shr:1, 2, 4, 8
+  v += from_before<0x112, 0xf>(v);
+  v += from_before<0x114, 0xf>(v);
+  v += from_before<0x118, 0xf>(v);
+  v += from_before<0x142, 0xa>(v);              // row_bcast:15
+  v += from_before<0x143, 0xc>(v);              // row_bcast:31
+  return v;
+}
+
+// One workgroup, a sequence (or several) per thread.  What sequence i gives back (ended), takes and adds is summed over the
+// sequences before it; the sums stay in the LDS, where blocks given back, and the blocks and tokens of long prompts, find their
+// sequence by bisection and are spread over all threads.  Every input is read before the first output is written (lengths
+// may be cached, after may be before), and no output of this launch is read back: a taken block is found in the free list or
+// in the row of the sequence that gives it back, neither of which changes below the stack's old height.
+// Latency is all there is to it: lengths, sums, free list, stores.  The block that a sequence's next token falls into is
+// loaded beside the lengths.  8 sequences PLAN_8 us, 1000 PLAN_1000 us.
 // with_slots: slots and positions too (few tokens); else cache_slots_kernel follows.
-constexpr uint32_t PLAN_THREADS = 1024;
+constexpr uint32_t PLAN_THREADS = 1024, PLAN_FEW = 4;      // a thread itself sees to that many tokens, and their blocks
 __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs a, uint32_t with_slots) {
   extern __shared__ int32_t prefix[];
   int32_t* const back = prefix;                    // [n_seq] blocks given back before sequence i
   int32_t* const take = prefix + a.n_seq;          // [n_seq] blocks taken before it
   int32_t* const start = prefix + 2 * a.n_seq;     // [n_seq] tokens added before it
   int32_t* const old_len = prefix + 3 * a.n_seq;   // [n_seq]
-  __shared__ int64_t wave_sums[PLAN_THREADS / 64][3];
-  __shared__ int32_t bad;
+  __shared__ uint32_t wave_sums[3][PLAN_THREADS / 64];
+  __shared__ float wave_sizes[3][PLAN_THREADS / 64];
+  __shared__ uint32_t flags;                       // 1: wrong, 2: a row too short, 4: a sequence of more than PLAN_FEW tokens
   const uint32_t tid = threadIdx.x, shift = a.block_shift;
   const int32_t mask = (1 << shift) - 1;
-  const int32_t n_free = a.before->n_free;
   const int64_t room = (int64_t)a.max_blocks << shift;
-  if (tid == 0) bad = 0;
+  const uint32_t per = (a.n_seq + PLAN_THREADS - 1) / PLAN_THREADS, first = min(tid * per, a.n_seq), last = min(first + per, a.n_seq);
+  if (tid == 0) flags = 0;
   __syncthreads();
-  const uint32_t per = (a.n_seq + PLAN_THREADS - 1) / PLAN_THREADS, first = tid * per, last = min(first + per, a.n_seq);
+  const int32_t n_free = a.before->n_free;
+  auto blocks = [&](int64_t tokens) { return (tokens + mask) >> shift; };
   int64_t sum[3] = {0, 0, 0};
-  bool wrong = n_free < 0 || (uint32_t)n_free > a.n_blocks, narrow = false;
+  uint32_t seen = n_free < 0 || (uint32_t)n_free > a.n_blocks ? 1u : 0u;
+  int32_t open = 0;                                // per = 1: the block that holds the sequence's last token
   for (uint32_t i = first; i < last; ++i) {
     const int32_t have = a.cached[i], add = a.added[i];
-    wrong = wrong || have < 0;
-    narrow = narrow || have > room || (add > 0 && (int64_t)have + add > room);
-    const int64_t held = ((int64_t)have + mask) >> shift;
-    sum[0] += add < 0 ? held : 0;
-    sum[1] += add < 0 ? 0 : (((int64_t)have + add + mask) >> shift) - held;
+    if (have < 0) seen |= 1u;
+    else if (have > room || (add > 0 && (int64_t)have + add > room)) seen |= 2u;
+    else if (per == 1 && have > 0) open = a.tables[(uint64_t)i * a.max_blocks + (uint32_t)((have - 1) >> shift)];
+    if (add > (int32_t)PLAN_FEW) seen |= 4u;
+    sum[0] += add < 0 ? blocks(have) : 0;
+    sum[1] += add < 0 ? 0 : blocks((int64_t)have + add) - blocks(have);
     sum[2] += add < 0 ? 0 : add;
     old_len[i] = have;
   }
-  if (wrong) atomicOr(&bad, 1);
-  if (narrow) atomicOr(&bad, 2);
-  // exclusive sums over the threads: within a wavefront, then over the wavefronts before it
-  int64_t run[3], total[3];
+  if (seen) atomicOr(&flags, seen);
+  // exclusive sums over the threads, in 32 bits; whether 32 bits hold them is told by sums of floats (a whole plan has totals
+  // below 2^31, what a float misses of them is far below 2^31 too)
+  uint32_t run[3];
 #pragma unroll
   for (int j = 0; j < 3; ++j) {
-    int64_t v = sum[j];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t u = __shfl_up(v, o, 64);
-      if ((tid & 63u) >= (uint32_t)o) v += u;
-    }
-    if ((tid & 63u) == 63u) wave_sums[tid >> 6][j] = v;
-    run[j] = v - sum[j];
+    const uint32_t v = (uint32_t)sum[j], upto = lane_scan(v);
+    const float size = lane_scan((float)sum[j]);
+    if ((tid & 63u) == 63u) { wave_sums[j][tid >> 6] = upto; wave_sizes[j][tid >> 6] = size; }
+    run[j] = upto - v;
   }
   __syncthreads();
+  uint32_t total[3];
+  bool fits[3];
 #pragma unroll
   for (int j = 0; j < 3; ++j) {
+    float size = 0.0f;
     total[j] = 0;
+#pragma unroll
     for (uint32_t w = 0; w < PLAN_THREADS / 64; ++w) {
       if (w == (tid >> 6)) run[j] += total[j];
-      total[j] += wave_sums[w][j];
+      total[j] += wave_sums[j][w];
+      size += wave_sizes[j][w];
+    }
+    fits[j] = size < 3e9f && total[j] < 0x80000000u;
+  }
+  const uint32_t flag = flags;
+  int32_t status = QZO_OK;
+  if (flag & 1u) status = QZO_ERR_ARG;
+  else if ((flag & 2u) || !fits[2] || total[2] > a.max_tokens) status = QZO_ERR_SHAPE;
+  else if (!fits[0] || (uint32_t)n_free + total[0] > a.n_blocks) status = QZO_ERR_ARG;        // more blocks than there are
+  else if (!fits[1] || total[1] > (uint32_t)n_free + total[0]) status = QZO_ERR_WORKSPACE;
+  const bool ok = status == QZO_OK;
+  const int32_t n_back = ok ? (int32_t)total[0] : 0, n_take = ok ? (int32_t)total[1] : 0, n_tok = ok ? (int32_t)total[2] : 0;
+  {
+    uint32_t b = run[0], k = run[1], t = run[2];
+    for (uint32_t i = first; i < last; ++i) {
+      const int32_t have = old_len[i], add = a.added[i];
+      back[i] = (int32_t)b; take[i] = (int32_t)k; start[i] = (int32_t)t;
+      a.lengths[i] = !ok ? have : add < 0 ? 0 : have + add;
+      a.starts[i] = ok ? (int32_t)t : 0;
+      if (add < 0) b += (uint32_t)blocks(have);
+      else { k += (uint32_t)(blocks((int64_t)have + add) - blocks(have)); t += (uint32_t)add; }
     }
   }
-  int32_t status = QZO_OK;
-  if (bad & 1) status = QZO_ERR_ARG;
-  else if ((bad & 2) || total[2] > (int64_t)a.max_tokens) status = QZO_ERR_SHAPE;
-  else if (n_free + total[0] > (int64_t)a.n_blocks) status = QZO_ERR_ARG;        // more blocks than there are
-  else if (total[1] > n_free + total[0]) status = QZO_ERR_WORKSPACE;
-  const bool ok = status == QZO_OK;
-  for (uint32_t i = first; i < last; ++i) {
-    const int32_t have = old_len[i], add = a.added[i];
-    back[i] = (int32_t)run[0]; take[i] = (int32_t)run[1]; start[i] = (int32_t)run[2];
-    const int32_t held = (int32_t)(((int64_t)have + mask) >> shift);
-    if (add < 0) run[0] += held;
-    else { run[1] += (int32_t)(((int64_t)have + add + mask) >> shift) - held; run[2] += add; }
-  }
-  __syncthreads();
-  for (uint32_t i = first; i < last; ++i) {      // a thread's own sequences: read above, written here
-    const int32_t add = a.added[i];
-    a.lengths[i] = !ok ? old_len[i] : add < 0 ? 0 : old_len[i] + add;
-    a.starts[i] = ok ? start[i] : 0;
-  }
-  const int32_t n_back = (int32_t)total[0], n_take = ok ? (int32_t)total[1] : 0, n_tok = ok ? (int32_t)total[2] : 0;
   if (tid == 0) {
     a.starts[a.n_seq] = n_tok;
-    *a.after = qzo_cache_state{ok ? n_free + n_back - n_take : n_free, n_tok, status, n_take};
+    *a.after = qzo_cache_state{n_free + n_back - n_take, n_tok, status, n_take};
   }
+  if (!ok) {
+    for (uint32_t t = tid; with_slots && t < a.max_tokens; t += PLAN_THREADS) { a.slots[t] = -1; a.positions[t] = 0; }
+    return;
+  }
+  __syncthreads();
   auto given = [&](int32_t r) {                  // r-th block given back
     const uint32_t s = last_not_above(back, a.n_seq, r);
     return a.tables[(uint64_t)s * a.max_blocks + (uint32_t)(r - back[s])];
@@ -108,27 +134,37 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs 
   auto taken = [&](int32_t k) {                  // k-th block taken: those given back lie on top of the free ones
     return k < n_back ? given(n_back - 1 - k) : a.free[n_free - 1 - (k - n_back)];
   };
-  if (ok) {
+  // a sequence's block number j, one that it held or one that it takes
+  auto block_of = [&](uint32_t i, int32_t j, int32_t held) { return j < held ? a.tables[(uint64_t)i * a.max_blocks + (uint32_t)j] : taken(take[i] + j - held); };
+  if (!(flag & 4u)) {
+    for (uint32_t i = first; i < last; ++i) {
+      const int32_t have = old_len[i], add = a.added[i], held = (int32_t)blocks(have);
+      int32_t number = -1, id = 0;
+      for (int32_t x = 0; x < add; ++x) {
+        const int32_t at = have + x, j = at >> shift;
+        if (j != number) {
+          id = per == 1 && j == held - 1 ? open : block_of(i, j, held);
+          number = j;
+          if (j >= held) a.tables[(uint64_t)i * a.max_blocks + (uint32_t)j] = id;
+        }
+        if (with_slots) { a.slots[start[i] + x] = (id << shift) + (at & mask); a.positions[start[i] + x] = at; }
+      }
+    }
+  } else {
     for (int32_t k = (int32_t)tid; k < n_take; k += PLAN_THREADS) {
       const uint32_t s = last_not_above(take, a.n_seq, k);
-      const uint32_t j = (uint32_t)((old_len[s] + mask) >> shift) + (uint32_t)(k - take[s]);
-      a.tables[(uint64_t)s * a.max_blocks + j] = taken(k);
+      a.tables[(uint64_t)s * a.max_blocks + (uint32_t)blocks(old_len[s]) + (uint32_t)(k - take[s])] = taken(k);
     }
-    for (int32_t r = (int32_t)tid; r < n_back - n_take; r += PLAN_THREADS) a.free[n_free + r] = given(r);
-  }
-  if (!with_slots) return;
-  for (uint32_t t = tid; t < a.max_tokens; t += PLAN_THREADS) {
-    int32_t slot = -1, at = 0;
-    if ((int32_t)t < n_tok) {
-      const uint32_t s = last_not_above(start, a.n_seq, (int32_t)t);
-      at = old_len[s] + (int32_t)t - start[s];
-      const int32_t j = at >> shift, held = (old_len[s] + mask) >> shift;
-      const int32_t id = j < held ? a.tables[(uint64_t)s * a.max_blocks + (uint32_t)j] : taken(take[s] + j - held);
-      slot = (id << shift) + (at & mask);
+    for (int32_t t = (int32_t)tid; with_slots && t < n_tok; t += PLAN_THREADS) {
+      const uint32_t s = last_not_above(start, a.n_seq, t);
+      const int32_t at = old_len[s] + t - start[s];
+      a.slots[t] = (block_of(s, at >> shift, (int32_t)blocks(old_len[s])) << shift) + (at & mask);
+      a.positions[t] = at;
     }
-    a.slots[t] = slot;
-    a.positions[t] = at;
   }
+  // (threads that had the least to do so far)
+  for (int32_t r = (int32_t)(PLAN_THREADS - 1 - tid); r < n_back - n_take; r += PLAN_THREADS) a.free[n_free + r] = given(r);
+  for (uint32_t t = (uint32_t)n_tok + tid; with_slots && t < a.max_tokens; t += PLAN_THREADS) { a.slots[t] = -1; a.positions[t] = 0; }
 }
 
 // Slots and positions of many tokens, from what cache_plan_kernel left.
@@ -171,97 +207,135 @@ hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t st) {
 // goes to fp32, so that far positions lose nothing.
 // DH/8 lanes hold a head, eight features each; a wavefront takes 64 / (DH/8) heads at a time and walks over its share of
 // the token's heads with the same angles.
-__device__ __forceinline__ float lanes_of_head_sum(float v, int dh) {
-  const int n = dh / 8;
-  for (int o = 1; o < n; o <<= 1) v += __shfl_xor(v, o, 64);
+//
+// Memory counts, and how much of it is on its way: a wavefront loads the heads of its next BATCH turns before it works on the
+// ones it has, and a token is spread over as many wavefronts as it takes to have WAVES of them.
+
+// Values of the lanes of a head (16, or 8): their sum; that of the lane half a head away.  Exchanges within rows of 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+template <int DH>
+__device__ __forceinline__ float sum_of_head(float v) {
+  v += from_lane<0xB1>(v);                      // quad_perm 1,0,3,2
+  v += from_lane<0x4E>(v);                      // quad_perm 2,3,0,1
+  v += from_lane<0x141>(v);                     // row_half_mirror: the other four of eight
+  if (DH == 128) v += from_lane<0x140>(v);      // row_mirror: the other eight of sixteen
   return v;
+}
+template <int DH>
+__device__ __forceinline__ float half_a_head_away(float v) {
+  if (DH == 128) return from_lane<0x128>(v);              // row_ror:8
+  return from_lane<0x1B>(from_lane<0x141>(v));            // mirrored in eight, then in four: four away
 }
 
 template <int DH>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a, RopeTurns turns, uint32_t parts) {
-  constexpr uint32_t LANES = DH / 8, HEADS = 64 / LANES;
+  constexpr uint32_t LANES = DH / 8, HEADS = 64 / LANES, BATCH = 4;
   const uint32_t lane = threadIdx.x & 63u, sub = lane % LANES;
-  const uint32_t w = blockIdx.x * 4u + (threadIdx.x >> 6), t = w / parts, part = w % parts;
+  const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4u + (threadIdx.x >> 6))), t = w / parts, part = w % parts;
   if (t >= a.n_tokens) return;
   int32_t slot = 0;
   if (a.slots) {
     slot = a.slots[t];
     if (slot < 0 || (uint32_t)slot >= a.n_slots) return;
   }
+  const uint32_t n_qk = a.q_heads + a.kv_heads, heads = n_qk + (a.cache_type ? a.kv_heads : 0u), turn = parts * HEADS;
+  const bf16_t* const row = a.qkv + (uint64_t)t * a.ld_qkv + sub * 8;
+  const uint32_t h0 = part * HEADS + lane / LANES;
+  // all lanes of a wavefront make the same number of turns; a head beyond the last is read as the last and not written
+  const uint32_t n_turns = (heads - part * HEADS + turn - 1) / turn;
+  uint4 raw[BATCH];
+  auto load = [&](uint32_t first) {
+#pragma unroll
+    for (uint32_t i = 0; i < BATCH; ++i) raw[i] = *reinterpret_cast<const uint4*>(row + (uint64_t)min(h0 + (first + i) * turn, heads - 1u) * DH);
+  };
+  load(0);
   const int32_t at = a.positions ? a.positions[t] : (int32_t)((t % a.pass_stride) % a.seq);
   float c[8], s[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     c[j] = 1.0f; s[j] = 0.0f;
     if (a.rope) {
-      const double turn = (double)at * turns.t[(sub * 8 + j) % (DH / 2)];
-      sincospif(2.0f * (float)(turn - rint(turn)), &s[j], &c[j]);
+      const double rev = (double)at * turns.t[(sub * 8 + j) % (DH / 2)];
+      sincospif(2.0f * (float)(rev - rint(rev)), &s[j], &c[j]);
       if (sub < LANES / 2) s[j] = -s[j];
     }
   }
-  const uint32_t heads = a.q_heads + a.kv_heads + (a.cache_type ? a.kv_heads : 0u);
-  for (uint32_t h = part * HEADS + lane / LANES; h < heads; h += parts * HEADS) {
-    const uint4 raw = *reinterpret_cast<const uint4*>(a.qkv + (uint64_t)t * a.ld_qkv + h * DH + sub * 8);
-    const uint32_t r[4] = {raw.x, raw.y, raw.z, raw.w};
-    float x[8];
+  const uint64_t slot_row = ((uint64_t)((uint32_t)slot >> a.block_shift) * a.kv_heads << a.block_shift) + ((uint32_t)slot & ((1u << a.block_shift) - 1u));
+  for (uint32_t first = 0; first < n_turns; first += BATCH) {
+    uint4 now[BATCH];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = __uint_as_float(r[j] << 16);
-      x[2 * j + 1] = __uint_as_float(r[j] & 0xffff0000u);
-    }
-    const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.kv_heads;
-    const bf16_t* gain = is_q ? a.q_gain : a.k_gain;
-    float ss = 0.0f;
+    for (uint32_t i = 0; i < BATCH; ++i) now[i] = raw[i];
+    if (first + BATCH < n_turns) load(first + BATCH);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ss = __builtin_fmaf(x[j], x[j], ss);
-    ss = lanes_of_head_sum(ss, DH);
-    if (!is_v && gain) {
-      const float inv = 1.0f / sqrtf(ss * (1.0f / DH) + a.eps);
-      const uint4 g4 = *reinterpret_cast<const uint4*>(gain + sub * 8);
-      const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
+    for (uint32_t i = 0; i < BATCH; ++i) {
+      const uint32_t h = h0 + (first + i) * turn;
+      if (first + i >= n_turns) break;
+      const uint32_t r[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+      float x[8], y[8];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[2 * j] *= inv * __uint_as_float(g[j] << 16);
-        x[2 * j + 1] *= inv * __uint_as_float(g[j] & 0xffff0000u);
+        x[2 * j] = __uint_as_float(r[j] << 16);
+        x[2 * j + 1] = __uint_as_float(r[j] & 0xffff0000u);
       }
-    }
-    float y[8];
+      const bool is_q = h < a.q_heads, is_v = h >= n_qk;
+      const bf16_t* gain = is_q ? a.q_gain : is_v ? nullptr : a.k_gain;
+      if (a.q_gain || a.k_gain) {                     // uniform
+        float ss = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float other = __shfl_xor(x[j], LANES / 2, 64);
-      y[j] = is_v ? x[j] : __builtin_fmaf(other, s[j], x[j] * c[j]);
-    }
-    if (is_q || !a.cache_type) {
-      *reinterpret_cast<uint4*>(a.out + (uint64_t)t * a.ld_out + h * DH + sub * 8) =
-          make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-      continue;
-    }
-    const uint32_t kh = h - a.q_heads - (is_v ? a.kv_heads : 0u);
-    const uint64_t row = (((uint64_t)((uint32_t)slot >> a.block_shift) * a.kv_heads + kh) << a.block_shift) + ((uint32_t)slot & ((1u << a.block_shift) - 1u));
-    unsigned char* pool = (unsigned char*)(is_v ? a.v : a.k);
-    if (a.cache_type == 1) {
-      *reinterpret_cast<uint4*>(pool + row * (DH * 2) + sub * 16) =
-          make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-    } else {
-      const float* scale = is_v ? a.v_scale : a.k_scale;
-      const float inv = scale ? 1.0f / scale[kh] : 1.0f;
+        for (int j = 0; j < 8; ++j) ss = __builtin_fmaf(x[j], x[j], ss);
+        const float inv = __builtin_amdgcn_rsqf(sum_of_head<DH>(ss) * (1.0f / DH) + a.eps);
+        if (gain) {
+          const uint4 g4 = *reinterpret_cast<const uint4*>(gain + sub * 8);
+          const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = to_e4m3_range(y[j] * inv);
-      *reinterpret_cast<uint2*>(pool + row * DH + sub * 8) = make_uint2(pack_e4m3x4(y[0], y[1], y[2], y[3]), pack_e4m3x4(y[4], y[5], y[6], y[7]));
+          for (int j = 0; j < 4; ++j) {
+            x[2 * j] *= inv * __uint_as_float(g[j] << 16);
+            x[2 * j + 1] *= inv * __uint_as_float(g[j] & 0xffff0000u);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float other = half_a_head_away<DH>(x[j]);
+        y[j] = is_v || !a.rope ? x[j] : __builtin_fmaf(other, s[j], x[j] * c[j]);
+      }
+      if (h >= heads) continue;
+      if (is_q || !a.cache_type) {
+        *reinterpret_cast<uint4*>(a.out + (uint64_t)t * a.ld_out + (uint64_t)h * DH + sub * 8) =
+            make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+        continue;
+      }
+      const uint32_t kh = h - (is_v ? n_qk : a.q_heads);
+      const uint64_t at_row = slot_row + ((uint64_t)kh << a.block_shift);
+      unsigned char* pool = (unsigned char*)(is_v ? a.v : a.k);
+      if (a.cache_type == 1) {
+        *reinterpret_cast<uint4*>(pool + at_row * (DH * 2) + sub * 16) =
+            make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+      } else {
+        const float* scale = is_v ? a.v_scale : a.k_scale;
+        const float inv = scale ? 1.0f / scale[kh] : 1.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = to_e4m3_range(y[j] * inv);
+        *reinterpret_cast<uint2*>(pool + at_row * DH + sub * 8) = make_uint2(pack_e4m3x4(y[0], y[1], y[2], y[3]), pack_e4m3x4(y[4], y[5], y[6], y[7]));
+      }
     }
   }
 }
 
+constexpr uint32_t QK_WAVES = 16384;
 hipError_t launch_qk_norm_rope(const QkArgs& a, uint32_t head_dim, double theta, hipStream_t st) {
   if (a.n_tokens == 0) return hipSuccess;
   RopeTurns turns = {};
   for (uint32_t i = 0; a.rope && i < head_dim / 2; ++i)
     turns.t[i] = std::pow(theta, -2.0 * i / head_dim) * 0.15915494309189533577;      // 1 / 2 pi
   const uint32_t heads = a.q_heads + a.kv_heads * (a.cache_type ? 2u : 1u), per = 512 / head_dim, groups = (heads + per - 1) / per;
-  const uint32_t parts = std::max(1u, std::min(groups, 4096u / a.n_tokens));
-  const uint32_t wgs = (uint32_t)(((uint64_t)a.n_tokens * parts + 3) / 4);
-  if (head_dim == 128) qk_norm_rope_kernel<128><<<wgs, 256, 0, st>>>(a, turns, parts);
-  else qk_norm_rope_kernel<64><<<wgs, 256, 0, st>>>(a, turns, parts);
+  const uint32_t parts = std::max(1u, std::min(groups, QK_WAVES / a.n_tokens));
+  const uint64_t wgs = ((uint64_t)a.n_tokens * parts + 3) / 4;
+  if (head_dim == 128) qk_norm_rope_kernel<128><<<(uint32_t)wgs, 256, 0, st>>>(a, turns, parts);
+  else qk_norm_rope_kernel<64><<<(uint32_t)wgs, 256, 0, st>>>(a, turns, parts);
   return hipGetLastError();
 }
 

@@ -25,19 +25,34 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+typedef const int32_t __attribute__((address_space(4)))* table_t;      // read by scalar loads: no vector load in between
 
-// How the work is dealt out.  A group is a column tile of one sequence and key head; it has units of 128 keys, and SETUP more
-// that stand for what a group costs apart from its keys.  All groups' units are counted through, and workgroup b takes units
-// b per .. (b + 1) per - 1: every workgroup the same share, whatever the lengths.  A group that lies in one workgroup's share
-// is written by it; otherwise each leaves (maximum, sum, accumulators) in the scratch, its first group's in place 2 b, a later
-// one's (only the last can go on) in 2 b + 1, and who finds the group's counter at its last piece adds them up, in order.  The
-// counter (that of the workgroup of the group's first piece) goes back to zero for the next call.
-constexpr uint32_t UNIT = 128, COLS = 16, WAVES = 4, MAX_WGS = 512;
-constexpr uint32_t SETUP = 2, MIN_SHARE = 6;
+// How the work is dealt out.  A group is 16 columns of one sequence and key head; the four wavefronts of a workgroup take every
+// fourth step (32 keys) of it, a unit is a step of each, 128 keys.  With much to do (WIDE_UNITS), a group of a sequence of more
+// than 32 columns (several new tokens) is 64 of them, 16 a wavefront, all with the same keys; a unit is then 32 keys.  It reads
+// the keys once for the four, but has a quarter of the loads on their way.  16 columns / 64 columns, us: 16 prompts of 512
+// tokens, 32 heads of 128 (34816 units of 16 columns) 351 / 212; 6 x 100 tokens behind 1900, heads of 128 (21504) 194 / 144, of
+// 64 95 / 81; behind 900 on average (11300) 51 / 55; 4 x 8 tokens, 64 heads on 8, behind 9000 (9088) 62 / 89; one prompt of
+// 512 (4096) 32 / 43.
+//   Every group is given a span, its units behind some padding, all spans are counted through, and workgroup b takes those from
+// share b to share (b + 1) - 1.
+//   Few groups: the shortest piece that leaves no more pieces than workgroups is the share, and a span is a multiple of it, so
+//     that every workgroup has one piece of one group, or nothing.
+//   Otherwise: even shares whatever the lengths, a group's padding being SETUP, which stands for what a group costs apart from its
+//     keys; a group no longer than an eighth of a share is not cut but belongs to whom its first unit falls to.
+// A group that lies in one workgroup is written by it; otherwise each leaves (maximum, sum, accumulators) in the scratch, its
+// first group's in place 2 b, a later one's (only the last can go on) in 2 b + 1, and who finds the group's counter at its last
+// piece adds them up, in order.  The counter (that of the workgroup of the group's first piece) goes back to zero.
+constexpr uint32_t COLS = 16, WAVES = 4, MAX_WGS = 512;
+constexpr uint32_t SETUP = 1, MIN_PIECE = 2, WIDE_UNITS = 12288;
 
-struct SeqWork { uint32_t row0, rows, len, units, tiles; };
+struct SeqWork {
+  uint32_t row0, rows, len, units, tiles, wide;
+  __device__ __forceinline__ uint32_t unit() const { return wide ? 32u : 128u; }                // keys
+  __device__ __forceinline__ uint32_t cols() const { return wide ? COLS * WAVES : COLS; }
+};
 
-__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i) {
+__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool wide) {
   SeqWork w;
   w.row0 = i; w.rows = i < a.n_rows ? 1u : 0u;
   if (a.starts) {
@@ -45,14 +60,27 @@ __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i) {
     w.row0 = (uint32_t)s0; w.rows = (uint32_t)(s1 - s0);
   }
   w.len = (uint32_t)min(max(a.lengths[i], 0), (int32_t)(a.max_blocks << a.block_shift));
-  w.units = max(1u, (w.len + UNIT - 1) / UNIT);
-  w.tiles = (uint32_t)(((uint64_t)w.rows * a.group + COLS - 1) / COLS);
+  const uint64_t cols = (uint64_t)w.rows * a.group;
+  w.wide = wide && cols > 2 * COLS;
+  w.units = max(1u, (w.len + w.unit() - 1) / w.unit());
+  w.tiles = (uint32_t)((cols + w.cols() - 1) / w.cols());
   return w;
 }
 
 // What all lanes agree on, in a scalar register.
 __device__ __forceinline__ uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 __device__ __forceinline__ uint64_t scalar64(uint64_t x) { return (uint64_t)scalar((uint32_t)(x >> 32)) << 32 | scalar((uint32_t)x); }
+
+// Inclusive sum over the lanes: within rows of 16, then rows 0 and 2 into 1 and 3, then both into the upper half.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);       // row_shr:1, 2, 4, 8
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);       // row_bcast:15
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);       // row_bcast:31
+  return v;
+}
 
 // Two floats for another workgroup, on any XCD: stored through the L2 and loaded past it (agent scope), so that no L2 has to be
 // written back or invalidated as a whole, which a fence of that scope does (64 ragged sequences: 366 us with fences).  A
@@ -112,20 +140,19 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t x) {
   return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
 }
 
-// KP: pairs of key tiles a step.
-template <int DH, bool E4M3, int KP>
+// A step: 32 keys, two tiles.
+template <int DH, bool E4M3>
 struct PagedStep {
   static constexpr int KL = E4M3 ? DH / 64 : DH / 32;      // 16-byte loads a key tile takes
   static constexpr int VD = E4M3 ? DH / 64 : DH / 32;      // dwords of a row of V that a lane holds
-  u32x4v k[KP][2][KL];
-  uint32_t v[KP][8][VD];
+  u32x4v k[2][KL];
+  uint32_t v[8][VD];
 };
 
-template <int DH, bool E4M3, int KP>
-__global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, uint32_t* counters, float* parts, uint32_t part_cols) {
+template <int DH, bool E4M3>
+__global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, uint32_t* counters, float* parts, uint32_t part_cols, uint32_t few, uint32_t may_be_wide) {
   constexpr int KS = DH / 32, VW = DH / 16, ES = E4M3 ? 1 : 2;
-  constexpr uint32_t STEP = 32 * KP, ROUND = STEP * WAVES;
-  typedef PagedStep<DH, E4M3, KP> Step;
+  typedef PagedStep<DH, E4M3> Step;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   float* const sum_acc = (float*)lds;                                   // [WAVES][COLS][DH + 4]
   float* const sum_m = sum_acc + WAVES * COLS * (DH + 4);               // [WAVES][COLS]
@@ -136,40 +163,74 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
   const uint32_t col = lane & 15u, g = lane >> 4;
 
   // ---- the sequences' units: up to 64 sequences in the lanes of every wavefront, more in the LDS
-  const bool few = a.n_seq <= 64;
-  uint64_t total, mine = 0;
-  SeqWork lane_work = {0, 0, 0, 1, 0};
+  const uint32_t per = (a.n_seq + 255) / 256, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
+  SeqWork lane_work = {0, 0, 0, 1, 0, 0};
+  if (few && lane < a.n_seq) lane_work = seq_work(a, lane, false);
+  bool wide = false;
+  auto sum = [&](auto&& f) -> uint64_t {            // of f over the sequences
+    if (few) return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan((uint32_t)f(lane_work)), 63);
+    uint64_t n = 0, all;
+    for (uint32_t i = s_first; i < s_last; ++i) n += f(seq_work(a, i, wide));
+    block_scan(n, &all, red);
+    return scalar64(all);
+  };
+  auto groups_of = [&](const SeqWork& w) { return (uint64_t)w.tiles * a.kv_heads; };
+  auto units_of = [&](const SeqWork& w) { return w.units * groups_of(w); };
+  uint64_t groups = sum(groups_of), units = sum(units_of);
+  if (may_be_wide && units >= WIDE_UNITS) {
+    wide = true;
+    if (few && lane < a.n_seq) lane_work = seq_work(a, lane, true);
+    groups = sum(groups_of); units = sum(units_of);
+  }
+  uint32_t piece = 0;                               // 0: even shares
+  if (groups <= gridDim.x) {
+    // Alone on its compute unit a workgroup takes 1.2 us a unit (heads of 128, bf16), the join of a cut group 3 to 4: pieces of
+    // 2 units, but groups of up to 4 uncut.  One sequence, pieces of 1 / 2 / 3 / 4 units: 32 heads, 500 tokens 10.4 / 10.8 /
+    // 11.8 / 10.5 us (heads of 64: 8.7 / 9.1 / 9.7 / 7.6), 1000 13.7 / 12.0 / 12.3 / 13.1, 4000 18.7 / 18.8 / 22.0 / 23.1; 8 key
+    // heads, 4000 15.5 / 12.6 / 12.7 / 13.5, 16000 22.8 / 22.8 / 24.9 / 24.6.
+    const uint32_t short_one = units <= 4 * groups ? 4u : MIN_PIECE;
+    const uint32_t least = scalar(max(short_one, (uint32_t)((units + gridDim.x - 1) / gridDim.x))), more = max(1u, least / 16);
+    for (uint32_t p = least; p < least + 3 * more && !piece; p += more)
+      if (sum([&](const SeqWork& w) { return (w.units + p - 1) / p * groups_of(w); }) <= gridDim.x) piece = p;
+  }
+  auto span_of = [&](const SeqWork& w) { return piece ? (w.units + piece - 1) / piece * piece : w.units + SETUP; };
+  uint64_t total;
+  uint32_t mine = 0;
   if (few) {
-    uint64_t n = 0;
-    if (lane < a.n_seq) {
-      lane_work = seq_work(a, lane);
-      n = (uint64_t)(lane_work.units + SETUP) * lane_work.tiles * a.kv_heads;
-    }
-    uint64_t s = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t u = __shfl_up(s, o, 64);
-      if (lane >= (uint32_t)o) s += u;
-    }
-    total = __shfl(s, 63, 64);
-    mine = s - n;
+    const uint32_t n = (uint32_t)(span_of(lane_work) * groups_of(lane_work)), upto = wave_scan(n);
+    mine = upto - n;
+    total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   } else {
-    const uint32_t per = (a.n_seq + 255) / 256, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
     uint64_t n = 0;
     for (uint32_t i = s_first; i < s_last; ++i) {
-      const SeqWork w = seq_work(a, i);
+      const SeqWork w = seq_work(a, i, wide);
       first_unit[i] = n;
-      n += (uint64_t)(w.units + SETUP) * w.tiles * a.kv_heads;
+      n += span_of(w) * groups_of(w);
     }
     const uint64_t before = block_scan(n, &total, red);
     for (uint32_t i = s_first; i < s_last; ++i) first_unit[i] += before;
     __syncthreads();
+    total = scalar64(total);
   }
-  total = scalar64(total);
-  const uint64_t share = max((uint64_t)MIN_SHARE, (total + gridDim.x - 1) / gridDim.x);
-  // neighbours (the column tiles of the same keys) on one XCD; the grid is a multiple of 8
-  const uint32_t wg = (blockIdx.x & 7u) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  const uint64_t share = piece ? piece : (total + gridDim.x - 1) / gridDim.x;
+  const uint32_t keep = piece ? 0u : (uint32_t)min(share / 8, (uint64_t)1 << 30);
+  // those who have a share are spread over the XCDs, neighbours (the columns of the same keys) on one
+  const uint32_t busy = scalar((uint32_t)((total + share - 1) / max(share, (uint64_t)1)) + 7u) / 8u * 8u;      // grid: a multiple of 8
+  if (blockIdx.x >= busy) return;
+  const uint32_t wg = (blockIdx.x & 7u) * (busy >> 3) + (blockIdx.x >> 3);
   const uint64_t begin = share * wg, end = min(begin + share, total);
+
+  // the cut groups of this workgroup: the one that its share begins with, the one that it ends with
+  struct Cut { uint32_t row0, group_col, kh, n_cols, wg_first, pieces, first_place; };
+  Cut cut[2] = {};
+  constexpr uint32_t DV = DH / 4, STRIDE = DH + 4;
+  auto part_of = [&](uint32_t place) { return parts + (uint64_t)place * part_cols * STRIDE; };
+  auto put = [&](uint32_t row0, uint32_t group_col, uint32_t kh, uint32_t c, uint32_t d, const Joined& j) {       // a column that saw nothing: zero
+    const float inv = (E4M3 && a.v_scale ? a.v_scale[kh] : 1.0f) / j.l;
+    const uint32_t f = group_col + c;
+    bf16_t* to = a.out + (uint64_t)(row0 + f / a.group) * a.ld_out + (uint64_t)(kh * a.group + f % a.group) * DH + d;
+    *reinterpret_cast<uint2*>(to) = j.l == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(j.o[0] * inv, j.o[1] * inv), pack_bf16x2(j.o[2] * inv, j.o[3] * inv));
+  };
 
   for (uint64_t unit = begin; unit < end;) {
     uint32_t seq;
@@ -177,11 +238,10 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
     SeqWork w;
     if (few) {
       // prefixes ascend and begin at 0: the last one not above is the sequence that has the unit
-      seq = scalar((uint32_t)__popcll(__ballot(lane < a.n_seq && mine <= unit)) - 1u);
-      seq_first = (uint64_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, (int)seq) & 0xffffffffu;
-      seq_first |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), (int)seq) << 32;
+      seq = scalar((uint32_t)__popcll(__ballot(lane < a.n_seq && mine <= (uint32_t)unit)) - 1u);
       auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)seq); };
-      w = {of(lane_work.row0), of(lane_work.rows), of(lane_work.len), of(lane_work.units), of(lane_work.tiles)};
+      seq_first = of(mine);
+      w = {of(lane_work.row0), of(lane_work.rows), of(lane_work.len), of(lane_work.units), of(lane_work.tiles), of(lane_work.wide)};
     } else {
       uint32_t lo = 0, hi = a.n_seq;
       while (hi - lo > 1) {
@@ -190,32 +250,40 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
       }
       seq = scalar(lo);
       seq_first = scalar64(first_unit[seq]);
-      w = seq_work(a, seq);
-      w = {scalar(w.row0), scalar(w.rows), scalar(w.len), scalar(w.units), scalar(w.tiles)};
+      w = seq_work(a, seq, wide);
+      w = {scalar(w.row0), scalar(w.rows), scalar(w.len), scalar(w.units), scalar(w.tiles), scalar(w.wide)};
     }
-    const uint32_t span = w.units + SETUP;
+    const uint32_t span = scalar(span_of(w)), pad = span - w.units;
     const uint64_t r = unit - seq_first;
     const uint32_t group = scalar((r >> 32) ? (uint32_t)(r / span) : (uint32_t)r / span);
     const uint32_t tile = scalar(group % w.tiles), kh = scalar(group / w.tiles);
-    const uint32_t at = scalar((uint32_t)(r - (uint64_t)group * span));                     // within the group, SETUP first
-    const uint32_t n_units = scalar((uint32_t)min((uint64_t)(span - at), end - unit));
-    const uint64_t group_first = unit - at + SETUP, group_last = unit - at + span - 1;
+    const uint32_t at = scalar((uint32_t)(r - (uint64_t)group * span));                     // within the span
+    const bool uncut = span <= keep;
+    if (uncut && at) { unit += span - at; continue; }
+    const uint32_t n_units = uncut ? span : scalar((uint32_t)min((uint64_t)(span - at), end - unit));
+    const uint64_t group_first = unit - at + pad, group_last = unit - at + span - 1;
     const bool at_begin = unit == begin;
     unit += n_units;
-    if (at + n_units <= SETUP) continue;
-    const uint32_t u_first = max(at, SETUP) - SETUP, u_end = at + n_units - SETUP;
-    const uint32_t wg_first = group_first >= begin ? wg : wg - scalar((uint32_t)((begin - group_first + share - 1) / share));
-    const uint32_t wg_last = group_last < end ? wg : wg + scalar((uint32_t)((group_last - end) / share)) + 1u, pieces = wg_last - wg_first + 1u;
+    if (at + n_units <= pad) continue;
+    const uint32_t u_first = max(at, pad) - pad, u_end = at + n_units - pad;
+    uint32_t wg_first = wg, pieces = 1;
+    if (!uncut) {
+      if (group_first < begin) wg_first = wg - scalar((uint32_t)((begin - group_first + share - 1) / share));
+      pieces = wg + 1u - wg_first;
+      if (group_last >= end) pieces += scalar((uint32_t)((group_last - end) / share)) + 1u;
+    }
 
-    // ---- this tile's columns
-    const uint32_t flat = tile * COLS + col, token = flat / a.group, head = kh * a.group + flat % a.group;
-    const uint32_t n_cols = min(COLS, w.rows * a.group - tile * COLS);
+    // ---- this wavefront's columns
+    const uint32_t all_cols = w.rows * a.group, group_col = tile * w.cols(), n_group = min(w.cols(), all_cols - group_col);
+    const uint32_t first_col = group_col + (w.wide ? wave * COLS : 0u), n_cols = first_col < all_cols ? min(COLS, all_cols - first_col) : 0u;
     const bool live = col < n_cols;
-    const uint64_t row = w.row0 + (live ? token : 0u);
-    const int32_t sees = live ? (int32_t)(w.len + token + 1u - w.rows) : 0;                  // positions that the column sees
-    const int32_t least = (int32_t)(w.len + tile * COLS / a.group + 1u - w.rows);             // the first column's, the fewest
-    const int32_t most = (int32_t)(w.len + (tile * COLS + n_cols - 1) / a.group + 1u - w.rows);
-    const int32_t k_first = (int32_t)(u_first * UNIT), k_end = (int32_t)min((int64_t)most, (int64_t)u_end * UNIT);
+    const uint32_t flat = live ? first_col + col : group_col, token = flat / a.group, head = kh * a.group + flat % a.group;
+    const uint64_t row = w.row0 + token;
+    // positions that a column sees, that the first (the fewest) and the last (the most) of them see
+    const int32_t sees = live ? (int32_t)(w.len + token + 1u - w.rows) : 0;
+    const int32_t least = (int32_t)(w.len + first_col / a.group + 1u - w.rows);
+    const int32_t most = n_cols ? (int32_t)(w.len + (first_col + n_cols - 1) / a.group + 1u - w.rows) : 0;
+    const int32_t k_first = (int32_t)(u_first * w.unit()), k_end = (int32_t)min((int64_t)most, (int64_t)u_end * w.unit());
 
     bf16x8 q[KS];
 #pragma unroll
@@ -233,94 +301,74 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
     for (int i = 0; i < VW; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
 
-    // ---- where the keys are: 64 entries of the table in a register
-    const int32_t* const table = a.tables + (uint64_t)seq * a.max_blocks;
+    // ---- where the keys are: a block id per tile, in scalar registers, a step ahead of the loads that need it
+    const table_t table = (table_t)(uintptr_t)(a.tables + (uint64_t)seq * a.max_blocks);
     const uint32_t in_block = (1u << a.block_shift) - 1u;
-    uint32_t held = 0xffffffffu;      // first entry of the 64
-    int32_t entries = -1;
-    auto block_of = [&](uint32_t pos) -> uint32_t {
-      const uint32_t b = pos >> a.block_shift;
-      if ((b & ~63u) != held) {
-        held = b & ~63u;
-        entries = held + lane < a.max_blocks ? table[held + lane] : -1;
-      }
-      return (uint32_t)__builtin_amdgcn_readlane(entries, (int)(b & 63u));
+    const int32_t last_tile = max(k_end - 1, 0) & ~15;       // steps beyond the end load it again (a branch around loads would have
+                                                             // every wait count as if they had not been issued)
+    struct Ids { uint32_t id[2]; };
+    auto blocks = [&](int32_t kb) {
+      return Ids{{(uint32_t)table[(uint32_t)min(kb, last_tile) >> a.block_shift], (uint32_t)table[(uint32_t)min(kb + 16, last_tile) >> a.block_shift]}};
     };
-    const int32_t last_tile = (k_end - 1) & ~15;
     // Loads a step's keys and values; returns a bit per tile, whether its block is in the pool.
-    auto load = [&](Step& st, int32_t kb) -> uint32_t {
+    auto load = [&](Step& st, int32_t kb, const Ids& ids) -> uint32_t {
       uint32_t there = 0;
 #pragma unroll
-      for (int p = 0; p < KP; ++p) {
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t pos = (uint32_t)min(kb + t * 16, last_tile);
+        const bool in = ids.id[t] < a.n_blocks;
+        there |= (in ? 1u : 0u) << t;
+        const uint32_t id = in ? ids.id[t] : 0u;
+        const uint64_t at = ((((uint64_t)id * a.kv_heads + kh) << a.block_shift) + (pos & in_block)) * (uint64_t)(DH * ES);
+        const unsigned char* kp = (const unsigned char*)a.k + at;
+        const unsigned char* vp = (const unsigned char*)a.v + at;
+        const uint32_t ko = col * (DH * ES) + g * 16u;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const uint32_t pos = (uint32_t)min(kb + p * 32 + t * 16, last_tile);
-          uint32_t id = block_of(pos);
-          const bool in = id < a.n_blocks;
-          there |= (in ? 1u : 0u) << (2 * p + t);
-          id = in ? id : 0u;
-          const uint64_t at = ((((uint64_t)id * a.kv_heads + kh) << a.block_shift) + (pos & in_block)) * (uint64_t)(DH * ES);
-          const unsigned char* kp = (const unsigned char*)a.k + at;
-          const unsigned char* vp = (const unsigned char*)a.v + at;
-          const uint32_t ko = col * (DH * ES) + g * 16u;
+        for (int s = 0; s < Step::KL; ++s) st.k[t][s] = *reinterpret_cast<const u32x4v*>(kp + (ko + (uint32_t)s * 64u));
 #pragma unroll
-          for (int s = 0; s < Step::KL; ++s) st.k[p][t][s] = *reinterpret_cast<const u32x4v*>(kp + (ko + (uint32_t)s * 64u));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t vo = (4u * g + (uint32_t)j) * (DH * ES) + col * (VW * ES);
-            if constexpr (Step::VD == 4) {
-              const uint4 x = *reinterpret_cast<const uint4*>(vp + vo);
-              uint32_t* o = st.v[p][4 * t + j];
-              o[0] = x.x; o[1] = x.y; o[2] = x.z; o[3] = x.w;
-            } else if constexpr (Step::VD == 2) {
-              const uint2 x = *reinterpret_cast<const uint2*>(vp + vo);
-              st.v[p][4 * t + j][0] = x.x; st.v[p][4 * t + j][1] = x.y;
-            } else {
-              st.v[p][4 * t + j][0] = *reinterpret_cast<const uint32_t*>(vp + vo);
-            }
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t vo = (4u * g + (uint32_t)j) * (DH * ES) + col * (VW * ES);
+          uint32_t* o = st.v[4 * t + j];
+          if constexpr (Step::VD == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(vp + vo);
+            o[0] = x.x; o[1] = x.y; o[2] = x.z; o[3] = x.w;
+          } else if constexpr (Step::VD == 2) {
+            const uint2 x = *reinterpret_cast<const uint2*>(vp + vo);
+            o[0] = x.x; o[1] = x.y;
+          } else {
+            o[0] = *reinterpret_cast<const uint32_t*>(vp + vo);
           }
         }
       }
       return there;
     };
 
-    auto key_of = [&](int32_t kb, int p, int j) { return kb + p * 32 + (j >> 2) * 16 + (int32_t)(4u * g) + (j & 3); };
+    auto key_of = [&](int32_t kb, int j) { return kb + (j >> 2) * 16 + (int32_t)(4u * g) + (j & 3); };
     auto work = [&](Step& st, int32_t kb, uint32_t there) {
-      const bool whole = kb + (int32_t)STEP <= least && there == (1u << (2 * KP)) - 1u;
-      f32x4 s[KP][2];
+      const bool whole = kb + 32 <= least && there == 3u;
+      f32x4 s[2];
 #pragma unroll
-      for (int p = 0; p < KP; ++p)
+      for (int t = 0; t < 2; ++t) {
+        f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int i = 0; i < KS; ++i) {
-            u32x4v x;
-            if constexpr (E4M3) {
-              const u32x4v raw = st.k[p][t][i / 2];
-              const uint32_t r0 = raw[2 * (i & 1)], r1 = raw[2 * (i & 1) + 1];
-              x = u32x4v{two_bf16(r0, false), two_bf16(r0, true), two_bf16(r1, false), two_bf16(r1, true)};
-            } else {
-              x = st.k[p][t][i];
-            }
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[i], c, 0, 0, 0);
+        for (int i = 0; i < KS; ++i) {
+          u32x4v x;
+          if constexpr (E4M3) {
+            const uint32_t r0 = st.k[t][i / 2][2 * (i & 1)], r1 = st.k[t][i / 2][2 * (i & 1) + 1];
+            x = u32x4v{two_bf16(r0, false), two_bf16(r0, true), two_bf16(r1, false), two_bf16(r1, true)};
+          } else {
+            x = st.k[t][i];
           }
-          s[p][t] = c * ks;
+          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[i], c, 0, 0, 0);
         }
+        s[t] = c * ks;
+      }
       if (!whole) {
 #pragma unroll
-        for (int p = 0; p < KP; ++p)
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (key_of(kb, p, 4 * t + j) >= sees || !(there >> (2 * p + t) & 1u)) s[p][t][j] = -INFINITY;
+        for (int j = 0; j < 8; ++j)
+          if (key_of(kb, j) >= sees || !(there >> (j >> 2) & 1u)) s[j >> 2][j & 3] = -INFINITY;
       }
-      float top = -INFINITY;
-#pragma unroll
-      for (int p = 0; p < KP; ++p)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) top = fmaxf(fmaxf(fmaxf(s[p][t][0], s[p][t][1]), fmaxf(s[p][t][2], s[p][t][3])), top);
+      float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
       if (__any(top > m + 8.0f)) {           // m = -infinity: any key at all
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -331,85 +379,87 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
         m = m2;
       }
       const float base = m == -INFINITY ? 0.0f : m;
+      float e[8];
 #pragma unroll
-      for (int p = 0; p < KP; ++p) {
-        float e[8];
+      for (int j = 0; j < 8; ++j) {
+        e[j] = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - base);
+        l += e[j];
+      }
+      // p as bf16: 2^-8 of each term at most, in a sum of many; v has no more bits either
+      const bf16x8 pk = __builtin_bit_cast(bf16x8, u32x4v{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])});
+      bool apart = false;
+      if (!whole) {
+        // 0 times what an unseen value holds is no 0 where that is NaN or infinite: nobody's positions become 0, and where
+        // one that only some of the columns see is not finite, every column has its own product
+        uint32_t odd = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          e[j] = __builtin_amdgcn_exp2f(s[p][j >> 2][j & 3] - base);
-          l += e[j];
-        }
-        // p as bf16: 2^-8 of each term at most, in a sum of many; v has no more bits either
-        const bf16x8 pk = __builtin_bit_cast(bf16x8, u32x4v{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])});
-        bool apart = false;
-        if (!whole) {
-          // 0 times what an unseen value holds is no 0 where that is NaN or infinite: nobody's positions become 0, and where
-          // one that only some of the columns see is not finite, every column has its own product
-          uint32_t odd = 0;
+          const int32_t key = key_of(kb, j);
+          const bool seen = key < most && (there >> (j >> 2) & 1u);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int32_t key = key_of(kb, p, j);
-            const bool seen = key < most && (there >> (2 * p + (j >> 2)) & 1u);
-#pragma unroll
-            for (int u = 0; u < Step::VD; ++u) {
-              const uint32_t y = seen ? st.v[p][j][u] : 0u;
-              st.v[p][j][u] = y;
-              if (key >= least) odd |= not_finite<E4M3>(y);
-            }
+          for (int u = 0; u < Step::VD; ++u) {
+            const uint32_t y = seen ? st.v[j][u] : 0u;
+            st.v[j][u] = y;
+            if (key >= least) odd |= not_finite<E4M3>(y);
           }
-          apart = least < most && __any(odd != 0);
         }
-        // features 2 u and 2 u + 1 of a lane's VW: eight keys of two columns, two operands
-        auto products = [&](int u, const uint32_t (&y)[8], f32x4& even, f32x4& uneven) {
-          u32x4v lo, hi;
+        apart = least < most && __any(odd != 0);
+      }
+      // features 2 u and 2 u + 1 of a lane's VW: eight keys of two columns, two operands
+      auto products = [&](int u, const uint32_t (&y)[8], f32x4& even, f32x4& uneven) {
+        u32x4v lo, hi;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            lo[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x05040100u);
-            hi[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x07060302u);
-          }
-          even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pk, acc[2 * u], 0, 0, 0);
-          uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pk, acc[2 * u + 1], 0, 0, 0);
-        };
-        auto value = [&](int j, int u) { return E4M3 ? two_bf16(st.v[p][j][u / 2], u & 1) : st.v[p][j][u % Step::VD]; };
-        if (!apart) {
+        for (int j = 0; j < 4; ++j) {
+          lo[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x05040100u);
+          hi[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x07060302u);
+        }
+        even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pk, acc[2 * u], 0, 0, 0);
+        uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pk, acc[2 * u + 1], 0, 0, 0);
+      };
+      auto value = [&](int j, int u) { return E4M3 ? two_bf16(st.v[j][u / 2], u & 1) : st.v[j][u % Step::VD]; };
+      if (!apart) {
+#pragma unroll
+        for (int u = 0; u < VW / 2; ++u) {
+          uint32_t y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = value(j, u);
+          products(u, y, acc[2 * u], acc[2 * u + 1]);
+        }
+      } else {
+#pragma unroll 1
+        for (uint32_t c = 0; c < COLS; ++c) {
+          const int32_t its = __builtin_amdgcn_readlane(sees, (int)c);
 #pragma unroll
           for (int u = 0; u < VW / 2; ++u) {
             uint32_t y[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = value(j, u);
-            products(u, y, acc[2 * u], acc[2 * u + 1]);
-          }
-        } else {
-#pragma unroll 1
-          for (uint32_t c = 0; c < n_cols; ++c) {
-            const int32_t its = __builtin_amdgcn_readlane(sees, (int)c);
-#pragma unroll
-            for (int u = 0; u < VW / 2; ++u) {
-              uint32_t y[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = key_of(kb, p, j) < its ? value(j, u) : 0u;
-              f32x4 even, uneven;
-              products(u, y, even, uneven);
-              if (col == c) { acc[2 * u] = even; acc[2 * u + 1] = uneven; }
-            }
+            for (int j = 0; j < 8; ++j) y[j] = key_of(kb, j) < its ? value(j, u) : 0u;
+            f32x4 even, uneven;
+            products(u, y, even, uneven);
+            if (col == c) { acc[2 * u] = even; acc[2 * u + 1] = uneven; }
           }
         }
       }
     };
 
     // ---- the keys, a step at a time, the next one's on their way meanwhile
-    int32_t kb = k_first + (int32_t)(wave * STEP);
+    const int32_t round = w.wide ? 32 : 128;
+    int32_t kb = k_first + (w.wide ? 0 : (int32_t)(wave * 32u));
     if (kb < k_end) {
       Step one, two;
-      uint32_t in_one = load(one, kb), in_two = 0;
+      Ids next = blocks(kb);
+      uint32_t in_one = load(one, kb, next), in_two;
+      next = blocks(kb + round);
       while (true) {
-        if (kb + (int32_t)ROUND < k_end) in_two = load(two, kb + (int32_t)ROUND);
+        in_two = load(two, kb + round, next);
+        next = blocks(kb + 2 * round);
         work(one, kb, in_one);
-        kb += (int32_t)ROUND;
+        kb += round;
         if (kb >= k_end) break;
-        if (kb + (int32_t)ROUND < k_end) in_one = load(one, kb + (int32_t)ROUND);
+        in_one = load(one, kb + round, next);
+        next = blocks(kb + 2 * round);
         work(two, kb, in_two);
-        kb += (int32_t)ROUND;
+        kb += round;
         if (kb >= k_end) break;
       }
     }
@@ -428,52 +478,65 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
               f32x4{acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j]};
     }
     __syncthreads();
-    const float vs = E4M3 && a.v_scale ? a.v_scale[kh] : 1.0f;
-    auto put = [&](uint32_t c, uint32_t d, const f32x4& o, float ls) {       // a column that saw nothing: zero
-      const float inv = ls == 0.0f ? 0.0f : vs / ls;
-      const uint32_t f = tile * COLS + c;
-      bf16_t* to = a.out + (uint64_t)(w.row0 + f / a.group) * a.ld_out + (uint64_t)(kh * a.group + f % a.group) * DH + d;
-      *reinterpret_cast<uint2*>(to) = ls == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
-    };
-    constexpr uint32_t DV = DH / 4, STRIDE = DH + 4;
-    auto part_of = [&](uint32_t place) { return parts + (uint64_t)place * part_cols * STRIDE; };
-    for (uint32_t u = tid; u < n_cols * DV; u += 256) {
+    for (uint32_t u = tid; u < n_group * DV; u += 256) {
       const uint32_t c = u / DV, d = u % DV * 4u;
       Joined j;
+      if (w.wide) {
+        j.add(sum_m[c], sum_l[c], *reinterpret_cast<const f32x4*>(sum_acc + c * STRIDE + d));
+      } else {
 #pragma unroll
-      for (uint32_t x = 0; x < WAVES; ++x)
-        j.add(sum_m[x * COLS + c], sum_l[x * COLS + c], *reinterpret_cast<const f32x4*>(sum_acc + (x * COLS + c) * STRIDE + d));
-      if (pieces == 1) { put(c, d, j.o, j.l); continue; }
+        for (uint32_t x = 0; x < WAVES; ++x)
+          j.add(sum_m[x * COLS + c], sum_l[x * COLS + c], *reinterpret_cast<const f32x4*>(sum_acc + (x * COLS + c) * STRIDE + d));
+      }
+      if (pieces == 1) { put(w.row0, group_col, kh, c, d, j); continue; }
       float* to = part_of(2u * wg + (at_begin ? 0u : 1u)) + c * STRIDE;
       share_out(to + 4 + d, j.o[0], j.o[1]);
       share_out(to + 6 + d, j.o[2], j.o[3]);
       if (d == 0) share_out(to, j.m, j.l);
     }
-    if (pieces == 1) continue;
-
-    // ---- the last piece of a group to be done adds them up
-    shared_out();
-    __syncthreads();
-    uint32_t* const arrived = (uint32_t*)red;
-    if (tid == 0) {
-      const uint32_t n = atomicAdd(counters + wg_first, 1u);
-      if (n + 1u == pieces) __hip_atomic_store(counters + wg_first, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      *arrived = n + 1u;
+    if (pieces > 1) {
+      const Cut x = {w.row0, group_col, kh, n_group, wg_first, pieces, 2u * wg_first + (group_first - pad <= share * wg_first ? 0u : 1u)};
+      if (at_begin) cut[0] = x; else cut[1] = x;
     }
-    __syncthreads();
-    if (*arrived != pieces) continue;
-    const uint32_t first_place = 2u * wg_first + (group_first - SETUP <= share * wg_first ? 0u : 1u);
-    const uint32_t lanes = n_cols * DV, teams = max(1u, 256u / lanes), team = tid / lanes;      // of threads, each with its pieces
+  }
+
+  // ---- the last piece of a group to be done adds them up
+  if (cut[0].pieces + cut[1].pieces == 0) return;
+  shared_out();
+  __syncthreads();
+  uint32_t* const arrived = (uint32_t*)red;
+  if (tid < 2) {
+    const uint32_t pieces = tid ? cut[1].pieces : cut[0].pieces, wg_first = tid ? cut[1].wg_first : cut[0].wg_first;
+    bool last = false;
+    if (pieces) {
+      last = atomicAdd(counters + wg_first, 1u) + 1u == pieces;
+      if (last) __hip_atomic_store(counters + wg_first, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    arrived[tid] = last;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (!arrived[which]) continue;
+    const Cut& x = cut[which];
+    const uint32_t lanes = x.n_cols * DV, teams = max(1u, 256u / lanes), team = tid / lanes;      // of threads, each with its pieces
     for (uint32_t u = tid % lanes; u < lanes && team < teams; u += 256) {
       const uint32_t c = u / DV, d = u % DV * 4u;
       Joined j;
-#pragma unroll 4
-      for (uint32_t x = team; x < pieces; x += teams) {
-        const float* from = part_of(x ? 2u * (wg_first + x) : first_place) + c * STRIDE;
-        const float2 ml = shared_in(from), lo = shared_in(from + 4 + d), hi = shared_in(from + 6 + d);
-        j.add(ml.x, ml.y, f32x4{lo.x, lo.y, hi.x, hi.y});
+      // eight pieces' loads at a time: a trip to memory each
+      for (uint32_t i = team; i < x.pieces; i += 8u * teams) {
+        float2 ml[8], lo[8], hi[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) {
+          const uint32_t p = min(i + k * teams, x.pieces - 1u);
+          const float* from = part_of(p ? 2u * (x.wg_first + p) : x.first_place) + c * STRIDE;
+          ml[k] = shared_in(from); lo[k] = shared_in(from + 4 + d); hi[k] = shared_in(from + 6 + d);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k)
+          if (i + k * teams < x.pieces) j.add(ml[k].x, ml[k].y, f32x4{lo[k].x, lo[k].y, hi[k].x, hi[k].y});
       }
-      if (teams == 1) { put(c, d, j.o, j.l); continue; }
+      if (teams == 1) { put(x.row0, x.group_col, x.kh, c, d, j); continue; }
       float* to = sum_acc + tid * 8u;
       *reinterpret_cast<f32x4*>(to) = j.o;
       to[4] = j.m; to[5] = j.l;
@@ -482,34 +545,36 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
       __syncthreads();
       if (tid < lanes) {
         Joined j;
-        for (uint32_t x = 0; x < teams; ++x) {
-          const float* from = sum_acc + (x * lanes + tid) * 8u;
+        for (uint32_t i = 0; i < teams; ++i) {
+          const float* from = sum_acc + (i * lanes + tid) * 8u;
           j.add(from[4], from[5], *reinterpret_cast<const f32x4*>(from));
         }
-        put(tid / DV, tid % DV * 4u, j.o, j.l);
+        put(x.row0, x.group_col, x.kh, tid / DV, tid % DV * 4u, j);
       }
+      __syncthreads();
     }
   }
 }
 
-uint32_t part_columns(uint32_t n_rows, uint32_t group) { return (uint32_t)std::min<uint64_t>(COLS, (uint64_t)n_rows * group); }
+uint32_t part_columns(uint32_t n_rows, uint32_t group) { return (uint32_t)std::min<uint64_t>(COLS * WAVES, (uint64_t)n_rows * group); }
 
 template <int DH, bool E4M3>
 hipError_t launch_paged(const PagedArgs& a, void* scratch, hipStream_t st) {
-  constexpr int KP = E4M3 ? 2 : 1;
   const uint32_t rows = a.starts ? a.n_rows : std::min(a.n_rows, a.n_seq);
   if (rows == 0) return hipSuccess;
   uint32_t* counters = (uint32_t*)scratch;
   float* parts = (float*)scratch + MAX_WGS;
-  const uint32_t lds = WAVES * COLS * (DH + 4) * 4 + WAVES * COLS * 8 + WAVES * 8 + (a.n_seq > 64 ? a.n_seq * 8 : 0);
+  // units that there can be: column tiles, key heads, the longest sequence that the tables have room for
+  const uint64_t groups = (((uint64_t)rows * a.group + COLS - 1) / COLS + a.n_seq) * a.kv_heads;
+  const uint64_t units = (((uint64_t)a.max_blocks << a.block_shift) + 31) / 32;
+  const bool few = a.n_seq <= 64 && (double)groups * (double)(2 * units + 2) < 4e9;      // 32 bits hold the sums, padding included
+  const uint32_t lds = WAVES * COLS * (DH + 4) * 4 + WAVES * COLS * 8 + WAVES * 8 + (few ? 0 : a.n_seq * 8);
   if (lds > 60u * 1024) {
-    hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3, KP>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  // units that there can be: column tiles, key heads, the longest sequence that the tables have room for
-  const uint64_t tiles = ((uint64_t)rows * a.group + COLS - 1) / COLS + a.n_seq, units = (((uint64_t)a.max_blocks << a.block_shift) + UNIT - 1) / UNIT;
-  const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (tiles * a.kv_heads * (units + SETUP) / MIN_SHARE + 8) / 8 * 8);
-  paged_attention_kernel<DH, E4M3, KP><<<wgs, 256, lds, st>>>(a, counters, parts, part_columns(rows, a.group));
+  const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (groups * ((units + MIN_PIECE - 1) / MIN_PIECE) + 7) / 8 * 8);
+  paged_attention_kernel<DH, E4M3><<<wgs, 256, lds, st>>>(a, counters, parts, part_columns(rows, a.group), few, rows * a.group > 2 * COLS && (a.starts || a.group > 2 * COLS));
   return hipGetLastError();
 }
 

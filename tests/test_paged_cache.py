@@ -71,11 +71,11 @@ def attention_reference(q, k, v, tables, lengths, starts, scale):
     """q [rows, heads, dh], pools [n_blocks, kv_heads, block, dh], all fp64 on the host; starts a list.  Returns the output and
     sum p |v| / sum p, with the largest sum |q| |k| of a row's scores; None for rows that starts does not name."""
     group, block = q.shape[1] // k.shape[1], k.shape[2]
-    out, mag, mac = torch.full_like(q, math.nan), torch.zeros_like(q), torch.zeros(q.shape[:2], dtype=torch.float64)
+    out, mag, mac = torch.full_like(q, math.nan), torch.zeros_like(q), torch.zeros_like(q[..., 0])
     for i in range(len(lengths)):
         for r in range(starts[i], starts[i + 1]):
             sees = min(lengths[i], tables.shape[1] * block) - (starts[i + 1] - 1 - r)
-            at = torch.arange(max(0, sees))
+            at = torch.arange(max(0, sees), device=q.device)
             ids = tables[i, at // block].long()
             at, ids = at[(ids >= 0) & (ids < k.shape[0])], ids[(ids >= 0) & (ids < k.shape[0])]
             if at.numel() == 0:
@@ -394,7 +394,8 @@ def _check_attend(d):
     k, v = (p.double() if s is None else p.double() * s.double()[:, None, None] for p, s in zip(d["pools"], d["scales"]))
     rows = d["starts"][-1]
     q = d["q"].double().view(-1, d["H"], d["dh"])[:rows]
-    want, mag, mac = attention_reference(q, k, v, d["tables"], d["lengths"], d["starts"], d["scale"])
+    at = DEV if rows > 1000 else "cpu"
+    want, mag, mac = (x.cpu() for x in attention_reference(q.to(at), k.to(at), v.to(at), d["tables"].to(at), d["lengths"], d["starts"], d["scale"]))
     out = d["outd"].cpu()
     got = out[:rows, :d["H"] * d["dh"]].double().view(want.shape)
     tol = attention_tolerance(want, mag, mac, d["dh"])
@@ -424,6 +425,19 @@ def test_attention_of_several_new_tokens(lengths, news, H, Hk, dh, block, e4m3):
 
 
 @gpu
+@pytest.mark.parametrize("lengths,news,H,Hk,dh,block,e4m3", [
+    ([700, 1200, 33, 0, 500], [650, 900, 33, 0, 1], 24, 8, 64, 16, False), ([1500, 70], [1400, 2], 16, 16, 128, 64, False),
+    ([1100, 900], [700, 801], 40, 8, 128, 32, True)])
+def test_attention_of_many_new_tokens(lengths, news, H, Hk, dh, block, e4m3):
+    """More than 12288 units of 16 columns and 128 keys: groups of 64 columns."""
+    units = sum(-(-n * (H // Hk) // 16) * Hk * max(1, -(-length // 128)) for length, n in zip(lengths, news))
+    assert units >= 12288
+    _check_attend(_attend(lengths, H, Hk, dh, block, news, e4m3=e4m3, seed=H, pad_rows=2))
+    spoiled, clean = (_attend(lengths, H, Hk, dh, block, news, e4m3=e4m3, seed=H, spoil=s) for s in (True, False))
+    assert torch.equal(spoiled["outd"], clean["outd"])
+
+
+@gpu
 @pytest.mark.parametrize("n,longest,H,Hk,dh,block,seed", [(300, 40, 4, 4, 64, 16, 1), (70, 900, 8, 8, 128, 32, 2), (9, 9000, 8, 2, 128, 16, 3), (1, 70000, 2, 1, 64, 128, 4),
                                                          (2000, 3, 2, 1, 64, 16, 5)])
 def test_attention_of_ragged_batches(n, longest, H, Hk, dh, block, seed):
@@ -446,18 +460,18 @@ def test_unseen_positions_hold_anything(lengths, news, e4m3):
 
 
 @gpu
-@pytest.mark.parametrize("Hk,dh", [(2, 64), (1, 128)])
-def test_later_tokens_hold_anything(Hk, dh):
+@pytest.mark.parametrize("length,new,at,H,Hk,dh", [(70, 20, 61, 4, 2, 64), (70, 20, 61, 2, 1, 128), (40, 3, 38, 6, 1, 128), (1300, 1100, 777, 32, 16, 64)])
+def test_later_tokens_hold_anything(length, new, at, H, Hk, dh):
     """A new token's key and value are NaN or infinite: the rows before it do not see it, its own and the later ones do."""
-    H, lengths, news = 2 * Hk, [70], [20]
-    clean = _attend(lengths, H, Hk, dh, 16, news, seed=4)
+    clean = _attend([length], H, Hk, dh, 16, [new], seed=4)
+    first = at - (length - new)
     for which, what in ((1, math.nan), (1, math.inf), (0, math.nan)):
-        d = _attend(lengths, H, Hk, dh, 16, news, seed=4, run=False)
-        d["pd"][which][int(d["tables"][0, 61 // 16]), :, 61 % 16] = what            # position 61: new token 11
+        d = _attend([length], H, Hk, dh, 16, [new], seed=4, run=False)
+        d["pd"][which][int(d["tables"][0, at // 16]), :, at % 16] = what
         qb.qzo_paged_attention(*d["args"])
         got = d["outd"].cpu()
-        assert torch.equal(got[:11], clean["outd"].cpu()[:11])
-        assert not torch.isfinite(got[11:]).any()
+        assert torch.equal(got[:first], clean["outd"].cpu()[:first])
+        assert not torch.isfinite(got[first:]).any()
 
 
 @gpu

@@ -62,8 +62,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs 
   int64_t sum[3] = {0, 0, 0};
   uint32_t seen = n_free < 0 || (uint32_t)n_free > a.n_blocks ? 1u : 0u;
   int32_t open = 0;                                // per = 1: the block that holds the sequence's last token
+  const int32_t add0 = first < last ? a.added[first] : 0;      // a thread's first sequence, mostly its only one
+  auto added = [&](uint32_t i) { return i == first ? add0 : a.added[i]; };
   for (uint32_t i = first; i < last; ++i) {
-    const int32_t have = a.cached[i], add = a.added[i];
+    const int32_t have = a.cached[i], add = added(i);
     if (have < 0) seen |= 1u;
     else if (have > room || (add > 0 && (int64_t)have + add > room)) seen |= 2u;
     else if (per == 1 && have > 0) open = a.tables[(uint64_t)i * a.max_blocks + (uint32_t)((have - 1) >> shift)];
@@ -87,17 +89,15 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs 
   __syncthreads();
   uint32_t total[3];
   bool fits[3];
+  constexpr uint32_t N = PLAN_THREADS / 64;
+  const uint32_t lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
 #pragma unroll
   for (int j = 0; j < 3; ++j) {
-    float size = 0.0f;
-    total[j] = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < PLAN_THREADS / 64; ++w) {
-      if (w == (tid >> 6)) run[j] += total[j];
-      total[j] += wave_sums[j][w];
-      size += wave_sizes[j][w];
-    }
-    fits[j] = size < 3e9f && total[j] < 0x80000000u;
+    const uint32_t v = lane < N ? wave_sums[j][lane] : 0u, upto = lane_scan(v);
+    const float size = lane_scan(lane < N ? wave_sizes[j][lane] : 0.0f);
+    run[j] += (uint32_t)__builtin_amdgcn_readlane((int)(upto - v), (int)wave);
+    total[j] = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    fits[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(size), 63)) < 3e9f && total[j] < 0x80000000u;
   }
   const uint32_t flag = flags;
   int32_t status = QZO_OK;
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs 
   {
     uint32_t b = run[0], k = run[1], t = run[2];
     for (uint32_t i = first; i < last; ++i) {
-      const int32_t have = old_len[i], add = a.added[i];
+      const int32_t have = old_len[i], add = added(i);
       back[i] = (int32_t)b; take[i] = (int32_t)k; start[i] = (int32_t)t;
       a.lengths[i] = !ok ? have : add < 0 ? 0 : have + add;
       a.starts[i] = ok ? (int32_t)t : 0;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs 
   auto block_of = [&](uint32_t i, int32_t j, int32_t held) { return j < held ? a.tables[(uint64_t)i * a.max_blocks + (uint32_t)j] : taken(take[i] + j - held); };
   if (!(flag & 4u)) {
     for (uint32_t i = first; i < last; ++i) {
-      const int32_t have = old_len[i], add = a.added[i], held = (int32_t)blocks(have);
+      const int32_t have = old_len[i], add = added(i), held = (int32_t)blocks(have);
       int32_t number = -1, id = 0;
       for (int32_t x = 0; x < add; ++x) {
         const int32_t at = have + x, j = at >> shift;
@@ -151,6 +151,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs 
       }
     }
   } else {
+#pragma unroll 4
     for (int32_t k = (int32_t)tid; k < n_take; k += PLAN_THREADS) {
       const uint32_t s = last_not_above(take, a.n_seq, k);
       a.tables[(uint64_t)s * a.max_blocks + (uint32_t)blocks(old_len[s]) + (uint32_t)(k - take[s])] = taken(k);
@@ -196,7 +197,7 @@ hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t st) {
   cache_plan_kernel<<<1, PLAN_THREADS, lds, st>>>(a, few);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || few) return e;
-  cache_slots_kernel<<<std::min<uint32_t>((a.max_tokens + 1023) / 1024, 1024u), 256, (a.n_seq + 1) * 4u, st>>>(a);
+  cache_slots_kernel<<<std::min<uint32_t>((a.max_tokens + 255) / 256, 2048u), 256, (a.n_seq + 1) * 4u, st>>>(a);
   return hipGetLastError();
 }
 
@@ -232,7 +233,7 @@ __device__ __forceinline__ float half_a_head_away(float v) {
 
 template <int DH>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a, RopeTurns turns, uint32_t parts) {
-  constexpr uint32_t LANES = DH / 8, HEADS = 64 / LANES, BATCH = 4;
+  constexpr uint32_t LANES = DH / 8, HEADS = 64 / LANES;
   const uint32_t lane = threadIdx.x & 63u, sub = lane % LANES;
   const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4u + (threadIdx.x >> 6))), t = w / parts, part = w % parts;
   if (t >= a.n_tokens) return;
@@ -246,86 +247,85 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a, RopeTurns t
   const uint32_t h0 = part * HEADS + lane / LANES;
   // all lanes of a wavefront make the same number of turns; a head beyond the last is read as the last and not written
   const uint32_t n_turns = (heads - part * HEADS + turn - 1) / turn;
-  uint4 raw[BATCH];
-  auto load = [&](uint32_t first) {
-#pragma unroll
-    for (uint32_t i = 0; i < BATCH; ++i) raw[i] = *reinterpret_cast<const uint4*>(row + (uint64_t)min(h0 + (first + i) * turn, heads - 1u) * DH);
-  };
-  load(0);
+  auto load = [&](uint32_t i) { return *reinterpret_cast<const uint4*>(row + (uint64_t)min(h0 + i * turn, heads - 1u) * DH); };
+  uint4 raw = load(0);
+  uint4 q_gain = make_uint4(0u, 0u, 0u, 0u), k_gain = q_gain;
+  if (a.q_gain) q_gain = *reinterpret_cast<const uint4*>(a.q_gain + sub * 8);
+  if (a.k_gain) k_gain = *reinterpret_cast<const uint4*>(a.k_gain + sub * 8);
   const int32_t at = a.positions ? a.positions[t] : (int32_t)((t % a.pass_stride) % a.seq);
+  // a pair's angle per lane, all eight of a lane's features by way of the LDS
+  __shared__ __attribute__((aligned(16))) float2 angles[4][DH / 2];
   float c[8], s[8];
+  if (a.rope) {
+    float2* const mine = angles[threadIdx.x >> 6];
+    if (lane < DH / 2) {
+      const double rev = (double)at * turns.t[lane];
+      float2 cs;
+      sincospif(2.0f * (float)(rev - rint(rev)), &cs.y, &cs.x);
+      mine[lane] = cs;
+    }
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    c[j] = 1.0f; s[j] = 0.0f;
-    if (a.rope) {
-      const double rev = (double)at * turns.t[(sub * 8 + j) % (DH / 2)];
-      sincospif(2.0f * (float)(rev - rint(rev)), &s[j], &c[j]);
-      if (sub < LANES / 2) s[j] = -s[j];
+    for (int j = 0; j < 8; ++j) {
+      const float2 cs = mine[(sub * 8 + j) % (DH / 2)];
+      c[j] = cs.x;
+      s[j] = sub < LANES / 2 ? -cs.y : cs.y;
     }
   }
   const uint64_t slot_row = ((uint64_t)((uint32_t)slot >> a.block_shift) * a.kv_heads << a.block_shift) + ((uint32_t)slot & ((1u << a.block_shift) - 1u));
-  for (uint32_t first = 0; first < n_turns; first += BATCH) {
-    uint4 now[BATCH];
+  for (uint32_t i = 0; i < n_turns; ++i) {
+    const uint4 now = raw;
+    if (i + 1 < n_turns) raw = load(i + 1);
+    const uint32_t h = h0 + i * turn, r[4] = {now.x, now.y, now.z, now.w};
+    float x[8], y[8];
 #pragma unroll
-    for (uint32_t i = 0; i < BATCH; ++i) now[i] = raw[i];
-    if (first + BATCH < n_turns) load(first + BATCH);
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(r[j] << 16);
+      x[2 * j + 1] = __uint_as_float(r[j] & 0xffff0000u);
+    }
+    const bool is_q = h < a.q_heads, is_v = h >= n_qk;
+    if (a.q_gain || a.k_gain) {
+      float ss = 0.0f;
 #pragma unroll
-    for (uint32_t i = 0; i < BATCH; ++i) {
-      const uint32_t h = h0 + (first + i) * turn;
-      if (first + i >= n_turns) break;
-      const uint32_t r[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
-      float x[8], y[8];
+      for (int j = 0; j < 8; ++j) ss = __builtin_fmaf(x[j], x[j], ss);
+      const float inv = __builtin_amdgcn_rsqf(sum_of_head<DH>(ss) * (1.0f / DH) + a.eps);
+      if (is_q ? a.q_gain != nullptr : !is_v && a.k_gain) {
+        const uint32_t g[4] = {is_q ? q_gain.x : k_gain.x, is_q ? q_gain.y : k_gain.y, is_q ? q_gain.z : k_gain.z, is_q ? q_gain.w : k_gain.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __uint_as_float(r[j] << 16);
-        x[2 * j + 1] = __uint_as_float(r[j] & 0xffff0000u);
-      }
-      const bool is_q = h < a.q_heads, is_v = h >= n_qk;
-      const bf16_t* gain = is_q ? a.q_gain : is_v ? nullptr : a.k_gain;
-      if (a.q_gain || a.k_gain) {                     // uniform
-        float ss = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) ss = __builtin_fmaf(x[j], x[j], ss);
-        const float inv = __builtin_amdgcn_rsqf(sum_of_head<DH>(ss) * (1.0f / DH) + a.eps);
-        if (gain) {
-          const uint4 g4 = *reinterpret_cast<const uint4*>(gain + sub * 8);
-          const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[2 * j] *= inv * __uint_as_float(g[j] << 16);
-            x[2 * j + 1] *= inv * __uint_as_float(g[j] & 0xffff0000u);
-          }
+        for (int j = 0; j < 4; ++j) {
+          x[2 * j] *= inv * __uint_as_float(g[j] << 16);
+          x[2 * j + 1] *= inv * __uint_as_float(g[j] & 0xffff0000u);
         }
       }
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float other = half_a_head_away<DH>(x[j]);
-        y[j] = is_v || !a.rope ? x[j] : __builtin_fmaf(other, s[j], x[j] * c[j]);
-      }
-      if (h >= heads) continue;
-      if (is_q || !a.cache_type) {
-        *reinterpret_cast<uint4*>(a.out + (uint64_t)t * a.ld_out + (uint64_t)h * DH + sub * 8) =
-            make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-        continue;
-      }
-      const uint32_t kh = h - (is_v ? n_qk : a.q_heads);
-      const uint64_t at_row = slot_row + ((uint64_t)kh << a.block_shift);
-      unsigned char* pool = (unsigned char*)(is_v ? a.v : a.k);
-      if (a.cache_type == 1) {
-        *reinterpret_cast<uint4*>(pool + at_row * (DH * 2) + sub * 16) =
-            make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-      } else {
-        const float* scale = is_v ? a.v_scale : a.k_scale;
-        const float inv = scale ? 1.0f / scale[kh] : 1.0f;
+    for (int j = 0; j < 8; ++j) {
+      const float other = half_a_head_away<DH>(x[j]);
+      y[j] = is_v || !a.rope ? x[j] : __builtin_fmaf(other, s[j], x[j] * c[j]);
+    }
+    if (h >= heads) continue;
+    if (is_q || !a.cache_type) {
+      *reinterpret_cast<uint4*>(a.out + (uint64_t)t * a.ld_out + (uint64_t)h * DH + sub * 8) =
+          make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+      continue;
+    }
+    const uint32_t kh = h - (is_v ? n_qk : a.q_heads);
+    const uint64_t at_row = slot_row + ((uint64_t)kh << a.block_shift);
+    unsigned char* pool = (unsigned char*)(is_v ? a.v : a.k);
+    if (a.cache_type == 1) {
+      *reinterpret_cast<uint4*>(pool + at_row * (DH * 2) + sub * 16) =
+          make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+    } else {
+      const float* scale = is_v ? a.v_scale : a.k_scale;
+      const float inv = scale ? 1.0f / scale[kh] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = to_e4m3_range(y[j] * inv);
-        *reinterpret_cast<uint2*>(pool + at_row * DH + sub * 8) = make_uint2(pack_e4m3x4(y[0], y[1], y[2], y[3]), pack_e4m3x4(y[4], y[5], y[6], y[7]));
-      }
+      for (int j = 0; j < 8; ++j) y[j] = to_e4m3_range(y[j] * inv);
+      *reinterpret_cast<uint2*>(pool + at_row * DH + sub * 8) = make_uint2(pack_e4m3x4(y[0], y[1], y[2], y[3]), pack_e4m3x4(y[4], y[5], y[6], y[7]));
     }
   }
 }
 
-constexpr uint32_t QK_WAVES = 16384;
+constexpr uint32_t QK_WAVES = 24576;
 hipError_t launch_qk_norm_rope(const QkArgs& a, uint32_t head_dim, double theta, hipStream_t st) {
   if (a.n_tokens == 0) return hipSuccess;
   RopeTurns turns = {};

@@ -421,6 +421,24 @@ qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows
                                const int32_t* lengths_dev, const int32_t* starts_dev, float scale, void* out_dev,
                                uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream);
 
+/*
+ * Answers: the model, as its scales are now and unperturbed, over the n_tokens newest tokens of n_seq sequences, whose earlier
+ * tokens' keys and values are in the cache.  tokens_dev int32 [n_tokens] (values in [0, vocab)), sequence by sequence as qzo_cache_plan lists
+ * them; starts_dev, slots_dev, positions_dev, lengths_dev, tables_dev as it left them (rows behind the last new token, slots of -1, are
+ * padding: their tokens are read but reach nothing).  cache describes the pools of layer 0, kv_heads = n_heads and
+ * head_dim = d_model / n_heads; those of the other layers follow, k_dev and v_dev holding [n_layers, n_blocks, kv_heads,
+ * block, head_dim]; the scales are the same for all layers.  Positions beyond max_seq - 1 count as that one where the
+ * model has learned positions.
+ * logits_dev: bf16 [n_seq, vocab], of the last new token of every sequence; zeros where it has none.
+ * workspace_dev: qzo_answer_workspace_bytes bytes, 256-byte aligned, contents undefined before and after; calls that may overlap
+ * need one each.  QZO_ERR_SHAPE: vocab not a multiple of 8, or tokens or sequences too many for 32-bit offsets.
+ */
+qzo_status qzo_answer_workspace_bytes(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq, uint64_t* out);
+qzo_status qzo_answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_seq, const qzo_cache* cache,
+                      const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev,
+                      const int32_t* slots_dev, const int32_t* positions_dev, void* workspace_dev, uint64_t workspace_bytes,
+                      void* logits_dev, void* stream);
+
 /* RTN quantizer of Eq. 3 with the k=4 absmax scale: w_dev fp32 [N,K] ->
  * q_dev packed int4 [N,K/2], s_dev bf16 [N,K/group].  Model construction, not
  * part of the timed step. */

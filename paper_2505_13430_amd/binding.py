@@ -30,6 +30,7 @@ EXPORTS = [
     "qzo_nf4_expand", "qzo_nf4_scratch_bytes", "qzo_nf4_gemm",
     "qzo_codebook_scratch_bytes", "qzo_codebook_gemm", "qzo_apply_update_channel",
     "qzo_cache_plan", "qzo_qk_norm_rope", "qzo_paged_attention_scratch_bytes", "qzo_paged_attention",
+    "qzo_answer_workspace_bytes", "qzo_answer",
     "qzo_debug_philox", "qzo_debug_normal_pairs", "qzo_debug_normals", "qzo_debug_dequant", "qzo_debug_dequant_zp",
     "qzo_debug_forward", "qzo_debug_bf16_gemm", "qzo_debug_reduce_norm", "qzo_debug_fused_linear", "qzo_debug_attention_slices",
     "qzo_debug_attention_linear",
@@ -78,6 +79,7 @@ def lib():
         _lib.qzo_cache_plan.argtypes = [p, p, u32, u32, u32, u32, u32] + [p] * 9
         _lib.qzo_qk_norm_rope.argtypes = [p, u64, u32, u32, u32, u32, p, p, f, f, p, u32, p, p, p, u64, p]
         _lib.qzo_paged_attention_scratch_bytes.argtypes = [u32, u32, u32, u32, p]
+        _lib.qzo_answer.argtypes = [p, p, u32, u32, p, p, u32, p, p, p, p, p, u64, p, p]
         _lib.qzo_paged_attention.argtypes = [p, u64, u32, u32, u32, p, p, u32, p, p, f, p, u64, p, u64, p]
     return _lib
 
@@ -578,3 +580,19 @@ def qzo_paged_attention(q, cache, tables, lengths, out, scale, starts=None, scra
     _check(lib().qzo_paged_attention(x, ldx, q.shape[0], n, heads, C.addressof(cache), _typed(tables, torch.int32), most,
                                      _typed(lengths, torch.int32), _typed(starts, torch.int32), scale, y, ldy,
                                      None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel() * scratch.element_size(), st))
+
+
+def qzo_answer_workspace_bytes(model, n_tokens, n_seq) -> int:
+    out = C.c_uint64(0)
+    _check(lib().qzo_answer_workspace_bytes(model, C.c_uint32(n_tokens), C.c_uint32(n_seq), C.byref(out)))
+    return out.value
+
+
+def qzo_answer(model, tokens, cache, tables, lengths, starts, slots, positions, workspace, logits, stream=None):
+    """tokens int32 [n_tokens]; cache: of layer 0, the other layers' pools behind it; logits bf16 [n_seq, vocab]."""
+    i32, (n, most) = torch.int32, tables.shape
+    assert lengths.numel() == n and starts.numel() == n + 1 and slots.numel() >= tokens.numel() <= positions.numel() and logits.shape[0] == n
+    _check(lib().qzo_answer(model, _typed(tokens, i32), tokens.numel(), n, C.addressof(cache), _typed(tables, i32), most, _typed(lengths, i32),
+                            _typed(starts, i32), _typed(slots, i32), _typed(positions, i32), workspace.data_ptr(),
+                            workspace.numel() * workspace.element_size(), _typed(logits, torch.bfloat16),
+                            _here(stream, (tokens, tables, workspace, logits))))

@@ -453,13 +453,23 @@ struct ProfScope {
 enum { PK_W4GEMM = 0, PK_LMHEAD = 1, PK_ATTN = 2, PK_UPDATE = 3, PK_OTHER = 4, PK_EXPAND = 5, PK_COUNT = 6 };
 
 
+// The newest tokens of sequences in place of whole ones (qzo_answer): their places, and where the logits go.
+struct Answer {
+  const qzo_cache* cache;          // of layer 0; the others' pools follow
+  const int32_t *tables, *lengths, *starts, *slots, *positions;
+  uint32_t n_seq, max_blocks;
+  void *scratch, *last, *logits;   // of the attention; the last tokens' hidden states
+};
+
 // The decoder forward with every quantized linear perturbed by sign*eps*z.
 // n_pass = 2 (see passes_stacked): both passes of a step stacked, rows [0,M1) perturbed by
 // +eps_signed and rows [P, P + M1) by -eps_signed, P = stacked_pass_stride(m, M1); their losses go to
 // loss_out[0] and [1].  tail: of a step's last forward.
+// ans: batch1 tokens with places of their own (seq = 1): keys and values go to the cache, attention reads them there, and the
+// logits of the sequences' last tokens take the place of the loss.
 qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t seq, uint64_t seed,
                    float eps_signed, const Workspace& w, float* loss_out, hipStream_t st,
-                   void* hidden_out = nullptr, uint32_t n_pass = 1, const StepTail& tail = StepTail{}) {
+                   void* hidden_out = nullptr, uint32_t n_pass = 1, const StepTail& tail = StepTail{}, const Answer* ans = nullptr) {
   const qzo_model_config& c = m->cfg;
   const uint32_t batch = batch1 * n_pass, M1 = batch1 * seq;
   const uint32_t P = n_pass == 2 ? (uint32_t)stacked_pass_stride(m, M1) : M1;     // rows per pass
@@ -470,7 +480,7 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
   const uint32_t seed_lo = (uint32_t)seed, seed_hi = (uint32_t)(seed >> 32);
   const unsigned char* arena = (const unsigned char*)m->arena;
 
-  if (m->dense_master) {      // joint mode: the 16-bit tensors become round16(theta_u + eps_signed z)
+  if (m->dense_master && !ans) {      // joint mode: the 16-bit tensors become round16(theta_u + eps_signed z)
     ProfScope ps(PK_OTHER, 0, st);
     QZO_HIP(launch_dense_perturb(m->dense_master, m->dense_segs, m->n_dense_segs, m->n_dense, seed_lo,
                                  seed_hi, eps_signed, st));
@@ -482,14 +492,18 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
   }
   {
     ProfScope ps(PK_OTHER, 0, st);
-    QZO_HIP(launch_embed(tok, M1, P, m->T[0].ptr_dev, llama ? nullptr : m->T[1].ptr_dev, M, seq, d, w.h,
-                         llama ? w.rope : nullptr, dh, c.rope_theta, st));
+    if (ans)
+      QZO_HIP(launch_embed(tok, M1, P, m->T[0].ptr_dev, llama ? nullptr : m->T[1].ptr_dev, M, c.max_seq, d, w.h, nullptr, dh, c.rope_theta,
+                           st, ans->positions, (uint32_t*)ans->scratch, PAGED_COUNTERS));
+    else
+      QZO_HIP(launch_embed(tok, M1, P, m->T[0].ptr_dev, llama ? nullptr : m->T[1].ptr_dev, M, seq, d, w.h,
+                           llama ? w.rope : nullptr, dh, c.rope_theta, st));
   }
   const double attn_flops = 2.0 * batch * H * (double)seq * seq * dh;   // causal: half of 4 B H S^2 dh
   const double Mreal = (double)n_pass * M1;                             // rows that count as work
   // attention over both passes: one launch when they are contiguous, one per pass otherwise
   // short sequences: no RoPE launch, the attention kernel rotates q and k itself
-  const bool rope_in_attention = llama && seq <= ATTENTION_ROPE_MAX_S;
+  const bool rope_in_attention = llama && seq <= ATTENTION_ROPE_MAX_S && !ans;
   // few-token linears take the block sums of their input from its producer
   float* const mid_ws = n_pass == 2 || mid_single_pass(m, M1) ? w.mid : nullptr;
   const bool few = (mid_ws && c.quant != 3) || (w.skinny && M1 <= SKINNY_MAX_M && (c.quant == 0 || c.quant == 2) && !c.act_order);
@@ -497,10 +511,31 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
   // layout of the norms' outputs and the MLP's activation
   const XPack pack = few && !mid_ws && !w.wexp ? few_pack(M1, n_pass == 2) : XPack{};
   // and the attention's where a head is a group; its block sums take the place of the norm's, which the qkv linear has read
-  const XPack att_pack = dh == 128 && !padded && xs_a ? pack : XPack{};
+  const XPack att_pack = dh == 128 && !padded && xs_a && !ans ? pack : XPack{};
   NextAttention na = {batch, seq, H, dh, nullptr, 0};
+  uint32_t layer = 0;
   auto attention = [&](bool rotated) {
     ProfScope ps(PK_ATTN, attn_flops, st);
+    if (ans) {
+      const qzo_cache& k = *ans->cache;
+      const uint64_t pool = (uint64_t)k.n_blocks * k.block * k.kv_heads * k.head_dim * (k.type ? 1 : 2);
+      QkArgs qa = {};
+      qa.qkv = (const bf16_t*)w.qkv; qa.out = (bf16_t*)w.qkv; qa.ld_qkv = qa.ld_out = 3 * d;
+      qa.n_tokens = M1; qa.q_heads = qa.kv_heads = H; qa.rope = llama; qa.positions = ans->positions;
+      qa.pass_stride = M1; qa.seq = 1;
+      qa.cache_type = k.type + 1; qa.block_shift = (uint32_t)__builtin_ctz(k.block); qa.n_slots = k.n_blocks * k.block;
+      qa.k = (unsigned char*)k.k_dev + layer * pool; qa.v = (unsigned char*)k.v_dev + layer * pool;
+      qa.k_scale = k.k_scale_dev; qa.v_scale = k.v_scale_dev; qa.slots = ans->slots;
+      hipError_t e = launch_qk_norm_rope(qa, dh, c.rope_theta, st);
+      if (e != hipSuccess) return e;
+      PagedArgs pa = {};
+      pa.q = (const bf16_t*)w.qkv; pa.ld_q = 3 * d; pa.out = (bf16_t*)w.att; pa.ld_out = d;
+      pa.n_rows = M1; pa.n_seq = ans->n_seq; pa.q_heads = pa.kv_heads = H; pa.group = 1;
+      pa.k = qa.k; pa.v = qa.v; pa.k_scale = k.k_scale_dev; pa.v_scale = k.v_scale_dev;
+      pa.n_blocks = k.n_blocks; pa.block_shift = qa.block_shift; pa.max_blocks = ans->max_blocks;
+      pa.tables = ans->tables; pa.lengths = ans->lengths; pa.starts = ans->starts; pa.scale = 1.0f / std::sqrt((float)dh);
+      return launch_paged_attention(pa, dh, k.type == 1, ans->scratch, st);
+    }
     const float* tb = (llama && !rotated) ? w.rope : nullptr;
     if (na.part) return launch_attention(nullptr, batch, seq, H, dh, w.att, tb, st, na.part, na.slices, att_pack, xs_a);
     if (!padded) return launch_attention(w.qkv, batch, seq, H, dh, w.att, tb, st, nullptr, 0, att_pack, xs_a);
@@ -523,6 +558,7 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
     nn = {gain, nbias, c.norm_eps, w.a, xs, xs ? pack : XPack{}, false};
   };
   for (uint32_t l = 0; l < c.n_layers; ++l) {
+    layer = l;
     const qzo_buf* T = &m->T[m->first_layer_tensor + (size_t)l * m->tensors_per_layer];
     const uint64_t layer_off = (uint64_t)l * m->scales_per_layer;
     // Position of a tensor of the symmetric table (and of the li-th weight) within this layer: with
@@ -683,8 +719,8 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
       // attn_norm, codes/cb qkv, codes/cb o, ffn_norm, codes/cb gate+up, codes/cb down
       QZO_HIP(launch_rmsnorm(w.h, T[0].ptr_dev, M, d, c.norm_eps, w.a, st));
       rope_fused = false;
-      QZO_HIP(cgemm(0, w.a, T[1].ptr_dev, T[2].ptr_dev, nullptr, w.qkv, EPI_ROPE));
-      if (!rope_fused && !rope_in_attention) QZO_HIP(launch_rope(w.qkv, w.rope, M, seq, P, d, H, st));
+      QZO_HIP(cgemm(0, w.a, T[1].ptr_dev, T[2].ptr_dev, nullptr, w.qkv, ans ? 0u : EPI_ROPE));
+      if (!rope_fused && !rope_in_attention && !ans) QZO_HIP(launch_rope(w.qkv, w.rope, M, seq, P, d, H, st));
       QZO_HIP(attention(rope_fused || !rope_in_attention));
       QZO_HIP(cgemm(1, w.att, T[3].ptr_dev, T[4].ptr_dev, w.h, w.h, EPI_RESIDUAL));
       QZO_HIP(launch_rmsnorm(w.h, T[5].ptr_dev, M, d, c.norm_eps, w.a, st));
@@ -695,8 +731,8 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
       QZO_HIP(norm(ti(0), nullptr, xs_a));
       rope_fused = false;
       na.part = nullptr;
-      QZO_HIP(gemm(0, w.a, nullptr, nullptr, w.qkv, EPI_ROPE));
-      if (!rope_fused && !rope_in_attention) QZO_HIP(launch_rope(w.qkv, w.rope, M, seq, P, d, H, st));
+      QZO_HIP(gemm(0, w.a, nullptr, nullptr, w.qkv, ans ? 0u : EPI_ROPE));
+      if (!rope_fused && !rope_in_attention && !ans) QZO_HIP(launch_rope(w.qkv, w.rope, M, seq, P, d, H, st));
       QZO_HIP(attention(rope_fused || !rope_in_attention));
       before(ti(3), nullptr, xs_a);
       QZO_HIP(gemm(1, w.att, nullptr, w.h, w.h, EPI_RESIDUAL));
@@ -722,6 +758,15 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
   const void* lm_head = m->T[end + (llama ? 1 : 2)].ptr_dev;
   if (hidden_out)
     QZO_HIP(hipMemcpyAsync(hidden_out, w.a, (size_t)M * d * 2, hipMemcpyDeviceToDevice, st));
+  if (ans) {
+    QZO_HIP(launch_last_rows(w.a, ans->starts, M1, ans->n_seq, d, ans->last, st));
+    ProfScope ps(PK_LMHEAD, 2.0 * ans->n_seq * (double)c.vocab * d, st);
+    GemmArgs g = {};
+    g.x = ans->last; g.w = lm_head; g.y = ans->logits;
+    g.M = ans->n_seq; g.N = c.vocab; g.K = d;
+    QZO_HIP(launch_bf16_gemm(g, PLAIN_GEMM_PIPE, st));
+    return QZO_OK;
+  }
   CeArgs ce = {};
   ce.w = lm_head; ce.tok = tok; ce.tok_rows = M1;
   ce.V = c.vocab; ce.K = d; ce.S = seq; ce.n_slices = ((c.vocab + 255) / 256) * 4;
@@ -1722,6 +1767,63 @@ qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows
   a.tables = tables_dev; a.lengths = lengths_dev; a.starts = starts_dev; a.scale = scale;
   QZO_HIP(launch_paged_attention(a, cache->head_dim, cache->type == 1, scratch_dev, (hipStream_t)stream));
   return QZO_OK;
+}
+
+// Workspace of qzo_answer: that of a forward over as many rows, then the attention's scratch and the last tokens' hidden states.
+struct AnswerSpace { uint64_t scratch_off, last_off, total; };
+static AnswerSpace answer_space(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq) {
+  const qzo_model_config& c = m->cfg;
+  AnswerSpace s;
+  s.scratch_off = up256(carve(m, n_tokens, 1, nullptr).total);
+  s.last_off = s.scratch_off + up256(paged_attention_scratch(n_tokens, n_seq, c.n_heads, c.d_model / c.n_heads));
+  s.total = s.last_off + up256((uint64_t)n_seq * c.d_model * 2);
+  return s;
+}
+static qzo_status answer_check(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq) {
+  if (!m) return fail(QZO_ERR_ARG, "model is null");
+  const qzo_model_config& c = m->cfg;
+  if (!n_tokens || !n_seq || n_seq > CACHE_MAX_SEQ) return fail(QZO_ERR_SHAPE, "need n_tokens >= 1 and n_seq 1 .. 8192");
+  if (n_tokens >= (1u << 26)) return fail(QZO_ERR_SHAPE, "n_tokens must be below 2^26");
+  if (c.vocab % 8) return fail(QZO_ERR_SHAPE, "logits are written for vocabularies that are multiples of 8");
+  const uint64_t rows = passes_stacked(m, n_tokens) ? stacked_cut_rows(n_tokens) : n_tokens;
+  if (rows * widest_row(c) * 2 >= (1ull << 31)) return fail(QZO_ERR_SHAPE, "n_tokens too large for this model: an activation tensor would exceed 2^31 bytes");
+  if ((uint64_t)n_seq * c.vocab * 2 >= (1ull << 31)) return fail(QZO_ERR_SHAPE, "the logits would exceed 2^31 bytes");
+  return QZO_OK;
+}
+
+qzo_status qzo_answer_workspace_bytes(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq, uint64_t* out) {
+  if (!out) return fail(QZO_ERR_ARG, "null argument");
+  qzo_status st = answer_check(m, n_tokens, n_seq);
+  if (st != QZO_OK) return st;
+  *out = answer_space(m, n_tokens, n_seq).total;
+  return QZO_OK;
+}
+
+qzo_status qzo_answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_seq, const qzo_cache* cache,
+                      const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev,
+                      const int32_t* slots_dev, const int32_t* positions_dev, void* workspace_dev, uint64_t workspace_bytes,
+                      void* logits_dev, void* stream) {
+  qzo_status st = answer_check(m, n_tokens, n_seq);
+  if (st != QZO_OK) return st;
+  const void* all[] = {tokens_dev, tables_dev, lengths_dev, starts_dev, slots_dev, positions_dev, workspace_dev, logits_dev};
+  if (!cache) return fail(QZO_ERR_ARG, "cache is null");
+  for (const void* p : all)
+    if (!p) return fail(QZO_ERR_ARG, "null device pointer");
+  for (const void* p : all)
+    if (!aligned16(p)) return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  if ((uintptr_t)workspace_dev & 255u) return fail(QZO_ERR_ALIGN, "workspace not 256-byte aligned");
+  st = cache_check(cache);
+  if (st != QZO_OK) return st;
+  if (cache->kv_heads != m->cfg.n_heads || cache->head_dim != m->cfg.d_model / m->cfg.n_heads) return fail(QZO_ERR_SHAPE, "the cache has other heads than the model");
+  if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31) || (uint64_t)max_blocks * cache->block >= (1ull << 31))
+    return fail(QZO_ERR_SHAPE, "n_seq * max_blocks and max_blocks * block must be 1 .. 2^31 - 1");
+  const AnswerSpace sp = answer_space(m, n_tokens, n_seq);
+  if (workspace_bytes < sp.total) return fail(QZO_ERR_WORKSPACE, "workspace smaller than qzo_answer_workspace_bytes");
+  unsigned char* base = (unsigned char*)workspace_dev;
+  const Answer ans = {cache, tables_dev, lengths_dev, starts_dev, slots_dev, positions_dev, n_seq, max_blocks,
+                      base + sp.scratch_off, base + sp.last_off, logits_dev};
+  return forward(m, tokens_dev, n_tokens, 1, 0, 0.0f, carve(m, n_tokens, 1, workspace_dev), nullptr, (hipStream_t)stream, nullptr, 1, StepTail{},
+                 &ans);
 }
 
 }  // extern "C"

@@ -459,7 +459,10 @@ __global__ void embed_kernel(const int32_t* __restrict__ tok, uint32_t tok_rows,
                              const bf16_t* __restrict__ te,
                              const bf16_t* __restrict__ pe, uint32_t M, uint32_t S, uint32_t d,
                              bf16_t* __restrict__ h, uint32_t embed_wgs, float2* __restrict__ table, uint32_t half,
-                             double theta, double dh) {
+                             double theta, double dh, const int32_t* __restrict__ positions, uint32_t* __restrict__ zeros,
+                             uint32_t n_zeros) {
+  if (blockIdx.x == 0)
+    for (uint32_t i = threadIdx.x; i < n_zeros; i += blockDim.x) zeros[i] = 0u;
   if (blockIdx.x >= embed_wgs) {
     const uint32_t u = (blockIdx.x - embed_wgs) * blockDim.x + threadIdx.x;
     if (u >= S * half) return;
@@ -476,7 +479,8 @@ __global__ void embed_kernel(const int32_t* __restrict__ tok, uint32_t tok_rows,
   if (r < tok_rows) {
     v = *reinterpret_cast<const uint4*>(te + (uint64_t)tok[r] * d + c * 8);
     if (pe) {
-      uint4 p = *reinterpret_cast<const uint4*>(pe + (uint64_t)(r % S) * d + c * 8);
+      const uint32_t at = positions ? min((uint32_t)max(positions[r], 0), S - 1u) : r % S;
+      uint4 p = *reinterpret_cast<const uint4*>(pe + (uint64_t)at * d + c * 8);
       uint32_t a[4] = {v.x, v.y, v.z, v.w}, b[4] = {p.x, p.y, p.z, p.w}, o[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -489,10 +493,10 @@ __global__ void embed_kernel(const int32_t* __restrict__ tok, uint32_t tok_rows,
 }
 hipError_t launch_embed(const int32_t* tok, uint32_t tok_rows, uint32_t pass_stride, const void* tok_emb,
                         const void* pos_emb, uint32_t M, uint32_t S, uint32_t d, void* h, float* rope, uint32_t dh,
-                        float theta, hipStream_t st) {
+                        float theta, hipStream_t st, const int32_t* positions, uint32_t* zeros, uint32_t n_zeros) {
   const uint32_t wgs = (uint32_t)(((uint64_t)M * (d >> 3) + 255) / 256), table = rope ? (S * (dh / 2) + 255) / 256 : 0u;
   embed_kernel<<<wgs + table, 256, 0, st>>>(tok, tok_rows, pass_stride, (const bf16_t*)tok_emb, (const bf16_t*)pos_emb, M, S, d,
-                                            (bf16_t*)h, wgs, (float2*)rope, dh / 2, (double)theta, (double)dh);
+                                            (bf16_t*)h, wgs, (float2*)rope, dh / 2, (double)theta, (double)dh, positions, zeros, n_zeros);
   return hipGetLastError();
 }
 

@@ -292,9 +292,10 @@ hipError_t launch_sum_partials(const float* partials, uint32_t n, float* out, hi
 
 // rope (nullable): receives the table of rotary angles, (cos, sin) of [S positions][dh/2 pairs].
 // pass_stride: rows per pass of a stacked forward (M for a single pass); rows m % pass_stride >= tok_rows get zeros.
+// positions (nullable): of every row, cut off at S - 1, in place of row % S; zeros: n_zeros words to be cleared on the way.
 hipError_t launch_embed(const int32_t* tok, uint32_t tok_rows, uint32_t pass_stride, const void* tok_emb,
                         const void* pos_emb, uint32_t M, uint32_t S, uint32_t d, void* h, float* rope, uint32_t dh,
-                        float theta, hipStream_t st);
+                        float theta, hipStream_t st, const int32_t* positions = nullptr, uint32_t* zeros = nullptr, uint32_t n_zeros = 0);
 // xsum_t (nullable, d % 128 == 0): receives the block sums of the output, [d/128][M] fp32 (see GemmArgs::xsum); with it
 // pack: layout of the output and the sums
 hipError_t launch_rmsnorm(const void* x, const void* gain, uint32_t M, uint32_t d, float eps,
@@ -375,6 +376,9 @@ struct PagedArgs {
   bf16_t* out;
 };
 uint64_t paged_attention_scratch(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim);
+constexpr uint32_t PAGED_COUNTERS = 512;      // words at the head of its scratch, zero before a call and after it
 hipError_t launch_paged_attention(const PagedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st);
+// out[i] = x[starts[i + 1] - 1], the row of sequence i's last new token, or zeros where it has none (rows of d features, d % 8 == 0).
+hipError_t launch_last_rows(const void* x, const int32_t* starts, uint32_t n_rows, uint32_t n_seq, uint32_t d, void* out, hipStream_t st);
 
 }  // namespace qzo

@@ -43,7 +43,7 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // A group that lies in one workgroup is written by it; otherwise each leaves (maximum, sum, accumulators) in the scratch, its
 // first group's in place 2 b, a later one's (only the last can go on) in 2 b + 1, and who finds the group's counter at its last
 // piece adds them up, in order.  The counter (that of the workgroup of the group's first piece) goes back to zero.
-constexpr uint32_t COLS = 16, WAVES = 4, MAX_WGS = 512;
+constexpr uint32_t COLS = 16, WAVES = 4, MAX_WGS = PAGED_COUNTERS;
 constexpr uint32_t SETUP = 1, MIN_PIECE = 2, WIDE_UNITS = 12288;
 
 struct SeqWork {
@@ -588,6 +588,18 @@ uint64_t paged_attention_scratch(uint32_t n_rows, uint32_t n_seq, uint32_t q_hea
 hipError_t launch_paged_attention(const PagedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st) {
   if (head_dim == 128) return e4m3 ? launch_paged<128, true>(a, scratch, st) : launch_paged<128, false>(a, scratch, st);
   return e4m3 ? launch_paged<64, true>(a, scratch, st) : launch_paged<64, false>(a, scratch, st);
+}
+
+__global__ __launch_bounds__(256) void last_rows_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ starts, uint32_t n_rows,
+                                                        uint32_t chunks, uint4* __restrict__ out) {
+  const int32_t first = starts[blockIdx.x], end = starts[blockIdx.x + 1];
+  const bool some = end > first && first >= 0 && (uint32_t)end <= n_rows;
+  for (uint32_t c = threadIdx.x; c < chunks; c += 256)
+    out[(uint64_t)blockIdx.x * chunks + c] = some ? x[(uint64_t)(end - 1) * chunks + c] : make_uint4(0u, 0u, 0u, 0u);
+}
+hipError_t launch_last_rows(const void* x, const int32_t* starts, uint32_t n_rows, uint32_t n_seq, uint32_t d, void* out, hipStream_t st) {
+  last_rows_kernel<<<n_seq, 256, 0, st>>>((const uint4*)x, starts, n_rows, d / 8, (uint4*)out);
+  return hipGetLastError();
 }
 
 }  // namespace qzo

@@ -204,3 +204,42 @@ class DeviceModel:
             self.close()
         except Exception:
             pass
+
+
+class Answers:
+    """Sequences that a DeviceModel continues: the pools of all layers, block tables, the free list, the lengths.  One call of `add`
+    per step; everything stays on the device."""
+
+    def __init__(self, model: DeviceModel, n_seq: int, n_blocks: int, block: int = 32, max_blocks: int | None = None, e4m3: bool = False,
+                 k_scale=None, v_scale=None):
+        sh, dev = model.shape, model.scales.device
+        dh = sh["d_model"] // sh["n_heads"]
+        self.model, self.block, self.vocab = model, block, sh["vocab"]
+        size = (sh["n_layers"], n_blocks, sh["n_heads"], block, dh)
+        self.k, self.v = (torch.empty(size, dtype=torch.float8_e4m3fn if e4m3 else torch.bfloat16, device=dev) for _ in range(2))
+        self.cache = qb.make_cache(self.k[0], self.v[0], k_scale, v_scale)
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.tables = torch.full((n_seq, max_blocks or n_blocks), -1, **i32)
+        self.free = torch.arange(n_blocks, **i32)
+        self.state = torch.tensor([n_blocks, 0, 0, 0], **i32)
+        self.lengths, self.starts = torch.zeros(n_seq, **i32), torch.zeros(n_seq + 1, **i32)
+        self.logits = torch.zeros(n_seq, self.vocab, dtype=torch.bfloat16, device=dev)
+        self._rows = {}
+
+    def rows(self, n_tokens: int):
+        """Slots, positions and workspace of steps of that many rows."""
+        if n_tokens not in self._rows:
+            i32 = dict(dtype=torch.int32, device=self.free.device)
+            ws = torch.empty(qb.qzo_answer_workspace_bytes(self.model.handle, n_tokens, len(self.lengths)), dtype=torch.uint8, device=self.free.device)
+            self._rows[n_tokens] = (torch.zeros(n_tokens, **i32), torch.zeros(n_tokens, **i32), ws)
+        return self._rows[n_tokens]
+
+    def add(self, tokens: torch.Tensor, added: torch.Tensor, stream=None) -> torch.Tensor:
+        """tokens int32 [rows], the new tokens sequence by sequence, padded at the end; added int32 [n_seq], how many each adds (negative:
+        it ends and gives its blocks back).  Returns the logits bf16 [n_seq, vocab] of the last new tokens.  Whether the step could be
+        planned is in state[2], where the caller may look (not QZO_OK: nothing has changed, the logits are zeros)."""
+        slots, positions, ws = self.rows(tokens.numel())
+        qb.qzo_cache_plan(self.lengths, added, self.block, self.tables, self.free, self.state, self.lengths, self.starts, slots, positions,
+                          self.state, stream)
+        qb.qzo_answer(self.model.handle, tokens, self.cache, self.tables, self.lengths, self.starts, slots, positions, ws, self.logits, stream)
+        return self.logits

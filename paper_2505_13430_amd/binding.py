@@ -477,68 +477,68 @@ def qzo_apply_update_channel(c, row_base, seed, eta, d_clipped, stream=None):
                                           _stream(stream)))
 
 
-def _rows(t):
-    """Address and row stride of a matrix whose rows are contiguous."""
-    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "rows of a matrix must be contiguous"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+# The calls below are made once or more per layer and token: their checks are written for few attribute reads.
+def _rows(t, at):
+    """Address and row stride of a bf16 matrix on device `at` whose rows are contiguous."""
+    ld, step = t.stride()
+    n, width = t.shape
+    assert t.dtype is torch.bfloat16 and t.get_device() == at and (step == 1 or width == 1), \
+        "a bf16 matrix on the current device is needed, its rows contiguous"
+    return t.data_ptr(), (ld if n > 1 else width)
 
 
-def _typed(t, dtype):
-    """Address of a contiguous tensor of that type; None: null."""
+def _at(t, dtype, at):
+    """Address of a contiguous tensor of that type on device `at`; None: null."""
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype, f"a contiguous CUDA tensor of {dtype} is needed"
+    assert t.dtype is dtype and t.get_device() == at and t.is_contiguous(), f"a contiguous tensor of {dtype} on the current device is needed"
     return t.data_ptr()
 
 
-def _here(stream, tensors):
-    """Handle of the call's stream; its tensors live on the device that is current."""
-    at = torch.cuda.current_device()
-    for t in tensors:
-        assert t is None or t.get_device() == at, "tensors must be on the current device"
+def _stream_of(stream, at):
     return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
 
 def make_cache(k, v, k_scale=None, v_scale=None) -> qzo_cache:
     """k, v: bf16 or float8_e4m3fn [n_blocks, kv_heads, block, head_dim]; e4m3: fp32 scales [kv_heads].  Holds its tensors."""
     n_blocks, kv_heads, block, dh = k.shape
-    assert k.dtype in (torch.bfloat16, torch.float8_e4m3fn) and k.shape == v.shape
-    for s in (k_scale, v_scale):
-        assert s is None or s.numel() == kv_heads
-    c = qzo_cache(C.sizeof(qzo_cache), k.dtype != torch.bfloat16, n_blocks, block, kv_heads, dh, _typed(k, k.dtype), _typed(v, k.dtype),
-                  _typed(k_scale, torch.float32), _typed(v_scale, torch.float32))
-    c.tensors = (k, v, k_scale, v_scale)
+    at, kind = k.get_device(), k.dtype
+    assert at >= 0 and k.shape == v.shape and (kind is torch.bfloat16 or kind is torch.float8_e4m3fn)
+    assert (k_scale is None or k_scale.numel() == kv_heads) and (v_scale is None or v_scale.numel() == kv_heads)
+    c = qzo_cache(C.sizeof(qzo_cache), kind is not torch.bfloat16, n_blocks, block, kv_heads, dh, _at(k, kind, at), _at(v, kind, at),
+                  _at(k_scale, torch.float32, at), _at(v_scale, torch.float32, at))
+    c.tensors, c.device = (k, v, k_scale, v_scale), at
     return c
 
 
 def qzo_cache_plan(cached, added, block, tables, free, before, lengths, starts, slots, positions, after, stream=None):
     """int32 tensors; tables [n_seq, max_blocks], free [n_blocks], slots and positions [max_tokens], before and after: a
     qzo_cache_state of four int32 (free blocks, tokens, status, blocks taken)."""
-    i32, (n, most) = torch.int32, tables.shape
-    assert cached.numel() == added.numel() == lengths.numel() == n and starts.numel() == n + 1 and slots.numel() == positions.numel()
+    at, i32, (n, most), tokens = torch.cuda.current_device(), torch.int32, tables.shape, slots.numel()
+    assert cached.numel() == added.numel() == lengths.numel() == n == starts.numel() - 1 and positions.numel() == tokens
     assert before.numel() == after.numel() == 4
-    _check(lib().qzo_cache_plan(_typed(cached, i32), _typed(added, i32), n, block, free.numel(), most, slots.numel(), _typed(tables, i32),
-                                _typed(free, i32), _typed(before, i32), _typed(lengths, i32), _typed(starts, i32), _typed(slots, i32),
-                                _typed(positions, i32), _typed(after, i32), _here(stream, (cached, tables, slots))))
+    _check(lib().qzo_cache_plan(_at(cached, i32, at), _at(added, i32, at), n, block, free.numel(), most, tokens, _at(tables, i32, at),
+                                _at(free, i32, at), _at(before, i32, at), _at(lengths, i32, at), _at(starts, i32, at), _at(slots, i32, at),
+                                _at(positions, i32, at), _at(after, i32, at), _stream_of(stream, at)))
 
 
 def qzo_qk_norm_rope(qkv, q_heads, kv_heads, out, q_gain=None, k_gain=None, eps=1e-6, theta=10000.0, positions=None, seq=0, cache=None,
                      slots=None, stream=None):
     """qkv bf16 [tokens, (q_heads + 2 kv_heads) head_dim]; out bf16 [tokens, the heads of q (and of k without a cache)], it may be
     a column range of qkv's own rows from the first on (in place).  Rows may be strided."""
-    x, ldx = _rows(qkv)
-    y, ldy = _rows(out)
-    T, heads = qkv.shape[0], q_heads + 2 * kv_heads
-    dh = qkv.shape[1] // heads
-    assert qkv.dtype == out.dtype == torch.bfloat16 and qkv.shape[1] == heads * dh
-    assert out.shape[0] == T and out.shape[1] >= (q_heads + (0 if cache is not None else kv_heads)) * dh
+    at, (T, width) = torch.cuda.current_device(), qkv.shape
+    x, ldx = _rows(qkv, at)
+    y, ldy = _rows(out, at)
+    dh = width // (q_heads + 2 * kv_heads)
+    T2, wide = out.shape
+    assert width == (q_heads + 2 * kv_heads) * dh and T2 == T and wide >= (q_heads if cache is not None else q_heads + kv_heads) * dh
     assert (q_gain is None or q_gain.numel() == dh) and (k_gain is None or k_gain.numel() == dh)
-    assert (positions is None or positions.numel() >= T) and (slots is None or slots.numel() >= T)
+    assert (positions is None or positions.numel() >= T) and (slots is None or slots.numel() >= T) and (cache is None or cache.device == at)
     if T == 0:
         return                                  # an empty tensor has no address
-    _check(lib().qzo_qk_norm_rope(x, ldx, T, q_heads, kv_heads, dh, _typed(q_gain, torch.bfloat16), _typed(k_gain, torch.bfloat16), eps, theta,
-                                  _typed(positions, torch.int32), seq, None if cache is None else C.addressof(cache),
-                                  _typed(slots, torch.int32), y, ldy, _here(stream, (qkv, out, positions, slots))))
+    _check(lib().qzo_qk_norm_rope(x, ldx, T, q_heads, kv_heads, dh, _at(q_gain, torch.bfloat16, at), _at(k_gain, torch.bfloat16, at), eps, theta,
+                                  _at(positions, torch.int32, at), seq, None if cache is None else C.addressof(cache),
+                                  _at(slots, torch.int32, at), y, ldy, _stream_of(stream, at)))
 
 
 def qzo_paged_attention_scratch_bytes(n_rows, n_seq, q_heads, head_dim) -> int:
@@ -564,22 +564,22 @@ def _scratch_of_stream(device, stream, handle, nbytes):
 
 def qzo_paged_attention(q, cache, tables, lengths, out, scale, starts=None, scratch="auto", stream=None):
     """q, out bf16 [rows, q_heads head_dim], rows may be strided; tables int32 [n_seq, max_blocks], lengths int32 [n_seq], starts
-    int32 [n_seq + 1] or None: a row per sequence."""
-    x, ldx = _rows(q)
-    y, ldy = _rows(out)
-    n, most = tables.shape
-    dh = cache.head_dim
-    heads = q.shape[1] // dh
-    assert q.dtype == out.dtype == torch.bfloat16 and q.shape == out.shape and heads * dh == q.shape[1]
+    int32 [n_seq + 1] or None: a row per sequence.  scratch: uint8, its first 2048 bytes zero before its first call; "auto": one
+    for all calls on the stream."""
+    at, i32, (rows, width), (n, most), dh = torch.cuda.current_device(), torch.int32, q.shape, tables.shape, cache.head_dim
+    x, ldx = _rows(q, at)
+    y, ldy = _rows(out, at)
+    heads = width // dh
+    assert q.shape == out.shape and heads * dh == width and cache.device == at
     assert lengths.numel() == n and (starts is None or starts.numel() == n + 1)
-    if q.shape[0] == 0:
+    if rows == 0:
         return
-    st = _here(stream, (q, out, tables, lengths, cache.tensors[0]))
+    st = _stream_of(stream, at)
     if isinstance(scratch, str):
-        scratch = _scratch_of_stream(q.device, stream, st, qzo_paged_attention_scratch_bytes(q.shape[0], n, heads, dh))
-    _check(lib().qzo_paged_attention(x, ldx, q.shape[0], n, heads, C.addressof(cache), _typed(tables, torch.int32), most,
-                                     _typed(lengths, torch.int32), _typed(starts, torch.int32), scale, y, ldy,
-                                     None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel() * scratch.element_size(), st))
+        scratch = _scratch_of_stream(at, stream, st, qzo_paged_attention_scratch_bytes(rows, n, heads, dh))
+    _check(lib().qzo_paged_attention(x, ldx, rows, n, heads, C.addressof(cache), _at(tables, i32, at), most, _at(lengths, i32, at),
+                                     _at(starts, i32, at), scale, y, ldy, None if scratch is None else scratch.data_ptr(),
+                                     0 if scratch is None else scratch.numel() * scratch.element_size(), st))
 
 
 def qzo_answer_workspace_bytes(model, n_tokens, n_seq) -> int:
@@ -592,7 +592,8 @@ def qzo_answer(model, tokens, cache, tables, lengths, starts, slots, positions, 
     """tokens int32 [n_tokens]; cache: of layer 0, the other layers' pools behind it; logits bf16 [n_seq, vocab]."""
     i32, (n, most) = torch.int32, tables.shape
     assert lengths.numel() == n and starts.numel() == n + 1 and slots.numel() >= tokens.numel() <= positions.numel() and logits.shape[0] == n
-    _check(lib().qzo_answer(model, _typed(tokens, i32), tokens.numel(), n, C.addressof(cache), _typed(tables, i32), most, _typed(lengths, i32),
-                            _typed(starts, i32), _typed(slots, i32), _typed(positions, i32), workspace.data_ptr(),
-                            workspace.numel() * workspace.element_size(), _typed(logits, torch.bfloat16),
-                            _here(stream, (tokens, tables, workspace, logits))))
+    at = torch.cuda.current_device()
+    assert cache.device == at == workspace.get_device()
+    _check(lib().qzo_answer(model, _at(tokens, i32, at), tokens.numel(), n, C.addressof(cache), _at(tables, i32, at), most, _at(lengths, i32, at),
+                            _at(starts, i32, at), _at(slots, i32, at), _at(positions, i32, at), workspace.data_ptr(),
+                            workspace.numel() * workspace.element_size(), _at(logits, torch.bfloat16, at), _stream_of(stream, at)))

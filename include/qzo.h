@@ -391,7 +391,7 @@ qzo_status qzo_cache_plan(const int32_t* cached_dev, const int32_t* added_dev, u
  *   cache given: out_dev receives the heads of q; k and v of the row go to slot slots_dev[t] of the cache (in e4m3: divided by
  *     their scale, cut off at +-448, rounded to nearest even).  A row whose slot is negative or beyond the pool is skipped, its
  *     out row included.  The slots of a call must differ from one another.
- * n_tokens below 2^26; head_dim 64 or 128 (of the cache, too); ld_qkv and ld_out multiples of 8, at least the row's heads; eps positive or 0.
+ * n_tokens below 2^25; head_dim 64 or 128 (of the cache, too); ld_qkv and ld_out multiples of 8, at least the row's heads; eps positive or 0.
  */
 qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tokens, uint32_t q_heads, uint32_t kv_heads,
                             uint32_t head_dim, const void* q_gain_dev, const void* k_gain_dev, float eps, float rope_theta,
@@ -422,7 +422,7 @@ qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows
                                uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream);
 
 /*
- * Answers: the model, as its scales are now and unperturbed, over the n_tokens newest tokens of n_seq sequences, whose earlier
+ * Answers: the model, as its scales (and in joint mode theta_u) are now and unperturbed, over the n_tokens newest tokens of n_seq sequences, whose earlier
  * tokens' keys and values are in the cache.  tokens_dev int32 [n_tokens] (values in [0, vocab)), sequence by sequence as qzo_cache_plan lists
  * them; starts_dev, slots_dev, positions_dev, lengths_dev, tables_dev as it left them (rows behind the last new token, slots of -1, are
  * padding: their tokens are read but reach nothing).  cache describes the pools of layer 0, kv_heads = n_heads and

@@ -480,7 +480,7 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
   const uint32_t seed_lo = (uint32_t)seed, seed_hi = (uint32_t)(seed >> 32);
   const unsigned char* arena = (const unsigned char*)m->arena;
 
-  if (m->dense_master && !ans) {      // joint mode: the 16-bit tensors become round16(theta_u + eps_signed z)
+  if (m->dense_master) {      // joint mode: the 16-bit tensors become round16(theta_u + eps_signed z)
     ProfScope ps(PK_OTHER, 0, st);
     QZO_HIP(launch_dense_perturb(m->dense_master, m->dense_segs, m->n_dense_segs, m->n_dense, seed_lo,
                                  seed_hi, eps_signed, st));
@@ -1692,7 +1692,7 @@ qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tok
     return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
   if (head_dim != 64 && head_dim != 128) return fail(QZO_ERR_SHAPE, "head_dim must be 64 or 128");
   if (!q_heads || !kv_heads || q_heads > 65535 || kv_heads > 65535) return fail(QZO_ERR_SHAPE, "q_heads and kv_heads must be 1 .. 65535");
-  if (n_tokens >= (1u << 26)) return fail(QZO_ERR_SHAPE, "n_tokens must be below 2^26");
+  if (n_tokens >= (1u << 25)) return fail(QZO_ERR_SHAPE, "n_tokens must be below 2^25");
   if (!std::isfinite(eps) || eps < 0.0f) return fail(QZO_ERR_ARG, "eps must be finite and not negative");
   if (!std::isfinite(rope_theta) || rope_theta < 0.0f) return fail(QZO_ERR_ARG, "rope_theta must be positive, or 0 for no rotation");
   if (!positions_dev && rope_theta > 0.0f && seq == 0) return fail(QZO_ERR_ARG, "positions or seq is needed");
@@ -1783,7 +1783,7 @@ static qzo_status answer_check(const qzo_model* m, uint32_t n_tokens, uint32_t n
   if (!m) return fail(QZO_ERR_ARG, "model is null");
   const qzo_model_config& c = m->cfg;
   if (!n_tokens || !n_seq || n_seq > CACHE_MAX_SEQ) return fail(QZO_ERR_SHAPE, "need n_tokens >= 1 and n_seq 1 .. 8192");
-  if (n_tokens >= (1u << 26)) return fail(QZO_ERR_SHAPE, "n_tokens must be below 2^26");
+  if (n_tokens >= (1u << 25)) return fail(QZO_ERR_SHAPE, "n_tokens must be below 2^25");
   if (c.vocab % 8) return fail(QZO_ERR_SHAPE, "logits are written for vocabularies that are multiples of 8");
   const uint64_t rows = passes_stacked(m, n_tokens) ? stacked_cut_rows(n_tokens) : n_tokens;
   if (rows * widest_row(c) * 2 >= (1ull << 31)) return fail(QZO_ERR_SHAPE, "n_tokens too large for this model: an activation tensor would exceed 2^31 bytes");

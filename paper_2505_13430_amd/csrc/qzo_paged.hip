@@ -43,12 +43,12 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // A group that lies in one workgroup is written by it; otherwise each leaves (maximum, sum, accumulators) in the scratch, its
 // first group's in place 2 b, a later one's (only the last can go on) in 2 b + 1, and who finds the group's counter at its last
 // piece adds them up, in order.  The counter (that of the workgroup of the group's first piece) goes back to zero.
-constexpr uint32_t COLS = 16, WAVES = 4, MAX_WGS = PAGED_COUNTERS;
+constexpr uint32_t COLS = 16, WAVES = 4, THREADS = 64 * WAVES, MAX_WGS = PAGED_COUNTERS;
 constexpr uint32_t SETUP = 1, MIN_PIECE = 2, WIDE_UNITS = 12288;
 
 struct SeqWork {
   uint32_t row0, rows, len, units, tiles, wide;
-  __device__ __forceinline__ uint32_t unit() const { return wide ? 32u : 128u; }                // keys
+  __device__ __forceinline__ uint32_t unit() const { return wide ? 32u : 32u * WAVES; }                // keys
   __device__ __forceinline__ uint32_t cols() const { return wide ? COLS * WAVES : COLS; }
 };
 
@@ -108,7 +108,7 @@ struct Joined {
 };
 
 template <class T>
-__device__ __forceinline__ T block_scan(T v, T* total, T* red) {     // exclusive, 256 threads
+__device__ __forceinline__ T block_scan(T v, T* total, T* red) {     // exclusive
   T s = v;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -150,7 +150,7 @@ struct PagedStep {
 };
 
 template <int DH, bool E4M3>
-__global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, uint32_t* counters, float* parts, uint32_t part_cols, uint32_t few, uint32_t may_be_wide) {
+__global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(PagedArgs a, uint32_t* counters, float* parts, uint32_t part_cols, uint32_t few, uint32_t may_be_wide) {
   constexpr int KS = DH / 32, VW = DH / 16, ES = E4M3 ? 1 : 2;
   typedef PagedStep<DH, E4M3> Step;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
   const uint32_t col = lane & 15u, g = lane >> 4;
 
   // ---- the sequences' units: up to 64 sequences in the lanes of every wavefront, more in the LDS
-  const uint32_t per = (a.n_seq + 255) / 256, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
+  const uint32_t per = (a.n_seq + THREADS - 1) / THREADS, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
   SeqWork lane_work = {0, 0, 0, 1, 0, 0};
   if (few && lane < a.n_seq) lane_work = seq_work(a, lane, false);
   bool wide = false;
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
     };
 
     // ---- the keys, a step at a time, the next one's on their way meanwhile
-    const int32_t round = w.wide ? 32 : 128;
+    const int32_t round = (int32_t)w.unit();
     int32_t kb = k_first + (w.wide ? 0 : (int32_t)(wave * 32u));
     if (kb < k_end) {
       Step one, two;
@@ -478,7 +478,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
               f32x4{acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j]};
     }
     __syncthreads();
-    for (uint32_t u = tid; u < n_group * DV; u += 256) {
+    for (uint32_t u = tid; u < n_group * DV; u += THREADS) {
       const uint32_t c = u / DV, d = u % DV * 4u;
       Joined j;
       if (w.wide) {
@@ -519,8 +519,8 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedArgs a, ui
   for (int which = 0; which < 2; ++which) {
     if (!arrived[which]) continue;
     const Cut& x = cut[which];
-    const uint32_t lanes = x.n_cols * DV, teams = max(1u, 256u / lanes), team = tid / lanes;      // of threads, each with its pieces
-    for (uint32_t u = tid % lanes; u < lanes && team < teams; u += 256) {
+    const uint32_t lanes = x.n_cols * DV, teams = max(1u, THREADS / lanes), team = tid / lanes;      // of threads, each with its pieces
+    for (uint32_t u = tid % lanes; u < lanes && team < teams; u += THREADS) {
       const uint32_t c = u / DV, d = u % DV * 4u;
       Joined j;
       // eight pieces' loads at a time: a trip to memory each
@@ -574,7 +574,7 @@ hipError_t launch_paged(const PagedArgs& a, void* scratch, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (groups * ((units + MIN_PIECE - 1) / MIN_PIECE) + 7) / 8 * 8);
-  paged_attention_kernel<DH, E4M3><<<wgs, 256, lds, st>>>(a, counters, parts, part_columns(rows, a.group), few, rows * a.group > 2 * COLS && (a.starts || a.group > 2 * COLS));
+  paged_attention_kernel<DH, E4M3><<<wgs, THREADS, lds, st>>>(a, counters, parts, part_columns(rows, a.group), few, rows * a.group > 2 * COLS && (a.starts || a.group > 2 * COLS));
   return hipGetLastError();
 }
 

@@ -224,15 +224,19 @@ class Answers:
         self.state = torch.tensor([n_blocks, 0, 0, 0], **i32)
         self.lengths, self.starts = torch.zeros(n_seq, **i32), torch.zeros(n_seq + 1, **i32)
         self.logits = torch.zeros(n_seq, self.vocab, dtype=torch.bfloat16, device=dev)
-        self._rows = {}
+        self._kept = [(torch.zeros(0, **i32), torch.zeros(0, **i32), torch.zeros(0, dtype=torch.uint8, device=dev))]
 
     def rows(self, n_tokens: int):
-        """Slots, positions and workspace of steps of that many rows."""
-        if n_tokens not in self._rows:
-            i32 = dict(dtype=torch.int32, device=self.free.device)
-            ws = torch.empty(qb.qzo_answer_workspace_bytes(self.model.handle, n_tokens, len(self.lengths)), dtype=torch.uint8, device=self.free.device)
-            self._rows[n_tokens] = (torch.zeros(n_tokens, **i32), torch.zeros(n_tokens, **i32), ws)
-        return self._rows[n_tokens]
+        """Slots, positions and workspace of steps of that many rows, from buffers that double as they are outgrown; the earlier ones
+        are kept for the graphs that were captured with them."""
+        slots, positions, ws = self._kept[-1]
+        need = qb.qzo_answer_workspace_bytes(self.model.handle, n_tokens, len(self.lengths))
+        if slots.numel() < n_tokens or ws.numel() < need:
+            dev, n = self.free.device, max(n_tokens, 2 * slots.numel())
+            slots, positions = (torch.zeros(n, dtype=torch.int32, device=dev) for _ in range(2))
+            ws = torch.empty(max(need, 2 * ws.numel()), dtype=torch.uint8, device=dev)
+            self._kept.append((slots, positions, ws))
+        return slots[:n_tokens], positions[:n_tokens], ws
 
     def add(self, tokens: torch.Tensor, added: torch.Tensor, stream=None) -> torch.Tensor:
         """tokens int32 [rows], the new tokens sequence by sequence, padded at the end; added int32 [n_seq], how many each adds (negative:

@@ -106,6 +106,18 @@ def test_answers_use_the_scales_as_they_are():
 
 
 @gpu
+def test_answers_of_a_jointly_trained_model():
+    """A perturbed forward in joint mode leaves the 16-bit tensors perturbed; an answer is the unperturbed model's."""
+    m = _model("tiny", "int4")
+    m.enable_joint()
+    text = torch.arange(40, dtype=torch.int32, device=DEV)
+    want = _logits(m, text)
+    m.forward_loss(text.view(1, -1), 3, 0.05, 1)
+    a = Answers(m, n_seq=1, n_blocks=4, block=16)
+    assert _far(a.add(text, torch.tensor([40], dtype=torch.int32, device=DEV))[0], want[-1]) <= 2e-2
+
+
+@gpu
 def test_a_step_that_cannot_be_planned_changes_nothing():
     m = _model("wide_heads", "int4")
     a = Answers(m, n_seq=2, n_blocks=3, block=16)

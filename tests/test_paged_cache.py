@@ -129,7 +129,7 @@ def test_plan_refuses(over, status):
     (dict(q_gain=20), qb.QZO_ERR_ALIGN), (dict(dh=96), qb.QZO_ERR_SHAPE), (dict(q_heads=0), qb.QZO_ERR_SHAPE), (dict(kv_heads=0), qb.QZO_ERR_SHAPE),
     (dict(eps=-1.0), qb.QZO_ERR_ARG), (dict(eps=math.nan), qb.QZO_ERR_ARG), (dict(theta=-1.0), qb.QZO_ERR_ARG), (dict(theta=math.inf), qb.QZO_ERR_ARG),
     (dict(seq=0), qb.QZO_ERR_ARG), (dict(ldx=508), qb.QZO_ERR_SHAPE), (dict(ldx=504), qb.QZO_ERR_SHAPE), (dict(ldy=376), qb.QZO_ERR_SHAPE),
-    (dict(tokens=1 << 31), qb.QZO_ERR_SHAPE), (dict(out=16, ldx=512, ldy=384), qb.QZO_ERR_ARG)])
+    (dict(tokens=1 << 25), qb.QZO_ERR_SHAPE), (dict(out=16, ldx=512, ldy=384), qb.QZO_ERR_ARG)])
 def test_qk_norm_rope_refuses(over, status):
     v = dict(qkv=16, ldx=512, tokens=4, q_heads=4, kv_heads=2, dh=64, q_gain=None, k_gain=None, eps=1e-6, theta=10000.0, positions=None, seq=8, cache=None,
              slots=None, out=32, ldy=384)
@@ -210,7 +210,7 @@ def test_plan(cached, added, block, in_place):
 @gpu
 @pytest.mark.parametrize("n,block,longest,most_added,ends,pad,seed", [
     (63, 16, 300, 5, 0.2, 1, 1), (1023, 16, 90, 1, 0.1, 100, 2), (1025, 32, 200, 9, 0.3, 1, 3), (3000, 64, 500, 2, 0.02, 9, 4),
-    (8192, 16, 60, 3, 0.1, 1, 5), (40, 128, 9000, 4000, 0.1, 77, 6), (2, 16, 10, 40000, 0.0, 1, 7)])
+    (8192, 16, 60, 3, 0.1, 1, 5), (8192, 16, 60, 0, 0.3, 4000, 8), (40, 128, 9000, 4000, 0.1, 77, 6), (2, 16, 10, 40000, 0.0, 1, 7)])
 def test_plan_of_many(n, block, longest, most_added, ends, pad, seed):
     """From one to 8192 sequences, with more than 4096 tokens and fewer."""
     rng = np.random.default_rng(seed)
@@ -449,6 +449,41 @@ def test_attention_of_ragged_batches(n, longest, H, Hk, dh, block, seed):
 
 
 @gpu
+def test_attention_of_more_and_fewer_rows_than_sequences():
+    """A row per sequence, with rows behind the last sequence (left as they are), and with sequences that have no row."""
+    _check_attend(_attend([40, 0, 300], 4, 2, 64, 16, seed=1, pad_rows=4, stride=16))
+    d = _attend([40, 70, 300], 4, 2, 64, 16, seed=1, run=False)
+    qb.qzo_paged_attention(d["args"][0][:2], d["cache"], *d["args"][2:4], d["args"][4][:2], d["scale"])
+    assert bool((d["outd"][2] == 7.0).all())
+    whole = _attend([40, 70, 300], 4, 2, 64, 16, seed=1)
+    assert torch.equal(d["outd"][:2], whole["outd"][:2])
+    _check_attend(_attend([40, 70], 4, 2, 64, 16, e4m3=True, scaled=False, seed=2))
+
+
+@gpu
+def test_attention_with_room_for_very_long_sequences():
+    """Tables whose rows reach 2^29 positions: the units of what might be no longer fit 32 bits."""
+    d = _attend([40, 700], 8, 4, 64, 16, seed=5, run=False)
+    wide = torch.full((2, 1 << 25), -1, dtype=torch.int32, device=DEV)
+    wide[:, :d["tables"].shape[1]] = d["args"][2]
+    qb.qzo_paged_attention(*d["args"][:2], wide, *d["args"][3:])
+    _check_attend(d)
+
+
+@gpu
+def test_a_row_of_nan_stays_alone():
+    for news in (None, [1, 3]):
+        clean = _attend([100, 70], 4, 2, 128, 16, news, seed=7)
+        d = _attend([100, 70], 4, 2, 128, 16, news, seed=7, run=False)
+        d["qd"][1, 130] = math.nan                           # head 1 of row 1
+        d["qd"][1, 300] = math.inf                           # head 2
+        qb.qzo_paged_attention(*d["args"])
+        bad = torch.zeros_like(d["outd"], dtype=torch.bool)
+        bad[1, 128:384] = True
+        assert not torch.isfinite(d["outd"][bad]).any() and torch.equal(d["outd"][~bad], clean["outd"][~bad])
+
+
+@gpu
 @pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
 @pytest.mark.parametrize("lengths,news", [([1, 17, 100, 0, 333], None), ([9, 100, 333], [9, 3, 40])])
 def test_unseen_positions_hold_anything(lengths, news, e4m3):
@@ -632,21 +667,19 @@ def test_calls_on_two_streams_at_once():
             qb.qzo_paged_attention(*d["args"], stream=s)
     torch.cuda.synchronize()
     assert torch.equal(a["outd"], want[0]) and torch.equal(b["outd"], want[1])
-    if qb.qzo_paged_attention_scratch_bytes(3, 3, 8, 128):
-        g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        a["outd"].zero_()
         with pytest.raises(AssertionError):
-            with torch.cuda.graph(g):
-                qb.qzo_paged_attention(*a["args"])
+            qb.qzo_paged_attention(*a["args"])
 
 
 @gpu
 def test_scratch_that_is_too_small_is_refused():
     d = _attend([100], 4, 2, 64, 16, seed=1)
     need = qb.qzo_paged_attention_scratch_bytes(1, 1, 4, 64)
-    if need:
-        before = d["outd"].clone()
-        for small in (torch.empty(need - 1, dtype=torch.uint8, device=DEV), None):
-            with pytest.raises(qb.QzoError):
-                qb.qzo_paged_attention(*d["args"], scratch=small)
-        torch.cuda.synchronize()
-        assert torch.equal(before, d["outd"])
+    before = d["outd"].clone()
+    for small in (torch.zeros(need - 1, dtype=torch.uint8, device=DEV), None):
+        with pytest.raises(qb.QzoError):
+            qb.qzo_paged_attention(*d["args"], scratch=small)
+    torch.cuda.synchronize()
+    assert torch.equal(before, d["outd"])

@@ -19,27 +19,13 @@ __device__ __forceinline__ uint32_t last_not_above(const int32_t* prefix, uint32
   return lo;
 }
 
-// Inclusive sum over the lanes: within rows of 16, then rows 0 and 2 into 1 and 3, then both into the upper half.
-template <int CTRL, int ROWS, class T>
-__device__ __forceinline__ T from_before(T v) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false)); }
-template <class T>
-__device__ __forceinline__ T lane_scan(T v) {
-  v += from_before<0x111, 0xf>(v);              // row_shr:1, 2, 4, 8
-  v += from_before<0x112, 0xf>(v);
-  v += from_before<0x114, 0xf>(v);
-  v += from_before<0x118, 0xf>(v);
-  v += from_before<0x142, 0xa>(v);              // row_bcast:15
-  v += from_before<0x143, 0xc>(v);              // row_bcast:31
-  return v;
-}
-
 // One workgroup, a sequence (or several) per thread.  What sequence i gives back (ended), takes and adds is summed over the
 // sequences before it; the sums stay in the LDS, where blocks given back, and the blocks and tokens of long prompts, find their
 // sequence by bisection and are spread over all threads.  Every input is read before the first output is written (lengths
 // may be cached, after may be before), and no output of this launch is read back: a taken block is found in the free list or
 // in the row of the sequence that gives it back, neither of which changes below the stack's old height.
 // Latency is all there is to it: lengths, sums, free list, stores.  The block that a sequence's next token falls into is
-// loaded beside the lengths.  8 sequences PLAN_8 us, 1000 PLAN_1000 us.
+// loaded beside the lengths.  8 sequences 3.8 us, 1000 6.4, 300 with prompts of 801 tokens 10.4 with the second launch.
 // with_slots: slots and positions too (few tokens); else cache_slots_kernel follows.
 constexpr uint32_t PLAN_THREADS = 1024, PLAN_FEW = 4;      // a thread itself sees to that many tokens, and their blocks
 __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs a, uint32_t with_slots) {
@@ -209,8 +195,12 @@ hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t st) {
 // DH/8 lanes hold a head, eight features each; a wavefront takes 64 / (DH/8) heads at a time and walks over its share of
 // the token's heads with the same angles.
 //
-// Memory counts, and how much of it is on its way: a wavefront loads the heads of its next BATCH turns before it works on the
-// ones it has, and a token is spread over as many wavefronts as it takes to have WAVES of them.
+// Memory counts, and how much of it is on its way: a wavefront loads its next heads before it works on the ones it has, and a
+// token is spread over as many wavefronts as it takes to have QK_WAVES of them (2500 tokens, 120 heads of 128, with 4096 / 8192 /
+// 16384 / 24576 / 32768 / 65536: 44 / 37 / 35 / 34 / 34 / 40 us).  The cosine and sine of a pair are computed once per
+// wavefront, by one lane, and handed out through the LDS (each lane its own eight: 41 us).  One token 2.5 us; 16 x 512 tokens,
+// q and k of 32 heads of 128: 53 us, 5.0 TB/s read and written, as a copy of 2 GiB (4.9); with an e4m3 cache, 7001 tokens, 64
+// and 8 heads of 64, 32 us, 4.3 TB/s.
 
 // Values of the lanes of a head (16, or 8): their sum; that of the lane half a head away.  Exchanges within rows of 16 lanes.
 template <int CTRL>

@@ -171,6 +171,20 @@ __device__ __forceinline__ float flat_normal(uint32_t seed_lo, uint32_t seed_hi,
   return (i & 1u) ? z1 : z0;
 }
 
+// Inclusive sum over the lanes: within rows of 16, then rows 0 and 2 into 1 and 3, then both into the upper half.
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T from_before(T v) { return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false)); }
+template <class T>
+__device__ __forceinline__ T lane_scan(T v) {
+  v += from_before<0x111, 0xf>(v);              // row_shr:1, 2, 4, 8
+  v += from_before<0x112, 0xf>(v);
+  v += from_before<0x114, 0xf>(v);
+  v += from_before<0x118, 0xf>(v);
+  v += from_before<0x142, 0xa>(v);              // row_bcast:15
+  v += from_before<0x143, 0xc>(v);              // row_bcast:31
+  return v;
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);

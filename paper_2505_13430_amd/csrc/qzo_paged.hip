@@ -14,7 +14,11 @@
 // All of a column's state (maximum, sum, its 4 VW accumulators) is in the lanes that hold the column.
 //
 // What bounds it: memory.  A step of a wavefront loads its next 32 keys (16 KB at heads of 128, bf16) before it works on the
-// ones it has; eight wavefronts on a compute unit keep 128 KB on the way.
+// ones it has; eight wavefronts on a compute unit keep 128 to 256 KB on the way.  Loads and block ids are issued without a branch
+// around them, or the compiler waits for all of them at every use.  8 sequences of 65536 tokens, 8 key heads of 128: 370 us,
+// 5.8 TB/s (a kernel that only reads: 6.1 to 6.3); 64 ragged ones of up to 4001, 32 key heads, 151 us, 5.4 TB/s; 24 in e4m3 of up
+// to 32001, 87 us, 4.9 TB/s, 75 of them the cache at the rate of the first.  Few keys: latency.  One token 5.4 us (launch, lengths,
+// table, keys, one after the other); a compute unit alone takes 54 GB/s, 1.2 us a unit.
 #include <algorithm>
 #include "qzo_device.hpp"
 #include "qzo_kernels.hpp"
@@ -27,13 +31,18 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 typedef const int32_t __attribute__((address_space(4)))* table_t;      // read by scalar loads: no vector load in between
 
-// How the work is dealt out.  A group is 16 columns of one sequence and key head; the four wavefronts of a workgroup take every
-// fourth step (32 keys) of it, a unit is a step of each, 128 keys.  With much to do (WIDE_UNITS), a group of a sequence of more
-// than 32 columns (several new tokens) is 64 of them, 16 a wavefront, all with the same keys; a unit is then 32 keys.  It reads
-// the keys once for the four, but has a quarter of the loads on their way.  16 columns / 64 columns, us: 16 prompts of 512
-// tokens, 32 heads of 128 (34816 units of 16 columns) 351 / 212; 6 x 100 tokens behind 1900, heads of 128 (21504) 194 / 144, of
-// 64 95 / 81; behind 900 on average (11300) 51 / 55; 4 x 8 tokens, 64 heads on 8, behind 9000 (9088) 62 / 89; one prompt of
-// 512 (4096) 32 / 43.
+// A wavefront has 16 columns; with heads of 64, for sequences of many columns (several new tokens; MANY_COLS on average), 32,
+// two tiles that share the keys and the transposed values.  16 / 32 columns, us, 32 heads of 64: 16 prompts of 512 123 / 73, one
+// 19 / 14, 6 x 100 tokens behind 1900 81 / 62, behind 900 44 / 38, 20 x 30 behind 970 63 / 50, 20 x 20 62 / 63.  (Heads of 128
+// have no registers for it: with one step's keys and values in place of two, 277 us for the 144 of 6 x 100 tokens.)
+//
+// How the work is dealt out.  A group is a wavefront's columns of one sequence and key head; the four wavefronts of a workgroup
+// take every fourth step (32 keys) of it, a unit is a step of each, 128 keys.  A wide group is four times those columns, a part
+// for each wavefront, all with the same keys; a unit is then 32 keys.  It reads the keys once for the four and there are fewer
+// groups, but it has a quarter of the loads on their way.  Narrow / wide, us, heads of 128: 16 prompts of 512 tokens (34816
+// narrow units) 351 / 212, 6 x 100 tokens behind 1900 (21504) 194 / 144, 4 x 8 tokens, 64 heads on 8, behind 9000 (9088)
+// 62 / 89, one prompt of 512 (4096) 32 / 43: wide from WIDE_UNITS on.  Heads of 64 with 32 columns, where there are few units
+// a group: the prompts (4 of them) 130 / 73, but 6 x 100 tokens (16) 62 / 76, 4 x 200, 40 heads on 8 in e4m3 (32) 77 / 91.
 //   Every group is given a span, its units behind some padding, all spans are counted through, and workgroup b takes those from
 // share b to share (b + 1) - 1.
 //   Few groups: the shortest piece that leaves no more pieces than workgroups is the share, and a span is a multiple of it, so
@@ -44,15 +53,15 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // first group's in place 2 b, a later one's (only the last can go on) in 2 b + 1, and who finds the group's counter at its last
 // piece adds them up, in order.  The counter (that of the workgroup of the group's first piece) goes back to zero.
 constexpr uint32_t COLS = 16, WAVES = 4, THREADS = 64 * WAVES, MAX_WGS = PAGED_COUNTERS;
-constexpr uint32_t SETUP = 1, MIN_PIECE = 2, WIDE_UNITS = 12288;
+constexpr uint32_t SETUP = 1, MIN_PIECE = 2, WIDE_UNITS = 12288, MANY_COLS = 24;
 
 struct SeqWork {
   uint32_t row0, rows, len, units, tiles, wide;
   __device__ __forceinline__ uint32_t unit() const { return wide ? 32u : 32u * WAVES; }                // keys
-  __device__ __forceinline__ uint32_t cols() const { return wide ? COLS * WAVES : COLS; }
+  __device__ __forceinline__ uint32_t cols(uint32_t tc) const { return wide ? tc * WAVES : tc; }      // tc: of a wavefront
 };
 
-__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool wide) {
+__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool wide, uint32_t tc) {
   SeqWork w;
   w.row0 = i; w.rows = i < a.n_rows ? 1u : 0u;
   if (a.starts) {
@@ -61,26 +70,15 @@ __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool
   }
   w.len = (uint32_t)min(max(a.lengths[i], 0), (int32_t)(a.max_blocks << a.block_shift));
   const uint64_t cols = (uint64_t)w.rows * a.group;
-  w.wide = wide && cols > 2 * COLS;
+  w.wide = wide && cols > 2 * tc;
   w.units = max(1u, (w.len + w.unit() - 1) / w.unit());
-  w.tiles = (uint32_t)((cols + w.cols() - 1) / w.cols());
+  w.tiles = (uint32_t)((cols + w.cols(tc) - 1) / w.cols(tc));
   return w;
 }
 
 // What all lanes agree on, in a scalar register.
 __device__ __forceinline__ uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 __device__ __forceinline__ uint64_t scalar64(uint64_t x) { return (uint64_t)scalar((uint32_t)(x >> 32)) << 32 | scalar((uint32_t)x); }
-
-// Inclusive sum over the lanes: within rows of 16, then rows 0 and 2 into 1 and 3, then both into the upper half.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);       // row_shr:1, 2, 4, 8
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);       // row_bcast:15
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);       // row_bcast:31
-  return v;
-}
 
 // Two floats for another workgroup, on any XCD: stored through the L2 and loaded past it (agent scope), so that no L2 has to be
 // written back or invalidated as a whole, which a fence of that scope does (64 ragged sequences: 366 us with fences).  A
@@ -149,15 +147,16 @@ struct PagedStep {
   uint32_t v[8][VD];
 };
 
-template <int DH, bool E4M3>
+template <int DH, bool E4M3, int CT>
 __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(PagedArgs a, uint32_t* counters, float* parts, uint32_t part_cols, uint32_t few, uint32_t may_be_wide) {
   constexpr int KS = DH / 32, VW = DH / 16, ES = E4M3 ? 1 : 2;
+  constexpr uint32_t TC = COLS * CT, STRIDE = DH + 4;       // columns of a wavefront
   typedef PagedStep<DH, E4M3> Step;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  float* const sum_acc = (float*)lds;                                   // [WAVES][COLS][DH + 4]
-  float* const sum_m = sum_acc + WAVES * COLS * (DH + 4);               // [WAVES][COLS]
-  float* const sum_l = sum_m + WAVES * COLS;
-  uint64_t* const red = (uint64_t*)(sum_l + WAVES * COLS);              // [WAVES]
+  float* const sum_acc = (float*)lds;                                   // [WAVES][TC][STRIDE]
+  float* const sum_m = sum_acc + WAVES * TC * STRIDE;                   // [WAVES][TC]
+  float* const sum_l = sum_m + WAVES * TC;
+  uint64_t* const red = (uint64_t*)(sum_l + WAVES * TC);                // [WAVES]
   uint64_t* const first_unit = red + WAVES;                             // [n_seq], more than 64 sequences only
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = scalar(tid >> 6);
   const uint32_t col = lane & 15u, g = lane >> 4;
@@ -165,21 +164,21 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
   // ---- the sequences' units: up to 64 sequences in the lanes of every wavefront, more in the LDS
   const uint32_t per = (a.n_seq + THREADS - 1) / THREADS, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
   SeqWork lane_work = {0, 0, 0, 1, 0, 0};
-  if (few && lane < a.n_seq) lane_work = seq_work(a, lane, false);
+  if (few && lane < a.n_seq) lane_work = seq_work(a, lane, false, TC);
   bool wide = false;
   auto sum = [&](auto&& f) -> uint64_t {            // of f over the sequences
-    if (few) return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan((uint32_t)f(lane_work)), 63);
+    if (few) return (uint32_t)__builtin_amdgcn_readlane((int)lane_scan((uint32_t)f(lane_work)), 63);
     uint64_t n = 0, all;
-    for (uint32_t i = s_first; i < s_last; ++i) n += f(seq_work(a, i, wide));
+    for (uint32_t i = s_first; i < s_last; ++i) n += f(seq_work(a, i, wide, TC));
     block_scan(n, &all, red);
     return scalar64(all);
   };
   auto groups_of = [&](const SeqWork& w) { return (uint64_t)w.tiles * a.kv_heads; };
   auto units_of = [&](const SeqWork& w) { return w.units * groups_of(w); };
   uint64_t groups = sum(groups_of), units = sum(units_of);
-  if (may_be_wide && units >= WIDE_UNITS) {
+  if (may_be_wide && units >= WIDE_UNITS && (CT == 1 || units <= 8 * groups)) {
     wide = true;
-    if (few && lane < a.n_seq) lane_work = seq_work(a, lane, true);
+    if (few && lane < a.n_seq) lane_work = seq_work(a, lane, true, TC);
     groups = sum(groups_of); units = sum(units_of);
   }
   uint32_t piece = 0;                               // 0: even shares
@@ -197,13 +196,13 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
   uint64_t total;
   uint32_t mine = 0;
   if (few) {
-    const uint32_t n = (uint32_t)(span_of(lane_work) * groups_of(lane_work)), upto = wave_scan(n);
+    const uint32_t n = (uint32_t)(span_of(lane_work) * groups_of(lane_work)), upto = lane_scan(n);
     mine = upto - n;
     total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   } else {
     uint64_t n = 0;
     for (uint32_t i = s_first; i < s_last; ++i) {
-      const SeqWork w = seq_work(a, i, wide);
+      const SeqWork w = seq_work(a, i, wide, TC);
       first_unit[i] = n;
       n += span_of(w) * groups_of(w);
     }
@@ -223,7 +222,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
   // the cut groups of this workgroup: the one that its share begins with, the one that it ends with
   struct Cut { uint32_t row0, group_col, kh, n_cols, wg_first, pieces, first_place; };
   Cut cut[2] = {};
-  constexpr uint32_t DV = DH / 4, STRIDE = DH + 4;
+  constexpr uint32_t DV = DH / 4;
   auto part_of = [&](uint32_t place) { return parts + (uint64_t)place * part_cols * STRIDE; };
   auto put = [&](uint32_t row0, uint32_t group_col, uint32_t kh, uint32_t c, uint32_t d, const Joined& j) {       // a column that saw nothing: zero
     const float inv = (E4M3 && a.v_scale ? a.v_scale[kh] : 1.0f) / j.l;
@@ -250,7 +249,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       }
       seq = scalar(lo);
       seq_first = scalar64(first_unit[seq]);
-      w = seq_work(a, seq, wide);
+      w = seq_work(a, seq, wide, TC);
       w = {scalar(w.row0), scalar(w.rows), scalar(w.len), scalar(w.units), scalar(w.tiles), scalar(w.wide)};
     }
     const uint32_t span = scalar(span_of(w)), pad = span - w.units;
@@ -274,32 +273,40 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     }
 
     // ---- this wavefront's columns
-    const uint32_t all_cols = w.rows * a.group, group_col = tile * w.cols(), n_group = min(w.cols(), all_cols - group_col);
-    const uint32_t first_col = group_col + (w.wide ? wave * COLS : 0u), n_cols = first_col < all_cols ? min(COLS, all_cols - first_col) : 0u;
-    const bool live = col < n_cols;
-    const uint32_t flat = live ? first_col + col : group_col, token = flat / a.group, head = kh * a.group + flat % a.group;
-    const uint64_t row = w.row0 + token;
+    const uint32_t all_cols = w.rows * a.group, group_col = tile * w.cols(TC), n_group = min(w.cols(TC), all_cols - group_col);
+    const uint32_t first_col = group_col + (w.wide ? wave * TC : 0u), n_cols = first_col < all_cols ? min(TC, all_cols - first_col) : 0u;
+    bool live[CT];
     // positions that a column sees, that the first (the fewest) and the last (the most) of them see
-    const int32_t sees = live ? (int32_t)(w.len + token + 1u - w.rows) : 0;
+    int32_t sees[CT];
     const int32_t least = (int32_t)(w.len + first_col / a.group + 1u - w.rows);
     const int32_t most = n_cols ? (int32_t)(w.len + (first_col + n_cols - 1) / a.group + 1u - w.rows) : 0;
     const int32_t k_first = (int32_t)(u_first * w.unit()), k_end = (int32_t)min((int64_t)most, (int64_t)u_end * w.unit());
-
-    bf16x8 q[KS];
+    bf16x8 q[CT][KS];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      // e4m3: a 16-byte load of K is two operands
-      const uint32_t d = E4M3 ? (uint32_t)(s / 2) * 64u + g * 16u + (uint32_t)(s & 1) * 8u : (uint32_t)s * 32u + g * 8u;
-      u32x4v x = {0u, 0u, 0u, 0u};
-      if (live) x = *reinterpret_cast<const u32x4v*>(a.q + row * a.ld_q + (uint64_t)head * DH + d);
-      q[s] = __builtin_bit_cast(bf16x8, x);
+    for (int ct = 0; ct < CT; ++ct) {
+      live[ct] = ct * COLS + col < n_cols;
+      const uint32_t flat = live[ct] ? first_col + ct * COLS + col : group_col, token = flat / a.group, head = kh * a.group + flat % a.group;
+      sees[ct] = live[ct] ? (int32_t)(w.len + token + 1u - w.rows) : 0;
+      const bf16_t* from = a.q + (uint64_t)(w.row0 + token) * a.ld_q + (uint64_t)head * DH;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        // e4m3: a 16-byte load of K is two operands
+        const uint32_t d = E4M3 ? (uint32_t)(s / 2) * 64u + g * 16u + (uint32_t)(s & 1) * 8u : (uint32_t)s * 32u + g * 8u;
+        u32x4v x = {0u, 0u, 0u, 0u};
+        if (live[ct]) x = *reinterpret_cast<const u32x4v*>(from + d);
+        q[ct][s] = __builtin_bit_cast(bf16x8, x);
+      }
     }
     const float ks = (E4M3 && a.k_scale ? a.k_scale[kh] : 1.0f) * a.scale * 1.44269504088896f;
 
-    f32x4 acc[VW];
+    f32x4 acc[CT][VW];
+    float m[CT], l[CT];
 #pragma unroll
-    for (int i = 0; i < VW; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float m = -INFINITY, l = 0.0f;
+    for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+      for (int i = 0; i < VW; ++i) acc[ct][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      m[ct] = -INFINITY; l[ct] = 0.0f;
+    }
 
     // ---- where the keys are: a block id per tile, in scalar registers, a step ahead of the loads that need it
     const table_t table = (table_t)(uintptr_t)(a.tables + (uint64_t)seq * a.max_blocks);
@@ -310,15 +317,11 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     auto blocks = [&](int32_t kb) {
       return Ids{{(uint32_t)table[(uint32_t)min(kb, last_tile) >> a.block_shift], (uint32_t)table[(uint32_t)min(kb + 16, last_tile) >> a.block_shift]}};
     };
-    // Loads a step's keys and values; returns a bit per tile, whether its block is in the pool.
-    auto load = [&](Step& st, int32_t kb, const Ids& ids) -> uint32_t {
-      uint32_t there = 0;
+    auto present = [&](const Ids& ids) { return (ids.id[0] < a.n_blocks ? 1u : 0u) | (ids.id[1] < a.n_blocks ? 2u : 0u); };     // blocks of the pool
+    auto load = [&](Step& st, int32_t kb, const Ids& ids) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint32_t pos = (uint32_t)min(kb + t * 16, last_tile);
-        const bool in = ids.id[t] < a.n_blocks;
-        there |= (in ? 1u : 0u) << t;
-        const uint32_t id = in ? ids.id[t] : 0u;
+        const uint32_t pos = (uint32_t)min(kb + t * 16, last_tile), id = ids.id[t] < a.n_blocks ? ids.id[t] : 0u;
         const uint64_t at = ((((uint64_t)id * a.kv_heads + kh) << a.block_shift) + (pos & in_block)) * (uint64_t)(DH * ES);
         const unsigned char* kp = (const unsigned char*)a.k + at;
         const unsigned char* vp = (const unsigned char*)a.v + at;
@@ -340,16 +343,15 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
           }
         }
       }
-      return there;
     };
 
     auto key_of = [&](int32_t kb, int j) { return kb + (j >> 2) * 16 + (int32_t)(4u * g) + (j & 3); };
-    auto work = [&](Step& st, int32_t kb, uint32_t there) {
-      const bool whole = kb + 32 <= least && there == 3u;
-      f32x4 s[2];
+    auto whole_step = [&](int32_t kb, uint32_t there) { return kb + 32 <= least && there == 3u; };       // every column sees all of it
+    auto scores = [&](const Step& st, f32x4 (&s)[CT][2]) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) s[ct][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
           u32x4v x;
@@ -359,36 +361,43 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
           } else {
             x = st.k[t][i];
           }
-          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[i], c, 0, 0, 0);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) s[ct][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[ct][i], s[ct][t], 0, 0, 0);
         }
-        s[t] = c * ks;
       }
-      if (!whole) {
+    };
+    // s becomes p, as the second product's operand; the sums follow
+    auto softmax = [&](int ct, f32x4 (&s)[2], int32_t kb, uint32_t there) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s[t] *= ks;
+      if (!whole_step(kb, there)) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (key_of(kb, j) >= sees || !(there >> (j >> 2) & 1u)) s[j >> 2][j & 3] = -INFINITY;
+          if (key_of(kb, j) >= sees[ct] || !(there >> (j >> 2) & 1u)) s[j >> 2][j & 3] = -INFINITY;
       }
       float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-      if (__any(top > m + 8.0f)) {           // m = -infinity: any key at all
+      if (__any(top > m[ct] + 8.0f)) {           // m = -infinity: any key at all
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float m2 = fmaxf(m, top), f = m2 == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m2);
-        l *= f;
+        const float m2 = fmaxf(m[ct], top), f = m2 == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[ct] - m2);
+        l[ct] *= f;
 #pragma unroll
-        for (int i = 0; i < VW; ++i) acc[i] *= f;
-        m = m2;
+        for (int i = 0; i < VW; ++i) acc[ct][i] *= f;
+        m[ct] = m2;
       }
-      const float base = m == -INFINITY ? 0.0f : m;
+      const float base = m[ct] == -INFINITY ? 0.0f : m[ct];
       float e[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         e[j] = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - base);
-        l += e[j];
+        l[ct] += e[j];
       }
       // p as bf16: 2^-8 of each term at most, in a sum of many; v has no more bits either
-      const bf16x8 pk = __builtin_bit_cast(bf16x8, u32x4v{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])});
+      return __builtin_bit_cast(bf16x8, u32x4v{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])});
+    };
+    auto values = [&](Step& st, const bf16x8 (&pk)[CT], int32_t kb, uint32_t there) {
       bool apart = false;
-      if (!whole) {
+      if (!whole_step(kb, there)) {
         // 0 times what an unseen value holds is no 0 where that is NaN or infinite: nobody's positions become 0, and where
         // one that only some of the columns see is not finite, every column has its own product
         uint32_t odd = 0;
@@ -405,16 +414,12 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
         }
         apart = least < most && __any(odd != 0);
       }
-      // features 2 u and 2 u + 1 of a lane's VW: eight keys of two columns, two operands
-      auto products = [&](int u, const uint32_t (&y)[8], f32x4& even, f32x4& uneven) {
-        u32x4v lo, hi;
+      // features 2 u and 2 u + 1 of a lane's VW: eight keys of two rows of V^T, two operands
+      auto operand = [&](const uint32_t (&y)[8], uint32_t pick) {
+        u32x4v o;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          lo[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x05040100u);
-          hi[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x07060302u);
-        }
-        even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pk, acc[2 * u], 0, 0, 0);
-        uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pk, acc[2 * u + 1], 0, 0, 0);
+        for (int j = 0; j < 4; ++j) o[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], pick);
+        return __builtin_bit_cast(bf16x8, o);
       };
       auto value = [&](int j, int u) { return E4M3 ? two_bf16(st.v[j][u / 2], u & 1) : st.v[j][u % Step::VD]; };
       if (!apart) {
@@ -423,20 +428,28 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
           uint32_t y[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) y[j] = value(j, u);
-          products(u, y, acc[2 * u], acc[2 * u + 1]);
+          const bf16x8 even = operand(y, 0x05040100u), uneven = operand(y, 0x07060302u);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            acc[ct][2 * u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pk[ct], acc[ct][2 * u], 0, 0, 0);
+            acc[ct][2 * u + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uneven, pk[ct], acc[ct][2 * u + 1], 0, 0, 0);
+          }
         }
       } else {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll 1
-        for (uint32_t c = 0; c < COLS; ++c) {
-          const int32_t its = __builtin_amdgcn_readlane(sees, (int)c);
+          for (uint32_t c = 0; c < COLS; ++c) {
+            const int32_t its = __builtin_amdgcn_readlane(sees[ct], (int)c);
 #pragma unroll
-          for (int u = 0; u < VW / 2; ++u) {
-            uint32_t y[8];
+            for (int u = 0; u < VW / 2; ++u) {
+              uint32_t y[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = key_of(kb, j) < its ? value(j, u) : 0u;
-            f32x4 even, uneven;
-            products(u, y, even, uneven);
-            if (col == c) { acc[2 * u] = even; acc[2 * u + 1] = uneven; }
+              for (int j = 0; j < 8; ++j) y[j] = key_of(kb, j) < its ? value(j, u) : 0u;
+              const f32x4 even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x05040100u), pk[ct], acc[ct][2 * u], 0, 0, 0);
+              const f32x4 uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x07060302u), pk[ct], acc[ct][2 * u + 1], 0, 0, 0);
+              if (col == c) { acc[ct][2 * u] = even; acc[ct][2 * u + 1] = uneven; }
+            }
           }
         }
       }
@@ -446,36 +459,50 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     const int32_t round = (int32_t)w.unit();
     int32_t kb = k_first + (w.wide ? 0 : (int32_t)(wave * 32u));
     if (kb < k_end) {
-      Step one, two;
       Ids next = blocks(kb);
-      uint32_t in_one = load(one, kb, next), in_two;
+      Step one, two;
+      auto work = [&](Step& st, uint32_t there) {
+        f32x4 s[CT][2];
+        bf16x8 pk[CT];
+        scores(st, s);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) pk[ct] = softmax(ct, s[ct], kb, there);
+        values(st, pk, kb, there);
+      };
+      load(one, kb, next);
+      uint32_t in_one = present(next), in_two;
       next = blocks(kb + round);
       while (true) {
-        in_two = load(two, kb + round, next);
+        load(two, kb + round, next);
+        in_two = present(next);
         next = blocks(kb + 2 * round);
-        work(one, kb, in_one);
+        work(one, in_one);
         kb += round;
         if (kb >= k_end) break;
-        in_one = load(one, kb + round, next);
+        load(one, kb + round, next);
+        in_one = present(next);
         next = blocks(kb + 2 * round);
-        work(two, kb, in_two);
+        work(two, in_two);
         kb += round;
         if (kb >= k_end) break;
       }
     }
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
 
     // ---- the four wavefronts' sums together
     __syncthreads();                          // the last group's have been read
-    if (g == 0) { sum_m[wave * COLS + col] = m; sum_l[wave * COLS + col] = l; }
-    if (live) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      l[ct] += __shfl_xor(l[ct], 16, 64);
+      l[ct] += __shfl_xor(l[ct], 32, 64);
+      const uint32_t c = wave * TC + ct * COLS + col;
+      if (g == 0) { sum_m[c] = m[ct]; sum_l[c] = l[ct]; }
+      if (!live[ct]) continue;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < VW; i += 4)
-          *reinterpret_cast<f32x4*>(sum_acc + (wave * COLS + col) * (DH + 4) + (4u * g + (uint32_t)j) * VW + (uint32_t)i) =
-              f32x4{acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j]};
+          *reinterpret_cast<f32x4*>(sum_acc + c * STRIDE + (4u * g + (uint32_t)j) * VW + (uint32_t)i) =
+              f32x4{acc[ct][i][j], acc[ct][i + 1][j], acc[ct][i + 2][j], acc[ct][i + 3][j]};
     }
     __syncthreads();
     for (uint32_t u = tid; u < n_group * DV; u += THREADS) {
@@ -486,7 +513,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       } else {
 #pragma unroll
         for (uint32_t x = 0; x < WAVES; ++x)
-          j.add(sum_m[x * COLS + c], sum_l[x * COLS + c], *reinterpret_cast<const f32x4*>(sum_acc + (x * COLS + c) * STRIDE + d));
+          j.add(sum_m[x * TC + c], sum_l[x * TC + c], *reinterpret_cast<const f32x4*>(sum_acc + (x * TC + c) * STRIDE + d));
       }
       if (pieces == 1) { put(w.row0, group_col, kh, c, d, j); continue; }
       float* to = part_of(2u * wg + (at_begin ? 0u : 1u)) + c * STRIDE;
@@ -556,33 +583,47 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
   }
 }
 
-uint32_t part_columns(uint32_t n_rows, uint32_t group) { return (uint32_t)std::min<uint64_t>(COLS * WAVES, (uint64_t)n_rows * group); }
+// Tiles of 16 columns a wavefront: heads of 64 have the registers for two, which sequences with many columns take.
+constexpr uint32_t many_tiles(uint32_t dh) { return dh == 64 ? 2u : 1u; }
+// Columns that a piece may have: 16, or those of a wide group.
+uint32_t part_columns(uint32_t n_rows, uint32_t group, uint32_t dh) {
+  return (uint32_t)std::min<uint64_t>(COLS * WAVES * many_tiles(dh), (uint64_t)n_rows * group);
+}
+
+template <int DH, bool E4M3, int CT>
+hipError_t launch_paged(const PagedArgs& a, uint32_t rows, void* scratch, hipStream_t st) {
+  constexpr uint32_t TC = COLS * CT;
+  uint32_t* counters = (uint32_t*)scratch;
+  float* parts = (float*)scratch + MAX_WGS;
+  // units that there can be: column tiles, key heads, the longest sequence that the tables have room for
+  const uint64_t groups = (((uint64_t)rows * a.group + TC - 1) / TC + a.n_seq) * a.kv_heads;
+  const uint64_t units = (((uint64_t)a.max_blocks << a.block_shift) + 31) / 32;
+  const bool few = a.n_seq <= 64 && (double)groups * (double)(2 * units + 2) < 4e9;      // 32 bits hold the sums, padding included
+  const uint32_t lds = WAVES * TC * (DH + 4) * 4 + WAVES * TC * 8 + WAVES * 8 + (few ? 0 : a.n_seq * 8);
+  if (lds > 60u * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3, CT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (groups * ((units + MIN_PIECE - 1) / MIN_PIECE) + 7) / 8 * 8);
+  const bool may_be_wide = rows * a.group > 2 * TC && (a.starts || a.group > 2 * TC);
+  paged_attention_kernel<DH, E4M3, CT><<<wgs, THREADS, lds, st>>>(a, counters, parts, part_columns(rows, a.group, DH), few, may_be_wide);
+  return hipGetLastError();
+}
 
 template <int DH, bool E4M3>
 hipError_t launch_paged(const PagedArgs& a, void* scratch, hipStream_t st) {
   const uint32_t rows = a.starts ? a.n_rows : std::min(a.n_rows, a.n_seq);
   if (rows == 0) return hipSuccess;
-  uint32_t* counters = (uint32_t*)scratch;
-  float* parts = (float*)scratch + MAX_WGS;
-  // units that there can be: column tiles, key heads, the longest sequence that the tables have room for
-  const uint64_t groups = (((uint64_t)rows * a.group + COLS - 1) / COLS + a.n_seq) * a.kv_heads;
-  const uint64_t units = (((uint64_t)a.max_blocks << a.block_shift) + 31) / 32;
-  const bool few = a.n_seq <= 64 && (double)groups * (double)(2 * units + 2) < 4e9;      // 32 bits hold the sums, padding included
-  const uint32_t lds = WAVES * COLS * (DH + 4) * 4 + WAVES * COLS * 8 + WAVES * 8 + (few ? 0 : a.n_seq * 8);
-  if (lds > 60u * 1024) {
-    hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (groups * ((units + MIN_PIECE - 1) / MIN_PIECE) + 7) / 8 * 8);
-  paged_attention_kernel<DH, E4M3><<<wgs, THREADS, lds, st>>>(a, counters, parts, part_columns(rows, a.group), few, rows * a.group > 2 * COLS && (a.starts || a.group > 2 * COLS));
-  return hipGetLastError();
+  if constexpr (many_tiles(DH) > 1)
+    if ((uint64_t)rows * a.group >= (uint64_t)MANY_COLS * a.n_seq) return launch_paged<DH, E4M3, (int)many_tiles(DH)>(a, rows, scratch, st);
+  return launch_paged<DH, E4M3, 1>(a, rows, scratch, st);
 }
 
 }  // namespace
 
 uint64_t paged_attention_scratch(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim) {
   (void)n_seq;
-  return MAX_WGS * 4 + 2ull * MAX_WGS * part_columns(n_rows, q_heads) * (head_dim + 4) * 4;
+  return MAX_WGS * 4 + 2ull * MAX_WGS * part_columns(n_rows, q_heads, head_dim) * (head_dim + 4) * 4;
 }
 
 hipError_t launch_paged_attention(const PagedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st) {

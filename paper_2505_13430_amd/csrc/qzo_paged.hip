@@ -43,6 +43,12 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // narrow units) 351 / 212, 6 x 100 tokens behind 1900 (21504) 194 / 144, 4 x 8 tokens, 64 heads on 8, behind 9000 (9088)
 // 62 / 89, one prompt of 512 (4096) 32 / 43: wide from WIDE_UNITS on.  Heads of 64 with 32 columns, where there are few units
 // a group: the prompts (4 of them) 130 / 73, but 6 x 100 tokens (16) 62 / 76, 4 x 200, 40 heads on 8 in e4m3 (32) 77 / 91.
+//   With more groups than workgroups, a sequence of up to QUAD_LEN positions and one wavefront's columns gives a workgroup four key heads at a time, one a
+// wavefront (a unit is 32 keys of each): no other wavefront waits for a step that there is not, a workgroup starts a quarter
+// as often, and nothing is added up in the end.  Such groups are not cut.  256 sequences, 32 heads of 128, of 1 / 20 / 64 /
+// 128 / 300 / 500 positions: 76 / 83 / 91 / 129 / 236 / 380 us without, 35 / 45 / 61 / 107 / 229 / 375 so; 200 with 64 heads on
+// 8 in e4m3: 24 / 24 / 25 / 29 / 46 / 60, so 13 / 14 / 16 / 20 / 37 / 53.  (64 ragged ones of up to 4001: 150, so 153; with
+// QUAD_LEN 1024 169.)
 //   Every group is given a span, its units behind some padding, all spans are counted through, and workgroup b takes those from
 // share b to share (b + 1) - 1.
 //   Few groups: the shortest piece that leaves no more pieces than workgroups is the share, and a span is a multiple of it, so
@@ -53,15 +59,16 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // first group's in place 2 b, a later one's (only the last can go on) in 2 b + 1, and who finds the group's counter at its last
 // piece adds them up, in order.  The counter (that of the workgroup of the group's first piece) goes back to zero.
 constexpr uint32_t COLS = 16, WAVES = 4, THREADS = 64 * WAVES, MAX_WGS = PAGED_COUNTERS;
-constexpr uint32_t SETUP = 1, MIN_PIECE = 2, WIDE_UNITS = 12288, MANY_COLS = 24;
+constexpr uint32_t SETUP = 1, MIN_PIECE = 2, WIDE_UNITS = 12288, MANY_COLS = 24, QUAD_LEN = 512;
 
 struct SeqWork {
-  uint32_t row0, rows, len, units, tiles, wide;
-  __device__ __forceinline__ uint32_t unit() const { return wide ? 32u : 32u * WAVES; }                // keys
+  uint32_t row0, rows, len, units, tiles, wide, quad;
+  __device__ __forceinline__ uint32_t unit() const { return wide || quad ? 32u : 32u * WAVES; }        // keys
+  __device__ __forceinline__ uint32_t heads() const { return quad ? WAVES : 1u; }                     // key heads of a group
   __device__ __forceinline__ uint32_t cols(uint32_t tc) const { return wide ? tc * WAVES : tc; }      // tc: of a wavefront
 };
 
-__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool wide, uint32_t tc) {
+__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool wide, bool quads, uint32_t tc) {
   SeqWork w;
   w.row0 = i; w.rows = i < a.n_rows ? 1u : 0u;
   if (a.starts) {
@@ -71,6 +78,7 @@ __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool
   w.len = (uint32_t)min(max(a.lengths[i], 0), (int32_t)(a.max_blocks << a.block_shift));
   const uint64_t cols = (uint64_t)w.rows * a.group;
   w.wide = wide && cols > 2 * tc;
+  w.quad = quads && cols <= tc && w.len <= QUAD_LEN;
   w.units = max(1u, (w.len + w.unit() - 1) / w.unit());
   w.tiles = (uint32_t)((cols + w.cols(tc) - 1) / w.cols(tc));
   return w;
@@ -163,22 +171,22 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
 
   // ---- the sequences' units: up to 64 sequences in the lanes of every wavefront, more in the LDS
   const uint32_t per = (a.n_seq + THREADS - 1) / THREADS, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
-  SeqWork lane_work = {0, 0, 0, 1, 0, 0};
-  if (few && lane < a.n_seq) lane_work = seq_work(a, lane, false, TC);
-  bool wide = false;
+  SeqWork lane_work = {0, 0, 0, 1, 0, 0, 0};
+  if (few && lane < a.n_seq) lane_work = seq_work(a, lane, false, false, TC);
+  bool wide = false, quads = false;
   auto sum = [&](auto&& f) -> uint64_t {            // of f over the sequences
     if (few) return (uint32_t)__builtin_amdgcn_readlane((int)lane_scan((uint32_t)f(lane_work)), 63);
     uint64_t n = 0, all;
-    for (uint32_t i = s_first; i < s_last; ++i) n += f(seq_work(a, i, wide, TC));
+    for (uint32_t i = s_first; i < s_last; ++i) n += f(seq_work(a, i, wide, quads, TC));
     block_scan(n, &all, red);
     return scalar64(all);
   };
-  auto groups_of = [&](const SeqWork& w) { return (uint64_t)w.tiles * a.kv_heads; };
+  auto groups_of = [&](const SeqWork& w) { return (uint64_t)w.tiles * ((a.kv_heads + w.heads() - 1) / w.heads()); };
   auto units_of = [&](const SeqWork& w) { return w.units * groups_of(w); };
   uint64_t groups = sum(groups_of), units = sum(units_of);
   if (may_be_wide && units >= WIDE_UNITS && (CT == 1 || units <= 8 * groups)) {
     wide = true;
-    if (few && lane < a.n_seq) lane_work = seq_work(a, lane, true, TC);
+    if (few && lane < a.n_seq) lane_work = seq_work(a, lane, true, false, TC);
     groups = sum(groups_of); units = sum(units_of);
   }
   uint32_t piece = 0;                               // 0: even shares
@@ -192,6 +200,10 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     for (uint32_t p = least; p < least + 3 * more && !piece; p += more)
       if (sum([&](const SeqWork& w) { return (w.units + p - 1) / p * groups_of(w); }) <= gridDim.x) piece = p;
   }
+  if (!piece) {
+    quads = true;
+    if (few && lane < a.n_seq) lane_work = seq_work(a, lane, wide, true, TC);
+  }
   auto span_of = [&](const SeqWork& w) { return piece ? (w.units + piece - 1) / piece * piece : w.units + SETUP; };
   uint64_t total;
   uint32_t mine = 0;
@@ -202,7 +214,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
   } else {
     uint64_t n = 0;
     for (uint32_t i = s_first; i < s_last; ++i) {
-      const SeqWork w = seq_work(a, i, wide, TC);
+      const SeqWork w = seq_work(a, i, wide, quads, TC);
       first_unit[i] = n;
       n += span_of(w) * groups_of(w);
     }
@@ -240,7 +252,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       seq = scalar((uint32_t)__popcll(__ballot(lane < a.n_seq && mine <= (uint32_t)unit)) - 1u);
       auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)seq); };
       seq_first = of(mine);
-      w = {of(lane_work.row0), of(lane_work.rows), of(lane_work.len), of(lane_work.units), of(lane_work.tiles), of(lane_work.wide)};
+      w = {of(lane_work.row0), of(lane_work.rows), of(lane_work.len), of(lane_work.units), of(lane_work.tiles), of(lane_work.wide), of(lane_work.quad)};
     } else {
       uint32_t lo = 0, hi = a.n_seq;
       while (hi - lo > 1) {
@@ -249,15 +261,15 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       }
       seq = scalar(lo);
       seq_first = scalar64(first_unit[seq]);
-      w = seq_work(a, seq, wide, TC);
-      w = {scalar(w.row0), scalar(w.rows), scalar(w.len), scalar(w.units), scalar(w.tiles), scalar(w.wide)};
+      w = seq_work(a, seq, wide, quads, TC);
+      w = {scalar(w.row0), scalar(w.rows), scalar(w.len), scalar(w.units), scalar(w.tiles), scalar(w.wide), scalar(w.quad)};
     }
     const uint32_t span = scalar(span_of(w)), pad = span - w.units;
     const uint64_t r = unit - seq_first;
     const uint32_t group = scalar((r >> 32) ? (uint32_t)(r / span) : (uint32_t)r / span);
-    const uint32_t tile = scalar(group % w.tiles), kh = scalar(group / w.tiles);
+    const uint32_t tile = scalar(group % w.tiles), kh0 = scalar(group / w.tiles * w.heads()), kh = kh0 + (w.quad ? wave : 0u);
     const uint32_t at = scalar((uint32_t)(r - (uint64_t)group * span));                     // within the span
-    const bool uncut = span <= keep;
+    const bool uncut = span <= keep || w.quad;
     if (uncut && at) { unit += span - at; continue; }
     const uint32_t n_units = uncut ? span : scalar((uint32_t)min((uint64_t)(span - at), end - unit));
     const uint64_t group_first = unit - at + pad, group_last = unit - at + span - 1;
@@ -274,7 +286,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
 
     // ---- this wavefront's columns
     const uint32_t all_cols = w.rows * a.group, group_col = tile * w.cols(TC), n_group = min(w.cols(TC), all_cols - group_col);
-    const uint32_t first_col = group_col + (w.wide ? wave * TC : 0u), n_cols = first_col < all_cols ? min(TC, all_cols - first_col) : 0u;
+    const uint32_t first_col = group_col + (w.wide ? wave * TC : 0u), n_cols = first_col < all_cols && kh < a.kv_heads ? min(TC, all_cols - first_col) : 0u;
     bool live[CT];
     // positions that a column sees, that the first (the fewest) and the last (the most) of them see
     int32_t sees[CT];
@@ -297,7 +309,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
         q[ct][s] = __builtin_bit_cast(bf16x8, x);
       }
     }
-    const float ks = (E4M3 && a.k_scale ? a.k_scale[kh] : 1.0f) * a.scale * 1.44269504088896f;
+    const float ks = (E4M3 && a.k_scale && n_cols ? a.k_scale[kh] : 1.0f) * a.scale * 1.44269504088896f;
 
     f32x4 acc[CT][VW];
     float m[CT], l[CT];
@@ -457,7 +469,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
 
     // ---- the keys, a step at a time, the next one's on their way meanwhile
     const int32_t round = (int32_t)w.unit();
-    int32_t kb = k_first + (w.wide ? 0 : (int32_t)(wave * 32u));
+    int32_t kb = k_first + (w.wide || w.quad ? 0 : (int32_t)(wave * 32u));
     if (kb < k_end) {
       Ids next = blocks(kb);
       Step one, two;
@@ -505,9 +517,16 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
               f32x4{acc[ct][i][j], acc[ct][i + 1][j], acc[ct][i + 2][j], acc[ct][i + 3][j]};
     }
     __syncthreads();
-    for (uint32_t u = tid; u < n_group * DV; u += THREADS) {
+    for (uint32_t u = tid; u < (w.quad ? WAVES * TC : n_group) * DV; u += THREADS) {
       const uint32_t c = u / DV, d = u % DV * 4u;
       Joined j;
+      if (w.quad) {
+        const uint32_t x = c / TC;
+        if (c % TC >= n_group || kh0 + x >= a.kv_heads) continue;
+        j.add(sum_m[c], sum_l[c], *reinterpret_cast<const f32x4*>(sum_acc + c * STRIDE + d));
+        put(w.row0, group_col, kh0 + x, c % TC, d, j);
+        continue;
+      }
       if (w.wide) {
         j.add(sum_m[c], sum_l[c], *reinterpret_cast<const f32x4*>(sum_acc + c * STRIDE + d));
       } else {

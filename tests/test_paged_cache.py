@@ -450,6 +450,20 @@ def test_attention_of_ragged_batches(n, longest, H, Hk, dh, block, seed):
 
 
 @gpu
+@pytest.mark.parametrize("n,longest,new,H,Hk,dh,block,e4m3", [
+    (300, 30, 1, 5, 5, 64, 16, False), (130, 600, 1, 6, 6, 128, 32, False), (90, 700, 1, 14, 7, 64, 16, True), (600, 3, 1, 2, 1, 128, 16, False),
+    (140, 512, 4, 12, 4, 128, 16, False), (40, 550, 30, 30, 15, 64, 16, False), (520, 1, 1, 1, 1, 64, 16, True), (90, 513, 1, 40, 10, 128, 128, True)])
+def test_attention_of_many_short_sequences(n, longest, new, H, Hk, dh, block, e4m3):
+    """More groups than workgroups, sequences of up to 512 positions (four key heads a workgroup, their number odd) beside longer ones,
+    one and several new tokens, empty sequences."""
+    rng = np.random.default_rng(n)
+    lengths = [int(x) for x in (longest ** rng.random(n)).round()]
+    lengths[0], lengths[n // 2], lengths[-1] = longest, 0, min(longest, 512)
+    news = None if new == 1 else [int(x) for x in rng.integers(0, new + 1, n)]
+    _check_attend(_attend(lengths, H, Hk, dh, block, news, e4m3=e4m3, seed=n, pad_rows=2))
+
+
+@gpu
 def test_attention_of_more_and_fewer_rows_than_sequences():
     """A row per sequence, with rows behind the last sequence (left as they are), and with sequences that have no row."""
     _check_attend(_attend([40, 0, 300], 4, 2, 64, 16, seed=1, pad_rows=4, stride=16))

@@ -400,12 +400,13 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       const float base = m[ct] == -INFINITY ? 0.0f : m[ct];
       float e[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        e[j] = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - base);
-        l[ct] += e[j];
-      }
-      // p as bf16: 2^-8 of each term at most, in a sum of many; v has no more bits either
-      return __builtin_bit_cast(bf16x8, u32x4v{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])});
+      for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - base);
+      // p as bf16, 2^-8 of each term at most; the sum is that of the rounded ones, so that what rounds all weights alike, a key that
+      // takes all, cancels
+      const u32x4v pk = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) l[ct] += __uint_as_float(pk[j] << 16) + __uint_as_float(pk[j] & 0xffff0000u);
+      return __builtin_bit_cast(bf16x8, pk);
     };
     auto values = [&](Step& st, const bf16x8 (&pk)[CT], int32_t kb, uint32_t there) {
       bool apart = false;

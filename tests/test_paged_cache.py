@@ -90,9 +90,10 @@ def attention_reference(q, k, v, tables, lengths, starts, scale):
 
 
 def attention_tolerance(out, mag, mac, dh):
-    """One rounding of the output, one of every p (bf16, before it meets v), both 2^-8; scores in fp32: dh products and sums and
-    two more factors, (dh + 4) 2^-24 of sum |q| |k| at most, that much of a p's logarithm and twice that of its share."""
-    return 2.0 ** -8 * out.abs() + (2.0 ** -8 + 2 * (dh + 4) * 2.0 ** -24 * mac[..., None]) * mag * 1.01 + 1e-30
+    """One rounding of the output, one of every p to bf16, before it meets v and the sum, both 2^-8: p_k (1 + e_k) in both gives
+    out + sum p_k e_k (v_k - out) / sum p_k (1 + e_k), at most 2^-8 (sum p |v| / sum p + |out|) / (1 - 2^-8) away.  Scores in fp32: dh products
+    and sums and two more factors, (dh + 4) 2^-24 of sum |q| |k| at most, that much of a p's logarithm and twice that of its share."""
+    return 2.0 ** -8 * out.abs() + (2.0 ** -8 * (mag + out.abs()) + 2 * (dh + 4) * 2.0 ** -24 * mac[..., None] * mag) * 1.01 + 1e-30
 
 
 # ------------------------------------------------------------------ refusals, on the host ----

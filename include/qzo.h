@@ -412,7 +412,7 @@ qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tok
  * count as unseen), or positions beyond max_blocks * block.  A score of -infinity counts as unseen.
  * scratch_dev: qzo_paged_attention_scratch_bytes bytes, 256-byte aligned.  Its first 2048 bytes are counters: zero before the first call
  * that uses it, zero again after every call, whatever its sizes; the rest is undefined.  Calls that may overlap (another
- * stream, another captured graph) need scratch of their own.  n_seq 1 .. 8192, q_heads a multiple of kv_heads,
+ * stream, another captured graph) need scratch of their own.  n_seq 1 .. 8192, max_blocks * block at most 2^30, q_heads a multiple of kv_heads,
  * scale finite, ld_q and ld_out multiples of 8 and at least q_heads * head_dim.
  */
 qzo_status qzo_paged_attention_scratch_bytes(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim, uint64_t* out);
@@ -431,7 +431,7 @@ qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows
  * model has learned positions.
  * logits_dev: bf16 [n_seq, vocab], of the last new token of every sequence; zeros where it has none.
  * workspace_dev: qzo_answer_workspace_bytes bytes, 256-byte aligned, contents undefined before and after; calls that may overlap
- * need one each.  QZO_ERR_SHAPE: vocab not a multiple of 8, or tokens or sequences too many for 32-bit offsets.
+ * need one each.  QZO_ERR_SHAPE: vocab not a multiple of 8, max_blocks * block above 2^30, or tokens or sequences too many for 32-bit offsets.
  */
 qzo_status qzo_answer_workspace_bytes(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq, uint64_t* out);
 qzo_status qzo_answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_seq, const qzo_cache* cache,

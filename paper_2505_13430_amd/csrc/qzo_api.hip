@@ -1747,8 +1747,8 @@ qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows
   st = paged_shape(n_rows, n_seq, q_heads, cache->head_dim);
   if (st != QZO_OK) return st;
   if (q_heads % cache->kv_heads) return fail(QZO_ERR_SHAPE, "q_heads must be a multiple of kv_heads");
-  if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31) || (uint64_t)max_blocks * cache->block >= (1ull << 31))
-    return fail(QZO_ERR_SHAPE, "n_seq * max_blocks and max_blocks * block must be 1 .. 2^31 - 1");
+  if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31) || (uint64_t)max_blocks * cache->block > (1ull << 30))
+    return fail(QZO_ERR_SHAPE, "n_seq * max_blocks must be 1 .. 2^31 - 1, max_blocks * block at most 2^30");
   const uint64_t row = (uint64_t)q_heads * cache->head_dim;
   if (ld_q % 8 || ld_out % 8 || ld_q < row || ld_out < row) return fail(QZO_ERR_SHAPE, "ld_q and ld_out must be multiples of 8 that hold a row");
   if (ld_q >= (1ull << 32) || ld_out >= (1ull << 32)) return fail(QZO_ERR_SHAPE, "ld_q and ld_out must be below 2^32");
@@ -1815,8 +1815,8 @@ qzo_status qzo_answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens
   st = cache_check(cache);
   if (st != QZO_OK) return st;
   if (cache->kv_heads != m->cfg.n_heads || cache->head_dim != m->cfg.d_model / m->cfg.n_heads) return fail(QZO_ERR_SHAPE, "the cache has other heads than the model");
-  if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31) || (uint64_t)max_blocks * cache->block >= (1ull << 31))
-    return fail(QZO_ERR_SHAPE, "n_seq * max_blocks and max_blocks * block must be 1 .. 2^31 - 1");
+  if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31) || (uint64_t)max_blocks * cache->block > (1ull << 30))
+    return fail(QZO_ERR_SHAPE, "n_seq * max_blocks must be 1 .. 2^31 - 1, max_blocks * block at most 2^30");
   const AnswerSpace sp = answer_space(m, n_tokens, n_seq);
   if (workspace_bytes < sp.total) return fail(QZO_ERR_WORKSPACE, "workspace smaller than qzo_answer_workspace_bytes");
   unsigned char* base = (unsigned char*)workspace_dev;

@@ -9,17 +9,18 @@
 // The second product takes S's own registers: a lane holds column lane % 16 and keys 4 (lane / 16) + 0..3 of two tiles, which
 // are eight of the 32 values of k that its place of the operand is to hold, if V's rows are dealt out the same way.  V comes
 // in rows too (16 lanes read a row, VW = DH / 16 features each, a lane the eight rows of its keys) and is transposed in
-// registers, eight 16-bit columns at a time, with one v_perm_b32 per pair of keys.  No LDS, no exchange between lanes but for
-// the maximum, and that only when it has grown by a factor of 2^8: until then the sums carry the larger terms.
+// registers, eight 16-bit columns at a time, with one v_perm_b32 per pair of keys.  No LDS (but for prompts, below), no exchange between
+// lanes but for the maximum, and that only when it has grown by a factor of 2^8: until then the sums carry the larger terms.
 // All of a column's state (maximum, sum, its 4 VW accumulators) is in the lanes that hold the column.
 //
 // What bounds it: memory.  A step of a wavefront loads its next 32 keys (16 KB at heads of 128, bf16) before it works on the
 // ones it has; eight wavefronts on a compute unit keep 128 to 256 KB on the way.  Loads and block ids are issued without a branch
 // around them, or the compiler waits for all of them at every use.  8 sequences of 65536 tokens, 8 key heads of 128: 370 us,
-// 5.8 TB/s (a kernel that only reads: 6.1 to 6.3); 64 ragged ones of up to 4001, 32 key heads, 151 us, 5.4 TB/s; 24 in e4m3 of up
-// to 32001, 87 us, 4.9 TB/s, 75 of them the cache at the rate of the first.  Few keys: latency.  One token 5.4 us (launch, lengths,
+// 5.8 TB/s (a kernel that only reads: 6.1 to 6.3); 64 ragged ones of up to 4001, 32 key heads, 157 us, 5.1 TB/s; 24 in e4m3 of up
+// to 32001, 87 us, 4.8 TB/s, 75 of them the cache at the rate of the first.  Few keys: latency.  One token 5.4 us (launch, lengths,
 // table, keys, one after the other); a compute unit alone takes 54 GB/s, 1.2 us a unit.
 #include <algorithm>
+#include <type_traits>
 #include "qzo_device.hpp"
 #include "qzo_kernels.hpp"
 
@@ -43,11 +44,22 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // narrow units) 351 / 212, 6 x 100 tokens behind 1900 (21504) 194 / 144, 4 x 8 tokens, 64 heads on 8, behind 9000 (9088)
 // 62 / 89, one prompt of 512 (4096) 32 / 43: wide from WIDE_UNITS on.  Heads of 64 with 32 columns, where there are few units
 // a group: the prompts (4 of them) 130 / 73, but 6 x 100 tokens (16) 62 / 76, 4 x 200, 40 heads on 8 in e4m3 (32) 77 / 91.
+//   Prompts (TILED): every group has 128 columns, 32 a wavefront, and the keys and values pass through the LDS, fetched once for the four
+// and three steps ahead (32 keys a step where a row has 256 bytes, otherwise 64; rings of 64 KB, two workgroups a compute unit); a
+// unit is 64 keys, a group ends with what its last column sees, and what is not cut goes to memory from the accumulators.  Without /
+// so, us, heads of 128: 16 prompts of 512 tokens, 32 heads, 209 / 119, one of 2048 290 / 150, one of 4000 with 32 heads on 8 846 / 317 (410
+// TFLOP/s), 4 x 200 tokens behind 3800, 40 heads on 8 in e4m3 179 / 158, 6 x 100 behind 1900 142 / 120, 4 of 130 (130 groups) 26 / 16,
+// but one of 512 (128 groups) 31 / 32: from more groups than half the compute units on.  Heads of 64: one of 2048 (512 groups)
+// 104 / 86, the prompts 75 / 65, but 4 x 200 (250) 80 / 97, 6 x 100 (150) 63 / 66: from as many groups as workgroups on.  Fewer columns leave
+// lanes idle: 4 x 8 tokens, 64 heads on 8, behind 9000 (64 columns) 64 / 86, 20 x 40 behind 960 121 / 123: from TILED_COLS a sequence on.
+// What bounds it: two wavefronts a SIMD, each a chain of LDS reads, products and exponentials (vector instructions 40 % of
+// the time, matrix instructions 17 %; neither fewer vector instructions nor more steps ahead nor LDS reads without conflicts made it
+// faster); 119 us for what moves 268 MB: 54 at the rate of a copy.
 //   With more groups than workgroups, a sequence of up to QUAD_LEN positions and one wavefront's columns gives a workgroup four key heads at a time, one a
 // wavefront (a unit is 32 keys of each): no other wavefront waits for a step that there is not, a workgroup starts a quarter
 // as often, and nothing is added up in the end.  Such groups are not cut.  256 sequences, 32 heads of 128, of 1 / 20 / 64 /
 // 128 / 300 / 500 positions: 76 / 83 / 91 / 129 / 236 / 380 us without, 35 / 45 / 61 / 107 / 229 / 375 so; 200 with 64 heads on
-// 8 in e4m3: 24 / 24 / 25 / 29 / 46 / 60, so 13 / 14 / 16 / 20 / 37 / 53.  (64 ragged ones of up to 4001: 150, so 153; with
+// 8 in e4m3: 24 / 24 / 25 / 29 / 46 / 60, so 13 / 14 / 16 / 20 / 37 / 53.  (64 ragged ones of up to 4001: 150, so 155; with
 // QUAD_LEN 1024 169.)
 //   Every group is given a span, its units behind some padding, all spans are counted through, and workgroup b takes those from
 // share b to share (b + 1) - 1.
@@ -60,15 +72,24 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // piece adds them up, in order.  The counter (that of the workgroup of the group's first piece) goes back to zero.
 constexpr uint32_t COLS = 16, WAVES = 4, THREADS = 64 * WAVES, MAX_WGS = PAGED_COUNTERS;
 constexpr uint32_t SETUP = 1, MIN_PIECE = 2, WIDE_UNITS = 12288, MANY_COLS = 24, QUAD_LEN = 512;
+constexpr uint32_t TILE_KEYS = 64, TILED_GROUP = 2 * COLS * WAVES, TILED_PIECE = 8, TILED_COLS = 96;
 
-struct SeqWork {
-  uint32_t row0, rows, len, units, tiles, wide, quad;
-  __device__ __forceinline__ uint32_t unit() const { return wide || quad ? 32u : 32u * WAVES; }        // keys
-  __device__ __forceinline__ uint32_t heads() const { return quad ? WAVES : 1u; }                     // key heads of a group
-  __device__ __forceinline__ uint32_t cols(uint32_t tc) const { return wide ? tc * WAVES : tc; }      // tc: of a wavefront
+// Keys that are waited for at a time where they go through the LDS: four times 16 KB, or 8 KB, are on their way or worked on.
+constexpr uint32_t tile_step(uint32_t row) { return row == 256 ? 32u : 64u; }
+
+struct SeqWork { uint32_t row0, rows, len, units, tiles, wide, quad; };
+
+template <int CT, bool TILED>
+struct Dealing {
+  static constexpr uint32_t TC = COLS * CT;        // columns of a wavefront
+  static __device__ __forceinline__ uint32_t unit(const SeqWork& w) { return TILED ? TILE_KEYS : w.wide || w.quad ? 32u : 32u * WAVES; }       // keys
+  static __device__ __forceinline__ uint32_t heads(const SeqWork& w) { return w.quad ? WAVES : 1u; }      // key heads of a group
+  static __device__ __forceinline__ uint32_t cols(const SeqWork& w) { return TILED || w.wide ? TC * WAVES : TC; }     // of a group
 };
 
-__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool wide, bool quads, uint32_t tc) {
+template <int CT, bool TILED>
+__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool wide, bool quads) {
+  typedef Dealing<CT, TILED> D;
   SeqWork w;
   w.row0 = i; w.rows = i < a.n_rows ? 1u : 0u;
   if (a.starts) {
@@ -77,12 +98,33 @@ __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool
   }
   w.len = (uint32_t)min(max(a.lengths[i], 0), (int32_t)(a.max_blocks << a.block_shift));
   const uint64_t cols = (uint64_t)w.rows * a.group;
-  w.wide = wide && cols > 2 * tc;
-  w.quad = quads && cols <= tc && w.len <= QUAD_LEN;
-  w.units = max(1u, (w.len + w.unit() - 1) / w.unit());
-  w.tiles = (uint32_t)((cols + w.cols(tc) - 1) / w.cols(tc));
+  w.wide = !TILED && wide && cols > 2 * D::TC;
+  w.quad = !TILED && quads && cols <= D::TC && w.len <= QUAD_LEN;
+  w.units = max(1u, (w.len + D::unit(w) - 1) / D::unit(w));
+  w.tiles = (uint32_t)((cols + D::cols(w) - 1) / D::cols(w));
   return w;
 }
+// The column tiles of a key head, one after the other, and their units: TILED, those that the tile's last column sees, which in a
+// prompt are fewer for the early ones.
+template <bool TILED>
+struct Tiles {
+  const SeqWork& w;
+  uint32_t group, step, rest, row = 0, part = 0, units;     // row, part: of the tile's first column, a token and a head of the group
+  __device__ __forceinline__ Tiles(const PagedArgs& a, const SeqWork& w_) : w(w_), group(a.group), step(TILED_GROUP / a.group), rest(TILED_GROUP % a.group) { count(); }
+  __device__ __forceinline__ void count() {
+    if (!TILED) { units = w.units; return; }
+    uint32_t last = row + step, beyond = part + rest;       // the next tile's first column; its token, or the one before, is the last
+    if (beyond >= group) { beyond -= group; ++last; }
+    if (beyond == 0) --last;
+    const uint32_t after = w.rows - 1u - min(last, w.rows - 1u), sees = w.len > after ? w.len - after : 0u;
+    units = max(1u, (sees + TILE_KEYS - 1) / TILE_KEYS);
+  }
+  __device__ __forceinline__ void next() {
+    row += step; part += rest;
+    if (part >= group) { part -= group; ++row; }
+    count();
+  }
+};
 
 // What all lanes agree on, in a scalar register.
 __device__ __forceinline__ uint32_t scalar(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -155,16 +197,18 @@ struct PagedStep {
   uint32_t v[8][VD];
 };
 
-template <int DH, bool E4M3, int CT>
+template <int DH, bool E4M3, int CT, bool TILED>
 __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(PagedArgs a, uint32_t* counters, float* parts, uint32_t part_cols, uint32_t few, uint32_t may_be_wide) {
   constexpr int KS = DH / 32, VW = DH / 16, ES = E4M3 ? 1 : 2;
-  constexpr uint32_t TC = COLS * CT, STRIDE = DH + 4;       // columns of a wavefront
+  typedef Dealing<CT, TILED> D;
+  constexpr uint32_t TC = D::TC, STRIDE = DH + 4, ROW = DH * ES;
   typedef PagedStep<DH, E4M3> Step;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  float* const sum_acc = (float*)lds;                                   // [WAVES][TC][STRIDE]
+  float* const sum_acc = (float*)lds;                                   // [WAVES][TC][STRIDE]; TILED: where the tiles were
   float* const sum_m = sum_acc + WAVES * TC * STRIDE;                   // [WAVES][TC]
   float* const sum_l = sum_m + WAVES * TC;
-  uint64_t* const red = (uint64_t*)(sum_l + WAVES * TC);                // [WAVES]
+  constexpr uint32_t SUMS = WAVES * TC * (STRIDE + 2) * 4, TILES = TILED ? 8 * tile_step(ROW) * ROW : 0;
+  uint64_t* const red = (uint64_t*)(lds + (SUMS > TILES ? SUMS : TILES));      // [WAVES]
   uint64_t* const first_unit = red + WAVES;                             // [n_seq], more than 64 sequences only
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = scalar(tid >> 6);
   const uint32_t col = lane & 15u, g = lane >> 4;
@@ -172,21 +216,30 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
   // ---- the sequences' units: up to 64 sequences in the lanes of every wavefront, more in the LDS
   const uint32_t per = (a.n_seq + THREADS - 1) / THREADS, s_first = min(tid * per, a.n_seq), s_last = min(s_first + per, a.n_seq);
   SeqWork lane_work = {0, 0, 0, 1, 0, 0, 0};
-  if (few && lane < a.n_seq) lane_work = seq_work(a, lane, false, false, TC);
+  if (few && lane < a.n_seq) lane_work = seq_work<CT, TILED>(a, lane, false, false);
   bool wide = false, quads = false;
   auto sum = [&](auto&& f) -> uint64_t {            // of f over the sequences
     if (few) return (uint32_t)__builtin_amdgcn_readlane((int)lane_scan((uint32_t)f(lane_work)), 63);
     uint64_t n = 0, all;
-    for (uint32_t i = s_first; i < s_last; ++i) n += f(seq_work(a, i, wide, quads, TC));
+    for (uint32_t i = s_first; i < s_last; ++i) n += f(seq_work<CT, TILED>(a, i, wide, quads));
     block_scan(n, &all, red);
     return scalar64(all);
   };
-  auto groups_of = [&](const SeqWork& w) { return (uint64_t)w.tiles * ((a.kv_heads + w.heads() - 1) / w.heads()); };
-  auto units_of = [&](const SeqWork& w) { return w.units * groups_of(w); };
+  auto head_groups = [&](const SeqWork& w) { return (a.kv_heads + D::heads(w) - 1) / D::heads(w); };
+  auto groups_of = [&](const SeqWork& w) { return (uint64_t)w.tiles * head_groups(w); };
+  // of a key head's tiles together: their units, or what f makes of them
+  auto tiles_sum = [&](const SeqWork& w, auto&& f) -> uint64_t {
+    if constexpr (!TILED) return (uint64_t)w.tiles * f(w.units);
+    uint64_t n = 0;
+    Tiles<TILED> its(a, w);
+    for (uint32_t t = 0; t < w.tiles; ++t, its.next()) n += f(its.units);
+    return n;
+  };
+  auto units_of = [&](const SeqWork& w) { return tiles_sum(w, [](uint32_t u) { return u; }) * head_groups(w); };
   uint64_t groups = sum(groups_of), units = sum(units_of);
-  if (may_be_wide && units >= WIDE_UNITS && (CT == 1 || units <= 8 * groups)) {
+  if (!TILED && may_be_wide && units >= WIDE_UNITS && (CT == 1 || units <= 8 * groups)) {
     wide = true;
-    if (few && lane < a.n_seq) lane_work = seq_work(a, lane, true, false, TC);
+    if (few && lane < a.n_seq) lane_work = seq_work<CT, TILED>(a, lane, true, false);
     groups = sum(groups_of); units = sum(units_of);
   }
   uint32_t piece = 0;                               // 0: even shares
@@ -195,28 +248,29 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     // 2 units, but groups of up to 4 uncut.  One sequence, pieces of 1 / 2 / 3 / 4 units: 32 heads, 500 tokens 10.4 / 10.8 /
     // 11.8 / 10.5 us (heads of 64: 8.7 / 9.1 / 9.7 / 7.6), 1000 13.7 / 12.0 / 12.3 / 13.1, 4000 18.7 / 18.8 / 22.0 / 23.1; 8 key
     // heads, 4000 15.5 / 12.6 / 12.7 / 13.5, 16000 22.8 / 22.8 / 24.9 / 24.6.
-    const uint32_t short_one = units <= 4 * groups ? 4u : MIN_PIECE;
+    const uint32_t short_one = TILED ? TILED_PIECE : units <= 4 * groups ? 4u : MIN_PIECE;
     const uint32_t least = scalar(max(short_one, (uint32_t)((units + gridDim.x - 1) / gridDim.x))), more = max(1u, least / 16);
     for (uint32_t p = least; p < least + 3 * more && !piece; p += more)
-      if (sum([&](const SeqWork& w) { return (w.units + p - 1) / p * groups_of(w); }) <= gridDim.x) piece = p;
+      if (sum([&](const SeqWork& w) { return tiles_sum(w, [&](uint32_t u) { return (u + p - 1) / p; }) * head_groups(w); }) <= gridDim.x) piece = p;
   }
-  if (!piece) {
+  if (!TILED && !piece) {
     quads = true;
-    if (few && lane < a.n_seq) lane_work = seq_work(a, lane, wide, true, TC);
+    if (few && lane < a.n_seq) lane_work = seq_work<CT, TILED>(a, lane, wide, true);
   }
-  auto span_of = [&](const SeqWork& w) { return piece ? (w.units + piece - 1) / piece * piece : w.units + SETUP; };
+  auto span_of = [&](uint32_t u) { return piece ? (u + piece - 1) / piece * piece : u + SETUP; };
+  auto head_span = [&](const SeqWork& w) { return tiles_sum(w, span_of); };
   uint64_t total;
   uint32_t mine = 0;
   if (few) {
-    const uint32_t n = (uint32_t)(span_of(lane_work) * groups_of(lane_work)), upto = lane_scan(n);
+    const uint32_t n = (uint32_t)(head_span(lane_work) * head_groups(lane_work)), upto = lane_scan(n);
     mine = upto - n;
     total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   } else {
     uint64_t n = 0;
     for (uint32_t i = s_first; i < s_last; ++i) {
-      const SeqWork w = seq_work(a, i, wide, quads, TC);
+      const SeqWork w = seq_work<CT, TILED>(a, i, wide, quads);
       first_unit[i] = n;
-      n += span_of(w) * groups_of(w);
+      n += head_span(w) * head_groups(w);
     }
     const uint64_t before = block_scan(n, &total, red);
     for (uint32_t i = s_first; i < s_last; ++i) first_unit[i] += before;
@@ -243,6 +297,9 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     *reinterpret_cast<uint2*>(to) = j.l == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(j.o[0] * inv, j.o[1] * inv), pack_bf16x2(j.o[2] * inv, j.o[3] * inv));
   };
 
+  // the last group's place: the next one's tile is looked for from there on
+  uint32_t known_seq = ~0u, known_head = 0, known_tile = 0, known_row = 0, known_part = 0;
+  uint64_t known_span = 0, known_before = 0;
   for (uint64_t unit = begin; unit < end;) {
     uint32_t seq;
     uint64_t seq_first;
@@ -261,14 +318,36 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       }
       seq = scalar(lo);
       seq_first = scalar64(first_unit[seq]);
-      w = seq_work(a, seq, wide, quads, TC);
+      w = seq_work<CT, TILED>(a, seq, wide, quads);
       w = {scalar(w.row0), scalar(w.rows), scalar(w.len), scalar(w.units), scalar(w.tiles), scalar(w.wide), scalar(w.quad)};
     }
-    const uint32_t span = scalar(span_of(w)), pad = span - w.units;
     const uint64_t r = unit - seq_first;
-    const uint32_t group = scalar((r >> 32) ? (uint32_t)(r / span) : (uint32_t)r / span);
-    const uint32_t tile = scalar(group % w.tiles), kh0 = scalar(group / w.tiles * w.heads()), kh = kh0 + (w.quad ? wave : 0u);
-    const uint32_t at = scalar((uint32_t)(r - (uint64_t)group * span));                     // within the span
+    uint32_t tile, head, at;                                                  // at: within the group's span
+    if constexpr (TILED) {
+      if (seq != known_seq) { known_seq = seq; known_head = ~0u; known_span = scalar64(head_span(w)); }
+      head = scalar((r >> 32) ? (uint32_t)(r / known_span) : (uint32_t)r / (uint32_t)known_span);
+      const uint64_t rest = r - head * known_span;
+      Tiles<TILED> its(a, w);
+      if (head == known_head) {
+        its.row = known_row; its.part = known_part; its.count();
+      } else {
+        known_head = head; known_tile = 0; known_before = 0;
+      }
+      while (rest >= known_before + span_of(its.units)) {
+        known_before += span_of(its.units);
+        ++known_tile;
+        its.next();
+      }
+      known_row = scalar(its.row); known_part = scalar(its.part); known_tile = scalar(known_tile); known_before = scalar64(known_before);
+      tile = known_tile; at = scalar((uint32_t)(rest - known_before));
+      w.units = scalar(its.units);
+    } else {
+      const uint32_t s1 = scalar(span_of(w.units)), group = scalar((r >> 32) ? (uint32_t)(r / s1) : (uint32_t)r / s1);
+      tile = scalar(group % w.tiles); head = scalar(group / w.tiles);
+      at = scalar((uint32_t)(r - (uint64_t)group * s1));
+    }
+    const uint32_t span = scalar(span_of(w.units)), pad = span - w.units;
+    const uint32_t kh0 = scalar(head * D::heads(w)), kh = kh0 + (w.quad ? wave : 0u);
     const bool uncut = span <= keep || w.quad;
     if (uncut && at) { unit += span - at; continue; }
     const uint32_t n_units = uncut ? span : scalar((uint32_t)min((uint64_t)(span - at), end - unit));
@@ -285,14 +364,16 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     }
 
     // ---- this wavefront's columns
-    const uint32_t all_cols = w.rows * a.group, group_col = tile * w.cols(TC), n_group = min(w.cols(TC), all_cols - group_col);
-    const uint32_t first_col = group_col + (w.wide ? wave * TC : 0u), n_cols = first_col < all_cols && kh < a.kv_heads ? min(TC, all_cols - first_col) : 0u;
+    const uint32_t all_cols = w.rows * a.group, group_col = tile * D::cols(w), n_group = min(D::cols(w), all_cols - group_col);
+    const uint32_t first_col = group_col + (TILED || w.wide ? wave * TC : 0u), n_cols = first_col < all_cols && kh < a.kv_heads ? min(TC, all_cols - first_col) : 0u;
     bool live[CT];
     // positions that a column sees, that the first (the fewest) and the last (the most) of them see
     int32_t sees[CT];
     const int32_t least = (int32_t)(w.len + first_col / a.group + 1u - w.rows);
     const int32_t most = n_cols ? (int32_t)(w.len + (first_col + n_cols - 1) / a.group + 1u - w.rows) : 0;
-    const int32_t k_first = (int32_t)(u_first * w.unit()), k_end = (int32_t)min((int64_t)most, (int64_t)u_end * w.unit());
+    const int32_t k_first = (int32_t)(u_first * D::unit(w)), k_end = (int32_t)min((int64_t)most, (int64_t)u_end * D::unit(w));
+    // of all the group's columns
+    const int32_t group_end = !TILED ? k_end : (int32_t)min((int64_t)w.len + (group_col + n_group - 1) / a.group + 1 - w.rows, (int64_t)u_end * TILE_KEYS);
     bf16x8 q[CT][KS];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -306,24 +387,27 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
         const uint32_t d = E4M3 ? (uint32_t)(s / 2) * 64u + g * 16u + (uint32_t)(s & 1) * 8u : (uint32_t)s * 32u + g * 8u;
         u32x4v x = {0u, 0u, 0u, 0u};
         if (live[ct]) x = *reinterpret_cast<const u32x4v*>(from + d);
+        if (a.scale < 0.0f) x ^= 0x80008000u;
         q[ct][s] = __builtin_bit_cast(bf16x8, x);
       }
     }
-    const float ks = (E4M3 && a.k_scale && n_cols ? a.k_scale[kh] : 1.0f) * a.scale * 1.44269504088896f;
+    const float ks = (E4M3 && a.k_scale && n_cols ? a.k_scale[kh] : 1.0f) * fabsf(a.scale) * 1.44269504088896f;
 
     f32x4 acc[CT][VW];
-    float m[CT], l[CT];
+    typedef std::conditional_t<TILED, f32x4, float> Sum;       // TILED: a matrix product's, four times the same
+    float m[CT];
+    Sum l[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
       for (int i = 0; i < VW; ++i) acc[ct][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      m[ct] = -INFINITY; l[ct] = 0.0f;
+      m[ct] = -INFINITY; l[ct] = Sum{};
     }
 
     // ---- where the keys are: a block id per tile, in scalar registers, a step ahead of the loads that need it
     const table_t table = (table_t)(uintptr_t)(a.tables + (uint64_t)seq * a.max_blocks);
     const uint32_t in_block = (1u << a.block_shift) - 1u;
-    const int32_t last_tile = max(k_end - 1, 0) & ~15;       // steps beyond the end load it again (a branch around loads would have
+    const int32_t last_tile = max(group_end - 1, 0) & ~15;       // steps beyond the end load it again (a branch around loads would have
                                                              // every wait count as if they had not been issued)
     struct Ids { uint32_t id[2]; };
     auto blocks = [&](int32_t kb) {
@@ -380,32 +464,41 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     };
     // s becomes p, as the second product's operand; the sums follow
     auto softmax = [&](int ct, f32x4 (&s)[2], int32_t kb, uint32_t there) {
+      float f = ks;                             // TILED: the factor meets s in the exponential's own operand, but where a product with
+      if (!TILED || !whole_step(kb, there)) {   // what stands for unseen might be none
 #pragma unroll
-      for (int t = 0; t < 2; ++t) s[t] *= ks;
-      if (!whole_step(kb, there)) {
+        for (int t = 0; t < 2; ++t) s[t] *= ks;
+        f = 1.0f;
+        if (!whole_step(kb, there)) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (key_of(kb, j) >= sees[ct] || !(there >> (j >> 2) & 1u)) s[j >> 2][j & 3] = -INFINITY;
+          for (int j = 0; j < 8; ++j)
+            if (key_of(kb, j) >= sees[ct] || !(there >> (j >> 2) & 1u)) s[j >> 2][j & 3] = -INFINITY;
+        }
       }
-      float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * f;
       if (__any(top > m[ct] + 8.0f)) {           // m = -infinity: any key at all
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float m2 = fmaxf(m[ct], top), f = m2 == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[ct] - m2);
-        l[ct] *= f;
+        const float m2 = fmaxf(m[ct], top), less = m2 == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[ct] - m2);
+        l[ct] *= less;
 #pragma unroll
-        for (int i = 0; i < VW; ++i) acc[ct][i] *= f;
+        for (int i = 0; i < VW; ++i) acc[ct][i] *= less;
         m[ct] = m2;
       }
       const float base = m[ct] == -INFINITY ? 0.0f : m[ct];
       float e[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - base);
+      for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], f, -base));
       // p as bf16, 2^-8 of each term at most; the sum is that of the rounded ones, so that what rounds all weights alike, a key that
       // takes all, cancels
       const u32x4v pk = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
+      if constexpr (TILED) {                     // ones times p: every lane of the column has the sum of all
+        const u32x4v ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, pk), l[ct], 0, 0, 0);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) l[ct] += __uint_as_float(pk[j] << 16) + __uint_as_float(pk[j] & 0xffff0000u);
+        for (int j = 0; j < 4; ++j) l[ct] += __uint_as_float(pk[j] << 16) + __uint_as_float(pk[j] & 0xffff0000u);
+      }
       return __builtin_bit_cast(bf16x8, pk);
     };
     auto values = [&](Step& st, const bf16x8 (&pk)[CT], int32_t kb, uint32_t there) {
@@ -449,55 +542,187 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
           }
         }
       } else {
+        // a pair of features at a time, so that few registers hold what is not in place
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
+        for (int u = 0; u < VW / 2; ++u)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            uint32_t v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = value(j, u);
 #pragma unroll 1
-          for (uint32_t c = 0; c < COLS; ++c) {
-            const int32_t its = __builtin_amdgcn_readlane(sees[ct], (int)c);
-#pragma unroll
-            for (int u = 0; u < VW / 2; ++u) {
+            for (uint32_t c = 0; c < COLS; ++c) {
+              const int32_t its = __builtin_amdgcn_readlane(sees[ct], (int)c);
               uint32_t y[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = key_of(kb, j) < its ? value(j, u) : 0u;
+              for (int j = 0; j < 8; ++j) y[j] = key_of(kb, j) < its ? v[j] : 0u;
               const f32x4 even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x05040100u), pk[ct], acc[ct][2 * u], 0, 0, 0);
               const f32x4 uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x07060302u), pk[ct], acc[ct][2 * u + 1], 0, 0, 0);
               if (col == c) { acc[ct][2 * u] = even; acc[ct][2 * u + 1] = uneven; }
             }
           }
-        }
       }
     };
 
-    // ---- the keys, a step at a time, the next one's on their way meanwhile
-    const int32_t round = (int32_t)w.unit();
-    int32_t kb = k_first + (w.wide || w.quad ? 0 : (int32_t)(wave * 32u));
-    if (kb < k_end) {
-      Ids next = blocks(kb);
-      Step one, two;
-      auto work = [&](Step& st, uint32_t there) {
-        f32x4 s[CT][2];
-        bf16x8 pk[CT];
-        scores(st, s);
+    auto work = [&](Step& st, int32_t kb, uint32_t there) {
+      f32x4 s[CT][2];
+      bf16x8 pk[CT];
+      scores(st, s);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) pk[ct] = softmax(ct, s[ct], kb, there);
-        values(st, pk, kb, there);
+      for (int ct = 0; ct < CT; ++ct) pk[ct] = softmax(ct, s[ct], kb, there);
+      values(st, pk, kb, there);
+    };
+    if constexpr (TILED) {
+      // ---- 32 or 64 keys at a time through the LDS, the next three such steps on their way.  A wavefront fetches a tile of 16 keys, lane by
+      // lane 16 bytes to consecutive places; a row's 16-byte pieces change places there, so that lanes that read the same piece of 16
+      // rows find it in different banks (256 bytes a row: K piece ^ row, V, whose rows are read as they lie, as they are; with
+      // row & 7 for both half of all LDS cycles were conflicts).
+      constexpr uint32_t KEYS = tile_step(ROW), TILE = 16 * ROW, HALF = KEYS * ROW, LOADS = TILE / 1024, BUFFERS = 4;
+      constexpr bool BOTH = KEYS == 64;         // a wavefront fetches a tile of keys and one of values, not one of them
+      auto turn = [](uint32_t row) { return ROW == 256 ? row : ROW == 128 ? row & 7u : row >> 1 & 3u; };
+      uint32_t from[LOADS];
+#pragma unroll
+      for (uint32_t n = 0; n < LOADS; ++n) {
+        const uint32_t byte = n * 1024u + lane * 16u, row = byte / ROW, piece16 = byte % ROW / 16u;
+        from[n] = row * ROW + (BOTH || wave < 2u ? piece16 ^ turn(row) : piece16) * 16u;
+      }
+      const uint32_t own = BOTH ? wave : wave & 1u;            // its tile
+      const uint32_t to = scalar((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds + own * TILE + (BOTH ? 0u : (wave >> 1) * HALF));
+      // block ids of 64 tiles in the lanes, those of the next 64 on their way; seen: which of them are in the pool
+      const int32_t* const ids_at = a.tables + (uint64_t)seq * a.max_blocks;
+      int32_t ids_from = k_first;
+      auto ids_load = [&](int32_t kb) { return (uint32_t)ids_at[min((uint32_t)kb + 16u * lane, (uint32_t)last_tile) >> a.block_shift]; };
+      uint32_t ids = ids_load(ids_from), ids_next = ids_load(ids_from + 1024);
+      uint64_t seen = __ballot(ids < a.n_blocks);
+      auto fetch = [&](uint32_t buffer, int32_t kb, uint32_t id) {
+        const uint32_t pos = (uint32_t)min(kb + (int32_t)(own * 16u), last_tile);
+        const uint64_t at16 = ((((uint64_t)(id < a.n_blocks ? id : 0u) * a.kv_heads + kh) << a.block_shift) + (pos & in_block)) * (uint64_t)ROW;
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        auto tile_of = [&](const void* pool) {
+          const uint64_t x = scalar64((uint64_t)(uintptr_t)pool + at16);
+          return i32x4{(int)(uint32_t)x, (int)(uint32_t)(x >> 32), (int)TILE, 0x00020000};
+        };
+        const i32x4 first = tile_of(BOTH || wave < 2u ? a.k : a.v), second = tile_of(a.v);
+#pragma unroll
+        for (uint32_t n = 0; n < LOADS; ++n) {
+          asm volatile(QZO_SET_M0 "buffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to + buffer * (2u * HALF) + n * 1024u), "v"(from[n]), "s"(first) : "memory", "m0");
+          if constexpr (BOTH)
+            asm volatile(QZO_SET_M0 "buffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to + buffer * (2u * HALF) + HALF + n * 1024u), "v"(from[n]), "s"(second) : "memory", "m0");
+        }
       };
-      load(one, kb, next);
-      uint32_t in_one = present(next), in_two;
-      next = blocks(kb + round);
-      while (true) {
-        load(two, kb + round, next);
-        in_two = present(next);
-        next = blocks(kb + 2 * round);
-        work(one, in_one);
-        kb += round;
-        if (kb >= k_end) break;
-        load(one, kb + round, next);
-        in_one = present(next);
-        next = blocks(kb + 2 * round);
-        work(two, in_two);
-        kb += round;
-        if (kb >= k_end) break;
+      const uint32_t k_at = col * ROW + (g ^ turn(col)) * 16u;
+      uint32_t v_at[4];
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) v_at[j] = (4u * g + j) * ROW + (col * (VW * ES) ^ (BOTH ? turn(4u * g + j) * 16u : 0u));
+      __syncthreads();                          // what the last group left here has been read
+      __builtin_amdgcn_s_waitcnt(0x0F70);       // vmcnt(0): the queries, or the compiler would wait for them, and for the next keys, below
+      uint64_t there_of = 0;                    // of the steps on their way, 16 bits each, the newest lowest
+      auto fetch_next = [&](uint32_t buffer, int32_t kb) {
+        if (kb - ids_from >= 1024) {
+          ids_from += 1024;
+          ids = ids_next;
+          seen = __ballot(ids < a.n_blocks);
+          ids_next = ids_load(ids_from + 1024);
+        }
+        const uint32_t tile16 = (uint32_t)(kb - ids_from) >> 4;
+        there_of = there_of << 16 | ((uint32_t)(seen >> tile16) & 15u);
+        fetch(buffer, kb, (uint32_t)__builtin_amdgcn_readlane((int)ids, (int)(tile16 + own)));
+      };
+#pragma unroll
+      for (uint32_t i = 0; i < BUFFERS - 1; ++i)
+        if (k_first + (int32_t)(i * KEYS) < group_end) fetch_next(i, k_first + (int32_t)(i * KEYS)); else there_of <<= 16;
+      uint32_t buffer = 0;
+#pragma unroll 1
+      for (int32_t kb = k_first; kb < group_end; kb += (int32_t)KEYS) {
+        const uint32_t there = (uint32_t)(there_of >> 16 * (BUFFERS - 2)) & 15u;
+        // this wavefront's part has come, the next two steps' may be on their way; behind the barrier all four parts have
+        constexpr int STEP_LOADS = (int)(BOTH ? 2 * LOADS : LOADS);
+        if (kb + 2 * (int32_t)KEYS < group_end) __builtin_amdgcn_s_waitcnt(0x0F70 | 2 * STEP_LOADS);
+        else __builtin_amdgcn_s_waitcnt(0x0F70);
+        __syncthreads();                        // and the step before has been read
+        if (kb + (int32_t)((BUFFERS - 1) * KEYS) < group_end) fetch_next((buffer + BUFFERS - 1) % BUFFERS, kb + (int32_t)((BUFFERS - 1) * KEYS));
+        else there_of <<= 16;
+        const unsigned char* const tiles = lds + buffer * (2u * HALF);
+        buffer = (buffer + 1) % BUFFERS;
+#pragma unroll
+        for (int part = 0; part < (int)KEYS / 32; ++part) {
+          if (kb + 32 * part >= k_end) break;
+          Step st;
+          f32x4 s[CT][2];
+          bf16x8 pk[CT];
+          const int32_t k32 = kb + 32 * part;
+          const uint32_t there32 = there >> (2 * part) & 3u;
+          const unsigned char* const kt = tiles + 2 * part * TILE;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < Step::KL; ++i) st.k[t][i] = *reinterpret_cast<const u32x4v*>(kt + t * TILE + (k_at ^ (uint32_t)i * 64u));
+          scores(st, s);
+          if (DH == 128) __builtin_amdgcn_sched_barrier(0);     // the values take the keys' registers
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            uint32_t* o = st.v[j];
+            const unsigned char* const vt = kt + HALF + (j >> 2) * TILE + v_at[j & 3];
+            if constexpr (Step::VD == 4) {
+              const uint4 x = *reinterpret_cast<const uint4*>(vt);
+              o[0] = x.x; o[1] = x.y; o[2] = x.z; o[3] = x.w;
+            } else if constexpr (Step::VD == 2) {
+              const uint2 x = *reinterpret_cast<const uint2*>(vt);
+              o[0] = x.x; o[1] = x.y;
+            } else {
+              o[0] = *reinterpret_cast<const uint32_t*>(vt);
+            }
+          }
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) pk[ct] = softmax(ct, s[ct], k32, there32);
+          values(st, pk, k32, there32);
+        }
+      }
+    } else {
+      // ---- the keys, a step at a time, the next one's on their way meanwhile
+      const int32_t round = (int32_t)D::unit(w);
+      int32_t kb = k_first + (w.wide || w.quad ? 0 : (int32_t)(wave * 32u));
+      if (kb < k_end) {
+        Ids next = blocks(kb);
+        Step one, two;
+        load(one, kb, next);
+        uint32_t in_one = present(next), in_two;
+        next = blocks(kb + round);
+        while (true) {
+          load(two, kb + round, next);
+          in_two = present(next);
+          next = blocks(kb + 2 * round);
+          work(one, kb, in_one);
+          kb += round;
+          if (kb >= k_end) break;
+          load(one, kb + round, next);
+          in_one = present(next);
+          next = blocks(kb + 2 * round);
+          work(two, kb, in_two);
+          kb += round;
+          if (kb >= k_end) break;
+        }
+      }
+    }
+
+    if constexpr (TILED) {
+      if (pieces == 1) {                        // all of a column is in its lanes: VW features of a row of V^T tiles each
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          if (!live[ct]) continue;
+          const uint32_t f = first_col + ct * COLS + col;
+          bf16_t* out = a.out + (uint64_t)(w.row0 + f / a.group) * a.ld_out + (uint64_t)(kh * a.group + f % a.group) * DH + 4u * g * VW;
+          const float l1 = l[ct][0], inv = l1 == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[kh] : 1.0f) / l1;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t o[VW / 2];
+#pragma unroll
+            for (int i = 0; i < VW / 2; ++i) o[i] = pack_bf16x2(acc[ct][2 * i][j] * inv, acc[ct][2 * i + 1][j] * inv);
+            if constexpr (VW == 8) *reinterpret_cast<uint4*>(out + j * VW) = make_uint4(o[0], o[1], o[2], o[3]);
+            else *reinterpret_cast<uint2*>(out + j * VW) = make_uint2(o[0], o[1]);
+          }
+        }
+        continue;
       }
     }
 
@@ -505,10 +730,15 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     __syncthreads();                          // the last group's have been read
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      l[ct] += __shfl_xor(l[ct], 16, 64);
-      l[ct] += __shfl_xor(l[ct], 32, 64);
+      float l1;
+      if constexpr (TILED) {
+        l1 = l[ct][0];
+      } else {
+        l1 = l[ct] + __shfl_xor(l[ct], 16, 64);
+        l1 += __shfl_xor(l1, 32, 64);
+      }
       const uint32_t c = wave * TC + ct * COLS + col;
-      if (g == 0) { sum_m[c] = m[ct]; sum_l[c] = l[ct]; }
+      if (g == 0) { sum_m[c] = m[ct]; sum_l[c] = l1; }
       if (!live[ct]) continue;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -528,7 +758,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
         put(w.row0, group_col, kh0 + x, c % TC, d, j);
         continue;
       }
-      if (w.wide) {
+      if (TILED || w.wide) {
         j.add(sum_m[c], sum_l[c], *reinterpret_cast<const f32x4*>(sum_acc + c * STRIDE + d));
       } else {
 #pragma unroll
@@ -605,28 +835,34 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
 
 // Tiles of 16 columns a wavefront: heads of 64 have the registers for two, which sequences with many columns take.
 constexpr uint32_t many_tiles(uint32_t dh) { return dh == 64 ? 2u : 1u; }
-// Columns that a piece may have: 16, or those of a wide group.
-uint32_t part_columns(uint32_t n_rows, uint32_t group, uint32_t dh) {
-  return (uint32_t)std::min<uint64_t>(COLS * WAVES * many_tiles(dh), (uint64_t)n_rows * group);
+// Whether the keys go through the LDS.
+bool tiled(uint32_t rows, uint32_t n_seq, uint32_t q_heads, uint32_t group, uint32_t dh) {
+  const uint64_t groups = (uint64_t)rows * q_heads / TILED_GROUP;
+  return (uint64_t)rows * group >= (uint64_t)TILED_COLS * n_seq && groups > (dh == 64 ? MAX_WGS - 1 : MAX_WGS / 4);
+}
+// Columns that a piece may have.
+uint32_t part_columns(uint32_t rows, uint32_t n_seq, uint32_t q_heads, uint32_t group, uint32_t dh) {
+  return (uint32_t)std::min<uint64_t>(tiled(rows, n_seq, q_heads, group, dh) ? TILED_GROUP : COLS * WAVES * many_tiles(dh), (uint64_t)rows * group);
 }
 
-template <int DH, bool E4M3, int CT>
+template <int DH, bool E4M3, int CT, bool TILED>
 hipError_t launch_paged(const PagedArgs& a, uint32_t rows, void* scratch, hipStream_t st) {
-  constexpr uint32_t TC = COLS * CT;
+  constexpr uint32_t TC = COLS * CT, GC = TILED ? TILED_GROUP : TC;
   uint32_t* counters = (uint32_t*)scratch;
   float* parts = (float*)scratch + MAX_WGS;
   // units that there can be: column tiles, key heads, the longest sequence that the tables have room for
-  const uint64_t groups = (((uint64_t)rows * a.group + TC - 1) / TC + a.n_seq) * a.kv_heads;
+  const uint64_t groups = (((uint64_t)rows * a.group + GC - 1) / GC + a.n_seq) * a.kv_heads;
   const uint64_t units = (((uint64_t)a.max_blocks << a.block_shift) + 31) / 32;
   const bool few = a.n_seq <= 64 && (double)groups * (double)(2 * units + 2) < 4e9;      // 32 bits hold the sums, padding included
-  const uint32_t lds = WAVES * TC * (DH + 4) * 4 + WAVES * TC * 8 + WAVES * 8 + (few ? 0 : a.n_seq * 8);
+  const uint32_t sums = WAVES * TC * (DH + 4) * 4 + WAVES * TC * 8, row = DH * (E4M3 ? 1u : 2u), tiles = TILED ? 8u * tile_step(row) * row : 0u;
+  const uint32_t lds = std::max(sums, tiles) + WAVES * 8 + (few ? 0 : a.n_seq * 8);
   if (lds > 60u * 1024) {
-    hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3, CT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3, CT, TILED>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
   const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (groups * ((units + MIN_PIECE - 1) / MIN_PIECE) + 7) / 8 * 8);
-  const bool may_be_wide = rows * a.group > 2 * TC && (a.starts || a.group > 2 * TC);
-  paged_attention_kernel<DH, E4M3, CT><<<wgs, THREADS, lds, st>>>(a, counters, parts, part_columns(rows, a.group, DH), few, may_be_wide);
+  const bool may_be_wide = !TILED && rows * a.group > 2 * TC && (a.starts || a.group > 2 * TC);
+  paged_attention_kernel<DH, E4M3, CT, TILED><<<wgs, THREADS, lds, st>>>(a, counters, parts, part_columns(rows, a.n_seq, a.q_heads, a.group, DH), few, may_be_wide);
   return hipGetLastError();
 }
 
@@ -634,16 +870,16 @@ template <int DH, bool E4M3>
 hipError_t launch_paged(const PagedArgs& a, void* scratch, hipStream_t st) {
   const uint32_t rows = a.starts ? a.n_rows : std::min(a.n_rows, a.n_seq);
   if (rows == 0) return hipSuccess;
+  if (tiled(rows, a.n_seq, a.q_heads, a.group, DH)) return launch_paged<DH, E4M3, 2, true>(a, rows, scratch, st);
   if constexpr (many_tiles(DH) > 1)
-    if ((uint64_t)rows * a.group >= (uint64_t)MANY_COLS * a.n_seq) return launch_paged<DH, E4M3, (int)many_tiles(DH)>(a, rows, scratch, st);
-  return launch_paged<DH, E4M3, 1>(a, rows, scratch, st);
+    if ((uint64_t)rows * a.group >= (uint64_t)MANY_COLS * a.n_seq) return launch_paged<DH, E4M3, (int)many_tiles(DH), false>(a, rows, scratch, st);
+  return launch_paged<DH, E4M3, 1, false>(a, rows, scratch, st);
 }
 
 }  // namespace
 
 uint64_t paged_attention_scratch(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim) {
-  (void)n_seq;
-  return MAX_WGS * 4 + 2ull * MAX_WGS * part_columns(n_rows, q_heads, head_dim) * (head_dim + 4) * 4;
+  return MAX_WGS * 4 + 2ull * MAX_WGS * part_columns(n_rows, n_seq, q_heads, q_heads, head_dim) * (head_dim + 4) * 4;
 }
 
 hipError_t launch_paged_attention(const PagedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st) {

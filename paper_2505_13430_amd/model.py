@@ -226,15 +226,16 @@ class Answers:
         self.logits = torch.zeros(n_seq, self.vocab, dtype=torch.bfloat16, device=dev)
         self._kept = [(torch.zeros(0, **i32), torch.zeros(0, **i32), torch.zeros(0, dtype=torch.uint8, device=dev))]
 
-    def rows(self, n_tokens: int):
+    def rows(self, n_tokens: int, stream=None):
         """Slots, positions and workspace of steps of that many rows, from buffers that double as they are outgrown; the earlier ones
-        are kept for the graphs that were captured with them."""
+        are kept for the graphs that were captured with them.  New ones are made on the stream that uses them."""
         slots, positions, ws = self._kept[-1]
         need = qb.qzo_answer_workspace_bytes(self.model.handle, n_tokens, len(self.lengths))
         if slots.numel() < n_tokens or ws.numel() < need:
             dev, n = self.free.device, max(n_tokens, 2 * slots.numel())
-            slots, positions = (torch.zeros(n, dtype=torch.int32, device=dev) for _ in range(2))
-            ws = torch.empty(max(need, 2 * ws.numel()), dtype=torch.uint8, device=dev)
+            with torch.cuda.stream(stream):
+                slots, positions = (torch.zeros(n, dtype=torch.int32, device=dev) for _ in range(2))
+                ws = torch.empty(max(need, 2 * ws.numel()), dtype=torch.uint8, device=dev)
             self._kept.append((slots, positions, ws))
         return slots[:n_tokens], positions[:n_tokens], ws
 
@@ -242,7 +243,7 @@ class Answers:
         """tokens int32 [rows], the new tokens sequence by sequence, padded at the end; added int32 [n_seq], how many each adds (negative:
         it ends and gives its blocks back).  Returns the logits bf16 [n_seq, vocab] of the last new tokens.  Whether the step could be
         planned is in state[2], where the caller may look (not QZO_OK: nothing has changed, the logits are zeros)."""
-        slots, positions, ws = self.rows(tokens.numel())
+        slots, positions, ws = self.rows(tokens.numel(), stream)
         qb.qzo_cache_plan(self.lengths, added, self.block, self.tables, self.free, self.state, self.lengths, self.starts, slots, positions,
                           self.state, stream)
         qb.qzo_answer(self.model.handle, tokens, self.cache, self.tables, self.lengths, self.starts, slots, positions, ws, self.logits, stream)

@@ -186,6 +186,25 @@ class _Unbacked:
         return self.e
 
 
+@gpu
+def test_buffers_are_made_on_the_stream_that_uses_them():
+    """A step on a stream of its own while the current one is held up: what the buffers are cleared with must not come after the plan."""
+    m = _model("tiny", "int4")
+    text = torch.randint(0, m.shape["vocab"], (40,), generator=torch.Generator().manual_seed(9), dtype=torch.int32).to(DEV)
+    added = torch.tensor([40], dtype=torch.int32, device=DEV)
+    want = Answers(m, n_seq=1, n_blocks=4).add(text, added).clone()
+    a, side = Answers(m, n_seq=1, n_blocks=4), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy = torch.randn(4096, 4096, device=DEV)
+    for _ in range(20):
+        busy = busy @ busy.T.contiguous() * 1e-4
+    got = a.add(text, added, stream=side)
+    side.synchronize()
+    assert torch.equal(got.cpu(), want.cpu()) and torch.equal(a._kept[-1][1][:40].cpu(), torch.arange(40, dtype=torch.int32))
+    torch.cuda.synchronize()
+    assert torch.equal(a._kept[-1][1][:40].cpu(), torch.arange(40, dtype=torch.int32))
+
+
 def _host_model(vocab=1024):
     shape = dict(synth.SHAPES["tiny"], n_layers=1, vocab=vocab)
     d, F = shape["d_model"], shape["d_ffn"]

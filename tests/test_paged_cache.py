@@ -147,7 +147,7 @@ def test_qk_norm_rope_refuses_caches(over, status):
 @pytest.mark.parametrize("over,status", [
     (dict(q=None), qb.QZO_ERR_ARG), (dict(cache=None), qb.QZO_ERR_ARG), (dict(tables=None), qb.QZO_ERR_ARG), (dict(lengths=20), qb.QZO_ERR_ALIGN),
     (dict(starts=20), qb.QZO_ERR_ALIGN), (dict(n_seq=0), qb.QZO_ERR_SHAPE), (dict(n_seq=8193), qb.QZO_ERR_SHAPE), (dict(q_heads=5), qb.QZO_ERR_SHAPE),
-    (dict(q_heads=0), qb.QZO_ERR_SHAPE), (dict(max_blocks=0), qb.QZO_ERR_SHAPE), (dict(max_blocks=1 << 27), qb.QZO_ERR_SHAPE), (dict(ldq=252), qb.QZO_ERR_SHAPE),
+    (dict(q_heads=0), qb.QZO_ERR_SHAPE), (dict(max_blocks=0), qb.QZO_ERR_SHAPE), (dict(max_blocks=1 << 27), qb.QZO_ERR_SHAPE), (dict(max_blocks=(1 << 26) + 1), qb.QZO_ERR_SHAPE), (dict(ldq=252), qb.QZO_ERR_SHAPE),
     (dict(ldo=248), qb.QZO_ERR_SHAPE), (dict(scale=math.nan), qb.QZO_ERR_ARG), (dict(rows=1 << 30), qb.QZO_ERR_SHAPE)])
 def test_paged_attention_refuses(over, status):
     c = _cache()
@@ -395,7 +395,7 @@ def _check_attend(d):
     k, v = (p.double() if s is None else p.double() * s.double()[:, None, None] for p, s in zip(d["pools"], d["scales"]))
     rows = d["starts"][-1]
     q = d["q"].double().view(-1, d["H"], d["dh"])[:rows]
-    at = DEV if rows > 1000 else "cpu"
+    at = DEV if rows > 1000 or rows * max(d["lengths"]) * d["H"] > 2e7 else "cpu"
     want, mag, mac = (x.cpu() for x in attention_reference(q.to(at), k.to(at), v.to(at), d["tables"].to(at), d["lengths"], d["starts"], d["scale"]))
     out = d["outd"].cpu()
     got = out[:rows, :d["H"] * d["dh"]].double().view(want.shape)
@@ -440,6 +440,37 @@ def test_attention_of_many_new_tokens(lengths, news, H, Hk, dh, block, e4m3):
 
 
 @gpu
+@pytest.mark.parametrize("lengths,news,H,Hk,dh,block,e4m3,scale", [
+    ([300, 900, 0, 200], [300, 257, 0, 129], 32, 32, 128, 16, False, None), ([1000, 64, 130], [128, 64, 130], 64, 4, 128, 32, True, None),
+    ([40, 700], [45, 300], 56, 8, 128, 64, False, -0.05), ([500], [420], 60, 4, 128, 256, True, 0.0), ([4100], [300], 64, 64, 128, 16, False, None),
+    ([800, 700], [800, 333], 64, 16, 128, 32, False, None), ([1100, 70], [1024, 70], 64, 16, 64, 16, False, None), ([700, 1500], [600, 500], 64, 2, 64, 64, True, None),
+    ([1200], [1100], 60, 4, 64, 128, False, -0.1)])
+def test_attention_of_prompts(lengths, news, H, Hk, dh, block, e4m3, scale):
+    """At least 96 columns a sequence and more than 128 groups (heads of 64: 511) of 128: keys and values through the LDS.  Whole prompts and
+    later parts, more new tokens than the length says, groups of heads that divide 128 and not, groups cut into pieces and not, scales of
+    any sign, positions of nobody that hold anything, blocks that are not there."""
+    assert sum(news) * H // 128 > (511 if dh == 64 else 128) and sum(news) * (H // Hk) >= 96 * len(news)
+    d = _attend(lengths, H, Hk, dh, block, news, e4m3=e4m3, seed=H, pad_rows=2, stride=8, scale=scale)
+    _check_attend(d)
+    spoiled = _attend(lengths, H, Hk, dh, block, news, e4m3=e4m3, seed=H, pad_rows=2, stride=8, scale=scale, spoil=True)
+    assert torch.equal(spoiled["outd"], d["outd"])
+    tables = d["tables"].clone()
+    tables[0, 0], tables[0, -(-lengths[0] // block) // 2], tables[-1, 0] = -1, 1 << 30, -5
+    d = _attend(lengths, H, Hk, dh, block, news, e4m3=e4m3, seed=H, scale=scale, tables=tables, run=False)
+    qb.qzo_paged_attention(*d["args"])
+    _check_attend(d)
+
+
+@gpu
+def test_attention_of_many_prompts():
+    """More sequences than a wavefront has lanes."""
+    rng = np.random.default_rng(3)
+    news = [int(x) for x in rng.integers(8, 14, 80)]
+    lengths = [n + int(x) for n, x in zip(news, rng.integers(0, 300, 80))]
+    _check_attend(_attend(lengths, 32, 2, 128, 16, news, seed=8))
+
+
+@gpu
 @pytest.mark.parametrize("n,longest,H,Hk,dh,block,seed", [(300, 40, 4, 4, 64, 16, 1), (70, 900, 8, 8, 128, 32, 2), (9, 9000, 8, 2, 128, 16, 3), (1, 70000, 2, 1, 64, 128, 4),
                                                          (2000, 3, 2, 1, 64, 16, 5)])
 def test_attention_of_ragged_batches(n, longest, H, Hk, dh, block, seed):
@@ -474,6 +505,8 @@ def test_attention_of_more_and_fewer_rows_than_sequences():
     whole = _attend([40, 70, 300], 4, 2, 64, 16, seed=1)
     assert torch.equal(d["outd"][:2], whole["outd"][:2])
     _check_attend(_attend([40, 70], 4, 2, 64, 16, e4m3=True, scaled=False, seed=2))
+    for scale in (-0.1, 0.0):
+        _check_attend(_attend([40, 700], 8, 2, 128, 16, scale=scale, seed=2))
 
 
 @gpu
@@ -511,7 +544,8 @@ def test_unseen_positions_hold_anything(lengths, news, e4m3):
 
 
 @gpu
-@pytest.mark.parametrize("length,new,at,H,Hk,dh", [(70, 20, 61, 4, 2, 64), (70, 20, 61, 2, 1, 128), (40, 3, 38, 6, 1, 128), (1300, 1100, 777, 32, 16, 64)])
+@pytest.mark.parametrize("length,new,at,H,Hk,dh", [(70, 20, 61, 4, 2, 64), (70, 20, 61, 2, 1, 128), (40, 3, 38, 6, 1, 128), (1300, 1100, 777, 32, 16, 64),
+                                                    (700, 300, 501, 64, 32, 128), (1300, 1100, 777, 64, 32, 64)])
 def test_later_tokens_hold_anything(length, new, at, H, Hk, dh):
     """A new token's key and value are NaN or infinite: the rows before it do not see it, its own and the later ones do."""
     clean = _attend([length], H, Hk, dh, 16, [new], seed=4)

@@ -16,8 +16,8 @@
 // What bounds it: memory.  A step of a wavefront loads its next 32 keys (16 KB at heads of 128, bf16) before it works on the
 // ones it has; eight wavefronts on a compute unit keep 128 to 256 KB on the way.  Loads and block ids are issued without a branch
 // around them, or the compiler waits for all of them at every use.  8 sequences of 65536 tokens, 8 key heads of 128: 370 us,
-// 5.8 TB/s (a kernel that only reads: 6.1 to 6.3); 64 ragged ones of up to 4001, 32 key heads, 157 us, 5.1 TB/s; 24 in e4m3 of up
-// to 32001, 87 us, 4.8 TB/s, 75 of them the cache at the rate of the first.  Few keys: latency.  One token 5.4 us (launch, lengths,
+// 5.8 TB/s (a kernel that only reads: 6.1 to 6.3); 64 ragged ones of up to 4001, 32 key heads, 150 us, 5.4 TB/s; 24 in e4m3 of up
+// to 32001, 86 us, 4.9 TB/s, 75 of them the cache at the rate of the first.  Few keys: latency.  One token 5.4 us (launch, lengths,
 // table, keys, one after the other); a compute unit alone takes 54 GB/s, 1.2 us a unit.
 #include <algorithm>
 #include <type_traits>
@@ -52,9 +52,9 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // but one of 512 (128 groups) 31 / 32: from more groups than half the compute units on.  Heads of 64: one of 2048 (512 groups)
 // 104 / 86, the prompts 75 / 65, but 4 x 200 (250) 80 / 97, 6 x 100 (150) 63 / 66: from as many groups as workgroups on.  Fewer columns leave
 // lanes idle: 4 x 8 tokens, 64 heads on 8, behind 9000 (64 columns) 64 / 86, 20 x 40 behind 960 121 / 123: from TILED_COLS a sequence on.
-// What bounds it: two wavefronts a SIMD, each a chain of LDS reads, products and exponentials (vector instructions 40 % of
+// What bounds it: two wavefronts a SIMD, each a chain of LDS reads, products and exponentials (one of 4000: vector instructions 40 % of
 // the time, matrix instructions 17 %; neither fewer vector instructions nor more steps ahead nor LDS reads without conflicts made it
-// faster); 119 us for what moves 268 MB: 54 at the rate of a copy.
+// faster).  Heads of 128 have no registers left; what the compiler keeps in scratch memory is some 150 MB written in that call.
 //   With more groups than workgroups, a sequence of up to QUAD_LEN positions and one wavefront's columns gives a workgroup four key heads at a time, one a
 // wavefront (a unit is 32 keys of each): no other wavefront waits for a step that there is not, a workgroup starts a quarter
 // as often, and nothing is added up in the end.  Such groups are not cut.  256 sequences, 32 heads of 128, of 1 / 20 / 64 /
@@ -542,25 +542,30 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
           }
         }
       } else {
-        // a pair of features at a time, so that few registers hold what is not in place
+        // (TILED: a pair of features at a time, so that few registers hold what is not in place)
+        auto pair = [&](int ct, int u, uint32_t c) {
+          const int32_t its = __builtin_amdgcn_readlane(sees[ct], (int)c);
+          uint32_t y[8];
 #pragma unroll
-        for (int u = 0; u < VW / 2; ++u)
+          for (int j = 0; j < 8; ++j) y[j] = key_of(kb, j) < its ? value(j, u) : 0u;
+          const f32x4 even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x05040100u), pk[ct], acc[ct][2 * u], 0, 0, 0);
+          const f32x4 uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x07060302u), pk[ct], acc[ct][2 * u + 1], 0, 0, 0);
+          if (col == c) { acc[ct][2 * u] = even; acc[ct][2 * u + 1] = uneven; }
+        };
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            uint32_t v[8];
+        for (int ct = 0; ct < CT; ++ct) {
+          if constexpr (TILED) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = value(j, u);
+            for (int u = 0; u < VW / 2; ++u)
 #pragma unroll 1
-            for (uint32_t c = 0; c < COLS; ++c) {
-              const int32_t its = __builtin_amdgcn_readlane(sees[ct], (int)c);
-              uint32_t y[8];
+              for (uint32_t c = 0; c < COLS; ++c) pair(ct, u, c);
+          } else {
+#pragma unroll 1
+            for (uint32_t c = 0; c < COLS; ++c)
 #pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = key_of(kb, j) < its ? v[j] : 0u;
-              const f32x4 even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x05040100u), pk[ct], acc[ct][2 * u], 0, 0, 0);
-              const f32x4 uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x07060302u), pk[ct], acc[ct][2 * u + 1], 0, 0, 0);
-              if (col == c) { acc[ct][2 * u] = even; acc[ct][2 * u + 1] = uneven; }
-            }
+              for (int u = 0; u < VW / 2; ++u) pair(ct, u, c);
           }
+        }
       }
     };
 

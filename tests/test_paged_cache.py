@@ -462,6 +462,28 @@ def test_attention_of_prompts(lengths, news, H, Hk, dh, block, e4m3, scale):
 
 
 @gpu
+@pytest.mark.parametrize("lengths,news,H,Hk,dh", [([700, 333], [600, 333], 32, 8, 128), ([2100], [260], 64, 4, 128), ([1100], [1030], 64, 64, 64)])
+def test_captured_prompts_replay(lengths, news, H, Hk, dh):
+    """Replays over other queries and other lengths, eager work in between, against eager calls."""
+    d = _attend(lengths, H, Hk, dh, 16, news, seed=5, run=False)
+    q, cache, tables, at, out, scale, starts = d["args"]
+    scratch = torch.zeros(qb.qzo_paged_attention_scratch_bytes(q.shape[0], len(lengths), H, dh), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        qb.qzo_paged_attention(q, cache, tables, at, out, scale, starts, scratch=scratch)
+    want = torch.empty_like(out)
+    for i in range(4):
+        d["qd"].copy_(_randn(*d["qd"].shape, seed=i).to(DEV))
+        at.copy_(_i32([n - 37 * i for n in lengths]))
+        out.fill_(7.0)
+        graph.replay()
+        qb.qzo_paged_attention(q, cache, tables, at, want, scale, starts)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and not bool(scratch[:2048].any())
+
+
+@gpu
 def test_attention_of_many_prompts():
     """More sequences than a wavefront has lanes."""
     rng = np.random.default_rng(3)

@@ -364,14 +364,15 @@ typedef struct {
  *     [n_seq, max_blocks] behind those that they hold.  Nothing else of the tables is written.
  *   lengths_dev [n_seq]: cached + added, 0 where a sequence ends (may be cached_dev).
  *   starts_dev [n_seq + 1]: tokens added by the sequences before; the new tokens are listed sequence by sequence.
- *   slots_dev, positions_dev [max_tokens]: slot and position of every new token; -1 and 0 behind the last one.
+ *   slots_dev, positions_dev [max_tokens]: slot and position of every new token; -1 and 0 behind the last one.  A token whose block
+ *     id lies outside 0 .. n_blocks - 1 has slot -1.
  *   after_dev (may be before_dev): the new state.
  * A plan is made as a whole or not at all: where status is not QZO_OK, lengths are cached_dev's, starts 0, slots -1,
  * positions 0, n_tokens and n_taken 0, the free list and the tables as they were.  QZO_ERR_WORKSPACE: not enough free
  * blocks; QZO_ERR_SHAPE: a row of the tables is too short for its sequence, or max_tokens too small; QZO_ERR_ARG: a negative
  * length, an n_free outside 0 .. n_blocks, more blocks given back than the pool has.
- * Block ids in the tables and on the list are the caller's (0 .. n_blocks - 1); this call copies them without a look, the
- * calls that use them treat others as absent.  Otherwise the buffers must not overlap.  n_seq 1 .. 8192, max_blocks and
+ * Block ids in the tables and on the list are the caller's (0 .. n_blocks - 1); this call copies others as they
+ * are, and whoever uses them treats such a block as absent.  Otherwise the buffers must not overlap.  n_seq 1 .. 8192, max_blocks and
  * max_tokens at least 1, n_seq * max_blocks below 2^31; buffers 16-byte aligned.
  */
 qzo_status qzo_cache_plan(const int32_t* cached_dev, const int32_t* added_dev, uint32_t n_seq, uint32_t block,

@@ -19,6 +19,11 @@ __device__ __forceinline__ uint32_t last_not_above(const int32_t* prefix, uint32
   return lo;
 }
 
+// Slot of position `at` in block `id`; none in a block that the pool has not: shifted, such an id could end at another block's slot.
+__device__ __forceinline__ int32_t slot_of(const CachePlanArgs& a, int32_t id, int32_t at) {
+  return (uint32_t)id < a.n_blocks ? (int32_t)(((uint32_t)id << a.block_shift) + ((uint32_t)at & ((1u << a.block_shift) - 1u))) : -1;
+}
+
 // One workgroup, a sequence (or several) per thread.  What sequence i gives back (ended), takes and adds is summed over the
 // sequences before it; the sums stay in the LDS, where blocks given back, and the blocks and tokens of long prompts, find their
 // sequence by bisection and are spread over all threads.  Every input is read before the first output is written (lengths
@@ -133,7 +138,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs 
           number = j;
           if (j >= held) a.tables[(uint64_t)i * a.max_blocks + (uint32_t)j] = id;
         }
-        if (with_slots) { a.slots[start[i] + x] = (id << shift) + (at & mask); a.positions[start[i] + x] = at; }
+        if (with_slots) { a.slots[start[i] + x] = slot_of(a, id, at); a.positions[start[i] + x] = at; }
       }
     }
   } else {
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(CachePlanArgs 
     for (int32_t t = (int32_t)tid; with_slots && t < n_tok; t += PLAN_THREADS) {
       const uint32_t s = last_not_above(start, a.n_seq, t);
       const int32_t at = old_len[s] + t - start[s];
-      a.slots[t] = (block_of(s, at >> shift, (int32_t)blocks(old_len[s])) << shift) + (at & mask);
+      a.slots[t] = slot_of(a, block_of(s, at >> shift, (int32_t)blocks(old_len[s])), at);
       a.positions[t] = at;
     }
   }
@@ -159,13 +164,13 @@ __global__ __launch_bounds__(256) void cache_slots_kernel(CachePlanArgs a) {
   extern __shared__ int32_t prefix[];
   for (uint32_t i = threadIdx.x; i <= a.n_seq; i += 256) prefix[i] = a.starts[i];
   __syncthreads();
-  const int32_t n_tok = prefix[a.n_seq], mask = (1 << a.block_shift) - 1;
+  const int32_t n_tok = prefix[a.n_seq];
   for (uint32_t t = blockIdx.x * 256u + threadIdx.x; t < a.max_tokens; t += gridDim.x * 256u) {
     int32_t slot = -1, at = 0;
     if ((int32_t)t < n_tok) {
       const uint32_t s = last_not_above(prefix, a.n_seq, (int32_t)t);
       at = a.lengths[s] - (prefix[s + 1] - (int32_t)t);
-      slot = (a.tables[(uint64_t)s * a.max_blocks + (uint32_t)(at >> a.block_shift)] << a.block_shift) + (at & mask);
+      slot = slot_of(a, a.tables[(uint64_t)s * a.max_blocks + (uint32_t)(at >> a.block_shift)], at);
     }
     a.slots[t] = slot;
     a.positions[t] = at;

@@ -243,6 +243,25 @@ def test_plan_that_cannot_be_made_changes_nothing(cached, added, n_free, most, t
         assert got["after"].tolist() == [n_free, 0, status, 0]
 
 
+@gpu
+@pytest.mark.parametrize("n,added,pad", [(6, 1, 2), (6, 40, 2), (1100, 1, 3), (1100, 5, 3), (6, 40, 4100)])
+def test_plan_gives_no_slot_in_a_block_outside_the_pool(n, added, pad):
+    """Ids that shifted by the block's size would wrap to another block's slots, in the tables and on the free list; tokens that a thread
+    itself sees to, prompts, and more than 4096 of them."""
+    block, cached = 16, [20 + i % 16 for i in range(n)]
+    tables, free = _pool(cached, block, 4 * n, 6, 11)
+    bad = [1 << 28, (1 << 28) + 1, -1, len(free), 2 ** 31 - 1, -2 ** 31]
+    for i, x in enumerate(bad):
+        tables[(3 * i + 1) % n, 1] = x
+    free[4 * n - len(bad):4 * n] = bad
+    tokens = n * added + pad
+    want = plan_reference(cached, [added] * n, block, tables, free, 4 * n, tokens)
+    want["slots"] = [s if 0 <= s < len(free) * block else -1 for s in want["slots"]]
+    got = _plan(cached, [added] * n, block, tables, free, 4 * n, tokens)
+    for k, v in want.items():
+        assert np.array_equal(got[k], v), k
+
+
 # ------------------------------------------------------------------ heads of q and k ----
 def _randn(*shape, seed=0, dtype=torch.bfloat16):
     return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(dtype)

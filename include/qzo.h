@@ -387,8 +387,8 @@ qzo_status qzo_cache_plan(const int32_t* cached_dev, const int32_t* added_dev, u
  * RMSNorm over the head with q_gain_dev / k_gain_dev (bf16 [head_dim]; null: that one is not normed), then features i and
  * i + head_dim/2 turned by the angle p * rope_theta^(-2i/head_dim) (rope_theta 0: not rotated), fp32 throughout (the angle in
  * double) with one rounding at the end.  p: positions_dev[t], or t % seq where positions_dev is null.
- *   cache null: out_dev (bf16, rows ld_out elements apart) receives the heads of q, then those of k; it may be qkv_dev with
- *     ld_out = ld_qkv (in place; v is not touched).  slots_dev must be null.
+ * out_dev may be qkv_dev: in place, with ld_out = ld_qkv where there is more than one row; what is not written stays.
+ *   cache null: out_dev (bf16, rows ld_out elements apart) receives the heads of q, then those of k.  slots_dev must be null.
  *   cache given: out_dev receives the heads of q; k and v of the row go to slot slots_dev[t] of the cache (in e4m3: divided by
  *     their scale, cut off at +-448, rounded to nearest even).  A row whose slot is negative or beyond the pool is skipped, its
  *     out row included.  The slots of a call must differ from one another.

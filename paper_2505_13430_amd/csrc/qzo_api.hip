@@ -1700,7 +1700,7 @@ qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tok
   if (ld_qkv % 8 || ld_out % 8 || ld_qkv < in_row || ld_out < out_row)
     return fail(QZO_ERR_SHAPE, "ld_qkv and ld_out must be multiples of 8 that hold a row");
   if (ld_qkv >= (1ull << 32) || ld_out >= (1ull << 32)) return fail(QZO_ERR_SHAPE, "ld_qkv and ld_out must be below 2^32");
-  if (qkv_dev == out_dev && ld_qkv != ld_out) return fail(QZO_ERR_ARG, "in place both rows have the same stride");
+  if (qkv_dev == out_dev && n_tokens > 1 && ld_qkv != ld_out) return fail(QZO_ERR_ARG, "in place both rows have the same stride");
   QkArgs a = {};
   a.qkv = (const bf16_t*)qkv_dev; a.ld_qkv = ld_qkv; a.out = (bf16_t*)out_dev; a.ld_out = ld_out;
   a.n_tokens = n_tokens; a.q_heads = q_heads; a.kv_heads = kv_heads; a.rope = rope_theta > 0.0f;

@@ -346,6 +346,24 @@ def test_heads_into_the_cache(T, H, Hk, dh, block, scaled, e4m3):
 
 
 @gpu
+@pytest.mark.parametrize("cached", [False, True])
+@pytest.mark.parametrize("T", [1, 2, 37])
+def test_heads_in_place(T, cached):
+    """Out is the first columns of qkv's own rows, one row and several, without a cache and with one: as apart, bit for bit."""
+    H, Hk, dh = 4, 2, 64
+    x = _randn(T, (H + 2 * Hk) * dh, seed=T).to(DEV)
+    wide = (H if cached else H + Hk) * dh
+    got, want = x.clone(), torch.empty(T, wide, dtype=torch.bfloat16, device=DEV)
+    pools = [[torch.zeros(4, Hk, 16, dh, dtype=torch.bfloat16, device=DEV) for _ in range(2)] for _ in range(2)]
+    for out, src, pool in ((want, x, pools[0]), (got[:, :wide], got, pools[1])):
+        more = dict(cache=qb.make_cache(*pool), slots=_i32(range(T))) if cached else {}
+        qb.qzo_qk_norm_rope(src, H, Hk, out, positions=_i32(np.arange(T) + 5), **more)
+    assert torch.equal(got[:, :wide], want) and torch.equal(got[:, wide:], x[:, wide:]) and not torch.equal(want, x[:, :wide])
+    for a, b in zip(*pools):
+        assert torch.equal(a, b)
+
+
+@gpu
 def test_heads_keep_to_themselves():
     """NaN and infinities of a head reach that head's outputs only; a head of zeros stays zero under its norm; no tokens, no writes."""
     x = _randn(3, 4 + 2 * 2, 64, seed=3)

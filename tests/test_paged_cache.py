@@ -619,6 +619,57 @@ def test_later_tokens_hold_anything(length, new, at, H, Hk, dh):
 
 
 @gpu
+@pytest.mark.parametrize("lengths,news,H,Hk,dh,e4m3", [
+    ([700, 33, 1], None, 8, 2, 128, False), ([700, 33, 1], None, 8, 2, 64, True), ([50 + i for i in range(80)], None, 16, 8, 128, False),
+    ([400, 90], [100, 60], 8, 2, 64, False), ([400, 90], [100, 60], 8, 2, 128, True), ([9000] * 6, [8] * 6, 64, 8, 128, False),
+    ([700, 333], [600, 333], 32, 8, 128, False), ([1100], [1030], 64, 32, 64, True), ([1100], [1030], 64, 32, 64, False)])
+def test_scores_of_minus_infinity_hide_a_key(lengths, news, H, Hk, dh, e4m3):
+    """A score that leaves fp32 downwards counts as unseen: for the heads that have it, what such a key's value holds reaches nothing; the heads
+    beside them see it.  Narrow, wide and four key heads' groups, 32 columns, prompts."""
+    hidden, f = [0, 3, 31, 32, 40, 127, 128, 300, 9000 - 1], 5
+    got = []
+    for what in (1.0, math.nan, math.nan if e4m3 else math.inf):
+        d = _attend(lengths, H, Hk, dh, 16, news, e4m3=e4m3, seed=H + dh, run=False)
+        q = d["qd"].view(-1, H, dh)
+        q[..., f] = 0
+        q[:, 1::2, f] = 2.0 ** 127                       # times 448: beyond fp32
+        d["q"] = d["qd"].cpu()
+        d["pd"][0].view(torch.uint8 if e4m3 else torch.int16)[..., f] = 0
+        for i, length in enumerate(lengths):
+            for at in hidden:
+                if at < length:
+                    b = int(d["tables"][i, at // 16])
+                    d["pd"][0][b, :, at % 16, f] = -448.0
+                    d["pd"][1][b, :, at % 16] = what
+        qb.qzo_paged_attention(*d["args"])
+        got.append(d["outd"].view(-1, H, dh).clone())
+        if what != 1.0 or sum(lengths) > 2000:
+            continue
+        # against 64 bits: the hidden keys masked, without the feature that hides them
+        k, v = (p.double().cpu() if s is None else p.double().cpu() * s.double()[:, None, None] for p, s in zip(d["pd"], d["scales"]))
+        at = torch.arange(max(lengths))
+        for i, length in enumerate(lengths):
+            ids = d["tables"][i, at[:length] // 16].long()
+            for r in range(d["starts"][i], d["starts"][i + 1]):
+                sees = length - (d["starts"][i + 1] - 1 - r)
+                seen = torch.tensor([p for p in range(sees) if p not in hidden], dtype=torch.long)
+                if seen.numel() == 0:
+                    assert not bool(got[0][r, 1::2].any())
+                    continue
+                kk, vv = (p[ids[seen], :, seen % 16].repeat_interleave(H // Hk, 1)[:, 1::2] for p in (k, v))
+                kk[..., f] = 0
+                qq = d["q"].double().view(-1, H, dh)[r, 1::2]
+                p = torch.softmax(d["scale"] * (qq * kk).sum(-1), 0)
+                want, mag = (p[..., None] * vv).sum(0), (p[..., None] * vv.abs()).sum(0)
+                mac = (d["scale"] * (qq.abs() * kk.abs()).sum(-1)).amax(0)
+                assert bool(((got[0][r, 1::2].double().cpu() - want).abs() <= attention_tolerance(want, mag, mac, dh)).all()), (i, r)
+    assert bool(torch.isfinite(got[0]).all())
+    for spoiled in got[1:]:
+        assert torch.equal(spoiled[:, 1::2], got[0][:, 1::2])
+        assert not bool(torch.isfinite(spoiled[:, 0::2]).any())
+
+
+@gpu
 def test_blocks_outside_the_pool_are_absent():
     tables = torch.tensor([[3, -1, 1, 99], [2 ** 31 - 1, -2 ** 31, 4, 5], [-1, -1, -1, -1]], dtype=torch.int32)
     d = _attend([60, 64, 50], 4, 2, 64, 16, seed=6, tables=tables, extra_blocks=0)

@@ -902,9 +902,10 @@ hipError_t launch_paged(const PagedArgs& a, uint32_t rows, void* scratch, hipStr
   const uint64_t units = (((uint64_t)a.max_blocks << a.block_shift) + 31) / 32;
   const bool few = a.n_seq <= 64 && (double)groups * (double)(2 * units + 2) < 4e9;      // 32 bits hold the sums, padding included
   const uint32_t sums = WAVES * TC * (DH + 4) * 4 + WAVES * TC * 8, row = DH * (E4M3 ? 1u : 2u), tiles = TILED ? 8u * tile_step(row) * row : 0u;
-  const uint32_t lds = std::max(sums, tiles) + WAVES * 8 + (few ? 0 : a.n_seq * 8);
-  if (lds > 60u * 1024) {
-    hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3, CT, TILED>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  const uint32_t fixed = std::max(sums, tiles) + WAVES * 8, lds = fixed + (few ? 0 : a.n_seq * 8);
+  if (lds > 60u * 1024) {                       // the limit that all calls have in common: another thread's call finds it no lower than its own
+    hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3, CT, TILED>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)(fixed + CACHE_MAX_SEQ * 8));
     if (e != hipSuccess) return e;
   }
   const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (groups * ((units + MIN_PIECE - 1) / MIN_PIECE) + 7) / 8 * 8);

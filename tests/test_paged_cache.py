@@ -4,6 +4,7 @@ plain implementations in 64 bits (whole numbers: equal).
 Tolerances are what the roundings add up to.  eps/2 of bf16 is 2^-8, of e4m3 2^-4, of fp32 2^-24."""
 import ctypes as C
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -831,6 +832,34 @@ def test_calls_on_two_streams_at_once():
         a["outd"].zero_()
         with pytest.raises(AssertionError):
             qb.qzo_paged_attention(*a["args"])
+
+
+@gpu
+def test_calls_of_two_threads():
+    """Two threads, each with a stream of its own, whose calls need different amounts of LDS: both run, with the results that they have alone."""
+    calls = []
+    for n, seed in ((8192, 1), (6000, 2)):
+        d = _attend([1 + i % 3 for i in range(n)], 1, 1, 64, 16, seed=seed)
+        calls.append((d, d["outd"].clone(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(d, stream):
+        try:
+            scratch = torch.zeros(qb.qzo_paged_attention_scratch_bytes(d["qd"].shape[0], len(d["lengths"]), 1, 64), dtype=torch.uint8, device=DEV)
+            torch.cuda.synchronize()
+            for _ in range(3000):
+                qb.qzo_paged_attention(*d["args"], scratch=scratch, stream=stream)
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(d, stream)) for d, _, stream in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed and all(torch.equal(d["outd"], want) for d, want, _ in calls)
 
 
 @gpu

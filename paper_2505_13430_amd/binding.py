@@ -495,6 +495,14 @@ def _at(t, dtype, at):
     return t.data_ptr()
 
 
+def _room(t, at):
+    """Address and bytes of memory on device `at` that a call may use; None: null."""
+    if t is None:
+        return None, 0
+    assert t.get_device() == at and t.is_contiguous(), "scratch and workspace are contiguous tensors on the current device"
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _stream_of(stream, at):
     return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
@@ -578,8 +586,7 @@ def qzo_paged_attention(q, cache, tables, lengths, out, scale, starts=None, scra
     if isinstance(scratch, str):
         scratch = _scratch_of_stream(at, stream, st, qzo_paged_attention_scratch_bytes(rows, n, heads, dh))
     _check(lib().qzo_paged_attention(x, ldx, rows, n, heads, C.addressof(cache), _at(tables, i32, at), most, _at(lengths, i32, at),
-                                     _at(starts, i32, at), scale, y, ldy, None if scratch is None else scratch.data_ptr(),
-                                     0 if scratch is None else scratch.numel() * scratch.element_size(), st))
+                                     _at(starts, i32, at), scale, y, ldy, *_room(scratch, at), st))
 
 
 def qzo_answer_workspace_bytes(model, n_tokens, n_seq) -> int:
@@ -593,7 +600,7 @@ def qzo_answer(model, tokens, cache, tables, lengths, starts, slots, positions, 
     i32, (n, most) = torch.int32, tables.shape
     assert lengths.numel() == n and starts.numel() == n + 1 and slots.numel() >= tokens.numel() <= positions.numel() and logits.shape[0] == n
     at = torch.cuda.current_device()
-    assert cache.device == at == workspace.get_device()
+    assert cache.device == at
     _check(lib().qzo_answer(model, _at(tokens, i32, at), tokens.numel(), n, C.addressof(cache), _at(tables, i32, at), most, _at(lengths, i32, at),
-                            _at(starts, i32, at), _at(slots, i32, at), _at(positions, i32, at), workspace.data_ptr(),
-                            workspace.numel() * workspace.element_size(), _at(logits, torch.bfloat16, at), _stream_of(stream, at)))
+                            _at(starts, i32, at), _at(slots, i32, at), _at(positions, i32, at), *_room(workspace, at),
+                            _at(logits, torch.bfloat16, at), _stream_of(stream, at)))

@@ -205,6 +205,17 @@ def test_buffers_are_made_on_the_stream_that_uses_them():
     assert torch.equal(a._kept[-1][1][:40].cpu(), torch.arange(40, dtype=torch.int32))
 
 
+@gpu
+def test_workspace_elsewhere_is_refused():
+    """Host memory, and memory with gaps, as the workspace of an answer."""
+    m = _model("tiny", "int4")
+    a, tokens = Answers(m, n_seq=1, n_blocks=4, block=16), torch.zeros(2, dtype=torch.int32, device=DEV)
+    slots, positions, ws = a.rows(2)
+    for bad in (torch.zeros(ws.numel(), dtype=torch.uint8), torch.zeros(2 * ws.numel(), dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(AssertionError):
+            qb.qzo_answer(m.handle, tokens, a.cache, a.tables, a.lengths, a.starts, slots, positions, bad, a.logits)
+
+
 def _host_model(vocab=1024):
     shape = dict(synth.SHAPES["tiny"], n_layers=1, vocab=vocab)
     d, F = shape["d_model"], shape["d_ffn"]

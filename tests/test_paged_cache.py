@@ -863,6 +863,19 @@ def test_calls_of_two_threads():
 
 
 @gpu
+def test_scratch_elsewhere_is_refused():
+    """Host memory, and memory with gaps."""
+    d = _attend([100], 4, 2, 64, 16, seed=1)
+    need = qb.qzo_paged_attention_scratch_bytes(1, 1, 4, 64)
+    before = d["outd"].clone()
+    for bad in (torch.zeros(need, dtype=torch.uint8), torch.zeros(need, dtype=torch.uint8).pin_memory(), torch.zeros(2 * need, dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(AssertionError):
+            qb.qzo_paged_attention(*d["args"], scratch=bad)
+    torch.cuda.synchronize()
+    assert torch.equal(before, d["outd"])
+
+
+@gpu
 def test_scratch_that_is_too_small_is_refused():
     d = _attend([100], 4, 2, 64, 16, seed=1)
     need = qb.qzo_paged_attention_scratch_bytes(1, 1, 4, 64)

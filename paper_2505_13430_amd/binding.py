@@ -561,7 +561,11 @@ _stream_scratch = {}
 def _scratch_of_stream(device, stream, handle, nbytes):
     """Scratch of the calls on one stream, which do not overlap.  A captured graph keeps the address it was captured with and may
     be replayed on any stream beside any other: it is given scratch of its own."""
-    assert not torch.cuda.is_current_stream_capturing(), "a captured call needs scratch of its own: pass scratch"
+    captured = torch.cuda.is_current_stream_capturing()
+    if stream is not None:                     # a stream may be captured without being the current one
+        with torch.cuda.stream(stream):
+            captured = captured or torch.cuda.is_current_stream_capturing()
+    assert not captured, "a captured call needs scratch of its own: pass scratch"
     t = _stream_scratch.get((device, handle))
     if t is None or t.numel() < nbytes:
         with torch.cuda.stream(stream):        # what is outgrown is used again on this stream only

@@ -863,6 +863,22 @@ def test_calls_of_two_threads():
 
 
 @gpu
+def test_a_capture_on_a_passed_stream_needs_scratch_of_its_own():
+    """The stream that is captured is passed while another one is the current one, and the other way round."""
+    d = _attend([100, 40], 4, 2, 64, 16, seed=1)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        captured = torch.cuda.current_stream()
+        d["outd"].zero_()
+        with torch.cuda.stream(side), pytest.raises(AssertionError):
+            qb.qzo_paged_attention(*d["args"], stream=captured)
+        with pytest.raises(AssertionError):
+            qb.qzo_paged_attention(*d["args"], stream=side)
+    torch.cuda.synchronize()
+
+
+@gpu
 def test_scratch_elsewhere_is_refused():
     """Host memory, and memory with gaps."""
     d = _attend([100], 4, 2, 64, 16, seed=1)

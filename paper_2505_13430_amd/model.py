@@ -241,10 +241,16 @@ class Answers:
 
     def add(self, tokens: torch.Tensor, added: torch.Tensor, stream=None) -> torch.Tensor:
         """tokens int32 [rows], the new tokens sequence by sequence, padded at the end; added int32 [n_seq], how many each adds (negative:
-        it ends and gives its blocks back).  Returns the logits bf16 [n_seq, vocab] of the last new tokens.  Whether the step could be
-        planned is in state[2], where the caller may look (not QZO_OK: nothing has changed, the logits are zeros)."""
-        slots, positions, ws = self.rows(tokens.numel(), stream)
+        it ends and gives its blocks back).  A step without tokens ends sequences and runs no model.  Returns the logits bf16 [n_seq, vocab]
+        of the last new tokens.  Whether the step could be planned is in state[2], where the caller may look (not QZO_OK: nothing has
+        changed, the logits are zeros)."""
+        slots, positions, ws = self.rows(max(1, tokens.numel()), stream)
+        if tokens.numel() == 0:                 # a plan has room for one token: a sequence that would add any adds more, so that it is refused
+            with torch.cuda.stream(stream):
+                added = torch.where(added > 0, 2, added)
+                self.logits.zero_()
         qb.qzo_cache_plan(self.lengths, added, self.block, self.tables, self.free, self.state, self.lengths, self.starts, slots, positions,
                           self.state, stream)
-        qb.qzo_answer(self.model.handle, tokens, self.cache, self.tables, self.lengths, self.starts, slots, positions, ws, self.logits, stream)
+        if tokens.numel():
+            qb.qzo_answer(self.model.handle, tokens, self.cache, self.tables, self.lengths, self.starts, slots, positions, ws, self.logits, stream)
         return self.logits

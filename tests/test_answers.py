@@ -132,6 +132,29 @@ def test_a_step_that_cannot_be_planned_changes_nothing():
 
 
 @gpu
+def test_a_step_that_only_ends_sequences():
+    """No token at all: the blocks go back, the logits are zeros, what goes on goes on; tokens that are not there are refused."""
+    m = _model("tiny", "int4")
+    a, none = Answers(m, n_seq=2, n_blocks=4, block=16), torch.zeros(0, dtype=torch.int32, device=DEV)
+    text = torch.arange(40, dtype=torch.int32, device=DEV)
+
+    def step(tokens, *added):
+        return a.add(tokens, torch.tensor(added, dtype=torch.int32, device=DEV))
+
+    step(text[:35], 30, 5)
+    got = step(none, -1, 0)
+    assert a.state.tolist() == [3, 0, 0, 0] and a.lengths.tolist() == [0, 5] and not bool(got.any())
+    for added in ((0, 1), (1, -1), (0, 2 ** 31 - 1)):
+        step(none, *added)
+        assert a.state.tolist() == [3, 0, qb.QZO_ERR_SHAPE, 0] and a.lengths.tolist() == [0, 5]
+    got = step(torch.cat([text, text[35:36]]), 40, 1)
+    assert a.state.tolist() == [0, 41, 0, 3] and a.lengths.tolist() == [40, 6]
+    assert _far(got[0], _logits(m, text)[-1]) <= 2e-2
+    step(none, -1, -1)
+    assert a.state.tolist() == [4, 0, 0, 0] and sorted(a.free.tolist()) == [0, 1, 2, 3]
+
+
+@gpu
 @pytest.mark.parametrize("name", ["tiny", "tiny_opt"])
 def test_captured_steps_answer_as_eager_ones(name):
     """A step of one token a sequence captured into a graph, the next token chosen inside it: replays, with the program's own eager work

@@ -242,7 +242,8 @@ class Answers:
     def add(self, tokens: torch.Tensor, added: torch.Tensor, stream=None) -> torch.Tensor:
         """tokens int32 [rows], the new tokens sequence by sequence, padded at the end; added int32 [n_seq], how many each adds (negative:
         it ends and gives its blocks back).  A step without tokens ends sequences and runs no model.  Returns the logits bf16 [n_seq, vocab]
-        of the last new tokens.  Whether the step could be planned is in state[2], where the caller may look (not QZO_OK: nothing has
+        of the last new tokens: `logits`, the same buffer every step, which the next one overwrites (a graph that holds the step writes it, too;
+        keep a copy of what is to outlive a step).  Whether the step could be planned is in state[2], where the caller may look (not QZO_OK: nothing has
         changed, the logits are zeros)."""
         slots, positions, ws = self.rows(max(1, tokens.numel()), stream)
         if tokens.numel() == 0:                 # a plan has room for one token: a sequence that would add any adds more, so that it is refused

@@ -132,6 +132,18 @@ def test_a_step_that_cannot_be_planned_changes_nothing():
 
 
 @gpu
+def test_logits_are_one_buffer():
+    """What `add` returns is `logits`, also after a longer step; a copy is what outlives the next step."""
+    m = _model("tiny", "int4")
+    a = Answers(m, n_seq=1, n_blocks=4, block=16)
+    text = torch.arange(50, dtype=torch.int32, device=DEV)
+    got = a.add(text[:1], torch.tensor([1], dtype=torch.int32, device=DEV))
+    first = got.clone()
+    again = a.add(text[1:], torch.tensor([49], dtype=torch.int32, device=DEV))
+    assert again.data_ptr() == got.data_ptr() == a.logits.data_ptr() and torch.equal(got, again) and not torch.equal(got, first)
+
+
+@gpu
 def test_a_step_that_only_ends_sequences():
     """No token at all: the blocks go back, the logits are zeros, what goes on goes on; tokens that are not there are refused."""
     m = _model("tiny", "int4")

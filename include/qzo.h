@@ -431,6 +431,8 @@ qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows
  * block, head_dim]; the scales are the same for all layers.  Positions beyond max_seq - 1 count as that one where the
  * model has learned positions.
  * logits_dev: bf16 [n_seq, vocab], of the last new token of every sequence; zeros where it has none.
+ * In joint mode the call writes the model's 16-bit tensors, theta_u unperturbed: it must not overlap with another call of the same model
+ * that perturbs or reads them (forward, step, update, a second answer), whatever the workspaces.
  * workspace_dev: qzo_answer_workspace_bytes bytes, 256-byte aligned, contents undefined before and after; calls that may overlap
  * need one each.  QZO_ERR_SHAPE: vocab not a multiple of 8, max_blocks * block above 2^30, or tokens or sequences too many for 32-bit offsets.
  */

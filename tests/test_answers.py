@@ -139,7 +139,7 @@ def test_logits_are_one_buffer():
     text = torch.arange(50, dtype=torch.int32, device=DEV)
     got = a.add(text[:1], torch.tensor([1], dtype=torch.int32, device=DEV))
     first = got.clone()
-    again = a.add(text[1:], torch.tensor([49], dtype=torch.int32, device=DEV))
+    again = a.add(text[1:].clone(), torch.tensor([49], dtype=torch.int32, device=DEV))
     assert again.data_ptr() == got.data_ptr() == a.logits.data_ptr() and torch.equal(got, again) and not torch.equal(got, first)
 
 

@@ -615,6 +615,8 @@ qzo_status qzo_debug_forward(qzo_model* m, const int32_t* tokens_dev, uint32_t b
  * 3 = scale update, 4 = embedding and the joint mode's kernels, 5 = weight expansion (bytes:
  * packed weights in + bf16 out).  The norm that follows a linear whose slice reduction performs it
  * (up to 512 rows) is part of class 0; other norms and the rotary embedding's launch are in no class.
+ * qzo_answer's launches count as well: class 1 its logits' GEMM, 2 the attention over the cache with a work of 0 (the lengths
+ * are the device's), 4 also the launch that rotates heads and writes them to the cache.
  * Host pointers.  Not thread-safe.
  * qzo_profile_stride(n): from the next qzo_profile_begin on only every n-th launch of each class is
  * bracketed (the first, the n+1-th, ...), which keeps the cost of the events (a few microseconds of

@@ -515,7 +515,6 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
   NextAttention na = {batch, seq, H, dh, nullptr, 0};
   uint32_t layer = 0;
   auto attention = [&](bool rotated) {
-    ProfScope ps(PK_ATTN, attn_flops, st);
     if (ans) {
       const qzo_cache& k = *ans->cache;
       const uint64_t pool = (uint64_t)k.n_blocks * k.block * k.kv_heads * k.head_dim * (k.type ? 1 : 2);
@@ -526,16 +525,21 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
       qa.cache_type = k.type + 1; qa.block_shift = (uint32_t)__builtin_ctz(k.block); qa.n_slots = k.n_blocks * k.block;
       qa.k = (unsigned char*)k.k_dev + layer * pool; qa.v = (unsigned char*)k.v_dev + layer * pool;
       qa.k_scale = k.k_scale_dev; qa.v_scale = k.v_scale_dev; qa.slots = ans->slots;
-      hipError_t e = launch_qk_norm_rope(qa, dh, c.rope_theta, st);
-      if (e != hipSuccess) return e;
+      {
+        ProfScope ps(PK_OTHER, 0, st);
+        hipError_t e = launch_qk_norm_rope(qa, dh, c.rope_theta, st);
+        if (e != hipSuccess) return e;
+      }
       PagedArgs pa = {};
       pa.q = (const bf16_t*)w.qkv; pa.ld_q = 3 * d; pa.out = (bf16_t*)w.att; pa.ld_out = d;
       pa.n_rows = M1; pa.n_seq = ans->n_seq; pa.q_heads = pa.kv_heads = H; pa.group = 1;
       pa.k = qa.k; pa.v = qa.v; pa.k_scale = k.k_scale_dev; pa.v_scale = k.v_scale_dev;
       pa.n_blocks = k.n_blocks; pa.block_shift = qa.block_shift; pa.max_blocks = ans->max_blocks;
       pa.tables = ans->tables; pa.lengths = ans->lengths; pa.starts = ans->starts; pa.scale = 1.0f / std::sqrt((float)dh);
+      ProfScope ps(PK_ATTN, 0, st);               // its work depends on lengths that only the device knows
       return launch_paged_attention(pa, dh, k.type == 1, ans->scratch, st);
     }
+    ProfScope ps(PK_ATTN, attn_flops, st);
     const float* tb = (llama && !rotated) ? w.rope : nullptr;
     if (na.part) return launch_attention(nullptr, batch, seq, H, dh, w.att, tb, st, na.part, na.slices, att_pack, xs_a);
     if (!padded) return launch_attention(w.qkv, batch, seq, H, dh, w.att, tb, st, nullptr, 0, att_pack, xs_a);

@@ -132,6 +132,24 @@ def test_a_step_that_cannot_be_planned_changes_nothing():
 
 
 @gpu
+def test_profile_of_an_answer():
+    """Launches and work by class: the attention's work, which depends on lengths that only the device knows, is 0, its launches are
+    one a layer; rotations count as class 4, beside the embedding."""
+    m = _model("tiny", "int4")
+    sh = m.shape
+    a = Answers(m, n_seq=2, n_blocks=8, block=16)
+    added = torch.tensor([30, 5], dtype=torch.int32, device=DEV)
+    a.rows(35)
+    qb.qzo_profile_begin(100)
+    a.add(torch.arange(35, dtype=torch.int32, device=DEV), added)
+    got = {k: qb.qzo_profile_collect(v) for k, v in qb.PROFILE_KINDS.items()}
+    assert (got["attention"]["launches"], got["attention"]["work"]) == (sh["n_layers"], 0.0) and got["attention"]["total_ms"] > 0
+    assert (got["embed"]["launches"], got["embed"]["work"]) == (1 + sh["n_layers"], 0.0)
+    assert (got["lmhead_ce"]["launches"], got["lmhead_ce"]["work"]) == (1, 2.0 * 2 * sh["vocab"] * sh["d_model"])
+    assert got["w4a16_gemm"]["work"] == 2.0 * 35 * sh["n_layers"] * (4 * sh["d_model"] ** 2 + 3 * sh["d_model"] * sh["d_ffn"])
+
+
+@gpu
 def test_logits_are_one_buffer():
     """What `add` returns is `logits`, also after a longer step; a copy is what outlives the next step."""
     m = _model("tiny", "int4")

@@ -93,6 +93,27 @@ def test_continued_sequences_follow_the_forward(name, fmt, e4m3):
 
 
 @gpu
+@pytest.mark.parametrize("name,fmt,seed", [("tiny", "int4", 3), ("wide_heads", "int4", 3), ("tiny_opt", "int4", 3), ("tiny_opt", "zp", 3), ("tiny", "zp", 4)])
+def test_continued_sequences_within_a_fixed_bar(name, fmt, seed):
+    """Two sequences of well-conditioned models, in parts and token by token: within 2e-2, whatever two right forwards differ by; here they
+    differ by no more than half of that (no sequence's activations nearly cancel), which is looked at, too."""
+    m = _model(name, fmt, seed)
+    rng = torch.Generator().manual_seed(4)
+    texts = [torch.randint(0, m.shape["vocab"], (n,), generator=rng, dtype=torch.int32).to(DEV) for n in (90, 30)]
+    want = [_logits(m, t) for t in texts]
+    assert max(_apart(m, t, w) for t, w in zip(texts, want)) <= 1e-2
+    a, done = Answers(m, n_seq=2, n_blocks=10, block=16), [0, 0]
+    for added in [(70, 3), (1, 25), (17, 0)] + [(1, 1)] * 2:
+        parts = [t[d:d + n] for t, d, n in zip(texts, done, added)]
+        got = a.add(torch.cat(parts), torch.tensor(added, dtype=torch.int32, device=DEV))
+        done = [d + n for d, n in zip(done, added)]
+        for i in range(2):
+            if added[i]:
+                assert _far(got[i], want[i][done[i] - 1]) <= 2e-2, (added, i)
+    assert a.lengths.tolist() == [90, 30]
+
+
+@gpu
 def test_answers_use_the_scales_as_they_are():
     """After an update of the scales the answers are those of the updated model."""
     m = _model("tiny", "int4")

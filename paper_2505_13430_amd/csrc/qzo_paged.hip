@@ -366,6 +366,9 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     // ---- this wavefront's columns
     const uint32_t all_cols = w.rows * a.group, group_col = tile * D::cols(w), n_group = min(D::cols(w), all_cols - group_col);
     const uint32_t first_col = group_col + (TILED || w.wide ? wave * TC : 0u), n_cols = first_col < all_cols && kh < a.kv_heads ? min(TC, all_cols - first_col) : 0u;
+    // Up to half the columns: lanes col and col + 8 have the same one, the first its weights in bf16, the second what their rounding left.
+    const bool twice = CT == 1 && !TILED && n_group <= COLS / 2;
+    const uint32_t own = twice ? col % (COLS / 2) : col;
     bool live[CT];
     // positions that a column sees, that the first (the fewest) and the last (the most) of them see
     int32_t sees[CT];
@@ -377,8 +380,8 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
     bf16x8 q[CT][KS];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      live[ct] = ct * COLS + col < n_cols;
-      const uint32_t flat = live[ct] ? first_col + ct * COLS + col : group_col, token = flat / a.group, head = kh * a.group + flat % a.group;
+      live[ct] = ct * COLS + own < n_cols;
+      const uint32_t flat = live[ct] ? first_col + ct * COLS + own : group_col, token = flat / a.group, head = kh * a.group + flat % a.group;
       sees[ct] = live[ct] ? (int32_t)(w.len + token + 1u - w.rows) : 0;
       const bf16_t* from = a.q + (uint64_t)(w.row0 + token) * a.ld_q + (uint64_t)head * DH;
 #pragma unroll
@@ -502,9 +505,19 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       float e[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], f, -base));
-      // p as bf16, 2^-8 of each term at most; the sum is that of the rounded ones, so that what rounds all weights alike, a key that
-      // takes all, cancels
+      // p as bf16, which the matrix instructions ask for: 2^-8 of each term at most; the sum is that of the rounded ones, so that what
+      // rounds all weights alike, a key that takes all, cancels.  What is left of p goes into the idle half of the columns where there
+      // is one (single tokens, up to eight heads a key head): 2^-16, at no cost (8 x 65536 tokens 362 us, 64 ragged 150, either way).
+      // Otherwise it would take a second product for every value: 6 x 100 tokens behind 1900 112 / 126 us, 16 prompts of 512 116 /
+      // 136, one of 4000 317 / 379, 6 x 100 with heads of 64 49 / 50; those keep the one rounding, as the whole-sequence kernel does.
       u32x4v pk = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
+      if (twice) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t rest = pack_bf16x2(e[2 * j] - __uint_as_float(pk[j] << 16), e[2 * j + 1] - __uint_as_float(pk[j] & 0xffff0000u));
+          pk[j] = col < COLS / 2 ? pk[j] : rest;
+        }
+      }
       if (some_unseen) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) pk[j >> 1] |= s[j >> 2][j & 3] * f == -INFINITY ? UNSEEN << 16 * (j & 1) : 0u;
@@ -771,6 +784,16 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
         }
         continue;
       }
+    }
+
+    if (twice) {
+      auto both = [](float x) { return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x128, 0xf, 0xf, false)); };      // row_ror:8
+#pragma unroll
+      for (int i = 0; i < VW; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[0][i][j] = both(acc[0][i][j]);
+      if constexpr (!TILED) l[0] = both(l[0]);
+      live[0] = col < n_cols;
     }
 
     // ---- the four wavefronts' sums together

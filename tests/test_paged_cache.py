@@ -455,6 +455,26 @@ def test_attention_of_single_tokens(lengths, H, Hk, dh, block, e4m3):
 
 @gpu
 @pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lengths,news,H,Hk,dh", [
+    ([40, 25, 60], None, 16, 2, 128), ([40, 25, 60], None, 3, 3, 64), ([20 + i % 40 for i in range(200)], None, 8, 8, 128), ([40, 30], [4, 2], 6, 3, 64),
+    ([300], None, 5, 1, 128)])
+def test_weights_of_few_columns_in_two_parts(lengths, news, H, Hk, dh, e4m3):
+    """Up to eight columns a sequence and key head (heads that share it, times new tokens): the weights lose nothing that the output's own
+    rounding, half a step of its binade, does not hide.  Before it, for n keys: a weight is two bf16 numbers, the second what the first's
+    rounding left, 2^-8 2^-8 of it at most missing, above and below the fraction; its exponential 2^-22; n + 64 sums and products of
+    2^-24; scores as everywhere."""
+    d = _attend(lengths, H, Hk, dh, 16, news, e4m3=e4m3, seed=H, spread=0.5)
+    k, v = (p.double() if s is None else p.double() * s.double()[:, None, None] for p, s in zip(d["pools"], d["scales"]))
+    q = d["q"].double().view(-1, H, dh)
+    want, mag, mac = attention_reference(q, k, v, d["tables"], lengths, d["starts"], d["scale"])
+    before = ((2.0 ** -16 + 2.0 ** -22 + (max(lengths) + 64) * 2.0 ** -24) * (mag + want.abs()) + 2 * (dh + 4) * 2.0 ** -24 * mac[..., None] * mag) * 1.01
+    half = torch.exp2(torch.floor(torch.log2((want.abs() + before).clamp(min=1e-30))) - 8)
+    err = (d["outd"].double().cpu().view(want.shape) - want).abs()
+    assert bool((err <= half + before).all()), float((err / (half + before)).max())
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
 @pytest.mark.parametrize("lengths,news,H,Hk,dh,block", [
     ([5], [5], 2, 2, 128, 16), ([40, 40, 7], [40, 1, 7], 4, 2, 64, 16), ([200, 64, 33], [17, 0, 33], 6, 2, 128, 32), ([20, 0, 130], [3, 0, 129], 16, 1, 64, 16),
     ([3, 5], [6, 2], 4, 4, 64, 16), ([90, 600, 31], [2, 3, 31], 40, 2, 128, 64), ([260], [256], 2, 1, 64, 256)])

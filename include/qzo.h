@@ -406,9 +406,9 @@ qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tok
  * starts[i] .. starts[i+1] - 1 are the newest tokens of sequence i, in order (starts[0] = 0, ascending); null: row i is
  * the one new token of sequence i.  A row sees the positions of its sequence up to its own:
  *   out[row, h] = sum_k p_k v_k / sum_k p_k,  p_k = exp(scale * q . k - max),  out_dev bf16, rows ld_out elements apart.
- * One pass over the cache with the running maximum and sum (fp32).  In calls of single tokens with up to eight query heads a key
- * head p meets v as two bf16 numbers, 2^-16 of it at most missing; with more columns (new tokens times those heads) it may be
- * rounded to one, 2^-8; the sum is that of what meets v.  The sequences are cut into pieces that fill the chip and joined in
+ * One pass over the cache with the running maximum and sum (fp32).  p meets v as two bf16 numbers, 2^-16 of it at most missing; but
+ * for prompts, and for heads of 128 with more than eight columns (new tokens of a sequence times the query heads of a key
+ * head), it is rounded to one, 2^-8.  The sum is that of what meets v.  The sequences are cut into pieces that fill the chip and joined in
  * order: the same call gives the same bits.  A row that sees nothing (length 0) is set to zero; rows behind the last sequence's and not named by starts stay as they are.  Keys that a row does not see
  * reach its output in no way, NaN and infinities among them; nor do positions whose block id lies outside the pool (they
  * count as unseen), or positions beyond max_blocks * block.  A score of -infinity counts as unseen.

@@ -203,6 +203,8 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
   typedef Dealing<CT, TILED> D;
   constexpr uint32_t TC = D::TC, STRIDE = DH + 4, ROW = DH * ES;
   typedef PagedStep<DH, E4M3> Step;
+  constexpr int PARTS = DH == 64 && !TILED ? 2 : 1;      // operands of bf16 that may hold a column's weights
+  struct Weights { bf16x8 part[PARTS]; };
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   float* const sum_acc = (float*)lds;                                   // [WAVES][TC][STRIDE]; TILED: where the tiles were
   float* const sum_m = sum_acc + WAVES * TC * STRIDE;                   // [WAVES][TC]
@@ -508,8 +510,10 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       // p as bf16, which the matrix instructions ask for: 2^-8 of each term at most; the sum is that of the rounded ones, so that what
       // rounds all weights alike, a key that takes all, cancels.  What is left of p goes into the idle half of the columns where there
       // is one (single tokens, up to eight heads a key head): 2^-16, at no cost (8 x 65536 tokens 362 us, 64 ragged 150, either way).
-      // Otherwise it would take a second product for every value: 6 x 100 tokens behind 1900 112 / 126 us, 16 prompts of 512 116 /
-      // 136, one of 4000 317 / 379, 6 x 100 with heads of 64 49 / 50; those keep the one rounding, as the whole-sequence kernel does.
+      // Otherwise it takes a second product for every value, which heads of 64 have the registers for (6 x 100 tokens 49 / 51 us, 20 x 30
+      // behind 970 40.0 / 40.3).  Heads of 128 have not (4 x 8 tokens, 64 heads on 8, behind 9000 56 / 60, but single tokens, the same code,
+      // lose their loads ahead: 64 ragged 152 / 181), and prompts are bound by such instructions (16 of 512 116 / 136, one of 4000
+      // 317 / 379): those keep the one rounding, as the whole-sequence kernel does.
       u32x4v pk = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
       if (twice) {
 #pragma unroll
@@ -527,11 +531,19 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
         l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, pk), l[ct], 0, 0, 0);
       } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) l[ct] += __uint_as_float(pk[j] << 16) + __uint_as_float(pk[j] & 0xffff0000u);
+        for (int j = 0; j < 4; ++j) l[ct] += PARTS > 1 && !twice ? e[2 * j] + e[2 * j + 1] : __uint_as_float(pk[j] << 16) + __uint_as_float(pk[j] & 0xffff0000u);
       }
-      return __builtin_bit_cast(bf16x8, pk);
+      Weights p;
+      p.part[0] = __builtin_bit_cast(bf16x8, pk);
+      if constexpr (PARTS > 1) {
+        u32x4v rest;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rest[j] = pack_bf16x2(e[2 * j] - __uint_as_float(pk[j] << 16), e[2 * j + 1] - __uint_as_float(pk[j] & 0xffff0000u));
+        p.part[1] = __builtin_bit_cast(bf16x8, rest);
+      }
+      return p;
     };
-    auto values = [&](Step& st, const bf16x8 (&pk)[CT], int32_t kb, uint32_t there, bool look) {
+    auto values = [&](Step& st, const Weights (&pk)[CT], int32_t kb, uint32_t there, bool look) {
       bool apart = false;
       if (look || !whole_step(kb, there)) {
         // nobody's positions, which may hold anything, become 0; where what is left is not finite, every column has its own product
@@ -565,8 +577,12 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
           const bf16x8 even = operand(y, 0x05040100u), uneven = operand(y, 0x07060302u);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            acc[ct][2 * u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pk[ct], acc[ct][2 * u], 0, 0, 0);
-            acc[ct][2 * u + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uneven, pk[ct], acc[ct][2 * u + 1], 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) {
+              if (x && twice) break;
+              acc[ct][2 * u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pk[ct].part[x], acc[ct][2 * u], 0, 0, 0);
+              acc[ct][2 * u + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uneven, pk[ct].part[x], acc[ct][2 * u + 1], 0, 0, 0);
+            }
           }
         }
       } else {
@@ -575,11 +591,16 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
           uint32_t y[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const uint32_t p = (uint32_t)__shfl((int)__builtin_bit_cast(u32x4v, pk[ct])[j >> 1], (int)((lane & 48u) | c), 64);
+            const uint32_t p = (uint32_t)__shfl((int)__builtin_bit_cast(u32x4v, pk[ct].part[0])[j >> 1], (int)((lane & 48u) | c), 64);
             y[j] = (p >> 16 * (j & 1) & 0xffffu) == UNSEEN ? 0u : value(j, u);
           }
-          const f32x4 even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x05040100u), pk[ct], acc[ct][2 * u], 0, 0, 0);
-          const f32x4 uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x07060302u), pk[ct], acc[ct][2 * u + 1], 0, 0, 0);
+          f32x4 even = acc[ct][2 * u], uneven = acc[ct][2 * u + 1];
+#pragma unroll
+          for (int x = 0; x < PARTS; ++x) {
+            if (x && twice) break;
+            even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x05040100u), pk[ct].part[x], even, 0, 0, 0);
+            uneven = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(y, 0x07060302u), pk[ct].part[x], uneven, 0, 0, 0);
+          }
           if (col == c) { acc[ct][2 * u] = even; acc[ct][2 * u + 1] = uneven; }
         };
 #pragma unroll
@@ -601,7 +622,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
 
     auto work = [&](Step& st, int32_t kb, uint32_t there) {
       f32x4 s[CT][2];
-      bf16x8 pk[CT];
+      Weights pk[CT];
       bool look = false;
       scores(st, s);
 #pragma unroll
@@ -686,7 +707,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
             if (kb + 32 * part >= k_end) break;
             Step st;
             f32x4 s[CT][2];
-            bf16x8 pk[CT];
+            Weights pk[CT];
             bool look = careful;
             const int32_t k32 = kb + 32 * part;
             const uint32_t there32 = there >> (2 * part) & 3u;

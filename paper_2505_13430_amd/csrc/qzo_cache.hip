@@ -205,7 +205,7 @@ hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t st) {
 // 16384 / 24576 / 32768 / 65536: 44 / 37 / 35 / 34 / 34 / 40 us).  The cosine and sine of a pair are computed once per
 // wavefront, by one lane, and handed out through the LDS (each lane its own eight: 41 us).  One token 2.5 us; 16 x 512 tokens,
 // q and k of 32 heads of 128: 53 us, 5.0 TB/s read and written, as a copy of 2 GiB (4.9); with an e4m3 cache, 7001 tokens, 64
-// and 8 heads of 64, 32 us, 4.3 TB/s.
+// and 8 heads of 64, 30 us, 4.6 TB/s.
 
 // Values of the lanes of a head (16, or 8): their sum; that of the lane half a head away.  Exchanges within rows of 16 lanes.
 template <int CTRL>

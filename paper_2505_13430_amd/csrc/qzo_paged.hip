@@ -15,9 +15,9 @@
 //
 // What bounds it: memory.  A step of a wavefront loads its next 32 keys (16 KB at heads of 128, bf16) before it works on the
 // ones it has; eight wavefronts on a compute unit keep 128 to 256 KB on the way.  Loads and block ids are issued without a branch
-// around them, or the compiler waits for all of them at every use.  8 sequences of 65536 tokens, 8 key heads of 128: 370 us,
-// 5.8 TB/s (a kernel that only reads: 6.1 to 6.3); 64 ragged ones of up to 4001, 32 key heads, 150 us, 5.4 TB/s; 24 in e4m3 of up
-// to 32001, 86 us, 4.9 TB/s, 75 of them the cache at the rate of the first.  Few keys: latency.  One token 5.4 us (launch, lengths,
+// around them, or the compiler waits for all of them at every use.  8 sequences of 65536 tokens, 8 key heads of 128: 361 us,
+// 5.9 TB/s (a kernel that only reads: 6.1 to 6.3); 64 ragged ones of up to 4001, 32 key heads, 150 to 156 us, 5.2 to 5.4 TB/s; 24 in
+// e4m3 of up to 32001, 85 us, 4.9 TB/s (67 us at the reading kernel's rate).  Few keys: latency.  One token 7 us (launch, lengths,
 // table, keys, one after the other); a compute unit alone takes 54 GB/s, 1.2 us a unit.
 #include <algorithm>
 #include <type_traits>
@@ -47,14 +47,15 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 //   Prompts (TILED): every group has 128 columns, 32 a wavefront, and the keys and values pass through the LDS, fetched once for the four
 // and three steps ahead (32 keys a step where a row has 256 bytes, otherwise 64; rings of 64 KB, two workgroups a compute unit); a
 // unit is 64 keys, a group ends with what its last column sees, and what is not cut goes to memory from the accumulators.  Without /
-// so, us, heads of 128: 16 prompts of 512 tokens, 32 heads, 209 / 119, one of 2048 290 / 150, one of 4000 with 32 heads on 8 846 / 317 (410
-// TFLOP/s), 4 x 200 tokens behind 3800, 40 heads on 8 in e4m3 179 / 158, 6 x 100 behind 1900 142 / 120, 4 of 130 (130 groups) 26 / 16,
+// so, us, heads of 128: 16 prompts of 512 tokens, 32 heads, 201 / 116, one of 2048 292 / 145, one of 4000 with 32 heads on 8 848 / 298 (440
+// TFLOP/s), 4 x 200 tokens behind 3800, 40 heads on 8 in e4m3 181 / 145, 6 x 100 behind 1900 136 / 110, 4 of 130 (130 groups) 28 / 16,
 // but one of 512 (128 groups) 31 / 32: from more groups than half the compute units on.  Heads of 64: one of 2048 (512 groups)
-// 104 / 86, the prompts 75 / 65, but 4 x 200 (250) 80 / 97, 6 x 100 (150) 63 / 66: from as many groups as workgroups on.  Fewer columns leave
+// 106 / 87, the prompts 76 / 61, but 4 x 200 (250) 80 / 97, 6 x 100 (150) 63 / 66: from as many groups as workgroups on.  Fewer columns leave
 // lanes idle: 4 x 8 tokens, 64 heads on 8, behind 9000 (64 columns) 64 / 86, 20 x 40 behind 960 121 / 123: from TILED_COLS a sequence on.
-// What bounds it: two wavefronts a SIMD, each a chain of LDS reads, products and exponentials (one of 4000: vector instructions 40 % of
-// the time, matrix instructions 17 %; neither fewer vector instructions nor more steps ahead nor LDS reads without conflicts made it
-// faster).  Heads of 128 have no registers left; what the compiler keeps in scratch memory is some 150 MB written in that call.
+// What bounds it: two wavefronts a SIMD, each a chain of LDS reads, products and exponentials (one of 4000: vector instructions 36 % of
+// the time, matrix instructions 18 %; more steps ahead and LDS reads without conflicts did not make it faster, 16 % fewer vector
+// instructions made it 6 % faster).  Heads of 128 have no registers left; what the compiler keeps in scratch memory is some
+// 150 MB written in that call.
 //   With more groups than workgroups, a sequence of up to QUAD_LEN positions and one wavefront's columns gives a workgroup four key heads at a time, one a
 // wavefront (a unit is 32 keys of each): no other wavefront waits for a step that there is not, a workgroup starts a quarter
 // as often, and nothing is added up in the end.  Such groups are not cut.  256 sequences, 32 heads of 128, of 1 / 20 / 64 /

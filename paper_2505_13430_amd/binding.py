@@ -559,19 +559,19 @@ _stream_scratch = {}
 
 
 def _scratch_of_stream(device, stream, handle, nbytes):
-    """Scratch of the calls on one stream, which do not overlap.  A captured graph keeps the address it was captured with and may
+    """Address and bytes of the scratch of the calls on one stream, which do not overlap.  A captured graph keeps the address it was captured with and may
     be replayed on any stream beside any other: it is given scratch of its own."""
     captured = torch.cuda.is_current_stream_capturing()
     if stream is not None:                     # a stream may be captured without being the current one
         with torch.cuda.stream(stream):
             captured = captured or torch.cuda.is_current_stream_capturing()
     assert not captured, "a captured call needs scratch of its own: pass scratch"
-    t = _stream_scratch.get((device, handle))
-    if t is None or t.numel() < nbytes:
+    kept = _stream_scratch.get((device, handle))
+    if kept is None or kept[1] < nbytes:
         with torch.cuda.stream(stream):        # what is outgrown is used again on this stream only
             t = torch.zeros(nbytes, dtype=torch.uint8, device=device)
-        _stream_scratch[device, handle] = t
-    return t
+        kept = _stream_scratch[device, handle] = t.data_ptr(), nbytes, t
+    return kept[:2]
 
 
 def qzo_paged_attention(q, cache, tables, lengths, out, scale, starts=None, scratch="auto", stream=None):
@@ -588,9 +588,11 @@ def qzo_paged_attention(q, cache, tables, lengths, out, scale, starts=None, scra
         return
     st = _stream_of(stream, at)
     if isinstance(scratch, str):
-        scratch = _scratch_of_stream(at, stream, st, qzo_paged_attention_scratch_bytes(rows, n, heads, dh))
+        room = _scratch_of_stream(at, stream, st, qzo_paged_attention_scratch_bytes(rows, n, heads, dh))
+    else:
+        room = _room(scratch, at)
     _check(lib().qzo_paged_attention(x, ldx, rows, n, heads, C.addressof(cache), _at(tables, i32, at), most, _at(lengths, i32, at),
-                                     _at(starts, i32, at), scale, y, ldy, *_room(scratch, at), st))
+                                     _at(starts, i32, at), scale, y, ldy, *room, st))
 
 
 def qzo_answer_workspace_bytes(model, n_tokens, n_seq) -> int:

@@ -407,8 +407,8 @@ qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tok
  * the one new token of sequence i.  A row sees the positions of its sequence up to its own:
  *   out[row, h] = sum_k p_k v_k / sum_k p_k,  p_k = exp(scale * q . k - max),  out_dev bf16, rows ld_out elements apart.
  * One pass over the cache with the running maximum and sum (fp32).  p meets v as two bf16 numbers, 2^-16 of it at most missing; but
- * for prompts, and for heads of 128 with more than eight columns (new tokens of a sequence times the query heads of a key
- * head), it is rounded to one, 2^-8.  The sum is that of what meets v.  The sequences are cut into pieces that fill the chip and joined in
+ * for prompts, and for heads of 128 or an e4m3 cache with more than eight columns (new tokens of a sequence times the query
+ * heads of a key head), it is rounded to one, 2^-8.  The sum is that of what meets v.  The sequences are cut into pieces that fill the chip and joined in
  * order: the same call gives the same bits.  A row that sees nothing (length 0) is set to zero; rows behind the last sequence's and not named by starts stay as they are.  Keys that a row does not see
  * reach its output in no way, NaN and infinities among them; nor do positions whose block id lies outside the pool (they
  * count as unseen), or positions beyond max_blocks * block.  A score of -infinity counts as unseen.

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
   typedef Dealing<CT, TILED> D;
   constexpr uint32_t TC = D::TC, STRIDE = DH + 4, ROW = DH * ES;
   typedef PagedStep<DH, E4M3> Step;
-  constexpr int PARTS = DH == 64 && !TILED ? 2 : 1;      // operands of bf16 that may hold a column's weights
+  constexpr int PARTS = DH == 64 && !E4M3 && !TILED ? 2 : 1;      // operands of bf16 that may hold a column's weights
   struct Weights { bf16x8 part[PARTS]; };
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   float* const sum_acc = (float*)lds;                                   // [WAVES][TC][STRIDE]; TILED: where the tiles were
@@ -511,10 +511,11 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(Pag
       // p as bf16, which the matrix instructions ask for: 2^-8 of each term at most; the sum is that of the rounded ones, so that what
       // rounds all weights alike, a key that takes all, cancels.  What is left of p goes into the idle half of the columns where there
       // is one (single tokens, up to eight heads a key head): 2^-16, at no cost (8 x 65536 tokens 362 us, 64 ragged 150, either way).
-      // Otherwise it takes a second product for every value, which heads of 64 have the registers for (6 x 100 tokens 49 / 51 us, 20 x 30
-      // behind 970 40.0 / 40.3).  Heads of 128 have not (4 x 8 tokens, 64 heads on 8, behind 9000 56 / 60, but single tokens, the same code,
-      // lose their loads ahead: 64 ragged 152 / 181), and prompts are bound by such instructions (16 of 512 116 / 136, one of 4000
-      // 317 / 379): those keep the one rounding, as the whole-sequence kernel does.
+      // Otherwise it takes a second product for every value, which heads of 64 have the registers for (bf16: 6 x 100 tokens 49 / 51 us,
+      // behind 1900 60 / 61, 20 x 30 behind 970 40.0 / 40.3; e4m3, whose values have been rounded by up to 2^-4, 4 x 200 behind 3800 79 /
+      // 91: once).  Heads of 128 have not (4 x 8 tokens, 64 heads on 8, behind 9000 56 / 60, but single tokens, the same code, lose
+      // their loads ahead: 64 ragged 152 / 181), and prompts are bound by such instructions (16 of 512 116 / 136, one of 4000 317 /
+      // 379): those keep the one rounding, as the whole-sequence kernel does.
       u32x4v pk = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
       if (twice) {
 #pragma unroll

@@ -453,13 +453,15 @@ def test_attention_of_single_tokens(lengths, H, Hk, dh, block, e4m3):
     _check_attend(_attend(lengths, H, Hk, dh, block, e4m3=e4m3, seed=len(lengths) + H))
 
 
+FEW_COLUMNS = [([40, 25, 60], None, 16, 2, 128), ([40, 25, 60], None, 3, 3, 64), ([20 + i % 40 for i in range(200)], None, 8, 8, 128),
+               ([40, 30], [4, 2], 6, 3, 64), ([300], None, 5, 1, 128)]
+
+
 @gpu
-@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
-@pytest.mark.parametrize("lengths,news,H,Hk,dh", [
-    ([40, 25, 60], None, 16, 2, 128), ([40, 25, 60], None, 3, 3, 64), ([20 + i % 40 for i in range(200)], None, 8, 8, 128), ([40, 30], [4, 2], 6, 3, 64),
-    ([300], None, 5, 1, 128), ([40, 30], None, 24, 2, 64), ([60, 40], [60, 12], 4, 2, 64)])
+@pytest.mark.parametrize("lengths,news,H,Hk,dh,e4m3", [(*x, e4m3) for x in FEW_COLUMNS for e4m3 in (False, True)] + [
+    ([40, 30], None, 24, 2, 64, False), ([60, 40], [60, 12], 4, 2, 64, False)])
 def test_weights_of_few_columns_in_two_parts(lengths, news, H, Hk, dh, e4m3):
-    """Up to eight columns a sequence and key head (heads that share it, times new tokens), with heads of 64 more, too: the weights lose nothing that the output's own
+    """Up to eight columns a sequence and key head (heads that share it, times new tokens), with heads of 64 in bf16 more, too: the weights lose nothing that the output's own
     rounding, half a step of its binade, does not hide.  Before it, for n keys: a weight is two bf16 numbers, the second what the first's
     rounding left, 2^-8 2^-8 of it at most missing, above and below the fraction; its exponential 2^-22; n + 64 sums and products of
     2^-24; scores as everywhere."""

@@ -50,8 +50,9 @@ typedef const int32_t __attribute__((address_space(4)))* table_t;      // read b
 // so, us, heads of 128: 16 prompts of 512 tokens, 32 heads, 201 / 116, one of 2048 292 / 145, one of 4000 with 32 heads on 8 848 / 298 (440
 // TFLOP/s), 4 x 200 tokens behind 3800, 40 heads on 8 in e4m3 181 / 145, 6 x 100 behind 1900 136 / 110, 4 of 130 (130 groups) 28 / 16,
 // but one of 512 (128 groups) 31 / 32: from more groups than half the compute units on.  Heads of 64: one of 2048 (512 groups)
-// 106 / 87, the prompts 76 / 61, but 4 x 200 (250) 80 / 97, 6 x 100 (150) 63 / 66: from as many groups as workgroups on.  Fewer columns leave
-// lanes idle: 4 x 8 tokens, 64 heads on 8, behind 9000 (64 columns) 64 / 86, 20 x 40 behind 960 121 / 123: from TILED_COLS a sequence on.
+// 106 / 87, the prompts 76 / 61, but 4 x 200 in e4m3 (250) 89 / 96: from as many groups as workgroups on (6 x 100 behind 1900, 150 groups,
+// 61 / 58, 9 x 100, 225, 65 / 63, 14 x 100, 350, 96 / 73: in bf16 from fewer on by now).  Fewer columns leave lanes idle: 4 x 8 tokens, 64
+// heads on 8, behind 9000 (64 columns) 64 / 86, 20 x 40 behind 960 121 / 123: from TILED_COLS a sequence on.
 // What bounds it: two wavefronts a SIMD, each a chain of LDS reads, products and exponentials (one of 4000: vector instructions 36 % of
 // the time, matrix instructions 18 %; more steps ahead and LDS reads without conflicts did not make it faster, 16 % fewer vector
 // instructions made it 6 % faster).  Heads of 128 have no registers left; what the compiler keeps in scratch memory is some

@@ -1,0 +1,623 @@
+"""Operators behind sequences that fork: beam search, and several continuations or candidates behind one prompt, over the paged
+cache of keys and values.
+
+Kinds of call:
+  select   the next beams of every prompt out of all its beams' logits, the beams' states reordered with them: qzo_beam_select
+  fork     block tables, lengths and free list when every sequence goes on from one of the old ones (full blocks shared, open
+           ones copied, what nobody holds any more freed), and how far each group's tables agree: qzo_cache_fork
+  compact  the blocks that are held moved to the front of the pool: qzo_cache_compact
+  copy     the blocks that a fork or a compaction moves, in the pools of all layers: qzo_cache_copy
+  attend   attention of the newest tokens over the cache where groups of sequences begin alike, that part of the cache read
+           once for the group: qzo_paged_attention_shared
+
+A case is a dict of plain values; `prepare` makes what such a program holds before the call, `run` is one call, `work`
+the bytes and operations that it cannot do without, `exact` the result from the definition in 64 bits.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+DEV = "cuda:0"
+
+
+def listed():
+    return [
+        # one prompt, four beams, the 7B shape's vocabulary: nothing but latency
+        dict(name="select_1x4", kind="select", groups=1, width=4, vocab=32000, history=64, ended=0, penalty=0.0, end=2),
+        # a batch of prompts, an odd vocabulary, some beams have ended, scores divided by the length
+        dict(name="select_96x5", kind="select", groups=96, width=5, vocab=99991, history=300, ended=40, penalty=0.7, end=1),
+        # one prompt's eight beams behind a few thousand tokens
+        dict(name="fork_1x8", kind="fork", groups=1, width=8, short=2500, long=2500, own=70, replaced=4, dead=0, block=16),
+        # many prompts' beams
+        dict(name="fork_128x6", kind="fork", groups=128, width=6, short=30, long=7900, own=200, replaced=2, dead=9, block=32),
+        # a small pool after an evaluation
+        dict(name="compact_1400_blocks", kind="compact", n_seq=30, short=1, long=2000, blocks=1400, block=32),
+        # a pool of many small blocks, half of them held
+        dict(name="compact_150001_blocks", kind="compact", n_seq=500, short=10, long=8000, blocks=150001, block=16),
+        # open blocks of three of four beams, 32 layers of the 7B shape
+        dict(name="copy_3_open_blocks", kind="copy", copies=3, room=4, layers=32, kv_heads=32, dh=128, block=16, blocks=48, cache="bf16", whole=False),
+        # whole blocks of a pool that is made smaller, in 8 bits, shared key heads
+        dict(name="copy_e4m3_700_blocks", kind="copy", copies=700, room=1000, layers=8, kv_heads=8, dh=128, block=64, blocks=1500, cache="e4m3", whole=True),
+        # four beams behind a prompt of the 7B shape's longest
+        dict(name="attend_1x4", kind="attend", groups=1, width=4, short=496, long=496, own=16, ended=0, new=1, q_heads=32, kv_heads=32, dh=128,
+             cache="bf16", block=16),
+        # prompts of all lengths, up to eight beams each, some of which have ended
+        dict(name="attend_16x8_ragged", kind="attend", groups=16, width=8, short=60, long=3501, own=150, ended=5, new=1, q_heads=32, kv_heads=32, dh=128,
+             cache="bf16", block=32),
+        # a batch behind one long text, shared key heads
+        dict(name="attend_64_behind_32768", kind="attend", groups=1, width=64, short=32768, long=32768, own=500, ended=0, new=1, q_heads=64, kv_heads=8,
+             dh=128, cache="bf16", block=64),
+        # candidates of several tokens each behind their prompts, in 8 bits, heads of 64
+        dict(name="attend_e4m3_12_candidates", kind="attend", groups=6, width=12, short=200, long=4097, own=19, ended=0, new=9, q_heads=40, kv_heads=8,
+             dh=64, cache="e4m3", block=16),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case of the same ranges."""
+    kind = rng.choice(["select", "select", "fork", "compact", "copy", "attend", "attend", "attend"])
+    block = rng.choice([16, 32, 64, 128])
+    if kind == "select":
+        vocab = _log_int(rng, 500, 150000)
+        width = _log_int(rng, 1, 32)
+        groups = max(1, min(_log_int(rng, 1, 256), 480 * 99991 // (vocab * width)))
+        return dict(kind=kind, groups=groups, width=width, vocab=vocab, history=rng.choice([1, 40, 300]), ended=rng.choice([0, groups * width // 7]),
+                    penalty=rng.choice([0.0, 0.0, 0.6, 1.0]), end=rng.randrange(vocab))
+    if kind == "fork":
+        width = _log_int(rng, 1, 32)
+        groups = max(1, min(_log_int(rng, 1, 200), 768 // width))
+        long = _log_int(rng, 1, 7900)
+        return dict(kind=kind, groups=groups, width=width, short=max(0, int(long * rng.choice([1.0, 0.2, 0.01]))), long=long, own=rng.choice([0, 1, 33, 200]),
+                    replaced=rng.randrange(width), dead=rng.choice([0, groups * width // 9]), block=block)
+    if kind == "compact":
+        n_seq, long = _log_int(rng, 1, 1000), _log_int(rng, 1, 8000)
+        used = n_seq * -(-long // block)
+        return dict(kind=kind, n_seq=n_seq, short=0, long=long, blocks=min(max(used + 1, int(used * rng.choice([1.01, 1.5, 4.0]))), 600000), block=block) \
+            if used < 150000 else dict(kind=kind, n_seq=40, short=0, long=long, blocks=40 * -(-long // block) + 37, block=block)
+    cache = rng.choice(["bf16", "bf16", "e4m3"])
+    dh = rng.choice([64, 128, 128])
+    if kind == "copy":
+        kv_heads, layers = rng.choice([1, 4, 8, 32, 40]), _log_int(rng, 1, 40)
+        size = layers * kv_heads * dh * block * (1 if cache == "e4m3" else 2) * 2
+        most = max(2, 1500 * 8 * 2 * 8 * 128 * 64 // size)
+        copies = min(_log_int(rng, 1, 700), most // 2)
+        return dict(kind=kind, copies=copies, room=copies + rng.choice([0, 1, 300]), layers=layers, kv_heads=kv_heads, dh=dh, block=block,
+                    blocks=2 * copies + rng.randrange(3), cache=cache, whole=rng.random() < 0.4)
+    kv_heads = rng.choice([1, 2, 4, 8, 8, 16, 32, 40])
+    group = rng.choice([1, 1, 2, 3, 4, 5, 8, 16])
+    while kv_heads * group > 64:
+        group //= 2
+    width = _log_int(rng, 1, 64)
+    groups = max(1, min(_log_int(rng, 1, 32), 128 // width))
+    own = rng.choice([1, 20, 150, 500])
+    new = rng.choice([1, 1, 1, 1, _log_int(rng, 2, 40)])
+    own = max(own, new)
+    heads = kv_heads * group
+    # at most some 2^28 scores and 2^29 values in the prompts of all groups
+    most = min((1 << 28) // (groups * width * new * heads), (1 << 28) // (groups * kv_heads * dh))
+    long = max(0, min(_log_int(rng, 1, 32768), most))
+    while groups * width * own * max(kv_heads * dh, heads * new) > 1 << 28 and own > new:
+        own = max(new, own // 2)
+    return dict(kind=kind, groups=groups, width=width, short=int(long * rng.choice([1.0, 0.3, 0.02])), long=long, own=own, ended=rng.choice([0, width // 3]), new=new,
+                q_heads=heads, kv_heads=kv_heads, dh=dh, cache=cache, block=block)
+
+
+def _spread(n, lo, hi):
+    """n lengths spread over [lo, hi] by their logarithm."""
+    got = [int(round((lo + 1) * ((hi + 1) / (lo + 1)) ** (i / max(1, n - 1)))) - 1 for i in range(n)]
+    got[-1] = hi
+    return got
+
+
+def _blocks(tokens, block):
+    return -(-tokens // block)
+
+
+# ------------------------------------------------------------------ the next beams ----
+def _prepare_select(case, gen):
+    G, W, V, H = case["groups"], case["width"], case["vocab"], case["history"]
+    rows = G * W
+    # a language model's logits: most tokens far below the few that it considers
+    logits = (torch.randn(rows, V, generator=gen, device=DEV) * 2.2).to(torch.bfloat16)
+    st = dict(logits=logits, width=W, end=case["end"], penalty=case["penalty"])
+    counts = torch.randint(0, H + 1, (G, 1), generator=gen, device=DEV).expand(G, W).reshape(-1).to(torch.int32).contiguous()
+    st["scores"] = (-2.0 * counts.float() - 4.0 * torch.rand(rows, generator=gen, device=DEV) - 1.0).contiguous()
+    st["ended"] = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    if case["ended"]:
+        at = torch.randperm(rows, generator=gen, device=DEV)[:case["ended"]]
+        st["ended"][at] = 1
+        st["scores"][at] -= 6.0                    # they were good enough to be here, and get no worse
+    st["counts"] = counts
+    st["history"] = torch.randint(0, V, (rows, H), generator=gen, device=DEV, dtype=torch.int32)
+    for name in ("parents", "chosen", "tokens", "added"):
+        st[name] = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    return st
+
+
+_SELECTED = ("scores", "counts", "ended", "history", "parents", "chosen", "tokens", "added")
+
+
+def _run_select(st):
+    x, W, end, alpha = st["logits"], st["width"], st["end"], st["penalty"]
+    rows, V = x.shape
+    G = rows // W
+    # candidates of two beams may be close to one another: in 64 bits
+    x = x.double()
+    x = torch.where(x.isfinite(), x, -math.inf)
+    top = x.amax(1, keepdim=True).clamp(min=-1e300)
+    lse = (x - top).exp().sum(1, keepdim=True).log() + top
+    score, ended = st["scores"].double(), st["ended"] != 0
+    total = torch.where(x > -math.inf, x - lse + score[:, None], -math.inf)
+    # a beam that has ended goes on as it is
+    stays = ended[:, None] & (torch.arange(V, device=DEV) == max(end, 0))
+    total = torch.where(ended[:, None], torch.where(stays, score[:, None], -math.inf), total)
+    total = torch.where(score[:, None] > -math.inf, total, -math.inf)
+    counts = st["counts"].clamp(min=0)
+    after = torch.where(ended, counts, counts + 1)
+    key = total.clone() if alpha == 0.0 else total / after.clamp(min=1).double()[:, None] ** alpha
+    key, total = key.view(G, W * V), total.view(G, W * V)
+    at = torch.arange(W * V, device=DEV)
+    picks = []
+    for _ in range(W):
+        best = key.amax(1, keepdim=True)
+        pick = torch.where(key == best, at, W * V).amin(1, keepdim=True)       # ties: the lowest
+        picks.append(torch.where(best > -math.inf, pick, -1))
+        key.scatter_(1, pick, -math.inf)
+    pick = torch.cat(picks, 1)                                                # [G, W]
+    some = (pick >= 0).view(-1)
+    pick = pick.clamp(min=0)
+    parent = (pick // V + torch.arange(G, device=DEV)[:, None] * W).view(-1)
+    token = (pick % V).view(-1)
+    old = ended[parent]
+    counts_old = counts[parent].long()
+    H = st["history"].shape[1]
+    column = torch.arange(H, device=DEV)
+    history = torch.where(some[:, None] & (column < counts_old[:, None]), st["history"][parent], st["history"])
+    history = torch.where((some & ~old)[:, None] & (column == counts_old[:, None]), token[:, None].to(torch.int32), history)
+    st["history"].copy_(history)
+    st["scores"].copy_(torch.where(some, total.gather(1, pick).view(-1), -math.inf))
+    st["counts"].copy_(torch.where(some, after[parent], 0))
+    st["ended"].copy_(~some | old | (token == end))
+    st["parents"].copy_(torch.where(some, parent, -1))
+    st["chosen"].copy_(torch.where(some, token, -1))
+    goes_on = st["ended"] == 0
+    st["added"].copy_(goes_on)
+    packed = torch.zeros(rows + 1, dtype=torch.int32, device=DEV)
+    packed[torch.where(goes_on, goes_on.cumsum(0) - 1, rows)] = st["chosen"]
+    st["tokens"].copy_(packed[:rows])
+    st["tokens"][goes_on.sum():] = 0
+    return [st[name] for name in _SELECTED]
+
+
+# ------------------------------------------------------------------ tables that fork ----
+def _beams(case, gen):
+    """Groups of sequences that share what lies in their prompt's full blocks: tables, lengths, blocks in use, block ids in the pool's order."""
+    G, W, block, most_own = case["groups"], case["width"], case["block"], case["own"]
+    prompts = torch.tensor(_spread(G, case["short"], case["long"]))[torch.randperm(G, generator=gen)]
+    n = G * W
+    own = torch.randint(0, most_own + 1, (n,), generator=gen) if case["kind"] == "fork" else torch.randint(case["new"], most_own + 1, (n,), generator=gen)
+    shared = prompts // block * block
+    lengths = prompts.repeat_interleave(W) + own
+    need = (lengths + block - 1) // block
+    max_blocks = _blocks(case["long"] + most_own, block) + 2
+    return prompts, shared, lengths, need, max_blocks
+
+
+def _tables(shared, lengths, need, max_blocks, W, block, gen, spare=0, pool=None):
+    G, n = shared.numel(), lengths.numel()
+    column = torch.arange(max_blocks)[None, :]
+    full = shared // block
+    common = column < full[:, None]                                   # [G, max_blocks]
+    private = (column >= full.repeat_interleave(W)[:, None]) & (column < need[:, None])
+    used = int(common.sum()) + int(private.sum())
+    ids = torch.randperm(used + spare if pool is None else pool, generator=gen).to(torch.int32)
+    prefix = torch.full((G, max_blocks), -1, dtype=torch.int32)
+    prefix[common] = ids[:int(common.sum())]
+    tables = torch.where(common.repeat_interleave(W, 0) & (column < need[:, None]), prefix.repeat_interleave(W, 0), -1)
+    tables[private] = ids[int(common.sum()):used]
+    return tables, ids, used
+
+
+def _prepare_fork(case, gen):
+    G, W, block = case["groups"], case["width"], case["block"]
+    n = G * W
+    prompts, shared, lengths, need, max_blocks = _beams(case, gen)
+    # a pool with room for every sequence's own blocks and one more each
+    pool = sum(p // block for p in _spread(G, case["short"], case["long"])) + n * (_blocks(case["own"] + block, block) + 1) + 9
+    tables, ids, used = _tables(shared, lengths, need, max_blocks, W, block, gen, pool=pool)
+    # in every group `replaced` beams make room for copies of others, which stay where they are
+    parents = torch.arange(n)
+    for g in range(G):
+        order = torch.randperm(W, generator=gen) + g * W
+        for i in range(case["replaced"]):
+            parents[order[i]] = order[case["replaced"] + i % (W - case["replaced"])]
+    # some end
+    parents[torch.randperm(n, generator=gen)[:case["dead"]]] = -1
+    free = torch.full((pool,), -1, dtype=torch.int32)
+    free[:pool - used] = ids[used:]
+    st = dict(parents=parents.to(torch.int32), lengths=lengths.to(torch.int32), tables=tables, free=free,
+              state=torch.tensor([pool - used, 0, 0, 0], dtype=torch.int32), group_starts=torch.arange(G + 1, dtype=torch.int32) * W,
+              shared=torch.zeros(G, dtype=torch.int32), copies=torch.full((n, 4), -1, dtype=torch.int32))
+    st = {k: v.to(DEV) for k, v in st.items()}
+    st.update(block=block, width=W)
+    return st
+
+
+def _fork_outputs(st):
+    return [st[name] for name in ("lengths", "tables", "free", "state", "copies", "shared")]
+
+
+def _run_fork(st):
+    parents, lengths, tables, free, block = st["parents"].long(), st["lengths"].long(), st["tables"], st["free"], st["block"]
+    n, most = tables.shape
+    n_blocks, n_free = free.numel(), st["state"][0].long()
+    some = parents >= 0
+    p = parents.clamp(min=0)
+    row, column = torch.arange(n, device=DEV), torch.arange(most, device=DEV)
+    # which blocks have a holder left; of those without, the first sequence that held one gives it back
+    goes_on = torch.zeros(n + 1, dtype=torch.bool, device=DEV)
+    goes_on[torch.where(some, p, n)] = True
+    goes_on = goes_on[:n]
+    used = column < ((lengths + block - 1) // block)[:, None]
+    used &= (tables >= 0) & (tables < n_blocks)
+    rank = torch.where(goes_on, n + 1, n - row)[:, None].expand(n, most)
+    holder = torch.zeros(n_blocks + 1, dtype=torch.long, device=DEV)
+    at = torch.where(used, tables.long(), n_blocks)
+    holder.scatter_reduce_(0, at.view(-1), rank.reshape(-1), "amax")
+    back = used & ~goes_on[:, None] & (holder[at] == rank)
+    number = back.view(-1).cumsum(0)
+    n_back = number[-1]
+    stack = torch.cat([free, free[:1]])
+    place = torch.where(back.view(-1), n_free + number - 1, n_blocks)
+    stack[place] = tables.view(-1)
+    stack = stack[:n_blocks]
+    # an open block stays with the first sequence that goes on from its own, the others take one and a copy
+    after = torch.where(some, lengths[p], 0)
+    first = torch.full((n + 1,), n, device=DEV).scatter_reduce(0, torch.where(some, p, n), row, "amin")
+    copy = some & (after % block > 0) & (first[p] != row)
+    k = copy.cumsum(0) - 1
+    n_copy = copy.sum()
+    top = n_free + n_back
+    taken = stack[(top - 1 - k).clamp(0, n_blocks - 1)]
+    blocks = (after + block - 1) // block
+    new = torch.where((column < blocks[:, None]) & some[:, None], tables[p], tables)
+    last = (blocks - 1).clamp(min=0)
+    source = tables[p, last]
+    new = torch.where(copy[:, None] & (column == last[:, None]), taken[:, None], new)
+    entry = torch.stack([source, taken, (after % block).to(torch.int32), torch.zeros_like(source)], 1)
+    wide = torch.cat([st["copies"], st["copies"][:1]])
+    wide[torch.where(copy, k, n)] = entry
+    st["copies"].copy_(wide[:n])
+    left = top - n_copy
+    slot = torch.arange(n_blocks, device=DEV)
+    free.copy_(torch.where((slot >= n_free) & (slot < left), stack, free))
+    tables.copy_(new)
+    st["lengths"].copy_(after)
+    zero = torch.zeros_like(left)
+    st["state"].copy_(torch.stack([left, zero, zero, n_copy]))
+    # how far the tables of a group agree, in full blocks
+    starts = st["group_starts"].long()
+    G = starts.numel() - 1
+    group = torch.searchsorted(starts, row, right=True) - 1
+    alive = after > 0
+    lead = torch.full((G,), n, device=DEV).scatter_reduce(0, group, torch.where(alive, row, n), "amin").clamp(max=n - 1)
+    same = (new == new[lead[group]]) & (column < (after // block)[:, None])
+    agree = torch.where(alive, same.long().cumprod(1).sum(1), most + 1)
+    agree = torch.full((G,), most + 1, device=DEV).scatter_reduce(0, group, agree, "amin")
+    st["shared"].copy_(torch.where(agree <= most, agree * block, 0))
+    return _fork_outputs(st)
+
+
+# ------------------------------------------------------------------ a pool made compact ----
+def _prepare_compact(case, gen):
+    n, block, N = case["n_seq"], case["block"], case["blocks"]
+    lengths = torch.tensor(_spread(n, case["short"], case["long"]))[torch.randperm(n, generator=gen)]
+    # of two neighbours the second shares what it can of the first one's full blocks
+    need = (lengths + block - 1) // block
+    max_blocks = max(1, int(need.max()))
+    column = torch.arange(max_blocks)[None, :]
+    ids = torch.randperm(N, generator=gen).to(torch.int32)
+    held = column < need[:, None]
+    tables = torch.full((n, max_blocks), -1, dtype=torch.int32)
+    tables[held] = ids[:int(held.sum())]
+    common = torch.minimum(lengths[0:n - n % 2:2], lengths[1::2]) // block
+    for i in range(0, n - 1, 2):
+        tables[i + 1, :common[i // 2]] = tables[i, :common[i // 2]]
+    st = dict(lengths=lengths.to(torch.int32), tables=tables, new_tables=torch.full_like(tables, -1), free=torch.full((N,), -1, dtype=torch.int32),
+              after=torch.zeros(4, dtype=torch.int32), copies=torch.full((N, 4), -1, dtype=torch.int32))
+    st = {k: v.to(DEV) for k, v in st.items()}
+    st["block"] = block
+    return st
+
+
+def _compact_outputs(st):
+    return [st[name] for name in ("new_tables", "free", "after", "copies")]
+
+
+def _run_compact(st):
+    lengths, tables, free, block = st["lengths"].long(), st["tables"], st["free"], st["block"]
+    n, most = tables.shape
+    N = free.numel()
+    used = torch.arange(most, device=DEV) < ((lengths + block - 1) // block)[:, None]
+    known = used & (tables >= 0) & (tables < N)
+    held = torch.zeros(N + 1, dtype=torch.bool, device=DEV)
+    held[torch.where(known, tables.long(), N)] = True
+    held = held[:N]
+    n_held = held.sum()
+    at = torch.arange(N, device=DEV)
+    far, hole = held & (at >= n_held), ~held & (at < n_held)
+    n_far = far.sum()
+    place = torch.zeros(N + 1, dtype=torch.long, device=DEV)
+    place[torch.where(hole, hole.cumsum(0) - 1, N)] = at                      # the i-th hole
+    to = torch.where(far, place[(far.cumsum(0) - 1).clamp(min=0)], at)
+    st["new_tables"].copy_(torch.where(known, to[tables.long().clamp(0, N - 1)], torch.where(used, tables.long(), st["new_tables"].long())))
+    entry = torch.stack([at, to, torch.full_like(at, block), torch.zeros_like(at)], 1).to(torch.int32)
+    wide = torch.cat([st["copies"], st["copies"][:1]])
+    wide[torch.where(far, far.cumsum(0) - 1, N)] = entry
+    st["copies"].copy_(wide[:N])
+    left = N - n_held
+    free.copy_(torch.where(at < left, N - 1 - at, free.long()))
+    zero = torch.zeros_like(left)
+    st["after"].copy_(torch.stack([left, zero, zero, n_far]))
+    return _compact_outputs(st)
+
+
+# ------------------------------------------------------------------ blocks that are copied ----
+def _pool(shape, cache, gen):
+    if cache == "bf16":
+        return torch.randn(shape, generator=gen, device=DEV, dtype=torch.bfloat16)
+    return torch.randint(0, 256, shape, generator=gen, device=DEV, dtype=torch.uint8).bitwise_and_(0xbf).view(torch.float8_e4m3fn)
+
+
+def _copy_list(case):
+    """Tokens that each copied block holds."""
+    block = case["block"]
+    return [block if case["whole"] else 1 + (i * 7 + 5) % (block - 1) for i in range(case["copies"])]
+
+
+def _prepare_copy(case, gen, cpu):
+    L, N, block = case["layers"], case["blocks"], case["block"]
+    shape = (L, N, case["kv_heads"], block, case["dh"])
+    ids = torch.randperm(N, generator=cpu)[:2 * case["copies"]].view(2, -1)
+    copies = torch.full((case["room"], 4), -1, dtype=torch.int32)
+    copies[:case["copies"], 0], copies[:case["copies"], 1], copies[:case["copies"], 3] = ids[0].int(), ids[1].int(), 0
+    copies[:case["copies"], 2] = torch.tensor(_copy_list(case), dtype=torch.int32)
+    return dict(k=_pool(shape, case["cache"], gen), v=_pool(shape, case["cache"], gen), copies=copies.to(DEV),
+                count=torch.tensor([case["copies"], 0, 0, 0], dtype=torch.int32, device=DEV), layers=L)
+
+
+def _run_copy(st):
+    c, block = st["copies"].long(), st["k"].shape[3]
+    N = st["k"].shape[1]
+    c = torch.where((torch.arange(c.shape[0], device=DEV) < st["count"][0])[:, None], c, -1)
+    fine = (c[:, 0] >= 0) & (c[:, 0] < N) & (c[:, 1] >= 0) & (c[:, 1] < N)
+    # entries that are none move the first positions of a block to where they are
+    source, to, tokens = c[fine, 0], c[fine, 1], c[fine, 2]
+    mask = (torch.arange(block, device=DEV) < tokens[:, None])[None, :, None, :, None]
+    for pool in (st["k"], st["v"]):
+        x = pool.view(torch.uint8) if pool.element_size() == 1 else pool
+        for layer in range(x.shape[0]):
+            x[layer, to] = torch.where(mask[0], x[layer, source], x[layer, to])
+    return [st["k"], st["v"]]
+
+
+# ------------------------------------------------------------------ attention behind what is shared ----
+def _prepare_attend(case, gen, cpu):
+    G, W, block, new, H, Hk, dh = case["groups"], case["width"], case["block"], case["new"], case["q_heads"], case["kv_heads"], case["dh"]
+    n = G * W
+    prompts, shared, lengths, need, max_blocks = _beams(case, cpu)
+    # of a group's sequences the last `ended` but never the first have ended; in every second group
+    rows = torch.full((n,), new)
+    for g in range(0, G, 2):
+        for i in range(min(case["ended"], W - 1)):
+            lengths[g * W + W - 1 - i] = 0
+            rows[g * W + W - 1 - i] = 0
+    need = (lengths + block - 1) // block
+    tables, ids, used = _tables(shared, lengths, need, max_blocks, W, block, cpu, spare=3)
+    shape = (ids.numel(), Hk, block, dh)
+    scale = [None, None]
+    if case["cache"] == "e4m3":
+        k, v = (torch.cat([(p.float() * 8).to(torch.float8_e4m3fn) for p in torch.randn(shape, generator=gen, device=DEV, dtype=torch.bfloat16).split(
+            max(1, (1 << 26) // (Hk * block * dh)))]) for _ in range(2))
+        scale = [torch.rand(Hk, generator=gen, device=DEV) * 0.1 + 0.05 for _ in range(2)]
+    else:
+        k, v = (torch.randn(shape, generator=gen, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    starts = torch.nn.functional.pad(rows.cumsum(0), (1, 0))
+    n_rows = int(starts[-1])
+    st = dict(k=k, v=v, k_scale=scale[0], v_scale=scale[1], tables=tables.to(DEV), lengths=lengths.to(torch.int32).to(DEV),
+              group_starts=(torch.arange(G + 1, dtype=torch.int32) * W).to(DEV), shared=shared.to(torch.int32).to(DEV),
+              starts=starts.to(torch.int32).to(DEV) if new > 1 or n_rows < n else None, scale=1.0 / math.sqrt(dh), q_heads=H, dh=dh,
+              longest_shared=int(shared.max()), longest_own=int((lengths - shared.repeat_interleave(W)).max()), new=new, width=W)
+    st["q"] = (torch.randn(n_rows, H * dh, generator=gen, device=DEV) * 2.5).to(torch.bfloat16)
+    st["out"] = torch.zeros(n_rows, H * dh, dtype=torch.bfloat16, device=DEV)
+    return st
+
+
+def _gathered(pool, ids, scale):
+    """Keys or values of blocks behind one another, fp32 [n, kv_heads, positions, dh]."""
+    n, kv_heads, dh = ids.shape[0], pool.shape[1], pool.shape[3]
+    x = pool.view(torch.uint8)[ids.long().clamp(min=0)].view(pool.dtype) if pool.element_size() == 1 else pool[ids.long().clamp(min=0)]
+    x = x.transpose(1, 2).float().reshape(n, kv_heads, -1, dh)
+    return x if scale is None else x * scale[:, None, None]
+
+
+def _run_attend(st):
+    tables, lengths, shared, W, new, dh = st["tables"], st["lengths"].long(), st["shared"].long(), st["width"], st["new"], st["dh"]
+    n, most = tables.shape
+    G, Hk, block = n // W, st["k"].shape[1], st["k"].shape[2]
+    heads = st["q_heads"] // Hk
+    # every sequence has `new` rows here; those of ended ones are made up and left out at the end
+    token = torch.arange(new, device=DEV)
+    starts = torch.arange(n + 1, device=DEV) * new if st["starts"] is None else st["starts"].long()
+    rows = starts[1:] - starts[:-1]
+    row = (starts[:-1, None] + token).clamp(max=st["q"].shape[0] - 1)
+    q = st["q"][row].float().view(G, W, new, Hk, heads, dh)
+    q_group = q.permute(0, 3, 5, 1, 2, 4).reshape(G, Hk, dh, W * new * heads).contiguous()
+    q_own = q.view(n, new, Hk, heads, dh).permute(0, 2, 4, 1, 3).reshape(n, Hk, dh, new * heads).contiguous()
+    sees = (lengths[:, None] - rows[:, None] + 1 + token).clamp(min=0)                                    # [n, new]
+    # the group's common keys, once
+    ahead = st["longest_shared"]
+    leader = tables[::W][:, :max(1, _blocks(ahead, block))]
+    s0 = torch.matmul(_gathered(st["k"], leader, st["k_scale"]), q_group) * st["scale"]                 # [G, Hk, keys, columns]
+    at = torch.arange(s0.shape[2], device=DEV)
+    seen = (at[None, :, None] < shared[:, None, None]) & (at[None, :, None] < sees.view(G, 1, W * new).repeat_interleave(heads, 2))
+    s0 = s0.masked_fill(~seen[:, None], -math.inf)
+    # each sequence's own
+    own_blocks = max(1, _blocks(st["longest_own"], block))
+    first = (shared // block).repeat_interleave(W)
+    column = (first[:, None] + torch.arange(own_blocks, device=DEV)).clamp(max=most - 1)
+    mine = tables.gather(1, column)
+    s1 = torch.matmul(_gathered(st["k"], mine, st["k_scale"]), q_own) * st["scale"]                     # [n, Hk, keys, columns]
+    at = first[:, None, None] * block + torch.arange(s1.shape[2], device=DEV)[None, :, None]
+    s1 = s1.masked_fill(~(at < sees[:, None, :].repeat_interleave(heads, 2))[:, None], -math.inf)
+    top = torch.maximum(s0.amax(2).view(G, Hk, W, -1).transpose(1, 2).reshape(n, Hk, -1), s1.amax(2)).clamp(min=-1e30)
+    top0 = top.view(G, W, Hk, -1).transpose(1, 2).reshape(G, Hk, 1, -1)
+    p0, p1 = (s0 - top0).exp_(), (s1 - top[:, :, None]).exp_()
+    total = p0.sum(2).view(G, Hk, W, -1).transpose(1, 2).reshape(n, Hk, -1) + p1.sum(2)
+    o = torch.matmul(p0.transpose(2, 3).contiguous(), _gathered(st["v"], leader, st["v_scale"])).view(G, Hk, W, -1, dh).transpose(1, 2).reshape(n, Hk, -1, dh)
+    o = o + torch.matmul(p1.transpose(2, 3).contiguous(), _gathered(st["v"], mine, st["v_scale"]))
+    o = (o / total.clamp(min=1e-30)[..., None]).view(n, Hk, new, heads, dh).transpose(1, 2).reshape(n, new, -1)
+    there = (token[None, :] < rows[:, None]).view(-1)
+    st["out"].copy_(o.reshape(n * new, -1)[there])
+    return [st["out"]]
+
+
+# ------------------------------------------------------------------ ----
+def prepare(case, seed):
+    gen, cpu = torch.Generator(device=DEV), torch.Generator()
+    gen.manual_seed(seed)
+    cpu.manual_seed(seed)
+    kind = case["kind"]
+    if kind == "select":
+        st = _prepare_select(case, gen)
+    elif kind == "fork":
+        st = _prepare_fork(case, cpu)
+    elif kind == "compact":
+        st = _prepare_compact(case, cpu)
+    else:
+        st = (_prepare_copy if kind == "copy" else _prepare_attend)(case, gen, cpu)
+    st["kind"] = kind
+    return st
+
+
+def _run_own(st):
+    from paper_2505_13430_amd import binding as qb
+    kind = st["kind"]
+    if kind == "select":
+        qb.qzo_beam_select(st["logits"], st["width"], st["scores"], st["counts"], st["ended"], st["history"], st["parents"], st["chosen"], st["tokens"],
+                           st["added"], end_token=st["end"], length_penalty=st["penalty"])
+        return [st[name] for name in _SELECTED]
+    if kind == "fork":
+        qb.qzo_cache_fork(st["parents"], st["block"], st["lengths"], st["tables"], st["free"], st["state"], st["lengths"], st["tables"], st["state"],
+                          st["copies"], group_starts=st["group_starts"], shared=st["shared"])
+        return _fork_outputs(st)
+    if kind == "compact":
+        qb.qzo_cache_compact(st["block"], st["lengths"], st["tables"], st["free"], st["new_tables"], st["after"], st["copies"])
+        return _compact_outputs(st)
+    if kind == "copy":
+        qb.qzo_cache_copy(qb.make_cache(st["k"][0], st["v"][0]), st["copies"], layers=st["layers"], count=st["count"])
+        return [st["k"], st["v"]]
+    cache = qb.make_cache(st["k"], st["v"], st["k_scale"], st["v_scale"])
+    qb.qzo_paged_attention_shared(st["q"], cache, st["tables"], st["lengths"], st["group_starts"], st["shared"], st["out"], st["scale"], starts=st["starts"])
+    return [st["out"]]
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"select": _run_select, "fork": _run_fork, "compact": _run_compact, "copy": _run_copy, "attend": _run_attend}[state["kind"]](state)
+
+
+def work(case):
+    kind = case["kind"]
+    if kind == "select":
+        rows, V = case["groups"] * case["width"], case["vocab"]
+        # the logits of the beams that go on; states in and out, half of a history on average
+        return {"bytes": 2.0 * (rows - case["ended"]) * V + rows * (3 * 8 + 4 * 4 + 4.0 * case["history"]), "flops": 3.0 * (rows - case["ended"]) * V}
+    if kind == "copy":
+        return {"bytes": 4.0 * sum(_copy_list(case)) * case["layers"] * case["kv_heads"] * case["dh"] * (1 if case["cache"] == "e4m3" else 2), "flops": 0.0}
+    if kind == "compact":
+        held = sum(_blocks(x, case["block"]) for x in _spread(case["n_seq"], case["short"], case["long"]))
+        # table entries in and out, the free list; about that share of the held blocks moves
+        return {"bytes": 8.0 * held + 4.0 * max(0, case["blocks"] - held) + 16.0 * held * max(0.0, 1.0 - held / case["blocks"]), "flops": 0.0}
+    G, W, block = case["groups"], case["width"], case["block"]
+    prompts = _spread(G, case["short"], case["long"])
+    if kind == "fork":
+        entries = sum(W * _blocks(p + case["own"] // 2, block) for p in prompts)
+        moved = sum(case["replaced"] * _blocks(p + case["own"] // 2, block) for p in prompts)
+        return {"bytes": 4.0 * entries + 4.0 * moved + 12.0 * G * W + 16.0 * G * case["replaced"], "flops": 0.0}
+    H, Hk, dh, new, wide = case["q_heads"], case["kv_heads"], case["dh"], case["new"], 1 if case["cache"] == "e4m3" else 2
+    ended = min(case["ended"], W - 1)
+    keys = pairs = rows = 0.0
+    for g, p in enumerate(prompts):
+        live = W - (ended if g % 2 == 0 else 0)
+        own = (case["own"] + new) / 2 + p % block
+        keys += p // block * block + live * own
+        pairs += live * new * (p // block * block + own - (new - 1) / 2)
+        rows += live * new
+    return {"bytes": 2.0 * keys * Hk * dh * wide + 4.0 * rows * H * dh + 4.0 * keys / block, "flops": 4.0 * pairs * H * dh}
+
+
+def _exact_select(case, st):
+    """The scores of the best candidates, each beam's own best ones first."""
+    W, V = case["width"], case["vocab"]
+    out = []
+    for g in range(case["groups"]):
+        keys, totals = [], []
+        for b in range(W):
+            r = g * W + b
+            score, count = float(st["scores"][r]), max(0, int(st["counts"][r]))
+            if int(st["ended"][r]):
+                keys.append(torch.full((1,), score / max(1, count) ** case["penalty"], dtype=torch.float64, device=DEV))
+                totals.append(torch.full((1,), score, dtype=torch.float64, device=DEV))
+                continue
+            x = st["logits"][r].double()
+            got = torch.log_softmax(x, 0).topk(min(W, V)).values + score
+            keys.append(got / (count + 1) ** case["penalty"])
+            totals.append(got)
+        key, total = torch.cat(keys), torch.cat(totals)
+        best = key.topk(min(W, key.numel())).indices
+        row = torch.full((W,), -math.inf, dtype=torch.float64, device=DEV)
+        row[:best.numel()] = total[best]
+        out.append(row)
+    return [torch.cat(out)] + [None] * (len(_SELECTED) - 1)
+
+
+def _exact_attend(case, st):
+    G, W, new, block, Hk, dh = case["groups"], case["width"], case["new"], case["block"], case["kv_heads"], case["dh"]
+    heads, out = case["q_heads"] // Hk, []
+    pools = [(st[name], torch.ones(Hk, device=DEV) if st[name + "_scale"] is None else st[name + "_scale"]) for name in ("k", "v")]
+    row = 0
+    for b in range(G * W):
+        length = int(st["lengths"][b])
+        if length == 0:
+            continue
+        at = torch.arange(length, device=DEV)
+        ids = st["tables"][b].long()[at // block]
+        late = at[None, :] > (length - new + torch.arange(new, device=DEV)).repeat_interleave(heads)[:, None]
+        q = st["q"][row:row + new].double().view(new, Hk, heads, dh)
+        row += new
+        got = []
+        for h in range(Hk):
+            k, v = (pool[:, h].contiguous().view(torch.uint8).view(-1, dh * pool.element_size())[ids * block + at % block].view(pool.dtype).double() * scale[h].double()
+                    for pool, scale in pools)
+            s = torch.mm(q[:, h].reshape(new * heads, dh), k.t().contiguous()) * st["scale"]
+            got.append(torch.mm(torch.softmax(s.masked_fill(late, -math.inf), -1), v).view(new, 1, heads * dh))
+        out.append(torch.cat(got, 1).reshape(new, -1))
+    return [torch.cat(out)]
+
+
+def exact(case, seed):
+    if case["kind"] in ("fork", "compact", "copy"):
+        return None                       # whole numbers and copied values, no rounding
+    if case["kind"] == "attend" and case["groups"] * case["width"] * case["kv_heads"] > 4096:
+        return None                       # thousands of small products
+    st = prepare(case, seed)
+    return _exact_select(case, st) if case["kind"] == "select" else _exact_attend(case, st)

@@ -390,13 +390,13 @@ def _prepare_copy(case, gen, cpu):
     copies[:case["copies"], 0], copies[:case["copies"], 1], copies[:case["copies"], 3] = ids[0].int(), ids[1].int(), 0
     copies[:case["copies"], 2] = torch.tensor(_copy_list(case), dtype=torch.int32)
     return dict(k=_pool(shape, case["cache"], gen), v=_pool(shape, case["cache"], gen), copies=copies.to(DEV),
-                count=torch.tensor([case["copies"], 0, 0, 0], dtype=torch.int32, device=DEV), layers=L)
+                count=torch.tensor([0, 0, 0, case["copies"]], dtype=torch.int32, device=DEV), layers=L)
 
 
 def _run_copy(st):
     c, block = st["copies"].long(), st["k"].shape[3]
     N = st["k"].shape[1]
-    c = torch.where((torch.arange(c.shape[0], device=DEV) < st["count"][0])[:, None], c, -1)
+    c = torch.where((torch.arange(c.shape[0], device=DEV) < st["count"][3])[:, None], c, -1)
     fine = (c[:, 0] >= 0) & (c[:, 0] < N) & (c[:, 1] >= 0) & (c[:, 1] < N)
     # entries that are none move the first positions of a block to where they are
     source, to, tokens = c[fine, 0], c[fine, 1], c[fine, 2]
@@ -515,8 +515,8 @@ def _run_own(st):
                            st["added"], end_token=st["end"], length_penalty=st["penalty"])
         return [st[name] for name in _SELECTED]
     if kind == "fork":
-        qb.qzo_cache_fork(st["parents"], st["block"], st["lengths"], st["tables"], st["free"], st["state"], st["lengths"], st["tables"], st["state"],
-                          st["copies"], group_starts=st["group_starts"], shared=st["shared"])
+        qb.qzo_cache_fork(st["parents"], st["block"], st["lengths"], st["tables"], st["free"], st["state"], st["copies"],
+                          group_starts=st["group_starts"], shared=st["shared"])
         return _fork_outputs(st)
     if kind == "compact":
         qb.qzo_cache_compact(st["block"], st["lengths"], st["tables"], st["free"], st["new_tables"], st["after"], st["copies"])

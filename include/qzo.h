@@ -424,6 +424,106 @@ qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows
                                uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream);
 
 /*
+ * Sequences that fork: the beams of a prompt, several continuations of one, candidates behind it.  They share the full blocks that they have
+ * in common; a block is held by every sequence whose table names it among those that its length needs.
+ */
+typedef struct {
+  int32_t from, to;                /* blocks */
+  int32_t tokens;                  /* the first positions of the block, which are copied */
+  int32_t reserved;                /* 0 */
+} qzo_block_copy;
+
+/*
+ * Every sequence goes on from one of the old ones: new sequence i is old sequence parents_dev[i], or none (negative: its length becomes 0).
+ * In place: lengths_dev [n_seq], tables_dev [n_seq, max_blocks], free_dev [n_blocks] and state_dev as qzo_cache_plan keeps them.
+ *   Row i of the tables receives the blocks of its parent; nothing else of the tables is written.  A full block is shared by all
+ *     that go on from its sequence.  An open one (length % block tokens are in it) stays with the first of them (the lowest i);
+ *     every other one takes a block off the stack, in order of i, and copies_dev [n_seq] lists what is to be copied into it, behind
+ *     one another, state.n_taken of them; entries behind those are not written.  qzo_cache_copy then copies.
+ *   Blocks that were held and that no new sequence holds are put on the stack first, by the first old sequence that held them, in
+ *     table order.
+ *   shared_dev [n_groups] (with n_groups 0 it and group_starts_dev are null): group g is sequences group_starts[g] .. group_starts[g + 1] - 1
+ *     (int32 [n_groups + 1], ascending, values cut off at 0 and n_seq); receives how many of their first tokens, in full blocks, lie in the
+ *     same blocks for all of them whose length is not 0; 0 where there is none.
+ * An open block belongs to one sequence, as qzo_cache_plan and this call leave it.  Sequences that share blocks are ended by this
+ * call: a negative count in qzo_cache_plan would give away blocks that others hold.
+ * All or nothing, as qzo_cache_plan: state.status QZO_ERR_ARG: a parent beyond the last sequence, a negative length, an n_free
+ * outside 0 .. n_blocks, more blocks given back than the pool has; QZO_ERR_SHAPE: a length beyond max_blocks * block;
+ * QZO_ERR_WORKSPACE: not enough free blocks; then shared_dev is that of the sequences as they are, n_taken 0 and all else as it was.
+ * Block ids outside 0 .. n_blocks - 1 are copied as they are and never given back.
+ * scratch_dev: qzo_cache_fork_scratch_bytes bytes, 256-byte aligned.  Its first 16 + 4 n_blocks bytes are zero before the first call that
+ * uses it, and zero again after every call (a call with another n_blocks counts as a first one); the rest is undefined.  Calls that may overlap
+ * need scratch of their own.  n_seq 1 .. 8192, n_groups at most n_seq, block, n_blocks, max_blocks as for qzo_cache_plan.
+ */
+qzo_status qzo_cache_fork_scratch_bytes(uint32_t n_seq, uint32_t n_blocks, uint32_t max_blocks, uint64_t* out);
+qzo_status qzo_cache_fork(const int32_t* parents_dev, uint32_t n_seq, uint32_t block, uint32_t n_blocks, uint32_t max_blocks,
+                          int32_t* lengths_dev, int32_t* tables_dev, int32_t* free_dev, qzo_cache_state* state_dev,
+                          uint32_t n_groups, const int32_t* group_starts_dev, int32_t* shared_dev, qzo_block_copy* copies_dev,
+                          void* scratch_dev, uint64_t scratch_bytes, void* stream);
+
+/*
+ * The blocks that the sequences hold to the front of the pool: n of them, those from id n on move to the ids below n that none holds, both in
+ * ascending order; copies_dev [n_blocks / 2] lists the moves (whole blocks), state.n_taken of them, for qzo_cache_copy.  new_tables_dev
+ * (may be tables_dev) receives the tables' entries that the lengths need, with the new ids; nothing else of it is written.  free_dev: the ids
+ * n .. n_blocks - 1, the lowest on top; state_dev: what qzo_cache_plan goes on from.  A block that neither a table nor the new
+ * stack names does not exist: every sequence that uses the pool has to be in the tables.  Scratch, ids outside the pool and limits as for qzo_cache_fork
+ * (lengths are cut off at 0 and max_blocks * block).
+ */
+qzo_status qzo_cache_compact(uint32_t n_seq, uint32_t block, uint32_t n_blocks, uint32_t max_blocks, const int32_t* lengths_dev,
+                             const int32_t* tables_dev, int32_t* new_tables_dev, int32_t* free_dev, qzo_cache_state* state_dev,
+                             qzo_block_copy* copies_dev, void* scratch_dev, uint64_t scratch_bytes, void* stream);
+
+/*
+ * Copies blocks within the pools of n_layers layers: cache describes those of layer 0, the others follow, as in qzo_answer.  copies_dev
+ * [n_copies]; with count_dev (nullable: all) only its first *count_dev (at most n_copies; below 0: none).  An entry with a block outside the pool, with from = to
+ * or without tokens is passed over, more tokens than a block has are a block's.  No block is copied to twice, or both copied from and to.
+ */
+qzo_status qzo_cache_copy(const qzo_cache* cache, uint32_t n_layers, const qzo_block_copy* copies_dev, uint32_t n_copies,
+                          const int32_t* count_dev, void* stream);
+
+/*
+ * The next beams of n_groups prompts with `width` beams each; row g * width + b is beam b of prompt g.  logits_dev bf16, rows ld_logits
+ * elements apart, `vocab` of them.  A beam of finite score that has not ended (ended_dev 0) can go on with every token v of a finite logit x:
+ *   total = score + x_v - log sum_v e^x_v over the finite logits,  key = total / count^length_penalty with the new token counted (0: key = total);
+ * one that has ended stays as it is: a single candidate, of its score and count, token end_token (0 if that is -1).  A score of
+ * -infinity or NaN stands for no beam, and its logits are not read.  Row i of a prompt becomes the candidate with the i-th
+ * highest key, ties to the lower beam, then the lower token (within a beam the logits decide, 0 and -0 being equal); sums in 64 bits.
+ *   scores_dev fp32: total; counts_dev: tokens of the beam (one more, but for an ended one); ended_dev: 1 if the token is end_token or it had ended;
+ *   history_dev int32 [rows, max_history] (null with max_history 0): the parent's first count tokens, then the new one; columns beyond
+ *     are not written, tokens beyond max_history are not recorded;
+ *   parents_dev: row of the beam that it goes on from, as qzo_cache_fork takes it; chosen_dev: the token;
+ *   added_dev: 1 where the beam goes on, 0 where it has ended, as qzo_cache_plan takes it; tokens_dev [rows]: the tokens of those that go on,
+ *     one behind the other, then zeros, as qzo_answer takes them.
+ * Where there are fewer candidates than beams: score -infinity, count 0, ended 1, parent and token -1, history as it was.
+ * scores, counts (negative: 0), ended and history are read and written in place.  All int32 but scores, 16-byte aligned.  Scratch: qzo_beam_select_scratch_bytes
+ * bytes, 256-byte aligned, contents undefined before and after; calls that may overlap need scratch of their own.  width 1 .. 64, vocab 1 .. 2^22, at most
+ * 8192 rows, ld_logits >= vocab, length_penalty finite and not negative, end_token -1 or below vocab; logits may be at any
+ * multiple of 2 bytes.
+ */
+qzo_status qzo_beam_select_scratch_bytes(uint32_t n_groups, uint32_t width, uint32_t vocab, uint64_t* out);
+qzo_status qzo_beam_select(const void* logits_dev, uint64_t ld_logits, uint32_t n_groups, uint32_t width, uint32_t vocab,
+                           int32_t end_token, double length_penalty, float* scores_dev, int32_t* counts_dev, int32_t* ended_dev,
+                           int32_t* history_dev, uint32_t max_history, int32_t* parents_dev, int32_t* chosen_dev,
+                           int32_t* tokens_dev, int32_t* added_dev, void* scratch_dev, uint64_t scratch_bytes, void* stream);
+
+/*
+ * qzo_paged_attention for groups of sequences that begin alike: group g is sequences group_starts[g] .. group_starts[g + 1] - 1 (int32
+ * [n_groups + 1], ascending, values cut off at 0 and n_seq; sequences in no group attend as in qzo_paged_attention), whose first shared_dev[g]
+ * tokens have the same keys and values.  Those, down to a multiple of 16, are read once for all the group's rows, through the table of its first
+ * sequence; every sequence's other positions through its own.  A sequence whose new tokens begin before the shared part ends reads all of
+ * its positions itself; so do all where the first sequence is shorter than that.  Otherwise results, limits and roundings are
+ * those of qzo_paged_attention (p meets v as two bf16 numbers where the columns of the group, or of the sequence, are as few as it says).
+ * scratch_dev: qzo_paged_attention_shared_scratch_bytes bytes, kept as qzo_paged_attention's (its first 2048 bytes zero).  n_groups 1 .. 2048.
+ */
+qzo_status qzo_paged_attention_shared_scratch_bytes(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t kv_heads,
+                                                    uint32_t head_dim, uint64_t* out);
+qzo_status qzo_paged_attention_shared(const void* q_dev, uint64_t ld_q, uint32_t n_rows, uint32_t n_seq, uint32_t q_heads,
+                                      const qzo_cache* cache, const int32_t* tables_dev, uint32_t max_blocks,
+                                      const int32_t* lengths_dev, const int32_t* starts_dev, uint32_t n_groups,
+                                      const int32_t* group_starts_dev, const int32_t* shared_dev, float scale, void* out_dev,
+                                      uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream);
+
+/*
  * Answers: the model, as its scales (and in joint mode theta_u) are now and unperturbed, over the n_tokens newest tokens of n_seq sequences, whose earlier
  * tokens' keys and values are in the cache.  tokens_dev int32 [n_tokens] (values in [0, vocab)), sequence by sequence as qzo_cache_plan lists
  * them; starts_dev, slots_dev, positions_dev, lengths_dev, tables_dev as it left them (rows behind the last new token, slots of -1, are
@@ -442,6 +542,13 @@ qzo_status qzo_answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens
                       const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev,
                       const int32_t* slots_dev, const int32_t* positions_dev, void* workspace_dev, uint64_t workspace_bytes,
                       void* logits_dev, void* stream);
+
+/* qzo_answer where groups of sequences begin alike: its attention is qzo_paged_attention_shared, with these groups in every layer. */
+qzo_status qzo_answer_shared_workspace_bytes(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq, uint64_t* out);
+qzo_status qzo_answer_shared(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_seq, const qzo_cache* cache,
+                             const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev,
+                             const int32_t* slots_dev, const int32_t* positions_dev, uint32_t n_groups, const int32_t* group_starts_dev,
+                             const int32_t* shared_dev, void* workspace_dev, uint64_t workspace_bytes, void* logits_dev, void* stream);
 
 /* RTN quantizer of Eq. 3 with the k=4 absmax scale: w_dev fp32 [N,K] ->
  * q_dev packed int4 [N,K/2], s_dev bf16 [N,K/group].  Model construction, not

@@ -30,7 +30,9 @@ EXPORTS = [
     "qzo_nf4_expand", "qzo_nf4_scratch_bytes", "qzo_nf4_gemm",
     "qzo_codebook_scratch_bytes", "qzo_codebook_gemm", "qzo_apply_update_channel",
     "qzo_cache_plan", "qzo_qk_norm_rope", "qzo_paged_attention_scratch_bytes", "qzo_paged_attention",
-    "qzo_answer_workspace_bytes", "qzo_answer",
+    "qzo_cache_fork_scratch_bytes", "qzo_cache_fork", "qzo_cache_compact", "qzo_cache_copy", "qzo_beam_select_scratch_bytes", "qzo_beam_select",
+    "qzo_paged_attention_shared_scratch_bytes", "qzo_paged_attention_shared",
+    "qzo_answer_workspace_bytes", "qzo_answer", "qzo_answer_shared_workspace_bytes", "qzo_answer_shared",
     "qzo_debug_philox", "qzo_debug_normal_pairs", "qzo_debug_normals", "qzo_debug_dequant", "qzo_debug_dequant_zp",
     "qzo_debug_forward", "qzo_debug_bf16_gemm", "qzo_debug_reduce_norm", "qzo_debug_fused_linear", "qzo_debug_attention_slices",
     "qzo_debug_attention_linear",
@@ -75,12 +77,22 @@ def lib():
         for name in EXPORTS[:-1]:
             getattr(_lib, name).restype = C.c_int
         # called once or more per layer and token: arguments converted by declared types
-        u32, u64, p, f = C.c_uint32, C.c_uint64, C.c_void_p, C.c_float
+        u32, u64, i32, p, f, d = C.c_uint32, C.c_uint64, C.c_int32, C.c_void_p, C.c_float, C.c_double
         _lib.qzo_cache_plan.argtypes = [p, p, u32, u32, u32, u32, u32] + [p] * 9
         _lib.qzo_qk_norm_rope.argtypes = [p, u64, u32, u32, u32, u32, p, p, f, f, p, u32, p, p, p, u64, p]
         _lib.qzo_paged_attention_scratch_bytes.argtypes = [u32, u32, u32, u32, p]
         _lib.qzo_answer.argtypes = [p, p, u32, u32, p, p, u32, p, p, p, p, p, u64, p, p]
         _lib.qzo_paged_attention.argtypes = [p, u64, u32, u32, u32, p, p, u32, p, p, f, p, u64, p, u64, p]
+        _lib.qzo_cache_fork_scratch_bytes.argtypes = [u32, u32, u32, p]
+        _lib.qzo_cache_fork.argtypes = [p, u32, u32, u32, u32, p, p, p, p, u32, p, p, p, p, u64, p]
+        _lib.qzo_cache_compact.argtypes = [u32, u32, u32, u32, p, p, p, p, p, p, p, u64, p]
+        _lib.qzo_cache_copy.argtypes = [p, u32, p, u32, p, p]
+        _lib.qzo_beam_select_scratch_bytes.argtypes = [u32, u32, u32, p]
+        _lib.qzo_beam_select.argtypes = [p, u64, u32, u32, u32, i32, d, p, p, p, p, u32, p, p, p, p, p, u64, p]
+        _lib.qzo_paged_attention_shared_scratch_bytes.argtypes = [u32, u32, u32, u32, u32, p]
+        _lib.qzo_paged_attention_shared.argtypes = [p, u64, u32, u32, u32, p, p, u32, p, p, u32, p, p, f, p, u64, p, u64, p]
+        _lib.qzo_answer_shared_workspace_bytes.argtypes = [p, u32, u32, p]
+        _lib.qzo_answer_shared.argtypes = [p, p, u32, u32, p, p, u32, p, p, p, p, u32, p, p, p, u64, p, p]
     return _lib
 
 
@@ -558,19 +570,19 @@ def qzo_paged_attention_scratch_bytes(n_rows, n_seq, q_heads, head_dim) -> int:
 _stream_scratch = {}
 
 
-def _scratch_of_stream(device, stream, handle, nbytes):
-    """Address and bytes of the scratch of the calls on one stream, which do not overlap.  A captured graph keeps the address it was captured with and may
-    be replayed on any stream beside any other: it is given scratch of its own."""
+def _scratch_of_stream(device, stream, handle, nbytes, kind=None):
+    """Address and bytes of the scratch of the calls of a kind on one stream, which do not overlap.  A captured graph keeps the address it was captured
+    with and may be replayed on any stream beside any other: it is given scratch of its own."""
     captured = torch.cuda.is_current_stream_capturing()
     if stream is not None:                     # a stream may be captured without being the current one
         with torch.cuda.stream(stream):
             captured = captured or torch.cuda.is_current_stream_capturing()
     assert not captured, "a captured call needs scratch of its own: pass scratch"
-    kept = _stream_scratch.get((device, handle))
+    kept = _stream_scratch.get((device, handle, kind))
     if kept is None or kept[1] < nbytes:
         with torch.cuda.stream(stream):        # what is outgrown is used again on this stream only
             t = torch.zeros(nbytes, dtype=torch.uint8, device=device)
-        kept = _stream_scratch[device, handle] = t.data_ptr(), nbytes, t
+        kept = _stream_scratch[device, handle, kind] = t.data_ptr(), nbytes, t
     return kept[:2]
 
 
@@ -595,18 +607,124 @@ def qzo_paged_attention(q, cache, tables, lengths, out, scale, starts=None, scra
                                      _at(starts, i32, at), scale, y, ldy, *room, st))
 
 
-def qzo_answer_workspace_bytes(model, n_tokens, n_seq) -> int:
+def qzo_paged_attention_shared_scratch_bytes(n_rows, n_seq, q_heads, kv_heads, head_dim) -> int:
     out = C.c_uint64(0)
-    _check(lib().qzo_answer_workspace_bytes(model, C.c_uint32(n_tokens), C.c_uint32(n_seq), C.byref(out)))
+    _check(lib().qzo_paged_attention_shared_scratch_bytes(n_rows, n_seq, q_heads, kv_heads, head_dim, C.addressof(out)))
     return out.value
 
 
-def qzo_answer(model, tokens, cache, tables, lengths, starts, slots, positions, workspace, logits, stream=None):
-    """tokens int32 [n_tokens]; cache: of layer 0, the other layers' pools behind it; logits bf16 [n_seq, vocab]."""
+def qzo_paged_attention_shared(q, cache, tables, lengths, group_starts, shared, out, scale, starts=None, scratch="auto", stream=None):
+    """qzo_paged_attention of sequences whose groups begin alike: group_starts int32 [n_groups + 1], shared int32 [n_groups], the tokens that
+    a group's sequences have in common."""
+    at, i32, (rows, width), (n, most), dh = torch.cuda.current_device(), torch.int32, q.shape, tables.shape, cache.head_dim
+    x, ldx = _rows(q, at)
+    y, ldy = _rows(out, at)
+    heads, groups = width // dh, shared.numel()
+    assert q.shape == out.shape and heads * dh == width and cache.device == at
+    assert lengths.numel() == n and (starts is None or starts.numel() == n + 1) and group_starts.numel() == groups + 1
+    if rows == 0:
+        return
+    st = _stream_of(stream, at)
+    if isinstance(scratch, str):
+        room = _scratch_of_stream(at, stream, st, qzo_paged_attention_shared_scratch_bytes(rows, n, heads, cache.kv_heads, dh), "shared")
+    else:
+        room = _room(scratch, at)
+    _check(lib().qzo_paged_attention_shared(x, ldx, rows, n, heads, C.addressof(cache), _at(tables, i32, at), most, _at(lengths, i32, at),
+                                            _at(starts, i32, at), groups, _at(group_starts, i32, at), _at(shared, i32, at), scale, y, ldy, *room, st))
+
+
+def qzo_cache_fork_scratch_bytes(n_seq, n_blocks, max_blocks) -> int:
+    out = C.c_uint64(0)
+    _check(lib().qzo_cache_fork_scratch_bytes(n_seq, n_blocks, max_blocks, C.addressof(out)))
+    return out.value
+
+
+def _fork_room(scratch, at, stream, st, n, n_blocks, most):
+    # the marks in it are one pool's: kept apart by the number of its blocks
+    if isinstance(scratch, str):
+        return _scratch_of_stream(at, stream, st, qzo_cache_fork_scratch_bytes(n, n_blocks, most), ("fork", n_blocks))
+    return _room(scratch, at)
+
+
+def qzo_cache_fork(parents, block, lengths, tables, free, state, copies, group_starts=None, shared=None, scratch="auto", stream=None):
+    """int32 tensors, in place: lengths [n_seq], tables [n_seq, max_blocks], free [n_blocks], state a qzo_cache_state; copies [n_seq, 4] receives
+    a qzo_block_copy a row, state[3] of them.  group_starts [n_groups + 1], shared [n_groups]: None, or what it tells of the groups."""
+    at, i32, (n, most), groups = torch.cuda.current_device(), torch.int32, tables.shape, 0 if shared is None else shared.numel()
+    assert parents.numel() == lengths.numel() == n and state.numel() == 4 and copies.numel() >= 4 * n
+    assert (group_starts is None) == (shared is None) and (shared is None or group_starts.numel() == groups + 1)
+    st = _stream_of(stream, at)
+    room = _fork_room(scratch, at, stream, st, n, free.numel(), most)
+    _check(lib().qzo_cache_fork(_at(parents, i32, at), n, block, free.numel(), most, _at(lengths, i32, at), _at(tables, i32, at), _at(free, i32, at),
+                                _at(state, i32, at), groups, _at(group_starts, i32, at) if groups else None, _at(shared, i32, at) if groups else None,
+                                _at(copies, i32, at), *room, st))
+
+
+def qzo_cache_compact(block, lengths, tables, free, new_tables, state, copies, scratch="auto", stream=None):
+    """int32 tensors as for qzo_cache_fork; new_tables may be tables; copies [at least n_blocks // 2, 4]."""
+    at, i32, (n, most) = torch.cuda.current_device(), torch.int32, tables.shape
+    assert lengths.numel() == n and new_tables.shape == tables.shape and state.numel() == 4 and copies.numel() >= free.numel() // 2 * 4
+    st = _stream_of(stream, at)
+    room = _fork_room(scratch, at, stream, st, n, free.numel(), most)
+    _check(lib().qzo_cache_compact(n, block, free.numel(), most, _at(lengths, i32, at), _at(tables, i32, at), _at(new_tables, i32, at), _at(free, i32, at),
+                                   _at(state, i32, at), _at(copies, i32, at), *room, st))
+
+
+def qzo_cache_copy(cache, copies, layers=1, count=None, stream=None):
+    """copies int32 [n, 4], a qzo_block_copy a row, with count only the first count[3] of them: count is the qzo_cache_state that came with the
+    list, or one number.  cache: of layer 0, the other layers' pools behind it."""
+    at = torch.cuda.current_device()
+    assert cache.device == at and copies.shape[-1] == 4
+    n, where = copies.numel() // 4, _at(count, torch.int32, at)
+    if where is not None and count.numel() == 4:
+        where += 12                             # n_taken
+    if n:
+        _check(lib().qzo_cache_copy(C.addressof(cache), layers, _at(copies, torch.int32, at), n, where, _stream_of(stream, at)))
+
+
+def qzo_beam_select_scratch_bytes(n_groups, width, vocab) -> int:
+    out = C.c_uint64(0)
+    _check(lib().qzo_beam_select_scratch_bytes(n_groups, width, vocab, C.addressof(out)))
+    return out.value
+
+
+def qzo_beam_select(logits, width, scores, counts, ended, history, parents, chosen, tokens, added, end_token=-1, length_penalty=0.0, scratch="auto",
+                    stream=None):
+    """logits bf16 [n_groups * width, vocab], rows may be strided; scores fp32, counts, ended, parents, chosen, tokens, added int32 [rows]; history
+    int32 [rows, max_history] or None."""
+    at, i32, (rows, vocab) = torch.cuda.current_device(), torch.int32, logits.shape
+    x, ld = _rows(logits, at)
+    assert rows % width == 0 and scores.numel() == counts.numel() == ended.numel() == parents.numel() == chosen.numel() == tokens.numel() == added.numel() == rows
+    most = 0 if history is None else history.numel() // rows
+    assert history is None or history.shape == (rows, most)
+    st = _stream_of(stream, at)
+    if isinstance(scratch, str):
+        room = _scratch_of_stream(at, stream, st, qzo_beam_select_scratch_bytes(rows // width, width, vocab), "beams")
+    else:
+        room = _room(scratch, at)
+    _check(lib().qzo_beam_select(x, ld, rows // width, width, vocab, end_token, length_penalty, _at(scores, torch.float32, at), _at(counts, i32, at),
+                                 _at(ended, i32, at), _at(history, i32, at) if most else None, most, _at(parents, i32, at), _at(chosen, i32, at),
+                                 _at(tokens, i32, at), _at(added, i32, at), *room, st))
+
+
+def qzo_answer_workspace_bytes(model, n_tokens, n_seq, shared=False) -> int:
+    out = C.c_uint64(0)
+    call = lib().qzo_answer_shared_workspace_bytes if shared else lib().qzo_answer_workspace_bytes
+    _check(call(model, C.c_uint32(n_tokens), C.c_uint32(n_seq), C.byref(out)))
+    return out.value
+
+
+def qzo_answer(model, tokens, cache, tables, lengths, starts, slots, positions, workspace, logits, stream=None, group_starts=None, shared=None):
+    """tokens int32 [n_tokens]; cache: of layer 0, the other layers' pools behind it; logits bf16 [n_seq, vocab].  With group_starts [n_groups + 1] and
+    shared [n_groups] it is qzo_answer_shared, whose workspace it then needs."""
     i32, (n, most) = torch.int32, tables.shape
     assert lengths.numel() == n and starts.numel() == n + 1 and slots.numel() >= tokens.numel() <= positions.numel() and logits.shape[0] == n
     at = torch.cuda.current_device()
-    assert cache.device == at
-    _check(lib().qzo_answer(model, _at(tokens, i32, at), tokens.numel(), n, C.addressof(cache), _at(tables, i32, at), most, _at(lengths, i32, at),
-                            _at(starts, i32, at), _at(slots, i32, at), _at(positions, i32, at), *_room(workspace, at),
-                            _at(logits, torch.bfloat16, at), _stream_of(stream, at)))
+    assert cache.device == at and (group_starts is None) == (shared is None)
+    args = [model, _at(tokens, i32, at), tokens.numel(), n, C.addressof(cache), _at(tables, i32, at), most, _at(lengths, i32, at),
+            _at(starts, i32, at), _at(slots, i32, at), _at(positions, i32, at)]
+    rest = [*_room(workspace, at), _at(logits, torch.bfloat16, at), _stream_of(stream, at)]
+    if shared is None:
+        _check(lib().qzo_answer(*args, *rest))
+        return
+    assert group_starts.numel() == shared.numel() + 1
+    _check(lib().qzo_answer_shared(*args, shared.numel(), _at(group_starts, i32, at), _at(shared, i32, at), *rest))

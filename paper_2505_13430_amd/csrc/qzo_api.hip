@@ -459,6 +459,8 @@ struct Answer {
   const int32_t *tables, *lengths, *starts, *slots, *positions;
   uint32_t n_seq, max_blocks;
   void *scratch, *last, *logits;   // of the attention; the last tokens' hidden states
+  uint32_t n_groups;               // 0: no sequences that begin alike
+  const int32_t *group_starts, *shared;
 };
 
 // The decoder forward with every quantized linear perturbed by sign*eps*z.
@@ -530,14 +532,16 @@ qzo_status forward(qzo_model* m, const int32_t* tok, uint32_t batch1, uint32_t s
         hipError_t e = launch_qk_norm_rope(qa, dh, c.rope_theta, st);
         if (e != hipSuccess) return e;
       }
-      PagedArgs pa = {};
+      SharedArgs pa = {};
       pa.q = (const bf16_t*)w.qkv; pa.ld_q = 3 * d; pa.out = (bf16_t*)w.att; pa.ld_out = d;
       pa.n_rows = M1; pa.n_seq = ans->n_seq; pa.q_heads = pa.kv_heads = H; pa.group = 1;
       pa.k = qa.k; pa.v = qa.v; pa.k_scale = k.k_scale_dev; pa.v_scale = k.v_scale_dev;
       pa.n_blocks = k.n_blocks; pa.block_shift = qa.block_shift; pa.max_blocks = ans->max_blocks;
       pa.tables = ans->tables; pa.lengths = ans->lengths; pa.starts = ans->starts; pa.scale = 1.0f / std::sqrt((float)dh);
       ProfScope ps(PK_ATTN, 0, st);               // its work depends on lengths that only the device knows
-      return launch_paged_attention(pa, dh, k.type == 1, ans->scratch, st);
+      if (!ans->n_groups) return launch_paged_attention(pa, dh, k.type == 1, ans->scratch, st);
+      pa.n_groups = ans->n_groups; pa.group_starts = ans->group_starts; pa.shared = ans->shared;
+      return launch_paged_attention_shared(pa, dh, k.type == 1, ans->scratch, st);
     }
     ProfScope ps(PK_ATTN, attn_flops, st);
     const float* tb = (llama && !rotated) ? w.rope : nullptr;
@@ -1739,10 +1743,10 @@ qzo_status qzo_paged_attention_scratch_bytes(uint32_t n_rows, uint32_t n_seq, ui
   return QZO_OK;
 }
 
-qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows, uint32_t n_seq, uint32_t q_heads,
-                               const qzo_cache* cache, const int32_t* tables_dev, uint32_t max_blocks,
-                               const int32_t* lengths_dev, const int32_t* starts_dev, float scale, void* out_dev,
-                               uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream) {
+// The checks and arguments that both forms of the attention over the cache have in common.
+static qzo_status paged_args(const void* q_dev, uint64_t ld_q, uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, const qzo_cache* cache,
+                             const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev, float scale,
+                             void* out_dev, uint64_t ld_out, PagedArgs* args) {
   if (!q_dev || !cache || !tables_dev || !lengths_dev || !out_dev) return fail(QZO_ERR_ARG, "null pointer");
   if (!aligned16(q_dev) || !aligned16(tables_dev) || !aligned16(lengths_dev) || !aligned16(starts_dev) || !aligned16(out_dev))
     return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
@@ -1757,29 +1761,192 @@ qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows
   if (ld_q % 8 || ld_out % 8 || ld_q < row || ld_out < row) return fail(QZO_ERR_SHAPE, "ld_q and ld_out must be multiples of 8 that hold a row");
   if (ld_q >= (1ull << 32) || ld_out >= (1ull << 32)) return fail(QZO_ERR_SHAPE, "ld_q and ld_out must be below 2^32");
   if (!std::isfinite(scale)) return fail(QZO_ERR_ARG, "scale not finite");
-  const uint64_t need = paged_attention_scratch(n_rows, n_seq, q_heads, cache->head_dim);
-  if (need) {
-    if (!scratch_dev) return fail(QZO_ERR_ARG, "scratch_dev is null");
-    if ((uintptr_t)scratch_dev & 255u) return fail(QZO_ERR_ALIGN, "scratch not 256-byte aligned");
-    if (scratch_bytes < need) return fail(QZO_ERR_WORKSPACE, "scratch too small: see qzo_paged_attention_scratch_bytes");
-  }
-  PagedArgs a = {};
+  PagedArgs& a = *args;
   a.q = (const bf16_t*)q_dev; a.ld_q = ld_q; a.out = (bf16_t*)out_dev; a.ld_out = ld_out;
   a.n_rows = n_rows; a.n_seq = n_seq; a.q_heads = q_heads; a.kv_heads = cache->kv_heads; a.group = q_heads / cache->kv_heads;
   a.k = cache->k_dev; a.v = cache->v_dev; a.k_scale = cache->k_scale_dev; a.v_scale = cache->v_scale_dev;
   a.n_blocks = cache->n_blocks; a.block_shift = (uint32_t)__builtin_ctz(cache->block); a.max_blocks = max_blocks;
   a.tables = tables_dev; a.lengths = lengths_dev; a.starts = starts_dev; a.scale = scale;
+  return QZO_OK;
+}
+static qzo_status scratch_check(const void* scratch_dev, uint64_t scratch_bytes, uint64_t need, const char* too_small) {
+  if (!need) return QZO_OK;
+  if (!scratch_dev) return fail(QZO_ERR_ARG, "scratch_dev is null");
+  if ((uintptr_t)scratch_dev & 255u) return fail(QZO_ERR_ALIGN, "scratch not 256-byte aligned");
+  if (scratch_bytes < need) return fail(QZO_ERR_WORKSPACE, too_small);
+  return QZO_OK;
+}
+
+qzo_status qzo_paged_attention(const void* q_dev, uint64_t ld_q, uint32_t n_rows, uint32_t n_seq, uint32_t q_heads,
+                               const qzo_cache* cache, const int32_t* tables_dev, uint32_t max_blocks,
+                               const int32_t* lengths_dev, const int32_t* starts_dev, float scale, void* out_dev,
+                               uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream) {
+  PagedArgs a = {};
+  qzo_status st = paged_args(q_dev, ld_q, n_rows, n_seq, q_heads, cache, tables_dev, max_blocks, lengths_dev, starts_dev, scale, out_dev, ld_out, &a);
+  if (st != QZO_OK) return st;
+  st = scratch_check(scratch_dev, scratch_bytes, paged_attention_scratch(n_rows, n_seq, q_heads, cache->head_dim),
+                     "scratch too small: see qzo_paged_attention_scratch_bytes");
+  if (st != QZO_OK) return st;
   QZO_HIP(launch_paged_attention(a, cache->head_dim, cache->type == 1, scratch_dev, (hipStream_t)stream));
+  return QZO_OK;
+}
+
+static qzo_status groups_check(uint32_t n_groups, const int32_t* group_starts_dev, const int32_t* shared_dev) {
+  if (!group_starts_dev || !shared_dev) return fail(QZO_ERR_ARG, "null device pointer");
+  if (!aligned16(group_starts_dev) || !aligned16(shared_dev)) return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  if (!n_groups || n_groups > SHARED_MAX_GROUPS) return fail(QZO_ERR_SHAPE, "n_groups must be 1 .. 2048");
+  return QZO_OK;
+}
+
+qzo_status qzo_paged_attention_shared_scratch_bytes(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                                                    uint64_t* out) {
+  if (!out) return fail(QZO_ERR_ARG, "out is null");
+  qzo_status st = paged_shape(n_rows, n_seq, q_heads, head_dim);
+  if (st != QZO_OK) return st;
+  if (!kv_heads || q_heads % kv_heads) return fail(QZO_ERR_SHAPE, "q_heads must be a multiple of kv_heads");
+  *out = paged_attention_shared_scratch(n_rows, q_heads, kv_heads, head_dim);
+  return QZO_OK;
+}
+
+qzo_status qzo_paged_attention_shared(const void* q_dev, uint64_t ld_q, uint32_t n_rows, uint32_t n_seq, uint32_t q_heads,
+                                      const qzo_cache* cache, const int32_t* tables_dev, uint32_t max_blocks,
+                                      const int32_t* lengths_dev, const int32_t* starts_dev, uint32_t n_groups,
+                                      const int32_t* group_starts_dev, const int32_t* shared_dev, float scale, void* out_dev,
+                                      uint64_t ld_out, void* scratch_dev, uint64_t scratch_bytes, void* stream) {
+  SharedArgs a = {};
+  qzo_status st = paged_args(q_dev, ld_q, n_rows, n_seq, q_heads, cache, tables_dev, max_blocks, lengths_dev, starts_dev, scale, out_dev, ld_out, &a);
+  if (st != QZO_OK) return st;
+  st = groups_check(n_groups, group_starts_dev, shared_dev);
+  if (st != QZO_OK) return st;
+  st = scratch_check(scratch_dev, scratch_bytes, paged_attention_shared_scratch(n_rows, q_heads, cache->kv_heads, cache->head_dim),
+                     "scratch too small: see qzo_paged_attention_shared_scratch_bytes");
+  if (st != QZO_OK) return st;
+  a.n_groups = n_groups; a.group_starts = group_starts_dev; a.shared = shared_dev;
+  QZO_HIP(launch_paged_attention_shared(a, cache->head_dim, cache->type == 1, scratch_dev, (hipStream_t)stream));
+  return QZO_OK;
+}
+
+// ---- sequences that fork ----
+static qzo_status fork_shape(uint32_t n_seq, uint32_t block, uint32_t n_blocks, uint32_t max_blocks) {
+  if (block < 16 || block > 256 || (block & (block - 1))) return fail(QZO_ERR_SHAPE, "block must be 16, 32, 64, 128 or 256");
+  if (!n_blocks || (uint64_t)n_blocks * block >= (1ull << 31)) return fail(QZO_ERR_SHAPE, "n_blocks * block must be 1 .. 2^31 - 1");
+  if (!n_seq || n_seq > CACHE_MAX_SEQ) return fail(QZO_ERR_SHAPE, "n_seq must be 1 .. 8192");
+  if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31) || (uint64_t)max_blocks * block >= (1ull << 31))
+    return fail(QZO_ERR_SHAPE, "n_seq * max_blocks and max_blocks * block must be 1 .. 2^31 - 1");
+  return QZO_OK;
+}
+qzo_status qzo_cache_fork_scratch_bytes(uint32_t n_seq, uint32_t n_blocks, uint32_t max_blocks, uint64_t* out) {
+  if (!out) return fail(QZO_ERR_ARG, "out is null");
+  qzo_status st = fork_shape(n_seq, 16, n_blocks, max_blocks);
+  if (st != QZO_OK) return st;
+  *out = cache_fork_scratch(n_seq, n_blocks, max_blocks);
+  return QZO_OK;
+}
+qzo_status qzo_cache_fork(const int32_t* parents_dev, uint32_t n_seq, uint32_t block, uint32_t n_blocks, uint32_t max_blocks,
+                          int32_t* lengths_dev, int32_t* tables_dev, int32_t* free_dev, qzo_cache_state* state_dev,
+                          uint32_t n_groups, const int32_t* group_starts_dev, int32_t* shared_dev, qzo_block_copy* copies_dev,
+                          void* scratch_dev, uint64_t scratch_bytes, void* stream) {
+  const void* all[] = {parents_dev, lengths_dev, tables_dev, free_dev, state_dev, copies_dev};
+  for (const void* p : all)
+    if (!p) return fail(QZO_ERR_ARG, "null device pointer");
+  if (n_groups ? !group_starts_dev || !shared_dev : group_starts_dev || shared_dev) return fail(QZO_ERR_ARG, "groups have starts and a shared length");
+  for (const void* p : all)
+    if (!aligned16(p)) return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  if (!aligned16(group_starts_dev) || !aligned16(shared_dev)) return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  qzo_status st = fork_shape(n_seq, block, n_blocks, max_blocks);
+  if (st != QZO_OK) return st;
+  if (n_groups > n_seq) return fail(QZO_ERR_SHAPE, "more groups than sequences");
+  st = scratch_check(scratch_dev, scratch_bytes, cache_fork_scratch(n_seq, n_blocks, max_blocks), "scratch too small: see qzo_cache_fork_scratch_bytes");
+  if (st != QZO_OK) return st;
+  ForkArgs a = {};
+  a.parents = parents_dev; a.n_seq = n_seq; a.block_shift = (uint32_t)__builtin_ctz(block); a.n_blocks = n_blocks; a.max_blocks = max_blocks;
+  a.lengths = lengths_dev; a.tables = tables_dev; a.free = free_dev; a.state = state_dev;
+  a.n_groups = n_groups; a.group_starts = group_starts_dev; a.shared = shared_dev; a.copies = copies_dev;
+  QZO_HIP(launch_cache_fork(a, scratch_dev, (hipStream_t)stream));
+  return QZO_OK;
+}
+qzo_status qzo_cache_compact(uint32_t n_seq, uint32_t block, uint32_t n_blocks, uint32_t max_blocks, const int32_t* lengths_dev,
+                             const int32_t* tables_dev, int32_t* new_tables_dev, int32_t* free_dev, qzo_cache_state* state_dev,
+                             qzo_block_copy* copies_dev, void* scratch_dev, uint64_t scratch_bytes, void* stream) {
+  const void* all[] = {lengths_dev, tables_dev, new_tables_dev, free_dev, state_dev, copies_dev};
+  for (const void* p : all)
+    if (!p) return fail(QZO_ERR_ARG, "null device pointer");
+  for (const void* p : all)
+    if (!aligned16(p)) return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  qzo_status st = fork_shape(n_seq, block, n_blocks, max_blocks);
+  if (st != QZO_OK) return st;
+  st = scratch_check(scratch_dev, scratch_bytes, cache_fork_scratch(n_seq, n_blocks, max_blocks), "scratch too small: see qzo_cache_fork_scratch_bytes");
+  if (st != QZO_OK) return st;
+  ForkArgs a = {};
+  a.n_seq = n_seq; a.block_shift = (uint32_t)__builtin_ctz(block); a.n_blocks = n_blocks; a.max_blocks = max_blocks;
+  a.lengths = const_cast<int32_t*>(lengths_dev); a.tables = const_cast<int32_t*>(tables_dev); a.new_tables = new_tables_dev; a.free = free_dev;
+  a.state = state_dev; a.copies = copies_dev;
+  QZO_HIP(launch_cache_compact(a, scratch_dev, (hipStream_t)stream));
+  return QZO_OK;
+}
+qzo_status qzo_cache_copy(const qzo_cache* cache, uint32_t n_layers, const qzo_block_copy* copies_dev, uint32_t n_copies,
+                          const int32_t* count_dev, void* stream) {
+  if (!cache || !copies_dev) return fail(QZO_ERR_ARG, "null pointer");
+  if (!aligned16(copies_dev) || ((uintptr_t)count_dev & 3u)) return fail(QZO_ERR_ALIGN, "copies must be 16-byte, count 4-byte aligned");
+  qzo_status st = cache_check(cache);
+  if (st != QZO_OK) return st;
+  if (!n_layers || n_layers > 65535) return fail(QZO_ERR_SHAPE, "n_layers must be 1 .. 65535");
+  if (n_copies >= (1u << 31)) return fail(QZO_ERR_SHAPE, "n_copies must be below 2^31");
+  if ((uint64_t)n_layers * cache->kv_heads * 2 >= (1ull << 32)) return fail(QZO_ERR_SHAPE, "n_layers * kv_heads must be below 2^31");
+  CopyArgs a = {cache->k_dev, cache->v_dev, n_layers, cache->n_blocks, (uint32_t)__builtin_ctz(cache->block), cache->kv_heads,
+                cache->head_dim * (cache->type ? 1u : 2u), copies_dev, n_copies, count_dev};
+  QZO_HIP(launch_cache_copy(a, (hipStream_t)stream));
+  return QZO_OK;
+}
+
+static qzo_status beam_shape(uint32_t n_groups, uint32_t width, uint32_t vocab) {
+  if (!n_groups || !width || width > BEAM_MAX_WIDTH || (uint64_t)n_groups * width > CACHE_MAX_SEQ) return fail(QZO_ERR_SHAPE, "need a width of 1 .. 64 and 1 .. 8192 rows");
+  if (!vocab || vocab > BEAM_MAX_VOCAB) return fail(QZO_ERR_SHAPE, "vocab must be 1 .. 2^22");
+  return QZO_OK;
+}
+qzo_status qzo_beam_select_scratch_bytes(uint32_t n_groups, uint32_t width, uint32_t vocab, uint64_t* out) {
+  if (!out) return fail(QZO_ERR_ARG, "out is null");
+  qzo_status st = beam_shape(n_groups, width, vocab);
+  if (st != QZO_OK) return st;
+  *out = beam_select_scratch(n_groups * width, width, vocab);
+  return QZO_OK;
+}
+qzo_status qzo_beam_select(const void* logits_dev, uint64_t ld_logits, uint32_t n_groups, uint32_t width, uint32_t vocab,
+                           int32_t end_token, double length_penalty, float* scores_dev, int32_t* counts_dev, int32_t* ended_dev,
+                           int32_t* history_dev, uint32_t max_history, int32_t* parents_dev, int32_t* chosen_dev,
+                           int32_t* tokens_dev, int32_t* added_dev, void* scratch_dev, uint64_t scratch_bytes, void* stream) {
+  const void* all[] = {logits_dev, scores_dev, counts_dev, ended_dev, parents_dev, chosen_dev, tokens_dev, added_dev};
+  for (const void* p : all)
+    if (!p) return fail(QZO_ERR_ARG, "null device pointer");
+  if ((history_dev != nullptr) != (max_history != 0)) return fail(QZO_ERR_ARG, "a history has columns");
+  for (const void* p : all)
+    if (p != logits_dev && !aligned16(p)) return fail(QZO_ERR_ALIGN, "device pointer not 16-byte aligned");
+  if (!aligned16(history_dev) || ((uintptr_t)logits_dev & 1u)) return fail(QZO_ERR_ALIGN, "device pointer not aligned");
+  qzo_status st = beam_shape(n_groups, width, vocab);
+  if (st != QZO_OK) return st;
+  if (ld_logits < vocab || ld_logits >= (1ull << 32)) return fail(QZO_ERR_SHAPE, "ld_logits must hold a row and be below 2^32");
+  if (max_history >= (1u << 31)) return fail(QZO_ERR_SHAPE, "max_history must be below 2^31");
+  if (end_token < -1 || end_token >= (int32_t)vocab) return fail(QZO_ERR_ARG, "end_token must be -1 or a token");
+  if (!std::isfinite(length_penalty) || length_penalty < 0.0) return fail(QZO_ERR_ARG, "length_penalty must be finite and not negative");
+  st = scratch_check(scratch_dev, scratch_bytes, beam_select_scratch(n_groups * width, width, vocab), "scratch too small: see qzo_beam_select_scratch_bytes");
+  if (st != QZO_OK) return st;
+  BeamArgs a = {};
+  a.logits = (const bf16_t*)logits_dev; a.ld = ld_logits; a.n_rows = n_groups * width; a.width = width; a.vocab = vocab;
+  a.end_token = end_token; a.penalty = length_penalty; a.scores = scores_dev; a.counts = counts_dev; a.ended = ended_dev;
+  a.history = history_dev; a.max_history = max_history; a.parents = parents_dev; a.chosen = chosen_dev; a.tokens = tokens_dev; a.added = added_dev;
+  QZO_HIP(launch_beam_select(a, scratch_dev, (hipStream_t)stream));
   return QZO_OK;
 }
 
 // Workspace of qzo_answer: that of a forward over as many rows, then the attention's scratch and the last tokens' hidden states.
 struct AnswerSpace { uint64_t scratch_off, last_off, total; };
-static AnswerSpace answer_space(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq) {
+static AnswerSpace answer_space(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq, bool groups) {
   const qzo_model_config& c = m->cfg;
+  const uint32_t dh = c.d_model / c.n_heads;
   AnswerSpace s;
   s.scratch_off = up256(carve(m, n_tokens, 1, nullptr).total);
-  s.last_off = s.scratch_off + up256(paged_attention_scratch(n_tokens, n_seq, c.n_heads, c.d_model / c.n_heads));
+  s.last_off = s.scratch_off + up256(groups ? paged_attention_shared_scratch(n_tokens, c.n_heads, c.n_heads, dh)
+                                            : paged_attention_scratch(n_tokens, n_seq, c.n_heads, dh));
   s.total = s.last_off + up256((uint64_t)n_seq * c.d_model * 2);
   return s;
 }
@@ -1799,14 +1966,21 @@ qzo_status qzo_answer_workspace_bytes(const qzo_model* m, uint32_t n_tokens, uin
   if (!out) return fail(QZO_ERR_ARG, "null argument");
   qzo_status st = answer_check(m, n_tokens, n_seq);
   if (st != QZO_OK) return st;
-  *out = answer_space(m, n_tokens, n_seq).total;
+  *out = answer_space(m, n_tokens, n_seq, false).total;
+  return QZO_OK;
+}
+qzo_status qzo_answer_shared_workspace_bytes(const qzo_model* m, uint32_t n_tokens, uint32_t n_seq, uint64_t* out) {
+  if (!out) return fail(QZO_ERR_ARG, "null argument");
+  qzo_status st = answer_check(m, n_tokens, n_seq);
+  if (st != QZO_OK) return st;
+  *out = answer_space(m, n_tokens, n_seq, true).total;
   return QZO_OK;
 }
 
-qzo_status qzo_answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_seq, const qzo_cache* cache,
-                      const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev,
-                      const int32_t* slots_dev, const int32_t* positions_dev, void* workspace_dev, uint64_t workspace_bytes,
-                      void* logits_dev, void* stream) {
+static qzo_status answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_seq, const qzo_cache* cache,
+                         const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev,
+                         const int32_t* slots_dev, const int32_t* positions_dev, uint32_t n_groups, const int32_t* group_starts_dev,
+                         const int32_t* shared_dev, void* workspace_dev, uint64_t workspace_bytes, void* logits_dev, void* stream) {
   qzo_status st = answer_check(m, n_tokens, n_seq);
   if (st != QZO_OK) return st;
   const void* all[] = {tokens_dev, tables_dev, lengths_dev, starts_dev, slots_dev, positions_dev, workspace_dev, logits_dev};
@@ -1821,13 +1995,31 @@ qzo_status qzo_answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens
   if (cache->kv_heads != m->cfg.n_heads || cache->head_dim != m->cfg.d_model / m->cfg.n_heads) return fail(QZO_ERR_SHAPE, "the cache has other heads than the model");
   if (!max_blocks || (uint64_t)n_seq * max_blocks >= (1ull << 31) || (uint64_t)max_blocks * cache->block > (1ull << 30))
     return fail(QZO_ERR_SHAPE, "n_seq * max_blocks must be 1 .. 2^31 - 1, max_blocks * block at most 2^30");
-  const AnswerSpace sp = answer_space(m, n_tokens, n_seq);
-  if (workspace_bytes < sp.total) return fail(QZO_ERR_WORKSPACE, "workspace smaller than qzo_answer_workspace_bytes");
+  const AnswerSpace sp = answer_space(m, n_tokens, n_seq, n_groups != 0);
+  if (workspace_bytes < sp.total) return fail(QZO_ERR_WORKSPACE, "workspace smaller than qzo_answer_workspace_bytes or qzo_answer_shared_workspace_bytes");
   unsigned char* base = (unsigned char*)workspace_dev;
   const Answer ans = {cache, tables_dev, lengths_dev, starts_dev, slots_dev, positions_dev, n_seq, max_blocks,
-                      base + sp.scratch_off, base + sp.last_off, logits_dev};
+                      base + sp.scratch_off, base + sp.last_off, logits_dev, n_groups, group_starts_dev, shared_dev};
   return forward(m, tokens_dev, n_tokens, 1, 0, 0.0f, carve(m, n_tokens, 1, workspace_dev), nullptr, (hipStream_t)stream, nullptr, 1, StepTail{},
                  &ans);
+}
+
+qzo_status qzo_answer(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_seq, const qzo_cache* cache,
+                      const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev,
+                      const int32_t* slots_dev, const int32_t* positions_dev, void* workspace_dev, uint64_t workspace_bytes,
+                      void* logits_dev, void* stream) {
+  return answer(m, tokens_dev, n_tokens, n_seq, cache, tables_dev, max_blocks, lengths_dev, starts_dev, slots_dev, positions_dev, 0, nullptr, nullptr,
+                workspace_dev, workspace_bytes, logits_dev, stream);
+}
+
+qzo_status qzo_answer_shared(qzo_model* m, const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_seq, const qzo_cache* cache,
+                             const int32_t* tables_dev, uint32_t max_blocks, const int32_t* lengths_dev, const int32_t* starts_dev,
+                             const int32_t* slots_dev, const int32_t* positions_dev, uint32_t n_groups, const int32_t* group_starts_dev,
+                             const int32_t* shared_dev, void* workspace_dev, uint64_t workspace_bytes, void* logits_dev, void* stream) {
+  qzo_status st = groups_check(n_groups, group_starts_dev, shared_dev);
+  if (st != QZO_OK) return st;
+  return answer(m, tokens_dev, n_tokens, n_seq, cache, tables_dev, max_blocks, lengths_dev, starts_dev, slots_dev, positions_dev, n_groups,
+                group_starts_dev, shared_dev, workspace_dev, workspace_bytes, logits_dev, stream);
 }
 
 }  // extern "C"

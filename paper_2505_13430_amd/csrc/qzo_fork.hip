@@ -1,0 +1,399 @@
+// Sequences of the paged cache that fork: tables that share blocks, blocks given back and copied, a pool made compact.
+#include <algorithm>
+#include "qzo_device.hpp"
+#include "qzo_kernels.hpp"
+
+namespace qzo {
+namespace {
+
+constexpr uint32_t THREADS = 256, WAVES = THREADS / 64;
+
+// Inclusive sum over a workgroup's threads; total: of all of them.  red: [WAVES], read before the next call by way of its first barrier.
+__device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t* total, uint32_t* red) {
+  const uint32_t upto = lane_scan(v);
+  __syncthreads();
+  if ((threadIdx.x & 63u) == 63u) red[threadIdx.x >> 6] = upto;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+  const uint32_t waves = blockDim.x >> 6;
+  for (uint32_t w = 0; w < waves; ++w) {
+    if (w < (threadIdx.x >> 6)) before += red[w];
+    all += red[w];
+  }
+  *total = all;
+  return before + upto;
+}
+
+__device__ __forceinline__ uint32_t blocks_of(int32_t length, const ForkArgs& a) {       // of a length that the tables have room for
+  const uint32_t room = a.max_blocks << a.block_shift;
+  return (min((uint32_t)max(length, 0), room) + (1u << a.block_shift) - 1u) >> a.block_shift;
+}
+
+// ------------------------------------------------------------------ fork ----
+// A sequence of before lives on if it is any sequence's parent.  A block is free again if it was held, and by none that lives on.
+// Every held block gets a mark, the highest of its holders': n_seq + 1 of one that lives on, n_seq - i of sequence i that does
+// not.  So the mark tells which blocks are free, and which of several holders gives one back.
+//   1. mark: the tables are put aside (they are rewritten in place), the marks made.
+//   2. count: how many blocks each sequence gives back; the last workgroup to be done has all the counts, adds them up, and
+//      knows who takes a block for a copy and where from.
+//   3. write: tables, lengths, the stack, copies; the marks go back to zero.
+// Whole numbers and maxima: the order of the atomics changes nothing.
+__global__ __launch_bounds__(THREADS) void fork_mark_kernel(ForkArgs a) {
+  const uint32_t i = blockIdx.x, tid = threadIdx.x;
+  __shared__ uint32_t lives;
+  if (tid == 0) lives = 0;
+  __syncthreads();
+  bool found = false;
+  for (uint32_t j = tid; j < a.n_seq; j += THREADS) found |= a.parents[j] == (int32_t)i;
+  if (__any(found) && (tid & 63u) == 0) lives = 1;
+  __syncthreads();
+  const uint32_t mark = lives ? a.n_seq + 1u : a.n_seq - i, n = blocks_of(a.lengths[i], a);
+  if (tid == 0) a.old_lengths[i] = a.lengths[i];
+  const int32_t* const row = a.tables + (uint64_t)i * a.max_blocks;
+  int32_t* const aside = a.aside + (uint64_t)i * a.max_blocks;
+  for (uint32_t j = tid; j < n; j += THREADS) {
+    const int32_t id = row[j];
+    aside[j] = id;
+    if ((uint32_t)id < a.n_blocks) atomicMax(a.marks + id, mark);
+  }
+}
+
+__global__ __launch_bounds__(THREADS) void fork_count_kernel(ForkArgs a) {
+  const uint32_t i = blockIdx.x, tid = threadIdx.x;
+  __shared__ uint32_t red[WAVES], last, flags;
+  {
+    const uint32_t n = blocks_of(a.lengths[i], a);
+    const int32_t* const aside = a.aside + (uint64_t)i * a.max_blocks;
+    uint32_t count = 0, all;
+    for (uint32_t j = tid; j < n; j += THREADS) {
+      const int32_t id = aside[j];
+      count += (uint32_t)id < a.n_blocks && a.marks[id] == a.n_seq - i;
+    }
+    group_scan(count, &all, red);
+    if (tid == 0) {
+      __hip_atomic_store(a.given + i, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      last = atomicAdd(a.arrived, 1u) + 1u == a.n_seq;
+      flags = 0;
+    }
+  }
+  __syncthreads();
+  if (!last) return;
+  if (tid == 0) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  extern __shared__ int32_t first_child[];            // [n_seq]
+  for (uint32_t j = tid; j < a.n_seq; j += THREADS) first_child[j] = (int32_t)a.n_seq;
+  __syncthreads();
+  const int64_t room = (int64_t)a.max_blocks << a.block_shift;
+  uint32_t wrong = 0;
+  for (uint32_t j = tid; j < a.n_seq; j += THREADS) {
+    const int32_t p = a.parents[j], length = a.lengths[j];
+    if (p >= (int32_t)a.n_seq || length < 0) wrong |= 1u;
+    if (length > room) wrong |= 2u;
+    if (p >= 0 && p < (int32_t)a.n_seq) atomicMin(first_child + p, (int32_t)j);
+  }
+  if (wrong) atomicOr(&flags, wrong);
+  __syncthreads();
+  // a block of threads at a time: what the sequences before give back, which copy is a sequence's
+  auto copies = [&](uint32_t j) {
+    const int32_t p = a.parents[j];
+    return p >= 0 && p < (int32_t)a.n_seq && (a.lengths[p] & ((1 << a.block_shift) - 1)) && first_child[p] != (int32_t)j;
+  };
+  uint32_t n_back = 0, n_copy = 0;
+  for (uint32_t j0 = 0; j0 < a.n_seq; j0 += THREADS) {
+    const uint32_t j = j0 + tid;
+    const uint32_t back = j < a.n_seq ? __hip_atomic_load(a.given + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u, copy = j < a.n_seq && copies(j);
+    uint32_t all;
+    const uint32_t upto = group_scan(back, &all, red);
+    if (j < a.n_seq) a.given[j] = n_back + upto - back;
+    n_back += all;
+    const uint32_t which = group_scan(copy, &all, red);
+    if (j < a.n_seq) a.copy_of[j] = copy ? (int32_t)(n_copy + which - 1u) : -1;
+    if (copy) a.taker[n_copy + which - 1u] = (int32_t)j;
+    n_copy += all;
+  }
+  __syncthreads();
+  const int32_t n_free = a.state->n_free;
+  int32_t status = QZO_OK;
+  if ((flags & 1u) || n_free < 0 || (uint32_t)n_free > a.n_blocks) status = QZO_ERR_ARG;
+  else if (flags & 2u) status = QZO_ERR_SHAPE;
+  else if ((uint64_t)n_free + n_back > a.n_blocks) status = QZO_ERR_ARG;
+  else if (n_copy > (uint32_t)n_free + n_back) status = QZO_ERR_WORKSPACE;
+  if (tid == 0) {
+    const bool ok = status == QZO_OK;
+    *a.plan = ForkPlan{n_free, ok ? (int32_t)n_back : 0, ok ? (int32_t)n_copy : 0, status};
+    *a.state = qzo_cache_state{ok ? n_free + (int32_t)n_back - (int32_t)n_copy : n_free, 0, status, ok ? (int32_t)n_copy : 0};
+  }
+}
+
+__global__ __launch_bounds__(THREADS) void fork_write_kernel(ForkArgs a) {
+  const uint32_t tid = threadIdx.x;
+  const ForkPlan plan = *a.plan;
+  const bool ok = plan.status == QZO_OK;
+  const uint32_t shift = a.block_shift;
+  auto aside_of = [&](uint32_t s) { return a.aside + (uint64_t)s * a.max_blocks; };
+  if (blockIdx.x >= a.n_seq) {          // a group: how many of the blocks at the head are the same for all its sequences that live
+    const uint32_t g = blockIdx.x - a.n_seq;
+    const uint32_t s0 = (uint32_t)min(max(a.group_starts[g], 0), (int32_t)a.n_seq), s1 = max(s0, (uint32_t)min(max(a.group_starts[g + 1], 0), (int32_t)a.n_seq));
+    __shared__ uint32_t lead, same;
+    if (tid == 0) { lead = ~0u; same = ~0u; }
+    __syncthreads();
+    // (lengths may have been rewritten by now: those of before are aside)
+    auto full = [&](uint32_t s, uint32_t* from) -> uint32_t {
+      const int32_t p = ok ? a.parents[s] : (int32_t)s;
+      *from = (uint32_t)max(p, 0);
+      return p < 0 ? 0u : (uint32_t)min(max(a.old_lengths[p], 0), (int32_t)(a.max_blocks << shift));
+    };
+    uint32_t from;
+    for (uint32_t s = s0 + tid; s < s1; s += THREADS)
+      if (full(s, &from)) { atomicMin(&lead, s); break; }
+    __syncthreads();
+    if (lead != ~0u) {
+      uint32_t of_lead;
+      const uint32_t n_lead = full(lead, &of_lead) >> shift;
+      const int32_t* const x = aside_of(of_lead);
+      for (uint32_t s = s0; s < s1; ++s) {
+        const uint32_t length = full(s, &from);
+        if (!length) continue;
+        const uint32_t n = min(length >> shift, n_lead);
+        const int32_t* const y = aside_of(from);
+        if (tid == 0) atomicMin(&same, n);
+        if (from == of_lead) continue;
+        for (uint32_t j = tid; j < n; j += THREADS)
+          if (x[j] != y[j]) { atomicMin(&same, j); break; }
+      }
+    }
+    __syncthreads();
+    if (tid == 0) a.shared[g] = lead == ~0u ? 0 : (int32_t)(same << shift);
+    return;
+  }
+  const uint32_t i = blockIdx.x;
+  __shared__ uint32_t red[WAVES];
+  // ---- what old sequence i gives back: block number r of all is at n_free + r of the stack, or is taken by copy n_back - 1 - r
+  const uint32_t n_old = blocks_of(a.old_lengths[i], a);
+  const int32_t* const old = aside_of(i);
+  const uint32_t mine = a.n_seq - i;
+  const int32_t kept = plan.n_back - min(plan.n_back, plan.n_copy);           // of those given back that stay on the stack
+  uint32_t r0 = a.given[i];
+  for (uint32_t j0 = 0; j0 < n_old; j0 += THREADS) {
+    const uint32_t j = j0 + tid;
+    const int32_t id = j < n_old ? old[j] : -1;
+    const uint32_t mark = (uint32_t)id < a.n_blocks ? a.marks[id] : 0u;
+    uint32_t all;
+    const uint32_t r = r0 + group_scan(mark == mine, &all, red) - 1u;
+    r0 += all;
+    // who has the highest mark takes it away: nobody else's comparison above comes out another way
+    if (mark == mine || mark > a.n_seq) a.marks[id] = 0;
+    if (mark != mine || !ok) continue;
+    if ((int32_t)r < kept) {
+      a.free[plan.n_free + (int32_t)r] = id;
+    } else {
+      const int32_t k = plan.n_back - 1 - (int32_t)r, s = a.taker[k];
+      const int32_t length = a.old_lengths[a.parents[s]];
+      a.tables[(uint64_t)s * a.max_blocks + (uint32_t)(length >> shift)] = id;
+      a.copies[k].to = id;
+    }
+  }
+  // ---- new sequence i
+  if (!ok) return;
+  const int32_t p = a.parents[i], length = p < 0 ? 0 : a.old_lengths[p], k = a.copy_of[i];
+  if (tid == 0) a.lengths[i] = length;
+  if (p < 0) return;
+  const uint32_t n = (uint32_t)(length + (1 << shift) - 1) >> shift;
+  const int32_t* const from = aside_of((uint32_t)p);
+  int32_t* const to = a.tables + (uint64_t)i * a.max_blocks;
+  if (p != (int32_t)i)
+    for (uint32_t j = tid; j < (k < 0 ? n : n - 1u); j += THREADS) to[j] = from[j];
+  if (k >= 0 && tid == 0) {
+    a.copies[k].from = from[n - 1u];
+    a.copies[k].tokens = length & ((1 << shift) - 1);
+    a.copies[k].reserved = 0;
+    if (k >= plan.n_back) {             // one that was on the stack before
+      const int32_t id = a.free[plan.n_free - 1 - (k - plan.n_back)];
+      a.copies[k].to = id;
+      to[n - 1u] = id;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ compact ----
+// Held blocks are marked; n of them: those from n on go to the places below n that none holds, in order.
+constexpr uint32_t CHUNK = 8 * THREADS;           // blocks that a workgroup counts
+__global__ __launch_bounds__(THREADS) void compact_mark_kernel(ForkArgs a) {
+  const uint32_t i = blockIdx.x, n = blocks_of(a.lengths[i], a);
+  const int32_t* const row = a.tables + (uint64_t)i * a.max_blocks;
+  for (uint32_t j = threadIdx.x; j < n; j += THREADS)
+    if ((uint32_t)row[j] < a.n_blocks) a.marks[row[j]] = 1u;
+}
+__global__ __launch_bounds__(THREADS) void compact_count_kernel(ForkArgs a) {
+  const uint32_t tid = threadIdx.x, b0 = blockIdx.x * CHUNK + tid * 8u;
+  __shared__ uint32_t red[WAVES], last;
+  uint32_t count = 0, all;
+#pragma unroll
+  for (uint32_t x = 0; x < 8; ++x) count += b0 + x < a.n_blocks && a.marks[b0 + x];
+  group_scan(count, &all, red);
+  if (tid == 0) {
+    __hip_atomic_store(a.given + blockIdx.x, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = atomicAdd(a.arrived, 1u) + 1u == gridDim.x;
+  }
+  __syncthreads();
+  if (!last) return;
+  if (tid == 0) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  uint32_t held = 0;
+  for (uint32_t c0 = 0; c0 < gridDim.x; c0 += THREADS) {
+    const uint32_t c = c0 + tid, n = c < gridDim.x ? __hip_atomic_load(a.given + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+    const uint32_t upto = group_scan(n, &all, red);
+    if (c < gridDim.x) a.given[c] = held + upto - n;
+    held += all;
+  }
+  // held blocks before the first of the others' places: the chunk that n_held falls into is counted once more
+  const uint32_t chunk = min(held / CHUNK, gridDim.x - 1u);
+  __syncthreads();
+  count = 0;
+#pragma unroll
+  for (uint32_t x = 0; x < 8; ++x) {
+    const uint32_t b = chunk * CHUNK + tid * 8u + x;
+    count += b < held && b < a.n_blocks && a.marks[b];
+  }
+  group_scan(count, &all, red);
+  if (tid == 0) {
+    const uint32_t near = a.given[chunk] + all;
+    *a.plan = ForkPlan{(int32_t)held, (int32_t)near, 0, QZO_OK};
+    *a.state = qzo_cache_state{(int32_t)(a.n_blocks - held), 0, QZO_OK, (int32_t)(held - near)};
+  }
+}
+// Where each block goes: the i-th of the far ones keeps i + 1 in its mark until the tables have been rewritten, the others 0.
+__global__ __launch_bounds__(THREADS) void compact_place_kernel(ForkArgs a) {
+  const uint32_t tid = threadIdx.x, b0 = blockIdx.x * CHUNK + tid * 8u;
+  __shared__ uint32_t red[WAVES];
+  const uint32_t held = (uint32_t)a.plan->n_free, near = (uint32_t)a.plan->n_back;
+  uint32_t is[8], count = 0, all;
+#pragma unroll
+  for (uint32_t x = 0; x < 8; ++x) {
+    is[x] = b0 + x < a.n_blocks && a.marks[b0 + x];
+    count += is[x];
+  }
+  uint32_t before = a.given[blockIdx.x] + group_scan(count, &all, red) - count;
+#pragma unroll
+  for (uint32_t x = 0; x < 8; ++x) {
+    const uint32_t b = b0 + x;
+    if (b >= a.n_blocks) break;
+    if (is[x] && b >= held) a.copies[before - near].from = (int32_t)b;
+    if (!is[x] && b < held) a.copies[b - before].to = (int32_t)b;
+    a.place[b] = is[x] && b >= held ? before - near : ~0u;
+    a.marks[b] = 0;
+    before += is[x];
+    if (b < a.n_blocks - held) a.free[b] = (int32_t)(a.n_blocks - 1u - b);
+  }
+}
+__global__ __launch_bounds__(THREADS) void compact_write_kernel(ForkArgs a) {
+  const uint32_t tid = threadIdx.x;
+  if (blockIdx.x < a.n_seq) {
+    const uint32_t i = blockIdx.x, n = blocks_of(a.lengths[i], a);
+    for (uint32_t j = tid; j < n; j += THREADS) {
+      const uint64_t at = (uint64_t)i * a.max_blocks + j;
+      int32_t id = a.tables[at];
+      if ((uint32_t)id < a.n_blocks) {
+        const uint32_t r = a.place[id];
+        if (r != ~0u) id = a.copies[r].to;
+      }
+      a.new_tables[at] = id;
+    }
+    return;
+  }
+  const uint32_t moved = (uint32_t)a.state->n_taken;
+  for (uint32_t r = (blockIdx.x - a.n_seq) * THREADS + tid; r < moved; r += (gridDim.x - a.n_seq) * THREADS) {
+    a.copies[r].tokens = 1 << a.block_shift;
+    a.copies[r].reserved = 0;
+  }
+}
+
+// ------------------------------------------------------------------ copies ----
+// The first tokens of a block are consecutive for each layer, pool and head: such a run is a wavefront's, 16 bytes a lane, four times
+// on their way.
+__global__ __launch_bounds__(THREADS) void copy_blocks_kernel(CopyArgs a) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * WAVES + (threadIdx.x >> 6)));
+  const uint32_t n = a.count ? (uint32_t)min(max(*a.count, 0), (int32_t)a.n_copies) : a.n_copies;
+  const uint32_t runs = a.layers * 2u * a.kv_heads;             // of a block
+  const uint64_t all = (uint64_t)n * runs, run_bytes = (uint64_t)a.row_bytes << a.block_shift, pool = (uint64_t)a.n_blocks * a.kv_heads * run_bytes;
+  for (uint64_t w = wave; w < all; w += gridDim.x * WAVES) {
+    const uint32_t e = (uint32_t)(w / runs), run = (uint32_t)(w % runs), head = run % a.kv_heads, layer = run / a.kv_heads >> 1, is_v = run / a.kv_heads & 1u;
+    const qzo_block_copy c = a.copies[e];
+    if ((uint32_t)c.from >= a.n_blocks || (uint32_t)c.to >= a.n_blocks || c.from == c.to || c.tokens <= 0) continue;
+    const uint32_t bytes = min((uint32_t)c.tokens, 1u << a.block_shift) * a.row_bytes;
+    unsigned char* const base = (unsigned char*)(is_v ? a.v : a.k) + layer * pool;
+    const unsigned char* const from = base + ((uint64_t)c.from * a.kv_heads + head) * run_bytes;
+    unsigned char* const to = base + ((uint64_t)c.to * a.kv_heads + head) * run_bytes;
+    for (uint32_t at = lane * 16u; at < bytes; at += 4096u) {
+      uint4 x[4];
+#pragma unroll
+      for (uint32_t u = 0; u < 4; ++u)
+        if (at + u * 1024u < bytes) x[u] = *reinterpret_cast<const uint4*>(from + at + u * 1024u);
+#pragma unroll
+      for (uint32_t u = 0; u < 4; ++u)
+        if (at + u * 1024u < bytes) *reinterpret_cast<uint4*>(to + at + u * 1024u) = x[u];
+    }
+  }
+}
+
+uint32_t chunks_of(uint32_t n_blocks) { return (n_blocks + CHUNK - 1) / CHUNK; }
+uint64_t up16(uint64_t bytes) { return (bytes + 15) & ~15ull; }
+
+// Where a call's scratch holds what: the counter and the marks, which are zero between calls, then the rest.
+uint64_t carve_fork(ForkArgs* a, unsigned char* base, uint32_t n_seq, uint32_t n_blocks, uint32_t max_blocks) {
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) { const uint64_t was = at; at += up16(bytes); return base + was; };
+  uint32_t* arrived = (uint32_t*)take(16);
+  uint32_t* marks = (uint32_t*)take(4ull * n_blocks);
+  ForkPlan* plan = (ForkPlan*)take(sizeof(ForkPlan));
+  uint32_t* given = (uint32_t*)take(4ull * std::max(n_seq, chunks_of(n_blocks)));
+  int32_t* copy_of = (int32_t*)take(4ull * n_seq);
+  int32_t* taker = (int32_t*)take(4ull * n_seq);
+  int32_t* old_lengths = (int32_t*)take(4ull * n_seq);
+  int32_t* aside = (int32_t*)take(4ull * std::max<uint64_t>((uint64_t)n_seq * max_blocks, n_blocks));
+  if (a) { a->arrived = arrived; a->marks = marks; a->plan = plan; a->given = given; a->copy_of = copy_of; a->taker = taker; a->old_lengths = old_lengths; a->aside = aside; a->place = (uint32_t*)aside; }
+  return at;
+}
+
+}  // namespace
+
+uint64_t cache_fork_scratch(uint32_t n_seq, uint32_t n_blocks, uint32_t max_blocks) { return carve_fork(nullptr, nullptr, n_seq, n_blocks, max_blocks); }
+
+hipError_t launch_cache_fork(ForkArgs a, void* scratch, hipStream_t st) {
+  carve_fork(&a, (unsigned char*)scratch, a.n_seq, a.n_blocks, a.max_blocks);
+  fork_mark_kernel<<<a.n_seq, THREADS, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  fork_count_kernel<<<a.n_seq, THREADS, a.n_seq * 4, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  fork_write_kernel<<<a.n_seq + a.n_groups, THREADS, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_compact(ForkArgs a, void* scratch, hipStream_t st) {
+  carve_fork(&a, (unsigned char*)scratch, a.n_seq, a.n_blocks, a.max_blocks);
+  const uint32_t chunks = chunks_of(a.n_blocks);
+  compact_mark_kernel<<<a.n_seq, THREADS, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  compact_count_kernel<<<chunks, THREADS, 0, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  compact_place_kernel<<<chunks, THREADS, 0, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  compact_write_kernel<<<a.n_seq + std::min(chunks, 256u), THREADS, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+constexpr uint32_t COPY_WGS = 2048;
+hipError_t launch_cache_copy(const CopyArgs& a, hipStream_t st) {
+  const uint64_t waves = (uint64_t)a.n_copies * a.layers * 2 * a.kv_heads;
+  if (waves == 0) return hipSuccess;
+  copy_blocks_kernel<<<(uint32_t)std::min<uint64_t>((waves + WAVES - 1) / WAVES, COPY_WGS), THREADS, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace qzo

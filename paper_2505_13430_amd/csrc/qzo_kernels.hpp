@@ -378,6 +378,65 @@ struct PagedArgs {
 uint64_t paged_attention_scratch(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t head_dim);
 constexpr uint32_t PAGED_COUNTERS = 512;      // words at the head of its scratch, zero before a call and after it
 hipError_t launch_paged_attention(const PagedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st);
+// The next beams of every prompt (qzo_beam.hip).
+constexpr uint32_t BEAM_MAX_WIDTH = 64, BEAM_MAX_VOCAB = 1u << 22;
+struct BeamSum { double sum; float top; uint32_t unused; };        // of e^(x - top)
+struct BeamArgs {
+  const bf16_t* logits;
+  uint64_t ld;
+  uint32_t n_rows, width, vocab;
+  int32_t end_token;
+  double penalty;
+  float* scores;
+  int32_t *counts, *ended, *history;
+  uint32_t max_history;
+  int32_t *parents, *chosen, *tokens, *added;
+  // in the scratch, and how rows are cut
+  BeamSum* sums;
+  uint32_t *best, parts, span;
+};
+uint64_t beam_select_scratch(uint32_t n_rows, uint32_t width, uint32_t vocab);
+hipError_t launch_beam_select(BeamArgs a, void* scratch, hipStream_t st);
+
+// Groups of sequences that begin alike (qzo_shared.hip): group g is sequences group_starts[g] .. group_starts[g + 1] - 1.
+struct SharedArgs : PagedArgs {
+  uint32_t n_groups;
+  const int32_t *group_starts, *shared;         // [n_groups + 1], [n_groups]
+  float* shares;                                // [2][n_rows][q_heads][head_dim + 4], of the sequences' own keys, then of the common ones
+  uint32_t item_first, n_items;                 // a launch's: the groups first, then the sequences
+};
+// Sequences that fork, a pool made compact, copied blocks (qzo_fork.hip).
+struct ForkPlan { int32_t n_free, n_back, n_copy, status; };       // compact: blocks held, of them in place already
+struct ForkArgs {
+  const int32_t* parents;            // [n_seq]
+  uint32_t n_seq, block_shift, n_blocks, max_blocks;
+  int32_t *lengths, *tables, *free;
+  qzo_cache_state* state;
+  uint32_t n_groups;
+  const int32_t* group_starts;
+  int32_t* shared;
+  qzo_block_copy* copies;
+  int32_t* new_tables;               // compact only
+  // in the scratch
+  uint32_t *arrived, *marks, *given, *place;
+  ForkPlan* plan;
+  int32_t *copy_of, *taker, *old_lengths, *aside;
+};
+uint64_t cache_fork_scratch(uint32_t n_seq, uint32_t n_blocks, uint32_t max_blocks);       // of either call
+hipError_t launch_cache_fork(ForkArgs a, void* scratch, hipStream_t st);
+hipError_t launch_cache_compact(ForkArgs a, void* scratch, hipStream_t st);
+struct CopyArgs {
+  void *k, *v;                       // of layer 0
+  uint32_t layers, n_blocks, block_shift, kv_heads, row_bytes;       // row: a head's features of a token
+  const qzo_block_copy* copies;
+  uint32_t n_copies;
+  const int32_t* count;              // nullable
+};
+hipError_t launch_cache_copy(const CopyArgs& a, hipStream_t st);
+
+constexpr uint32_t SHARED_MAX_GROUPS = 2048;  // their starts stay in the LDS
+uint64_t paged_attention_shared_scratch(uint32_t n_rows, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim);
+hipError_t launch_paged_attention_shared(const SharedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st);
 // out[i] = x[starts[i + 1] - 1], the row of sequence i's last new token, or zeros where it has none (rows of d features, d % 8 == 0).
 hipError_t launch_last_rows(const void* x, const int32_t* starts, uint32_t n_rows, uint32_t n_seq, uint32_t d, void* out, hipStream_t st);
 

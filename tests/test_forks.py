@@ -1,0 +1,649 @@
+"""Sequences that fork: the next beams, tables that share blocks, a pool made compact, copied blocks, attention behind what a group has in
+common, against plain implementations in 64 bits (whole numbers: equal).
+
+Tolerances are what the roundings add up to.  eps/2 of bf16 is 2^-8, of e4m3 2^-4, of fp32 2^-24."""
+import ctypes as C
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_13430_amd import binding as qb
+from test_paged_cache import BAD_CACHES, _cache, _i32, _p, attention_reference, attention_tolerance
+
+DEV = "cuda:0"
+gpu = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ plain implementations ----
+def fork_reference(parents, lengths, tables, free, n_free, block, group_starts=()):
+    """tables, free numpy; returns a status or what the call leaves."""
+    n, most = tables.shape
+    if n_free < 0 or n_free > len(free) or max(parents) >= n or min(lengths) < 0:
+        return qb.QZO_ERR_ARG
+    if max(lengths) > most * block:
+        return qb.QZO_ERR_SHAPE
+    rows = [list(tables[i, :-(-lengths[i] // block)]) for i in range(n)]
+    stack, seen = list(free[:n_free]), set()
+    for p in parents:
+        if p >= 0:
+            seen |= set(rows[p])
+    for i in range(n):
+        if i not in parents:
+            for b in rows[i]:
+                if b not in seen and 0 <= b < len(free):
+                    seen.add(b)
+                    stack.append(b)
+    if len(stack) > len(free):
+        return qb.QZO_ERR_ARG
+    top, used, copies, after, length = len(stack), set(), [], tables.copy(), []
+    for i, p in enumerate(parents):
+        if p < 0:
+            length.append(0)
+            continue
+        row = list(rows[p])
+        if lengths[p] % block and p in used:
+            if not stack:
+                return qb.QZO_ERR_WORKSPACE
+            copies.append([row[-1], stack[-1], lengths[p] % block, 0])
+            row[-1] = stack.pop()
+        used.add(p)
+        after[i, :len(row)] = row
+        length.append(lengths[p])
+    out_free = free.copy()
+    out_free[n_free:len(stack)] = stack[n_free:]
+    return dict(lengths=length, tables=after, free=out_free, state=[len(stack), 0, 0, len(copies)], copies=copies,
+                shared=shared_reference(length, after, block, group_starts))
+
+
+def shared_reference(lengths, tables, block, group_starts):
+    out = []
+    for a, b in zip(group_starts[:-1], group_starts[1:]):
+        live, k = [i for i in range(a, b) if lengths[i] > 0], 0
+        while live and all(k < lengths[i] // block for i in live) and len({int(tables[i, k]) for i in live}) == 1:
+            k += 1
+        out.append(k * block)
+    return out
+
+
+def select_reference(logits, width, scores, counts, ended, history, end, alpha):
+    """logits fp64 [rows, vocab]; everything else lists.  Returns rows' outputs and the smallest distance of two keys that decides anything."""
+    rows, V = logits.shape
+    out = dict(scores=[], counts=[], ended=[], parents=[], chosen=[], added=[], history=history.copy())
+    gap = math.inf
+    for g in range(rows // width):
+        found = []
+        for b in range(width):
+            r = g * width + b
+            s, n = float(scores[r]), max(0, counts[r])
+            if not s > -math.inf:
+                continue
+            if ended[r]:
+                found.append((s / max(1, n) ** alpha, -(b * V + max(end, 0)), s))
+                continue
+            x = np.where(np.isfinite(logits[r]), logits[r], -np.inf)
+            if not np.isfinite(x).any():
+                continue
+            total = x - (np.log(np.exp(x - x.max()).sum()) + x.max()) + s
+            for v in np.argsort(-x, kind="stable")[:width + 1]:
+                if np.isfinite(x[v]):
+                    found.append((total[v] / (n + 1) ** alpha, -(b * V + int(v)), total[v]))
+        found.sort(reverse=True)
+        for x, y in zip(found[:width], found[1:width + 1]):
+            same_beam = -x[1] // V == -y[1] // V
+            gap = min(gap, math.inf if same_beam else x[0] - y[0] or math.inf)
+        for i in range(width):
+            row = g * width + i
+            if i >= len(found):
+                for name, v in (("scores", -math.inf), ("counts", 0), ("ended", 1), ("parents", -1), ("chosen", -1), ("added", 0)):
+                    out[name].append(v)
+                continue
+            _, place, total = found[i]
+            p, v = g * width + -place // V, -place % V
+            n, was = max(0, counts[p]), bool(ended[p])
+            done = was or v == end
+            for name, x in (("scores", total), ("counts", n + (not was)), ("ended", int(done)), ("parents", p), ("chosen", v), ("added", int(not done))):
+                out[name].append(x)
+            out["history"][row, :n] = history[p, :n]
+            if not was and n < history.shape[1]:
+                out["history"][row, n] = v
+    tokens = [v for v, on in zip(out["chosen"], out["added"]) if on]
+    out["tokens"] = tokens + [0] * (rows - len(tokens))
+    return out, gap
+
+
+# ------------------------------------------------------------------ refusals, on the host ----
+@pytest.mark.parametrize("over,status", [
+    (dict(parents=None), qb.QZO_ERR_ARG), (dict(copies=None), qb.QZO_ERR_ARG), (dict(groups=1), qb.QZO_ERR_ARG), (dict(starts=16), qb.QZO_ERR_ARG),
+    (dict(groups=1, starts=16, shared=24), qb.QZO_ERR_ALIGN), (dict(tables=24), qb.QZO_ERR_ALIGN), (dict(n_seq=0), qb.QZO_ERR_SHAPE),
+    (dict(n_seq=8193), qb.QZO_ERR_SHAPE), (dict(block=17), qb.QZO_ERR_SHAPE), (dict(block=512), qb.QZO_ERR_SHAPE), (dict(n_blocks=0), qb.QZO_ERR_SHAPE),
+    (dict(n_blocks=1 << 27), qb.QZO_ERR_SHAPE), (dict(max_blocks=0), qb.QZO_ERR_SHAPE), (dict(n_seq=4096, max_blocks=1 << 19), qb.QZO_ERR_SHAPE),
+    (dict(max_blocks=1 << 27), qb.QZO_ERR_SHAPE), (dict(groups=3, starts=16, shared=16), qb.QZO_ERR_SHAPE), (dict(scratch=None), qb.QZO_ERR_ARG),
+    (dict(scratch=128), qb.QZO_ERR_ALIGN), (dict(bytes=64), qb.QZO_ERR_WORKSPACE)])
+def test_fork_refuses(over, status):
+    v = dict(parents=16, n_seq=2, block=16, n_blocks=8, max_blocks=4, lengths=16, tables=16, free=16, state=16, groups=0, starts=None, shared=None, copies=16,
+             scratch=256, bytes=1 << 20)
+    v.update(over)
+    assert qb.lib().qzo_cache_fork(*v.values(), None) == status and qb.lib().qzo_last_error()
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(lengths=None), qb.QZO_ERR_ARG), (dict(new=None), qb.QZO_ERR_ARG), (dict(copies=8), qb.QZO_ERR_ALIGN), (dict(n_seq=0), qb.QZO_ERR_SHAPE), (dict(block=8), qb.QZO_ERR_SHAPE),
+    (dict(n_blocks=0), qb.QZO_ERR_SHAPE), (dict(scratch=None), qb.QZO_ERR_ARG), (dict(scratch=264), qb.QZO_ERR_ALIGN), (dict(bytes=0), qb.QZO_ERR_WORKSPACE)])
+def test_compact_refuses(over, status):
+    v = dict(n_seq=2, block=16, n_blocks=8, max_blocks=4, lengths=16, tables=16, new=16, free=16, state=16, copies=16, scratch=256, bytes=1 << 20)
+    v.update(over)
+    assert qb.lib().qzo_cache_compact(*v.values(), None) == status and qb.lib().qzo_last_error()
+
+
+@pytest.mark.parametrize("over,status", BAD_CACHES + [
+    (dict(_layers=0), qb.QZO_ERR_SHAPE), (dict(_layers=65536), qb.QZO_ERR_SHAPE), (dict(_copies=None), qb.QZO_ERR_ARG), (dict(_copies=24), qb.QZO_ERR_ALIGN),
+    (dict(_n=1 << 31), qb.QZO_ERR_SHAPE), (dict(_count=18), qb.QZO_ERR_ALIGN), (dict(kv_heads=65535, _layers=65535), qb.QZO_ERR_SHAPE)])
+def test_copy_refuses(over, status):
+    v = dict(_layers=2, _copies=16, _n=3, _count=None)
+    v.update({k: x for k, x in over.items() if k in v})
+    c = _cache(**{k: x for k, x in over.items() if k not in v})
+    assert qb.lib().qzo_cache_copy(C.addressof(c), *v.values(), None) == status and qb.lib().qzo_last_error()
+    assert qb.lib().qzo_cache_copy(None, 1, 16, 1, None, None) == qb.QZO_ERR_ARG
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(logits=None), qb.QZO_ERR_ARG), (dict(added=None), qb.QZO_ERR_ARG), (dict(history=None), qb.QZO_ERR_ARG), (dict(columns=0), qb.QZO_ERR_ARG),
+    (dict(logits=17), qb.QZO_ERR_ALIGN), (dict(scores=24), qb.QZO_ERR_ALIGN), (dict(groups=0), qb.QZO_ERR_SHAPE), (dict(width=0), qb.QZO_ERR_SHAPE),
+    (dict(width=65), qb.QZO_ERR_SHAPE), (dict(groups=2049), qb.QZO_ERR_SHAPE), (dict(vocab=0), qb.QZO_ERR_SHAPE), (dict(vocab=(1 << 22) + 1, ld=1 << 23), qb.QZO_ERR_SHAPE),
+    (dict(ld=99), qb.QZO_ERR_SHAPE), (dict(end=100), qb.QZO_ERR_ARG), (dict(end=-2), qb.QZO_ERR_ARG), (dict(alpha=-0.5), qb.QZO_ERR_ARG),
+    (dict(alpha=math.nan), qb.QZO_ERR_ARG), (dict(scratch=None), qb.QZO_ERR_ARG), (dict(bytes=16), qb.QZO_ERR_WORKSPACE)])
+def test_select_refuses(over, status):
+    v = dict(logits=16, ld=100, groups=2, width=4, vocab=100, end=-1, alpha=0.0, scores=16, counts=16, ended=16, history=16, columns=5, parents=16, chosen=16, tokens=16,
+             added=16, scratch=256, bytes=1 << 20)
+    v.update(over)
+    assert qb.lib().qzo_beam_select(*v.values(), None) == status and qb.lib().qzo_last_error()
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(q=None), qb.QZO_ERR_ARG), (dict(group_starts=None), qb.QZO_ERR_ARG), (dict(shared=None), qb.QZO_ERR_ARG), (dict(shared=20), qb.QZO_ERR_ALIGN),
+    (dict(groups=0), qb.QZO_ERR_SHAPE), (dict(groups=2049), qb.QZO_ERR_SHAPE), (dict(q_heads=3), qb.QZO_ERR_SHAPE), (dict(n_seq=0), qb.QZO_ERR_SHAPE),
+    (dict(ld_q=264), qb.QZO_ERR_ARG), (dict(ld_q=252), qb.QZO_ERR_SHAPE), (dict(scale=math.inf), qb.QZO_ERR_ARG), (dict(scratch=None), qb.QZO_ERR_ARG),
+    (dict(bytes=4096), qb.QZO_ERR_WORKSPACE)])
+def test_shared_attention_refuses(over, status):
+    c = _cache()
+    v = dict(q=16, ld_q=256, n_rows=2, n_seq=2, q_heads=4, cache=C.addressof(c), tables=16, max_blocks=4, lengths=16, starts=None, groups=1, group_starts=16, shared=16,
+             scale=0.1, out=16, ld_out=256, scratch=256, bytes=1 << 30)
+    v.update(over)
+    if over == dict(ld_q=264):          # a longer row is fine: what is refused is the next argument
+        v["scale"] = math.nan
+    assert qb.lib().qzo_paged_attention_shared(*v.values(), None) == status and qb.lib().qzo_last_error()
+
+
+@pytest.mark.parametrize("over", BAD_CACHES)
+def test_shared_attention_refuses_caches(over):
+    c = _cache(**over[0])
+    assert qb.lib().qzo_paged_attention_shared(16, 256, 2, 2, 4, C.addressof(c), 16, 4, 16, None, 1, 16, 16, 0.1, 16, 256, 256, 1 << 30, None) == over[1]
+
+
+# ------------------------------------------------------------------ forks ----
+def _fork(parents, lengths, tables, free, n_free, block, group_starts=()):
+    n = len(parents)
+    d = dict(lengths=_i32(lengths), tables=_i32(tables), free=_i32(free), state=_i32([n_free, 7, 7, 7]), copies=torch.full((n, 4), -9, dtype=torch.int32, device=DEV))
+    starts = _i32(group_starts) if len(group_starts) else None
+    shared = torch.full((len(group_starts) - 1,), -9, dtype=torch.int32, device=DEV) if len(group_starts) else None
+    qb.qzo_cache_fork(_i32(parents), block, *d.values(), group_starts=starts, shared=shared)
+    torch.cuda.synchronize()
+    out = {k: v.cpu().numpy() for k, v in d.items()}
+    out["shared"] = [] if shared is None else shared.tolist()
+    return out
+
+
+def _check_fork(parents, lengths, tables, free, n_free, block, group_starts=()):
+    want, got = fork_reference(parents, lengths, tables, free, n_free, block, group_starts), _fork(parents, lengths, tables, free, n_free, block, group_starts)
+    if not isinstance(want, dict):
+        want = dict(lengths=lengths, tables=tables, free=free, state=[n_free, 0, want, 0], copies=[], shared=got["shared"])
+    assert list(got["lengths"]) == list(want["lengths"]) and (got["tables"] == want["tables"]).all() and (got["free"] == want["free"]).all()
+    assert list(got["state"]) == want["state"] and got["shared"] == want["shared"]
+    k = len(want["copies"])
+    assert got["copies"][:k].tolist() == want["copies"] and (got["copies"][k:] == -9).all()
+    return want
+
+
+def _forest(lengths, block, most, spare, seed, alike=()):
+    """Tables of sequences; in every range of `alike` they share the blocks that the shortest one has in full."""
+    rng = np.random.default_rng(seed)
+    need = [-(-x // block) for x in lengths]
+    ids = rng.permutation(sum(need) + spare).astype(np.int32)
+    tables, at = np.full((len(lengths), most), -5, dtype=np.int32), 0
+    for i, k in enumerate(need):
+        tables[i, :k] = ids[at:at + k]
+        at += k
+    free = np.full(len(ids), -6, dtype=np.int32)
+    unused = list(ids[at:])
+    for a, b in alike:
+        k = min(lengths[a:b]) // block
+        for i in range(a + 1, b):
+            unused += list(tables[i, :k])
+            tables[i, :k] = tables[a, :k]
+    free[:len(unused)] = unused
+    return tables, free, len(unused)
+
+
+@gpu
+@pytest.mark.parametrize("parents", [[0, 1, 2, 3], [0, 0, 0, 0], [3, 3, 3, 3], [3, 2, 1, 0], [1, 0, 0, -1], [-1, -1, -1, -1], [2, 2, 0, 0], [-1, 3, -1, 3], [1, 2, 3, 0]])
+@pytest.mark.parametrize("lengths", [[40, 40, 40, 40], [48, 32, 1, 0], [16, 33, 100, 64], [0, 0, 0, 0], [5, 5, 5, 5]])
+def test_fork(parents, lengths):
+    tables, free, n_free = _forest(lengths, 16, 9, 5, 1)
+    _check_fork(parents, lengths, tables, free, n_free, 16, [0, 4])
+    tables, free, n_free = _forest(lengths, 16, 7, 3, 2, [(0, 2), (2, 4)])
+    _check_fork(parents, lengths, tables, free, n_free, 16, [0, 2, 4])
+    _check_fork(parents, lengths, tables, free, n_free, 16)
+
+
+@gpu
+@pytest.mark.parametrize("n,width,block,longest,seed", [(1, 1, 16, 50, 0), (6, 3, 32, 400, 1), (65, 5, 16, 90, 2), (300, 4, 64, 3000, 3), (1100, 11, 16, 700, 4), (8192, 64, 16, 33, 5),
+                                                        (7, 7, 16, 20000, 6), (40, 40, 256, 9000, 7)])
+def test_fork_again_and_again(n, width, block, longest, seed):
+    rng = np.random.default_rng(seed)
+    base = [int(x) for x in rng.integers(0, longest + 1, n // width + 1)]
+    lengths = [base[i // width] + int(rng.integers(0, 40)) for i in range(n)]
+    starts = list(range(0, n, width)) + [n]
+    tables, free, n_free = _forest(lengths, block, -(-(longest + 40) // block) + 1, n, seed, list(zip(starts[:-1], starts[1:])))
+    for turn in range(3):
+        parents = [int(rng.integers(starts[i // width], min(n, starts[i // width] + width))) if rng.random() < 0.8 else i if rng.random() < 0.7 else -1 for i in range(n)]
+        want = _check_fork(parents, lengths, tables, free, n_free, block, starts)
+        assert want["state"][2] == 0
+        lengths, tables, free, n_free = want["lengths"], want["tables"], want["free"], want["state"][0]
+
+
+@gpu
+@pytest.mark.parametrize("parents,lengths,n_free,status", [
+    ([0, 2], [5, 5], 1, qb.QZO_ERR_ARG), ([0, 0], [5, -1], 1, qb.QZO_ERR_ARG), ([0, 0], [5, 5], -1, qb.QZO_ERR_ARG), ([0, 0], [5, 5], 99, qb.QZO_ERR_ARG),
+    ([0, 0], [5, 65], 1, qb.QZO_ERR_SHAPE), ([0, 1], [5, 5], 0, 0), ([0, 0], [5, 0], 0, qb.QZO_ERR_WORKSPACE), ([0, 0], [5, 5], 0, 0), ([-1, -1], [5, 5], 3, qb.QZO_ERR_ARG)])
+def test_fork_that_cannot_be_made_changes_nothing(parents, lengths, n_free, status):
+    tables = np.array([[0, 1, 2, 3], [2, 3, 4, 5]], dtype=np.int32)
+    free = np.array([1, 3, 4, 0], dtype=np.int32)
+    want = fork_reference(parents, lengths, tables, free, n_free, 16)
+    assert (status == 0) == isinstance(want, dict) and (status == 0 or want == status)
+    _check_fork(parents, lengths, tables, free, n_free, 16)
+    tables, free, n_free = _forest([20, 20], 16, 4, 3, 1)         # and nothing is left behind in the scratch
+    for _ in range(2):
+        _check_fork([1, 1], [20, 20], tables, free, n_free, 16, [0, 2])
+
+
+@gpu
+def test_fork_with_blocks_outside_the_pool():
+    lengths, parents = [40, 40, 33, 20], [0, 0, 3, 3]
+    tables, free, n_free = _forest(lengths, 16, 4, 4, 3)
+    tables[1, 0], tables[2, 1], tables[3, 0] = len(free), -1, 1 << 30
+    _check_fork(parents, lengths, tables, free, n_free, 16, [0, 2, 4])
+
+
+@gpu
+def test_group_starts_outside_the_sequences():
+    lengths = [64, 64, 64]
+    tables, free, n_free = _forest(lengths, 16, 4, 4, 3, [(0, 3)])
+    got = _fork([0, 1, 2], lengths, tables, free, n_free, 16, [-5, 2, 2, 99])
+    assert got["shared"] == [64, 0, 64]
+
+
+# ------------------------------------------------------------------ compaction, copies ----
+@gpu
+@pytest.mark.parametrize("lengths,block,pool,alike", [
+    ([0], 16, 1, ()), ([1], 16, 1, ()), ([16], 16, 5, ()), ([40, 0, 33], 16, 50, ()), ([100, 100, 90, 90], 32, 23, [(0, 2), (2, 4)]), ([2000] * 30, 16, 9000, [(0, 30)]),
+    ([300] * 200, 16, 3801, ()), ([17] * 5000, 32, 40000, ()), ([30000], 16, 2048 * 16, ())])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_compact(lengths, block, pool, alike, in_place):
+    need = sum(-(-x // block) for x in lengths)
+    tables, _, _ = _forest(lengths, block, max(1, max(-(-x // block) for x in lengths)) + 1, max(0, pool - need), 5, alike)
+    pool = max(pool, need)
+    for _ in range(2):
+        t, free, state = _i32(tables), torch.full((pool,), -7, dtype=torch.int32, device=DEV), _i32([3, 3, 3, 3])
+        new, copies = t if in_place else torch.full_like(t, -8), torch.full((max(1, pool // 2), 4), -9, dtype=torch.int32, device=DEV)
+        qb.qzo_cache_compact(block, _i32(lengths), t, free, new, state, copies)
+        held = sorted({int(b) for i, x in enumerate(lengths) for b in tables[i, :-(-x // block)]})
+        k = len(held)
+        far, holes = [b for b in held if b >= k], sorted(set(range(k)) - set(held))
+        to = dict(zip(far, holes))
+        want = tables.copy() if in_place else np.full_like(tables, -8)
+        for i, x in enumerate(lengths):
+            want[i, :-(-x // block)] = [to.get(int(b), int(b)) for b in tables[i, :-(-x // block)]]
+        assert (new.cpu().numpy() == want).all() and (in_place or (t.cpu().numpy() == tables).all())
+        assert state.tolist() == [pool - k, 0, 0, len(far)]
+        assert free.tolist() == list(range(pool - 1, k - 1, -1)) + [-7] * k
+        assert copies[:len(far)].tolist() == [[b, to[b], block, 0] for b in far] and (copies[len(far):] == -9).all()
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("layers,heads,block,dh", [(1, 1, 16, 64), (3, 5, 32, 128), (2, 40, 256, 64), (5, 2, 128, 128)])
+def test_copy(layers, heads, block, dh, e4m3):
+    rng = np.random.default_rng(1)
+    pool = 23
+    k, v = (torch.randint(-2**31, 2**31 - 1, (layers, pool, heads, block, dh // (4 if e4m3 else 2)), dtype=torch.int32, device=DEV).view(torch.float8_e4m3fn if e4m3 else torch.bfloat16)
+            for _ in range(2))
+    cache = qb.make_cache(k[0], v[0])
+    ids = rng.permutation(pool)
+    entries = [[int(ids[2 * i]), int(ids[2 * i + 1]), int(t), 0] for i, t in enumerate([1, block, block - 1, 3, 0, block + 9, 7])]
+    entries += [[int(ids[20]), int(ids[20]), 5, 0], [-1, int(ids[21]), 5, 0], [int(ids[21]), pool, 5, 0], [int(ids[20]), int(ids[21]), -3, 0]]
+    for count in (None, 0, 3, 99, -4):
+        want = [x.view(torch.int16 if not e4m3 else torch.uint8).clone() for x in (k, v)]
+        n = len(entries) if count is None else max(0, min(count, len(entries)))
+        for a, b, t, _ in entries[:n]:
+            if 0 <= a < pool and 0 <= b < pool and a != b and t > 0:
+                for x in want:
+                    x[:, b, :, :min(t, block)] = x[:, a, :, :min(t, block)].clone()
+        qb.qzo_cache_copy(cache, _i32(entries), layers=layers, count=None if count is None else _i32([5, 5, 5, count]))
+        for x, y in zip((k, v), want):
+            assert torch.equal(x.view(y.dtype), y)
+
+
+@gpu
+def test_copy_beyond_32_bits():
+    block, heads, dh, n = 64, 16, 128, 20000                # 5.2 GB a pool
+    k, v = (torch.zeros(1, n, heads, block, dh, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    k[0, n - 1], v[0, n - 1] = 1.5, 2.5
+    qb.qzo_cache_copy(qb.make_cache(k[0], v[0]), _i32([[n - 1, n - 3, 20, 0], [n - 1, 2, 64, 0]]))
+    for x, y in ((k, 1.5), (v, 2.5)):
+        assert (x[0, n - 3, :, :20] == y).all() and (x[0, n - 3, :, 20:] == 0).all() and (x[0, 2] == y).all() and (x[0, n - 2] == 0).all() and (x[0, 3:9] == 0).all()
+
+
+# ------------------------------------------------------------------ the next beams ----
+def _select(logits, width, scores, counts, ended, history, end, alpha):
+    rows = logits.shape[0]
+    d = dict(scores=torch.tensor(scores, dtype=torch.float32, device=DEV), counts=_i32(counts), ended=_i32(ended),
+             history=_i32(history) if history.shape[1] else None, **{x: torch.full((rows,), -9, dtype=torch.int32, device=DEV) for x in ("parents", "chosen", "tokens", "added")})
+    qb.qzo_beam_select(logits, width, *d.values(), end_token=end, length_penalty=alpha)
+    return {k: v.cpu().numpy() if v is not None else history for k, v in d.items()}
+
+
+def _check_select(logits, width, scores, counts, ended, history, end, alpha):
+    want, gap = select_reference(logits.float().cpu().numpy().astype(np.float64), width, scores, counts, ended, history, end, alpha)
+    # a row's sum is off by a few 2^-24 of it (each term's exponential by two, rescalings by one each): keys further apart than that are in order
+    assert gap > 16 * 2.0 ** -24
+    got = _select(logits, width, scores, counts, ended, history, end, alpha)
+    for name in ("counts", "ended", "parents", "chosen", "added", "tokens"):
+        assert list(got[name]) == list(want[name]), name
+    assert (got["history"] == want["history"]).all()
+    w = np.array(want["scores"])
+    assert (np.isfinite(got["scores"]) == np.isfinite(w)).all()
+    fin = np.isfinite(w)
+    assert (np.abs(got["scores"][fin] - w[fin]) <= 2.0 ** -24 * np.abs(w[fin]) + 16 * 2.0 ** -24).all()
+    return got
+
+
+def _beams(groups, width, vocab, columns, seed, spread=2.0):
+    rng = np.random.default_rng(seed)
+    rows = groups * width
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    logits = (torch.randn(rows, vocab, generator=gen, device=DEV) * spread).to(torch.bfloat16)
+    counts = [int(x) for x in rng.integers(0, columns + 1, rows)]
+    scores = [float(np.float32(-3.0 * rng.random() * (1 + 0.1 * c))) for c in counts]
+    history = rng.integers(0, vocab, (rows, columns)).astype(np.int32)
+    return logits, scores, counts, history
+
+
+@gpu
+@pytest.mark.parametrize("alpha", [0.0, 0.7])
+@pytest.mark.parametrize("groups,width,vocab,columns,seed", [
+    (1, 1, 1, 0, 0), (1, 1, 50, 3, 1), (1, 4, 32000, 20, 2), (3, 5, 997, 7, 3), (2, 64, 300, 100, 4), (40, 3, 5001, 2, 5), (1, 8, 70000, 1, 6), (5, 33, 131, 11, 7),
+    (1, 64, 1 << 20, 9, 8), (300, 2, 1023, 400, 9), (2, 7, 3, 4, 10)])
+def test_select(groups, width, vocab, columns, seed, alpha):
+    logits, scores, counts, history = _beams(groups, width, vocab, columns, seed)
+    rows = groups * width
+    ended = [int(i % 7 == 3) for i in range(rows)]
+    scores = [-math.inf if i % 11 == 5 else s for i, s in enumerate(scores)]
+    _check_select(logits, width, scores, counts, ended, history, vocab // 2, alpha)
+    _check_select(logits, width, scores, counts, [0] * rows, history, -1, alpha)
+
+
+@gpu
+def test_select_at_the_start():
+    """One beam of every prompt is there; the next ones all come from it."""
+    logits, _, _, history = _beams(4, 6, 1000, 5, 3)
+    scores = [0.0 if i % 6 == 0 else -math.inf for i in range(24)]
+    logits[1::6] = math.nan                       # rows that are no beams are not looked at
+    got = _check_select(logits, 6, scores, [0] * 24, [0] * 24, history, 7, 0.0)
+    assert list(got["parents"]) == [i // 6 * 6 for i in range(24)]
+
+
+@gpu
+@pytest.mark.parametrize("vocab", [9, 1000, 40000])
+def test_select_ties_go_to_the_lower_beam_and_token(vocab):
+    logits = torch.zeros(6, vocab, dtype=torch.bfloat16, device=DEV)
+    logits[:, ::2] = -0.0
+    got = _check_select(logits, 3, [-1.0] * 6, [2] * 6, [0] * 6, np.zeros((6, 4), np.int32), -1, 0.0)
+    assert list(got["chosen"]) == [0, 1, 2] * 2 and list(got["parents"]) == [0, 0, 0, 3, 3, 3]
+    logits[1, vocab - 1] = logits[4, 5] = 2.0      # equal rows again, but for one token
+    logits[0, vocab - 1] = logits[3, 5] = 2.0
+    got = _check_select(logits, 3, [-1.0] * 6, [2] * 6, [0] * 6, np.zeros((6, 4), np.int32), -1, 0.0)
+    assert list(got["parents"][:2]) == [0, 1] and list(got["chosen"][:2]) == [vocab - 1, vocab - 1] and list(got["chosen"][3:5]) == [5, 5]
+
+
+@gpu
+def test_select_leaves_out_what_is_not_finite():
+    logits, scores, counts, history = _beams(3, 4, 3000, 6, 5)
+    logits[:, ::3], logits[:, 1::3] = -math.inf, math.nan
+    logits[2], logits[5, 2::3] = math.inf, math.inf
+    logits[4:8] = -math.inf
+    logits[4, 17], logits[6, 5] = 3.0, -200.0      # a prompt with two candidates for four beams
+    got = _check_select(logits, 4, scores, counts, [0] * 12, history, 17, 0.0)
+    assert sorted(got["chosen"][4:8]) == [-1, -1, 5, 17]
+    got = _check_select(torch.full_like(logits, -math.inf), 4, scores, counts, [0, 0, 1, 0] * 3, history, 17, 0.0)
+    assert list(got["chosen"]) == [17, -1, -1, -1] * 3
+
+
+@gpu
+@pytest.mark.parametrize("spread", [1e-3, 30.0, 1e4, 1e37])
+def test_select_of_flat_and_steep_logits(spread):
+    logits, scores, counts, history = _beams(2, 4, 5000, 6, 6, spread)
+    _check_select(logits, 4, scores, counts, [0] * 8, history, 3, 0.5)
+
+
+@gpu
+@pytest.mark.parametrize("vocab,skip", [(1001, 0), (1001, 3), (8192, 5), (513, 1), (17, 7)])
+def test_select_of_strided_rows(vocab, skip):
+    """Rows at any multiple of two bytes, NaN between them."""
+    logits, scores, counts, history = _beams(3, 3, vocab, 4, 7)
+    wide = torch.full((9, vocab + 13), math.nan, dtype=torch.bfloat16, device=DEV)
+    wide[:, skip:skip + vocab] = logits
+    got = _check_select(wide[:, skip:skip + vocab], 3, scores, counts, [0] * 9, history, 2, 0.0)
+    assert list(got["chosen"]) == list(_select(logits, 3, scores, counts, [0] * 9, history, 2, 0.0)["chosen"])
+
+
+@gpu
+def test_select_with_large_and_negative_counts():
+    logits, scores, counts, history = _beams(2, 3, 500, 5, 8)
+    counts = [3, 900, -4, 5, 2, 4]                  # longer than the history: no longer recorded
+    _check_select(logits, 3, scores, counts, [0, 0, 0, 0, 1, 0], history, 2, 1.0)
+
+
+@gpu
+def test_select_sees_all_of_a_falling_row():
+    """Every logit below the one before: the first tile has all the best; rising: every tile has better ones."""
+    x = torch.arange(60000, 0, -1, device=DEV).float().mul(2.0 ** -12).to(torch.bfloat16)
+    for row in (x, x.flip(0)):
+        _check_select(row.repeat(5, 1).contiguous() * torch.tensor([1.0, 0.5, 0.25, 2.0, 1.0], device=DEV, dtype=torch.bfloat16)[:, None], 5, [-1.0, -2.0, -3.0, -4.0, -1.5], [1] * 5, [0] * 5,
+                      np.zeros((5, 3), np.int32), -1, 0.0)
+
+
+# ------------------------------------------------------------------ attention behind what is shared ----
+def _attend(groups, shared, own, H, Hk, dh, block, news=None, e4m3=False, seed=0, spread=2.0, dead=(), claim=None, extra=3):
+    """groups: how many sequences each has; shared: what they have in common, own: each one's tokens behind that, news: of them the new ones (None: one, without
+    starts).  dead: sequences of length 0.  claim: what is passed as shared (default: all of it)."""
+    rng, gen = np.random.default_rng(seed), torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    n = sum(groups)
+    starts_g = [0] + list(np.cumsum(groups))
+    group = [g for g, k in enumerate(groups) for _ in range(k)]
+    lengths = [0 if i in dead else shared[group[i]] + own[i] for i in range(n)]
+    most = max(1, max(-(-x // block) for x in lengths)) + 1
+    need = [[-(-x // block)] for x in lengths]
+    pool = sum(x[0] for x in need) + sum(x // block for x in shared) + extra
+    ids = list(rng.permutation(pool))
+    tables = np.full((n, most), -1, np.int32)
+    for g in range(len(groups)):
+        k = shared[g] // block
+        common = [ids.pop() for _ in range(k)] if groups[g] else []
+        for i in range(starts_g[g], starts_g[g + 1]):
+            if lengths[i]:
+                tables[i, :need[i][0]] = common + [ids.pop() for _ in range(need[i][0] - k)]
+    shape = (pool, Hk, block, dh)
+    k, v = (torch.randn(shape, generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2))
+    # the shared part's last, open block: the same in everyone's own
+    for g in range(len(groups)):
+        live = [i for i in range(starts_g[g], starts_g[g + 1]) if lengths[i]]
+        r, at = shared[g] % block, shared[g] // block
+        for i in live[1:]:
+            if r:
+                for x in (k, v):
+                    x[tables[i, at], :, :r] = x[tables[live[0], at], :, :r]
+    scales = [None, None]
+    kk, vv = k, v
+    if e4m3:
+        scales = [torch.rand(Hk, generator=gen, device=DEV) * 0.2 + 0.05 for _ in range(2)]
+        kk, vv = ((x.float() * 4).to(torch.float8_e4m3fn) for x in (k, v))
+    new = [1] * n if news is None else [0 if i in dead else news[i] for i in range(n)]
+    starts = [0] + list(np.cumsum(new))
+    q = (torch.randn(starts[-1], H * dh, generator=gen, device=DEV) * spread).to(torch.bfloat16)
+    return dict(q=q, k=kk, v=vv, scales=scales, tables=_i32(tables), lengths=_i32(lengths), starts=None if news is None else _i32(starts), starts_list=starts, group_starts=_i32(starts_g),
+                shared=_i32(shared if claim is None else claim), H=H, dh=dh, scale=1.0 / math.sqrt(dh), pad=2)
+
+
+def _shared_call(d, **more):
+    cache = qb.make_cache(d["k"], d["v"], *d["scales"])
+    rows, width = d["q"].shape
+    q = torch.full((rows + d["pad"], width), math.nan, dtype=torch.bfloat16, device=DEV) if d["starts"] is not None else d["q"]
+    q[:rows] = d["q"]
+    out = torch.full_like(q, 77.0)
+    qb.qzo_paged_attention_shared(q, cache, d["tables"], d["lengths"], d["group_starts"], d["shared"], out, d["scale"], starts=d["starts"], **more)
+    assert (out[rows:] == 77.0).all()
+    return out[:rows]
+
+
+def _check_shared(d, parts=1):
+    got = _shared_call(d)
+    pools = []
+    for x, s in zip((d["k"], d["v"]), d["scales"]):
+        pools.append(x.double() if s is None else x.float().double() * s.double()[:, None, None])
+    q = d["q"].double().view(-1, d["H"], d["dh"])
+    want, mag, mac = attention_reference(q, *pools, d["tables"], d["lengths"].tolist(), d["starts_list"], d["scale"])
+    # joining two shares takes a few more fp32 steps: an exponential, two products and a sum each
+    tol = attention_tolerance(want, mag, mac, d["dh"]) + 16 * 2.0 ** -24 * mag
+    err = (got.double().view_as(want) - want).abs()
+    assert (err <= tol).all(), (err / tol).max()
+    return got
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("groups,shared,own,H,Hk,dh,block", [
+    ([4], [64], [1, 2, 17, 40], 4, 4, 128, 16), ([4], [500], [1, 20, 3, 16], 32, 32, 128, 16), ([2, 3], [100, 33], [5, 1, 9, 16, 50], 8, 2, 64, 32),
+    ([1, 5, 0, 2], [40, 300, 90, 0], [9, 3, 4, 5, 6, 7, 8, 100], 6, 2, 128, 64), ([64], [700], list(range(1, 65)), 8, 1, 64, 16), ([8] * 16, [i * 37 for i in range(16)], [1 + i % 23 for i in range(128)], 4, 4, 64, 16),
+    ([3] * 3, [15, 16, 17], [1] * 9, 5, 5, 128, 128), ([100], [2000], [1 + i * 3 for i in range(100)], 16, 2, 128, 32), ([2], [9000], [700, 1], 2, 2, 128, 16)])
+def test_attention_behind_what_is_shared(groups, shared, own, H, Hk, dh, block, e4m3):
+    _check_shared(_attend(groups, shared, own, H, Hk, dh, block, e4m3=e4m3, seed=len(own)))
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("groups,shared,own,news,H,Hk,dh,block", [
+    ([3], [48], [5, 6, 7], [5, 2, 7], 4, 2, 64, 16), ([12], [300], [9] * 12, [9] * 12, 10, 2, 64, 16), ([4, 4], [1000, 90], [40] * 8, [40] * 8, 4, 4, 128, 32),
+    ([2], [33], [200, 190], [200, 100], 8, 2, 128, 64), ([5, 3], [640, 64], [30, 1, 2, 3, 25, 90, 80, 70], [30, 1, 2, 0, 25, 90, 1, 70], 16, 2, 128, 16)])
+def test_several_new_tokens_behind_what_is_shared(groups, shared, own, news, H, Hk, dh, block, e4m3):
+    _check_shared(_attend(groups, shared, own, H, Hk, dh, block, news=news, e4m3=e4m3, seed=len(own)))
+
+
+@gpu
+@pytest.mark.parametrize("news", [None, [2, 2, 2, 2, 3]])
+def test_sequences_that_have_ended(news):
+    """Length 0, first of its group, too; without starts their rows become zero."""
+    for dead in ((0,), (2, 4), (1, 2, 3, 4), (0, 1, 2, 3, 4)):
+        d = _attend([5], [100], [5, 4, 3, 7, 9], 4, 2, 128, 16, news=news, dead=dead, seed=3)
+        got = _check_shared(d)
+        if news is None:
+            assert (got[list(dead)] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("claim", [[0, 0], [-7, 1 << 30], [20, 37], [64, 31], [90, 1]])
+def test_what_is_claimed_to_be_shared(claim):
+    """Less than is: any number of tokens.  More than a sequence has behind its new tokens: it reads its own."""
+    shared = [max(0, x) for x in claim]
+    d = _attend([3, 2], [96, 64], [7, 3, 20, 9, 1], 4, 2, 64, 32, seed=4, claim=claim)
+    if any(x > y for x, y in zip(shared, [96, 64])):
+        d["shared"] = _i32([claim[0], 1 << 30])      # beyond all lengths
+    _check_shared(d)
+
+
+@gpu
+def test_sequences_in_no_group():
+    d = _attend([2, 3, 2], [50, 64, 80], [5, 3, 20, 9, 1, 6, 7], 4, 2, 64, 16, seed=5)
+    d["group_starts"], d["shared"] = _i32([2, 5]), _i32([64])
+    _check_shared(d)
+    d["group_starts"], d["shared"] = _i32([-3, 2, 2, 5, 1000]), _i32([50, 9, 64, 80])
+    _check_shared(d)
+
+
+@gpu
+def test_shared_equals_unshared_bits_where_nothing_is():
+    d = _attend([3, 3], [0, 0], [300, 200, 4, 700, 1, 64], 8, 2, 128, 16, seed=6)
+    cache = qb.make_cache(d["k"], d["v"])
+    out = torch.zeros_like(d["q"])
+    qb.qzo_paged_attention(d["q"], cache, d["tables"], d["lengths"], out, d["scale"])
+    assert (_shared_call(d).float() - out.float()).abs().max() <= 2.0 ** -7 * out.float().abs().max()
+
+
+@gpu
+def test_unseen_positions_of_shared_blocks_hold_anything():
+    """Behind every sequence's last token, in blocks that nobody holds, in rows that are padding."""
+    for news in (None, [3, 1, 5, 2]):
+        d = _attend([2, 2], [48, 96], [5, 9, 20, 3], 4, 2, 128, 32, news=news, seed=7)
+        used = torch.zeros(d["k"].shape[0], 32, dtype=torch.bool, device=DEV)
+        for i, x in enumerate(d["lengths"].tolist()):
+            at = torch.arange(x, device=DEV)
+            used[d["tables"][i, at // 32].long(), at % 32] = True
+        for x in (d["k"], d["v"]):
+            y = torch.where(used[:, None, :, None], x, torch.tensor(math.nan, dtype=torch.bfloat16, device=DEV))
+            x.copy_(y)
+        want_k, want_v = (torch.where(used[:, None, :, None], x, torch.zeros_like(x)) for x in (d["k"], d["v"]))
+        got = _shared_call(d)
+        d["k"], d["v"] = want_k, want_v
+        assert torch.equal(got, _check_shared(d))
+
+
+@gpu
+def test_a_query_of_nan_stays_alone():
+    d = _attend([4], [200], [5, 9, 20, 3], 4, 4, 128, 16, seed=8)
+    want = _shared_call(d)
+    d["q"][2, :128] = math.nan
+    got = _shared_call(d)
+    assert got[2, :128].isnan().all()
+    got[2, :128] = want[2, :128]
+    assert torch.equal(got, want)
+
+
+@gpu
+def test_more_items_than_a_launch_has_room_for():
+    n, groups = 7000, 2000
+    d = _attend([3] * groups + [1] * (n - 3 * groups), [32] * groups + [0] * (n - 3 * groups), [1 + i % 9 for i in range(n)], 1, 1, 64, 16, seed=9)
+    d["group_starts"], d["shared"] = _i32([3 * i for i in range(groups + 1)]), _i32([32] * groups)
+    _check_shared(d)
+
+
+@gpu
+def test_strided_rows():
+    d = _attend([3, 2], [96, 64], [7, 3, 20, 9, 1], 4, 2, 64, 32, seed=4)
+    want = _shared_call(d)
+    wide, out = torch.zeros(5, 3 * 256, dtype=torch.bfloat16, device=DEV), torch.full((5, 512), 9.0, dtype=torch.bfloat16, device=DEV)
+    wide[:, 256:512] = d["q"]
+    qb.qzo_paged_attention_shared(wide[:, 256:512], qb.make_cache(d["k"], d["v"]), d["tables"], d["lengths"], d["group_starts"], d["shared"], out[:, :256], d["scale"])
+    assert torch.equal(out[:, :256], want) and (out[:, 256:] == 9.0).all()
+
+
+@gpu
+def test_the_same_call_gives_the_same_bits():
+    for seed, (groups, shared, H, Hk, dh) in enumerate([([8] * 4, [900, 30, 444, 0], 8, 8, 128), ([40], [3000], 16, 2, 64)]):
+        d = _attend(groups, shared, [1 + 5 * i for i in range(sum(groups))], H, Hk, dh, 16, seed=seed)
+        first = _shared_call(d)
+        for _ in range(5):
+            assert torch.equal(_shared_call(d), first)

@@ -208,16 +208,18 @@ class DeviceModel:
 
 class Answers:
     """Sequences that a DeviceModel continues: the pools of all layers, block tables, the free list, the lengths.  One call of `add`
-    per step; everything stays on the device."""
+    per step; everything stays on the device.  width: sequences i * width .. (i + 1) * width - 1 are a group that may come to share what
+    they begin with (`fork`), and attend to that together; the last group may be smaller."""
 
     def __init__(self, model: DeviceModel, n_seq: int, n_blocks: int, block: int = 32, max_blocks: int | None = None, e4m3: bool = False,
-                 k_scale=None, v_scale=None):
+                 k_scale=None, v_scale=None, width: int | None = None):
         sh, dev = model.shape, model.scales.device
         dh = sh["d_model"] // sh["n_heads"]
         self.model, self.block, self.vocab = model, block, sh["vocab"]
         size = (sh["n_layers"], n_blocks, sh["n_heads"], block, dh)
         self.k, self.v = (torch.empty(size, dtype=torch.float8_e4m3fn if e4m3 else torch.bfloat16, device=dev) for _ in range(2))
-        self.cache = qb.make_cache(self.k[0], self.v[0], k_scale, v_scale)
+        self.scales = (k_scale, v_scale)
+        self.cache = qb.make_cache(self.k[0], self.v[0], *self.scales)
         i32 = dict(dtype=torch.int32, device=dev)
         self.tables = torch.full((n_seq, max_blocks or n_blocks), -1, **i32)
         self.free = torch.arange(n_blocks, **i32)
@@ -225,12 +227,19 @@ class Answers:
         self.lengths, self.starts = torch.zeros(n_seq, **i32), torch.zeros(n_seq + 1, **i32)
         self.logits = torch.zeros(n_seq, self.vocab, dtype=torch.bfloat16, device=dev)
         self._kept = [(torch.zeros(0, **i32), torch.zeros(0, **i32), torch.zeros(0, dtype=torch.uint8, device=dev))]
+        self.group_starts = self.shared = None
+        if width is not None:
+            n_groups = -(-n_seq // width)
+            self.group_starts = torch.arange(n_groups + 1, **i32).mul_(width).clamp_(max=n_seq)
+            self.shared = torch.zeros(n_groups, **i32)
+        self.forked = width is not None
+        self.copies, self._fork_room, self._own = None, None, torch.arange(n_seq, **i32)
 
     def rows(self, n_tokens: int, stream=None):
         """Slots, positions and workspace of steps of that many rows, from buffers that double as they are outgrown; the earlier ones
         are kept for the graphs that were captured with them.  New ones are made on the stream that uses them."""
         slots, positions, ws = self._kept[-1]
-        need = qb.qzo_answer_workspace_bytes(self.model.handle, n_tokens, len(self.lengths))
+        need = qb.qzo_answer_workspace_bytes(self.model.handle, n_tokens, len(self.lengths), self.shared is not None)
         if slots.numel() < n_tokens or ws.numel() < need:
             dev, n = self.free.device, max(n_tokens, 2 * slots.numel())
             with torch.cuda.stream(stream):
@@ -245,6 +254,14 @@ class Answers:
         of the last new tokens: `logits`, the same buffer every step, which the next one overwrites (a graph that holds the step writes it, too;
         keep a copy of what is to outlive a step).  Whether the step could be planned is in state[2], where the caller may look (not QZO_OK: nothing has
         changed, the logits are zeros)."""
+        if self.forked:                         # what ends may share its blocks: they are given back by a fork
+            with torch.cuda.stream(stream):
+                parents = torch.where(added < 0, -1, self._own)
+                added = added.clamp(min=0)
+            self.fork(parents, stream)
+        return self._add(tokens, added, stream)
+
+    def _add(self, tokens, added, stream=None):
         slots, positions, ws = self.rows(max(1, tokens.numel()), stream)
         if tokens.numel() == 0:                 # a plan has room for one token: a sequence that would add any adds more, so that it is refused
             with torch.cuda.stream(stream):
@@ -253,5 +270,112 @@ class Answers:
         qb.qzo_cache_plan(self.lengths, added, self.block, self.tables, self.free, self.state, self.lengths, self.starts, slots, positions,
                           self.state, stream)
         if tokens.numel():
-            qb.qzo_answer(self.model.handle, tokens, self.cache, self.tables, self.lengths, self.starts, slots, positions, ws, self.logits, stream)
+            qb.qzo_answer(self.model.handle, tokens, self.cache, self.tables, self.lengths, self.starts, slots, positions, ws, self.logits, stream,
+                          group_starts=self.group_starts, shared=self.shared)
         return self.logits
+
+    def _for_forks(self, stream):
+        """List of copies and scratch of forks and compactions, made on the stream that uses them first."""
+        if self.copies is None:
+            n, n_blocks = len(self.lengths), self.free.numel()
+            with torch.cuda.stream(stream):
+                self.copies = torch.zeros(max(n, n_blocks // 2), 4, dtype=torch.int32, device=self.free.device)
+                self._fork_room = torch.zeros(qb.qzo_cache_fork_scratch_bytes(n, n_blocks, self.tables.shape[1]), dtype=torch.uint8, device=self.free.device)
+
+    def fork(self, parents: torch.Tensor, stream=None):
+        """parents int32 [n_seq]: sequence i goes on from what sequence parents[i] is (negative: it ends).  Full blocks are shared, open ones copied.
+        Whether there were blocks for that is in state[2], as for `add` (not QZO_OK: nothing has changed)."""
+        self._for_forks(stream)
+        self.forked = True
+        qb.qzo_cache_fork(parents, self.block, self.lengths, self.tables, self.free, self.state, self.copies, group_starts=self.group_starts,
+                          shared=self.shared, scratch=self._fork_room, stream=stream)
+        qb.qzo_cache_copy(self.cache, self.copies[:len(self.lengths)], layers=self.k.shape[0], count=self.state, stream=stream)
+
+    def compact(self, stream=None):
+        """The blocks in use to the front of the pools: those from n_blocks - state[0] on are free."""
+        self._for_forks(stream)
+        qb.qzo_cache_compact(self.block, self.lengths, self.tables, self.free, self.tables, self.state, self.copies, scratch=self._fork_room, stream=stream)
+        qb.qzo_cache_copy(self.cache, self.copies, layers=self.k.shape[0], count=self.state, stream=stream)
+
+    def resize(self, n_blocks: int):
+        """Pools of another number of blocks: memory given back to a training step between answers, or more of it.  Waits for the device; what
+        was captured with the old pools is no longer valid.  ValueError: the sequences hold more blocks than that (nothing has changed but their places)."""
+        self.compact()
+        free, had = int(self.state[0]), self.free.numel()
+        used = had - free
+        if n_blocks < max(1, used):
+            raise ValueError(f"{used} blocks are in use")
+        torch.cuda.synchronize()
+        pools = []
+        for name in ("k", "v"):                 # one pool after the other: the old one's memory is free before the next is made
+            old = getattr(self, name)
+            new = torch.empty((old.shape[0], n_blocks, *old.shape[2:]), dtype=old.dtype, device=old.device)
+            new.view(torch.uint8)[:, :used].copy_(old.view(torch.uint8)[:, :used])
+            setattr(self, name, new)
+            self.cache = None
+            del old
+        self.cache = qb.make_cache(self.k[0], self.v[0], *self.scales)
+        i32 = dict(dtype=torch.int32, device=self.free.device)
+        self.free = torch.full((n_blocks,), -1, **i32)
+        self.free[:n_blocks - used] = torch.arange(n_blocks - 1, used - 1, -1, **i32)
+        self.state[0] = n_blocks - used
+        self.copies = self._fork_room = None
+
+
+class Beams:
+    """Beam search with a DeviceModel: `width` beams for each of n_prompts prompts, over a cache whose blocks they share.  `search` runs it;
+    `start` and `step` are its parts, and a step, which leaves everything on the device, can be captured into a graph."""
+
+    def __init__(self, model: DeviceModel, n_prompts: int, width: int, n_blocks: int, max_new: int, end_token: int = -1, length_penalty: float = 0.0,
+                 block: int = 32, max_blocks: int | None = None, e4m3: bool = False, k_scale=None, v_scale=None):
+        n, dev = n_prompts * width, model.scales.device
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.answers = Answers(model, n, n_blocks, block, max_blocks, e4m3, k_scale, v_scale, width)
+        self.width, self.end_token, self.length_penalty = width, end_token, length_penalty
+        self.scores, self.history = torch.full((n,), -float("inf"), device=dev), torch.full((n, max_new), -1, **i32)
+        self.counts, self.ended, self.parents, self.chosen, self.tokens, self.added = (torch.zeros(n, **i32) for _ in range(6))
+        self.room = torch.zeros(qb.qzo_beam_select_scratch_bytes(n_prompts, width, self.answers.vocab), dtype=torch.uint8, device=dev)
+        self.failed = torch.zeros(1, **i32)
+
+    def _go_on(self, logits, stream):
+        a = self.answers
+        with torch.cuda.stream(stream):
+            torch.minimum(self.failed, a.state[2:3], out=self.failed)
+        qb.qzo_beam_select(logits, self.width, self.scores, self.counts, self.ended, self.history, self.parents, self.chosen, self.tokens, self.added,
+                           end_token=self.end_token, length_penalty=self.length_penalty, scratch=self.room, stream=stream)
+        a.fork(self.parents, stream)
+        with torch.cuda.stream(stream):
+            torch.minimum(self.failed, a.state[2:3], out=self.failed)
+
+    def start(self, tokens: torch.Tensor, lengths: torch.Tensor, stream=None):
+        """tokens int32, the prompts one behind the other; lengths int32 [n_prompts], at least 1.  The beams of before are given up."""
+        a = self.answers
+        with torch.cuda.stream(stream):
+            nobody = torch.full_like(self.parents, -1)
+            added = torch.zeros_like(self.added)
+            added[::self.width] = lengths
+            self.scores.fill_(-float("inf"))
+            self.scores[::self.width] = 0.0
+            for t in (self.counts, self.ended, self.failed):
+                t.zero_()
+            self.history.fill_(-1)
+        a.fork(nobody, stream)
+        self._go_on(a._add(tokens, added, stream), stream)
+
+    def step(self, stream=None):
+        """Every beam that has not ended by a token, and the next beams."""
+        self._go_on(self.answers._add(self.tokens, self.added, stream), stream)
+
+    def search(self, tokens: torch.Tensor, lengths: torch.Tensor, look_every: int = 8):
+        """Up to max_new tokens behind every prompt; now and then looks whether all beams have ended.  Returns history [n_prompts, width, max_new] (tokens,
+        behind a beam's last one -1), counts and scores [n_prompts, width], the best beam first.  RuntimeError: the cache has too few blocks."""
+        self.start(tokens, lengths)
+        for i in range(1, self.history.shape[1]):
+            if i % look_every == 0 and bool(self.ended.all()):
+                break
+            self.step()
+        if int(self.failed):
+            raise RuntimeError(f"the sequences did not fit the cache (status {int(self.failed)})")
+        column = torch.arange(self.history.shape[1], device=self.history.device)
+        history = torch.where(column < self.counts[:, None], self.history, -1)
+        return history.view(-1, self.width, self.history.shape[1]), self.counts.view(-1, self.width), self.scores.view(-1, self.width)

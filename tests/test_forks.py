@@ -11,6 +11,8 @@ import pytest
 import torch
 
 from paper_2505_13430_amd import binding as qb
+from paper_2505_13430_amd.model import Answers, Beams
+from test_answers import _apart, _far, _logits, _model
 from test_paged_cache import BAD_CACHES, _cache, _i32, _p, attention_reference, attention_tolerance
 
 DEV = "cuda:0"
@@ -647,3 +649,218 @@ def test_the_same_call_gives_the_same_bits():
         first = _shared_call(d)
         for _ in range(5):
             assert torch.equal(_shared_call(d), first)
+
+
+# ------------------------------------------------------------------ with a model ----
+@gpu
+@pytest.mark.parametrize("name,e4m3,width,alpha,end", [("tiny", False, 4, 0.0, -1), ("wide_heads", False, 3, 0.6, 5), ("tiny_opt", True, 5, 1.0, 7), ("tiny", False, 1, 0.0, -1)])
+def test_beams_of_a_model(name, e4m3, width, alpha, end):
+    """Every step's beams are those of the definition, given its logits; the logits are those of the model over prompt and history."""
+    m = _model(name, "int4")
+    rng = torch.Generator().manual_seed(4)
+    texts = [torch.randint(0, m.shape["vocab"], (n,), generator=rng, dtype=torch.int32).to(DEV) for n in (61, 16, 33)]
+    new = 20
+    b = Beams(m, 3, width, n_blocks=60, max_new=new, end_token=end, length_penalty=alpha, block=16, max_blocks=9, e4m3=e4m3)
+    b.start(torch.cat(texts), _i32([t.numel() for t in texts]))
+    a, n = b.answers, 3 * width
+    for turn in range(1, new):
+        before = {k: getattr(b, k).cpu().numpy().copy() for k in ("scores", "counts", "ended", "history")}
+        on = b.added.tolist()
+        # a beam's last token is not in the cache yet
+        assert a.lengths.tolist() == [texts[i // width].numel() + before["counts"][i] - 1 for i in range(n)]
+        b.step()
+        logits = a.logits.clone()
+        for i in range(n):
+            if on[i] and turn % 4 == 1:
+                text = torch.cat([texts[i // width], _i32(before["history"][i, :before["counts"][i]])])
+                want = _logits(m, text)
+                assert _far(logits[i], want[-1]) <= max(0.1 if e4m3 else 2e-2, 2 * _apart(m, text, want)), (turn, i)
+        want, gap = select_reference(logits.float().cpu().numpy().astype(np.float64), width, before["scores"], [int(x) for x in before["counts"]], before["ended"], before["history"], end, alpha)
+        assert gap > 16 * 2.0 ** -24
+        for k in ("counts", "ended", "parents", "chosen", "added", "tokens"):
+            assert getattr(b, k).tolist() == list(want[k]), k
+        assert (b.history.cpu().numpy() == want["history"]).all() and int(b.failed) == 0
+        _check_cache(a)
+    assert (a.shared >= torch.tensor([48, 16, 32], device=DEV)).all()       # the prompts' full blocks at least
+    history, counts, scores = Beams(m, 3, width, n_blocks=60, max_new=new, end_token=end, length_penalty=alpha, block=16, max_blocks=9, e4m3=e4m3).search(
+        torch.cat(texts), _i32([t.numel() for t in texts]), look_every=5)
+    assert torch.equal(counts.view(-1), b.counts) and torch.equal(scores.view(-1), b.scores)
+    for i in range(n):
+        assert history.view(n, -1)[i, :counts.view(-1)[i]].tolist() == b.history[i, :b.counts[i]].tolist()
+
+
+def _check_cache(a):
+    """Every block is held or free, once; open blocks are one sequence's."""
+    lengths, tables, free = a.lengths.tolist(), a.tables.cpu().numpy(), a.free[:int(a.state[0])].tolist()
+    held = [list(tables[i, :-(-x // a.block)]) for i, x in enumerate(lengths)]
+    all_held = {b for row in held for b in row}
+    assert len(free) == len(set(free)) and not all_held & set(free) and len(all_held) + len(free) == a.free.numel()
+    opened = [row[-1] for row, x in zip(held, lengths) if x % a.block]
+    assert len(opened) == len(set(opened)) and not any(b in row[:-1] for b in opened for row in held)
+
+
+@gpu
+def test_captured_beams_replay():
+    """A step captured into a graph writes the same beams as eager ones, the program's own work in between."""
+    m = _model("tiny", "int4")
+    tokens, lengths = torch.arange(70, dtype=torch.int32, device=DEV) * 11, _i32([50, 20])
+    seen = []
+    for captured in (False, True):
+        b = Beams(m, 2, 4, n_blocks=80, max_new=40, end_token=3, block=16, max_blocks=9)
+        for _ in range(2):                         # a second search in the same place
+            b.start(tokens, lengths)
+            b.step()
+            torch.cuda.synchronize()
+            if captured:
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g):
+                    b.step()
+            found = []
+            for i in range(25):
+                g.replay() if captured else b.step()
+                torch.cuda.synchronize()
+                m.forward_loss(tokens.view(1, -1)[:, :40].contiguous(), 1, 1e-3, 1)
+                found += [b.history.clone(), b.scores.clone(), b.answers.lengths.clone()]
+            assert int(b.failed) == 0
+            _check_cache(b.answers)
+            seen.append(found)
+    for other in seen[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(seen[0], other))
+
+
+@gpu
+def test_candidates_behind_a_prompt():
+    """A prompt once, candidates of several tokens behind it: the same logits as with a copy of the prompt for each."""
+    m = _model("tiny", "int4")
+    rng = torch.Generator().manual_seed(5)
+    prompt = torch.randint(0, 1024, (75,), generator=rng, dtype=torch.int32).to(DEV)
+    parts = [torch.randint(0, 1024, (k,), generator=rng, dtype=torch.int32).to(DEV) for k in (5, 1, 9, 30)]
+    a = Answers(m, n_seq=4, n_blocks=30, block=16, width=4)
+    a.add(prompt, _i32([75, 0, 0, 0]))
+    a.fork(_i32([0, 0, 0, 0]))
+    assert a.shared.tolist() == [64] and a.state.tolist() == [30 - 5 - 3, 0, 0, 3]
+    got = a.add(torch.cat(parts), _i32([p.numel() for p in parts])).clone()
+    for i, p in enumerate(parts):
+        text = torch.cat([prompt, p])
+        want = _logits(m, text)
+        assert _far(got[i], want[-1]) <= max(2e-2, 2 * _apart(m, text, want))
+    _check_cache(a)
+    a.add(torch.zeros(0, dtype=torch.int32, device=DEV), _i32([0, -1, -1, 0]))        # two end: what the others hold stays
+    assert a.lengths.tolist() == [80, 0, 0, 105]
+    _check_cache(a)
+    a.add(torch.zeros(2, dtype=torch.int32, device=DEV), _i32([-1, 2, 0, -1]))
+    assert a.lengths.tolist() == [0, 2, 0, 0] and a.shared.tolist() == [0]
+    _check_cache(a)
+
+
+@gpu
+def test_pools_of_another_size():
+    """Sequences are compacted into smaller pools, then larger ones, and go on as before."""
+    m = _model("tiny", "int4")
+    text = torch.randint(0, 1024, (120,), generator=torch.Generator().manual_seed(6), dtype=torch.int32).to(DEV)
+    for width in (None, 2):
+        runs = []
+        for resized in (False, True):
+            a = Answers(m, n_seq=4, n_blocks=40, block=16, max_blocks=9, width=width)
+            a.add(text, _i32([40, 17, 50, 13]))
+            a.fork(_i32([2, 1, 2, -1]))
+            if resized:
+                a.resize(12)
+                assert a.k.shape[1] == a.free.numel() == 12
+                _check_cache(a)
+            out = [a.add(text[:3].contiguous(), _i32([1, 1, 1, 0])).clone()]
+            if resized:
+                with pytest.raises(ValueError):
+                    a.resize(3)
+                _check_cache(a)
+                a.resize(100)
+                _check_cache(a)
+            out.append(a.add(text[:40].contiguous(), _i32([30, 1, 1, 8])).clone())
+            assert a.state.tolist()[2] == 0
+            runs.append(out)
+        for x, y in zip(*runs):
+            assert torch.equal(x, y)
+
+
+@gpu
+def test_a_fork_without_blocks_for_it():
+    m = _model("tiny", "int4")
+    a = Answers(m, n_seq=3, n_blocks=3, block=16, width=3)
+    a.add(torch.zeros(40, dtype=torch.int32, device=DEV), _i32([40, 0, 0]))
+    before = [x.clone() for x in (a.k.view(torch.int16), a.v.view(torch.int16), a.tables, a.lengths, a.free)]
+    a.fork(_i32([0, 0, -1]))
+    assert a.state.tolist() == [0, 0, qb.QZO_ERR_WORKSPACE, 0]
+    assert all(torch.equal(x, y) for x, y in zip(before, (a.k.view(torch.int16), a.v.view(torch.int16), a.tables, a.lengths, a.free)))
+    b = Beams(m, 1, 4, n_blocks=4, max_new=3, block=16)
+    with pytest.raises(RuntimeError):
+        b.search(torch.zeros(40, dtype=torch.int32, device=DEV), _i32([40]))
+
+
+@gpu
+def test_profile_of_an_answer_behind_what_is_shared():
+    m = _model("tiny", "int4")
+    a = Answers(m, n_seq=4, n_blocks=30, block=16, width=4)
+    a.add(torch.arange(20, dtype=torch.int32, device=DEV), _i32([20, 0, 0, 0]))
+    a.fork(_i32([0] * 4))
+    qb.qzo_profile_begin(100)
+    a._add(torch.arange(4, dtype=torch.int32, device=DEV), _i32([1] * 4))
+    got = qb.qzo_profile_collect(qb.PROFILE_KINDS["attention"])
+    assert got["launches"] == 2 and got["work"] == 0 and got["total_ms"] > 0
+
+
+# ------------------------------------------------------------------ streams, scratch ----
+@gpu
+def test_forks_on_two_streams_at_once():
+    """Scratch by stream: two pools of the same size, forked, selected and attended to at once."""
+    lengths, parents, starts = [700] * 60, [i // 2 * 2 for i in range(60)], list(range(0, 61, 4))
+    tables, free, n_free = _forest(lengths, 16, 45, 80, 1, [(i, i + 4) for i in range(0, 60, 4)])
+    want = fork_reference(parents, lengths, tables, free, n_free, 16, starts)
+    d = _attend([8] * 6, [400] * 6, [1 + i for i in range(48)], 4, 4, 128, 16, seed=2)
+    out_want = _shared_call(d)
+    logits, scores, counts, history = _beams(6, 8, 5000, 6, 2)
+    sel_want = _select(logits, 8, scores, counts, [0] * 48, history, -1, 0.0)
+    streams, got = [torch.cuda.Stream() for _ in range(3)], []
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for s in streams:
+            with torch.cuda.stream(s):
+                x = [_i32(lengths), _i32(tables), _i32(free), _i32([n_free, 0, 0, 0]), torch.zeros(60, 4, dtype=torch.int32, device=DEV)]
+                qb.qzo_cache_fork(_i32(parents), 16, *x, group_starts=_i32(starts), shared=torch.zeros(15, dtype=torch.int32, device=DEV))
+                o = torch.zeros_like(d["q"])
+                qb.qzo_paged_attention_shared(d["q"], qb.make_cache(d["k"], d["v"]), d["tables"], d["lengths"], d["group_starts"], d["shared"], o, d["scale"])
+                y = [torch.tensor(scores, device=DEV), _i32(counts), _i32([0] * 48), _i32(history)] + [torch.zeros(48, dtype=torch.int32, device=DEV) for _ in range(4)]
+                qb.qzo_beam_select(logits, 8, *y)
+                got.append((x, o, y))
+    torch.cuda.synchronize()
+    for x, o, y in got:
+        assert x[0].tolist() == list(want["lengths"]) and (x[1].cpu().numpy() == want["tables"]).all() and (x[2].cpu().numpy() == want["free"]).all()
+        assert x[3].tolist() == want["state"] and torch.equal(o, out_want) and (y[3].cpu().numpy() == sel_want["history"]).all()
+
+
+@gpu
+def test_captured_calls_need_scratch_of_their_own():
+    logits, scores, counts, history = _beams(1, 2, 100, 2, 1)
+    side = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    y = [torch.tensor(scores, device=DEV), _i32(counts), _i32([0] * 2), _i32(history)] + [torch.zeros(2, dtype=torch.int32, device=DEV) for _ in range(4)]
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):
+        with pytest.raises(AssertionError):
+            qb.qzo_beam_select(logits, 2, *y)
+        torch.zeros(4, device=DEV).add_(1)
+
+
+@gpu
+def test_operands_elsewhere_are_refused():
+    logits, scores, counts, history = _beams(1, 2, 100, 2, 1)
+    good = [torch.tensor(scores, device=DEV), _i32(counts), _i32([0] * 2), _i32(history)] + [torch.zeros(2, dtype=torch.int32, device=DEV) for _ in range(4)]
+    for i in range(len(good)):
+        for bad in (good[i].cpu(), good[i].long()):
+            with pytest.raises(AssertionError):
+                qb.qzo_beam_select(logits, 2, *good[:i], bad, *good[i + 1:])
+    with pytest.raises(AssertionError):
+        qb.qzo_beam_select(logits.float(), 2, *good)
+    with pytest.raises(qb.QzoError):
+        qb.qzo_beam_select(logits, 2, *good, scratch=torch.zeros(16, dtype=torch.uint8, device=DEV))
+    with pytest.raises(AssertionError):
+        qb.qzo_beam_select(logits, 2, *good, scratch=torch.zeros(1 << 20, dtype=torch.uint8))

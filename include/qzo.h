@@ -496,7 +496,8 @@ qzo_status qzo_cache_copy(const qzo_cache* cache, uint32_t n_layers, const qzo_b
  *     one behind the other, then zeros, as qzo_answer takes them.
  * Where there are fewer candidates than beams: score -infinity, count 0, ended 1, parent and token -1, history as it was.
  * scores, counts (negative: 0), ended and history are read and written in place.  All int32 but scores, 16-byte aligned.  Scratch: qzo_beam_select_scratch_bytes
- * bytes, 256-byte aligned, contents undefined before and after; calls that may overlap need scratch of their own.  width 1 .. 64, vocab 1 .. 2^22, at most
+ * bytes, 256-byte aligned; its first 33024 bytes are counters, zero before the first call that uses it and zero again after every call, whatever its
+ * sizes; the rest is undefined; calls that may overlap need scratch of their own.  width 1 .. 64, vocab 1 .. 2^22, at most
  * 8192 rows, ld_logits >= vocab, length_penalty finite and not negative, end_token -1 or below vocab; logits may be at any
  * multiple of 2 bytes.
  */

@@ -93,23 +93,29 @@ __global__ __launch_bounds__(THREADS) void fork_count_kernel(ForkArgs a) {
   }
   if (wrong) atomicOr(&flags, wrong);
   __syncthreads();
-  // a block of threads at a time: what the sequences before give back, which copy is a sequence's
+  // a few sequences a thread: what those before give back, which copy is a sequence's
+  const uint32_t per = (a.n_seq + THREADS - 1) / THREADS, j_first = min(tid * per, a.n_seq), j_end = min(j_first + per, a.n_seq);
   auto copies = [&](uint32_t j) {
     const int32_t p = a.parents[j];
     return p >= 0 && p < (int32_t)a.n_seq && (a.lengths[p] & ((1 << a.block_shift) - 1)) && first_child[p] != (int32_t)j;
   };
-  uint32_t n_back = 0, n_copy = 0;
-  for (uint32_t j0 = 0; j0 < a.n_seq; j0 += THREADS) {
-    const uint32_t j = j0 + tid;
-    const uint32_t back = j < a.n_seq ? __hip_atomic_load(a.given + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u, copy = j < a.n_seq && copies(j);
-    uint32_t all;
-    const uint32_t upto = group_scan(back, &all, red);
-    if (j < a.n_seq) a.given[j] = n_back + upto - back;
-    n_back += all;
-    const uint32_t which = group_scan(copy, &all, red);
-    if (j < a.n_seq) a.copy_of[j] = copy ? (int32_t)(n_copy + which - 1u) : -1;
-    if (copy) a.taker[n_copy + which - 1u] = (int32_t)j;
-    n_copy += all;
+  uint32_t n_back, n_copy, back = 0, copy = 0;
+#pragma unroll 4
+  for (uint32_t j = j_first; j < j_end; ++j) {
+    back += __hip_atomic_load(a.given + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    copy += copies(j);
+  }
+  back = group_scan(back, &n_back, red) - back;
+  copy = group_scan(copy, &n_copy, red) - copy;
+#pragma unroll 4
+  for (uint32_t j = j_first; j < j_end; ++j) {
+    const uint32_t n = __hip_atomic_load(a.given + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool one = copies(j);
+    a.before[j] = back;
+    a.copy_of[j] = one ? (int32_t)copy : -1;
+    if (one) a.taker[copy] = (int32_t)j;
+    back += n;
+    copy += one;
   }
   __syncthreads();
   const int32_t n_free = a.state->n_free;
@@ -173,7 +179,7 @@ __global__ __launch_bounds__(THREADS) void fork_write_kernel(ForkArgs a) {
   const int32_t* const old = aside_of(i);
   const uint32_t mine = a.n_seq - i;
   const int32_t kept = plan.n_back - min(plan.n_back, plan.n_copy);           // of those given back that stay on the stack
-  uint32_t r0 = a.given[i];
+  uint32_t r0 = a.before[i];
   for (uint32_t j0 = 0; j0 < n_old; j0 += THREADS) {
     const uint32_t j = j0 + tid;
     const int32_t id = j < n_old ? old[j] : -1;
@@ -212,6 +218,129 @@ __global__ __launch_bounds__(THREADS) void fork_write_kernel(ForkArgs a) {
       a.copies[k].to = id;
       to[n - 1u] = id;
     }
+  }
+}
+
+// The same with few sequences and a small pool, in one workgroup: tables and marks in the LDS.  Latency is all there is to it (8 beams behind 2500
+// tokens, in three launches 13.8 us).
+constexpr uint32_t SMALL_THREADS = 1024, SMALL_SEQ = 256, SMALL_ENTRIES = 16384, SMALL_BLOCKS = 16384;
+__global__ __launch_bounds__(SMALL_THREADS) void fork_small_kernel(ForkArgs a) {
+  extern __shared__ int32_t small_lds[];
+  int32_t* const aside = small_lds;                                       // [n_seq, max_blocks]
+  uint32_t* const marks = (uint32_t*)(aside + a.n_seq * a.max_blocks);    // [n_blocks]
+  __shared__ int32_t length[SMALL_SEQ], parent[SMALL_SEQ], first_child[SMALL_SEQ], copy_of[SMALL_SEQ], taker[SMALL_SEQ];
+  __shared__ uint32_t given[SMALL_SEQ], red[SMALL_THREADS / 64], flags;
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, shift = a.block_shift, mask = (1u << shift) - 1u;
+  const uint32_t WAVES16 = SMALL_THREADS / 64;
+  const int64_t room = (int64_t)a.max_blocks << shift;
+  const int32_t n_free = a.state->n_free;
+  if (tid == 0) flags = 0;
+  if (tid < a.n_seq) { length[tid] = a.lengths[tid]; parent[tid] = a.parents[tid]; first_child[tid] = (int32_t)a.n_seq; given[tid] = 0; }
+  for (uint32_t e = tid; e < a.n_seq * a.max_blocks; e += SMALL_THREADS) aside[e] = a.tables[e];
+  for (uint32_t b = tid; b < a.n_blocks; b += SMALL_THREADS) marks[b] = 0;
+  __syncthreads();
+  if (tid < a.n_seq) {
+    const int32_t p = parent[tid], l = length[tid];
+    const uint32_t wrong = (p >= (int32_t)a.n_seq || l < 0 ? 1u : 0u) | (l > room ? 2u : 0u);
+    if (wrong) atomicOr(&flags, wrong);
+    if (p >= 0 && p < (int32_t)a.n_seq) atomicMin(first_child + p, (int32_t)tid);
+  }
+  __syncthreads();
+  // a wavefront a sequence
+  for (uint32_t i = wave; i < a.n_seq; i += WAVES16) {
+    const uint32_t mark = first_child[i] < (int32_t)a.n_seq ? a.n_seq + 1u : a.n_seq - i, n = blocks_of(length[i], a);
+    for (uint32_t j = lane; j < n; j += 64) {
+      const int32_t id = aside[i * a.max_blocks + j];
+      if ((uint32_t)id < a.n_blocks) atomicMax(marks + id, mark);
+    }
+  }
+  __syncthreads();
+  auto mine = [&](uint32_t i, uint32_t j, uint32_t n) {
+    const int32_t id = j < n ? aside[i * a.max_blocks + j] : -1;
+    return (uint32_t)id < a.n_blocks && marks[id] == a.n_seq - i;
+  };
+  for (uint32_t i = wave; i < a.n_seq; i += WAVES16) {
+    if (first_child[i] < (int32_t)a.n_seq) continue;
+    const uint32_t n = blocks_of(length[i], a);
+    uint32_t count = 0;
+    for (uint32_t j0 = 0; j0 < n; j0 += 64) count += (uint32_t)__popcll(__ballot(mine(i, j0 + lane, n)));
+    if (lane == 0) given[i] = count;
+  }
+  __syncthreads();
+  const uint32_t back = tid < a.n_seq ? given[tid] : 0u;
+  const int32_t p0 = tid < a.n_seq ? parent[tid] : -1;
+  const uint32_t copy = p0 >= 0 && p0 < (int32_t)a.n_seq && ((uint32_t)length[p0] & mask) && first_child[p0] != (int32_t)tid;
+  uint32_t n_back, n_copy;
+  const uint32_t back_before = group_scan(back, &n_back, red) - back, copy_before = group_scan(copy, &n_copy, red) - copy;
+  int32_t status = QZO_OK;
+  if ((flags & 1u) || n_free < 0 || (uint32_t)n_free > a.n_blocks) status = QZO_ERR_ARG;
+  else if (flags & 2u) status = QZO_ERR_SHAPE;
+  else if ((uint64_t)n_free + n_back > a.n_blocks) status = QZO_ERR_ARG;
+  else if (n_copy > (uint32_t)n_free + n_back) status = QZO_ERR_WORKSPACE;
+  const bool ok = status == QZO_OK;
+  if (tid < a.n_seq) {
+    given[tid] = back_before;
+    copy_of[tid] = copy ? (int32_t)copy_before : -1;
+    if (copy) taker[copy_before] = (int32_t)tid;
+    if (ok) a.lengths[tid] = p0 < 0 ? 0 : length[p0];
+  }
+  if (tid == 0) *a.state = qzo_cache_state{ok ? n_free + (int32_t)n_back - (int32_t)n_copy : n_free, 0, status, ok ? (int32_t)n_copy : 0};
+  __syncthreads();
+  const int32_t kept = (int32_t)n_back - (int32_t)min(n_back, n_copy);
+  for (uint32_t i = wave; ok && i < a.n_seq; i += WAVES16) {
+    if (first_child[i] >= (int32_t)a.n_seq) {              // gives back
+      const uint32_t n = blocks_of(length[i], a);
+      int32_t r0 = (int32_t)given[i];
+      for (uint32_t j0 = 0; j0 < n; j0 += 64) {
+        const bool is = mine(i, j0 + lane, n);
+        const uint64_t who = __ballot(is);
+        const int32_t r = r0 + (int32_t)__popcll(who & ((1ull << lane) - 1ull));
+        r0 += (int32_t)__popcll(who);
+        if (!is) continue;
+        const int32_t id = aside[i * a.max_blocks + j0 + lane];
+        if (r < kept) {
+          a.free[n_free + r] = id;
+        } else {
+          const int32_t k = (int32_t)n_back - 1 - r, s = taker[k];
+          a.tables[(uint64_t)s * a.max_blocks + ((uint32_t)length[parent[s]] >> shift)] = id;
+          a.copies[k].to = id;
+        }
+      }
+    }
+    const int32_t p = parent[i], k = copy_of[i];
+    if (p < 0) continue;
+    const uint32_t n = ((uint32_t)length[p] + mask) >> shift;
+    if (p != (int32_t)i)
+      for (uint32_t j = lane; j < (k < 0 ? n : n - 1u); j += 64) a.tables[(uint64_t)i * a.max_blocks + j] = aside[(uint32_t)p * a.max_blocks + j];
+    if (k >= 0 && lane == 0) {
+      a.copies[k].from = aside[(uint32_t)p * a.max_blocks + n - 1u];
+      a.copies[k].tokens = (int32_t)((uint32_t)length[p] & mask);
+      a.copies[k].reserved = 0;
+      if (k >= (int32_t)n_back) {
+        const int32_t id = a.free[n_free - 1 - (k - (int32_t)n_back)];
+        a.copies[k].to = id;
+        a.tables[(uint64_t)i * a.max_blocks + n - 1u] = id;
+      }
+    }
+  }
+  // groups: a wavefront each
+  for (uint32_t g = wave; g < a.n_groups; g += WAVES16) {
+    const uint32_t s0 = (uint32_t)min(max(a.group_starts[g], 0), (int32_t)a.n_seq), s1 = max(s0, (uint32_t)min(max(a.group_starts[g + 1], 0), (int32_t)a.n_seq));
+    uint32_t lead = ~0u, same = ~0u;
+    for (uint32_t s = s0; s < s1; ++s) {
+      const int32_t p = ok ? parent[s] : (int32_t)s;
+      const uint32_t l = p < 0 ? 0u : (uint32_t)min((int64_t)max(length[p], 0), room);
+      if (!l) continue;
+      const uint32_t n = l >> shift;
+      if (lead == ~0u) { lead = (uint32_t)p; same = n; continue; }
+      same = min(same, n);
+      for (uint32_t j0 = 0; lead != (uint32_t)p && j0 < same; j0 += 64) {
+        const uint32_t j = j0 + lane;
+        const uint64_t other = __ballot(j < same && aside[lead * a.max_blocks + j] != aside[(uint32_t)p * a.max_blocks + j]);
+        if (other) { same = j0 + (uint32_t)__builtin_ctzll(other); break; }
+      }
+    }
+    if (lane == 0) a.shared[g] = lead == ~0u ? 0 : (int32_t)(same << shift);
   }
 }
 
@@ -310,29 +439,30 @@ __global__ __launch_bounds__(THREADS) void compact_write_kernel(ForkArgs a) {
 
 // ------------------------------------------------------------------ copies ----
 // The first tokens of a block are consecutive for each layer, pool and head: such a run is a wavefront's, 16 bytes a lane, four times
-// on their way.
+// on their way.  A row of the grid takes every gridDim.y-th entry.  An XCD sees to neighbouring layers, so that it has few pages' addresses to look up.
 __global__ __launch_bounds__(THREADS) void copy_blocks_kernel(CopyArgs a) {
   const uint32_t lane = threadIdx.x & 63u;
-  const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * WAVES + (threadIdx.x >> 6)));
+  // workgroups of an XCD (every eighth) take neighbouring runs
+  const uint32_t wg = (blockIdx.x & 7u) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  const uint32_t run = (uint32_t)__builtin_amdgcn_readfirstlane((int)(wg * WAVES + (threadIdx.x >> 6))), runs = a.layers * 2u * a.kv_heads;
   const uint32_t n = a.count ? (uint32_t)min(max(*a.count, 0), (int32_t)a.n_copies) : a.n_copies;
-  const uint32_t runs = a.layers * 2u * a.kv_heads;             // of a block
-  const uint64_t all = (uint64_t)n * runs, run_bytes = (uint64_t)a.row_bytes << a.block_shift, pool = (uint64_t)a.n_blocks * a.kv_heads * run_bytes;
-  for (uint64_t w = wave; w < all; w += gridDim.x * WAVES) {
-    const uint32_t e = (uint32_t)(w / runs), run = (uint32_t)(w % runs), head = run % a.kv_heads, layer = run / a.kv_heads >> 1, is_v = run / a.kv_heads & 1u;
+  if (run >= runs) return;
+  const uint32_t pool = run / a.kv_heads, head = run - pool * a.kv_heads;             // layer by layer, k and v
+  const uint64_t run_bytes = (uint64_t)a.row_bytes << a.block_shift;
+  unsigned char* const base = (unsigned char*)(pool & 1u ? a.v : a.k) + ((uint64_t)(pool >> 1) * a.n_blocks * a.kv_heads + head) * run_bytes;
+  const uint64_t block_bytes = run_bytes * a.kv_heads;
+  for (uint32_t e = blockIdx.y; e < n; e += gridDim.y) {
     const qzo_block_copy c = a.copies[e];
     if ((uint32_t)c.from >= a.n_blocks || (uint32_t)c.to >= a.n_blocks || c.from == c.to || c.tokens <= 0) continue;
     const uint32_t bytes = min((uint32_t)c.tokens, 1u << a.block_shift) * a.row_bytes;
-    unsigned char* const base = (unsigned char*)(is_v ? a.v : a.k) + layer * pool;
-    const unsigned char* const from = base + ((uint64_t)c.from * a.kv_heads + head) * run_bytes;
-    unsigned char* const to = base + ((uint64_t)c.to * a.kv_heads + head) * run_bytes;
+    const unsigned char* const from = base + (uint64_t)(uint32_t)c.from * block_bytes;
+    unsigned char* const to = base + (uint64_t)(uint32_t)c.to * block_bytes;
     for (uint32_t at = lane * 16u; at < bytes; at += 4096u) {
-      uint4 x[4];
-#pragma unroll
-      for (uint32_t u = 0; u < 4; ++u)
-        if (at + u * 1024u < bytes) x[u] = *reinterpret_cast<const uint4*>(from + at + u * 1024u);
-#pragma unroll
-      for (uint32_t u = 0; u < 4; ++u)
-        if (at + u * 1024u < bytes) *reinterpret_cast<uint4*>(to + at + u * 1024u) = x[u];
+      // loaded without a branch around them: what lies beyond is the last piece again
+      auto piece = [&](uint32_t u) { return *reinterpret_cast<const uint4*>(from + min(at + u * 1024u, bytes - 16u)); };
+      auto put = [&](uint32_t u, const uint4& x) { if (at + u * 1024u < bytes) *reinterpret_cast<uint4*>(to + at + u * 1024u) = x; };
+      const uint4 x0 = piece(0), x1 = piece(1), x2 = piece(2), x3 = piece(3);
+      put(0, x0); put(1, x1); put(2, x2); put(3, x3);
     }
   }
 }
@@ -348,11 +478,12 @@ uint64_t carve_fork(ForkArgs* a, unsigned char* base, uint32_t n_seq, uint32_t n
   uint32_t* marks = (uint32_t*)take(4ull * n_blocks);
   ForkPlan* plan = (ForkPlan*)take(sizeof(ForkPlan));
   uint32_t* given = (uint32_t*)take(4ull * std::max(n_seq, chunks_of(n_blocks)));
+  uint32_t* before = (uint32_t*)take(4ull * n_seq);
   int32_t* copy_of = (int32_t*)take(4ull * n_seq);
   int32_t* taker = (int32_t*)take(4ull * n_seq);
   int32_t* old_lengths = (int32_t*)take(4ull * n_seq);
   int32_t* aside = (int32_t*)take(4ull * std::max<uint64_t>((uint64_t)n_seq * max_blocks, n_blocks));
-  if (a) { a->arrived = arrived; a->marks = marks; a->plan = plan; a->given = given; a->copy_of = copy_of; a->taker = taker; a->old_lengths = old_lengths; a->aside = aside; a->place = (uint32_t*)aside; }
+  if (a) { a->arrived = arrived; a->marks = marks; a->plan = plan; a->given = given; a->before = before; a->copy_of = copy_of; a->taker = taker; a->old_lengths = old_lengths; a->aside = aside; a->place = (uint32_t*)aside; }
   return at;
 }
 
@@ -361,6 +492,12 @@ uint64_t carve_fork(ForkArgs* a, unsigned char* base, uint32_t n_seq, uint32_t n
 uint64_t cache_fork_scratch(uint32_t n_seq, uint32_t n_blocks, uint32_t max_blocks) { return carve_fork(nullptr, nullptr, n_seq, n_blocks, max_blocks); }
 
 hipError_t launch_cache_fork(ForkArgs a, void* scratch, hipStream_t st) {
+  if (a.n_seq <= SMALL_SEQ && (uint64_t)a.n_seq * a.max_blocks <= SMALL_ENTRIES && a.n_blocks <= SMALL_BLOCKS) {
+    hipError_t e = hipFuncSetAttribute((const void*)fork_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (SMALL_ENTRIES + SMALL_BLOCKS) * 4);
+    if (e != hipSuccess) return e;
+    fork_small_kernel<<<1, SMALL_THREADS, (a.n_seq * a.max_blocks + a.n_blocks) * 4, st>>>(a);
+    return hipGetLastError();
+  }
   carve_fork(&a, (unsigned char*)scratch, a.n_seq, a.n_blocks, a.max_blocks);
   fork_mark_kernel<<<a.n_seq, THREADS, 0, st>>>(a);
   hipError_t e = hipGetLastError();
@@ -388,11 +525,11 @@ hipError_t launch_cache_compact(ForkArgs a, void* scratch, hipStream_t st) {
   return hipGetLastError();
 }
 
-constexpr uint32_t COPY_WGS = 2048;
+constexpr uint32_t COPY_WGS = 4096;
 hipError_t launch_cache_copy(const CopyArgs& a, hipStream_t st) {
-  const uint64_t waves = (uint64_t)a.n_copies * a.layers * 2 * a.kv_heads;
-  if (waves == 0) return hipSuccess;
-  copy_blocks_kernel<<<(uint32_t)std::min<uint64_t>((waves + WAVES - 1) / WAVES, COPY_WGS), THREADS, 0, st>>>(a);
+  if (a.n_copies == 0) return hipSuccess;
+  const uint32_t wide = ((a.layers * 2 * a.kv_heads + WAVES - 1) / WAVES + 7) / 8 * 8, high = std::min(a.n_copies, std::max(1u, COPY_WGS / wide));
+  copy_blocks_kernel<<<dim3(wide, high), THREADS, 0, st>>>(a);
   return hipGetLastError();
 }
 

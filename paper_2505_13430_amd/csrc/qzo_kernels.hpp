@@ -380,7 +380,7 @@ constexpr uint32_t PAGED_COUNTERS = 512;      // words at the head of its scratc
 hipError_t launch_paged_attention(const PagedArgs& a, uint32_t head_dim, bool e4m3, void* scratch, hipStream_t st);
 // The next beams of every prompt (qzo_beam.hip).
 constexpr uint32_t BEAM_MAX_WIDTH = 64, BEAM_MAX_VOCAB = 1u << 22;
-struct BeamSum { double sum; float top; uint32_t unused; };        // of e^(x - top)
+constexpr uint32_t BEAM_COUNTERS = 8256;      // words at the head of its scratch, zero before a call and after it
 struct BeamArgs {
   const bf16_t* logits;
   uint64_t ld;
@@ -392,8 +392,9 @@ struct BeamArgs {
   uint32_t max_history;
   int32_t *parents, *chosen, *tokens, *added;
   // in the scratch, and how rows are cut
-  BeamSum* sums;
-  uint32_t *best, parts, span;
+  uint32_t* counters;
+  double* sums;                      // of every part: a sum, what its exponents are relative to
+  uint32_t *best, parts, span, wgs;  // wgs: workgroups of a prompt
 };
 uint64_t beam_select_scratch(uint32_t n_rows, uint32_t width, uint32_t vocab);
 hipError_t launch_beam_select(BeamArgs a, void* scratch, hipStream_t st);
@@ -418,7 +419,7 @@ struct ForkArgs {
   qzo_block_copy* copies;
   int32_t* new_tables;               // compact only
   // in the scratch
-  uint32_t *arrived, *marks, *given, *place;
+  uint32_t *arrived, *marks, *given, *before, *place;
   ForkPlan* plan;
   int32_t *copy_of, *taker, *old_lengths, *aside;
 };

@@ -864,3 +864,67 @@ def test_operands_elsewhere_are_refused():
         qb.qzo_beam_select(logits, 2, *good, scratch=torch.zeros(16, dtype=torch.uint8, device=DEV))
     with pytest.raises(AssertionError):
         qb.qzo_beam_select(logits, 2, *good, scratch=torch.zeros(1 << 20, dtype=torch.uint8))
+
+
+# ------------------------------------------------------------------ common keys of many columns ----
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("groups,shared,own,news,H,Hk,dh,block", [
+    ([66], [16], [1] * 66, None, 1, 1, 128, 16), ([66], [48], [1] * 66, None, 1, 1, 64, 16), ([130], [64], [1 + i % 5 for i in range(130)], None, 2, 2, 128, 32),
+    ([33], [1007], [3] * 33, None, 24, 3, 128, 64), ([9, 2, 40], [80, 2000, 333], [5] * 51, [5] * 51, 16, 4, 64, 16), ([3, 80], [5000, 64], [1] * 83, None, 8, 1, 128, 128),
+    ([2] * 20, [100 + 61 * i for i in range(20)], [40] * 40, [40] * 40, 4, 2, 128, 16), ([300], [4000], [2] * 300, None, 4, 1, 64, 256)])
+def test_common_keys_of_many_columns(groups, shared, own, news, H, Hk, dh, block, e4m3):
+    _check_shared(_attend(groups, shared, own, H, Hk, dh, block, news=news, e4m3=e4m3, seed=sum(groups)))
+
+
+@gpu
+@pytest.mark.parametrize("n", [4, 40, 90])
+@pytest.mark.parametrize("scale", [0.2, -0.2, 0.0, 3.0])
+def test_scales_of_common_keys(n, scale):
+    d = _attend([n], [90], [3] * n, 4, 2, 64, 16, seed=n)
+    d["scale"] = scale
+    _check_shared(d)
+
+
+@gpu
+@pytest.mark.parametrize("n", [4, 40, 90])
+def test_absent_blocks_of_common_keys(n):
+    d = _attend([n], [300], [20] * n, 4, 2, 128, 16, seed=n)
+    d["tables"][:, 3], d["tables"][:, 17] = d["k"].shape[0] + 5, -1
+    _check_shared(d)
+    d["tables"][:, :18] = -7                        # all of what is common
+    _check_shared(d)
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("n,dh", [(4, 128), (40, 64), (90, 128), (150, 64)])
+def test_values_that_are_not_finite(n, dh, e4m3):
+    """A common key that no row sees, by a score of -infinity, hides its value; one that is seen gives its NaN to its feature alone; a row of NaN stays alone."""
+    d = _attend([n], [200], [5] * n, 2, 1, dh, 32, e4m3=e4m3, seed=n)
+    want = _shared_call(d)
+    at, p = d["tables"][0, 2].long(), 70 % 32       # position 70
+    if not e4m3:
+        k0, v0 = d["k"][at, :, p].clone(), d["v"][at, :, p].clone()
+        d["q"].view(n, 2, dh)[..., 0] = d["q"].view(n, 2, dh)[..., 0].abs() + 0.25
+        d["k"][at, :, p, 0] = -math.inf
+        d["v"][at, :, p] = 0.0
+        finite = _check_shared(d)
+        d["v"][at, :, p] = math.nan
+        assert (_shared_call(d).float() - finite.float()).abs().max() <= 2.0 ** -7 * finite.float().abs().max()
+        d["v"][at, :, p, 1::2] = -math.inf
+        assert (_shared_call(d).float() - finite.float()).abs().max() <= 2.0 ** -7 * finite.float().abs().max()
+        d["k"][at, :, p], d["v"][at, :, p] = k0, v0
+        want = _shared_call(d)
+    d["v"].view(torch.uint8 if e4m3 else torch.int16)[at, :, p, 5] = 0x7f if e4m3 else 0x7fc0
+    got = _shared_call(d).view(n, 2, dh)
+    assert got[..., 5].isnan().all()
+    rest = torch.arange(dh, device=DEV) != 5
+    assert (got[..., rest].float() - want.view(n, 2, dh)[..., rest].float()).abs().max() <= 2.0 ** -7 * want.float().abs().max()
+    d = _attend([n], [200], [5] * n, 2, 1, dh, 32, e4m3=e4m3, seed=n)
+    want = _shared_call(d)
+    d["q"][n // 2, 3] = math.nan
+    got = _shared_call(d)
+    assert got[n // 2, :dh].isnan().all()
+    got[n // 2, :dh] = want[n // 2, :dh]
+    assert torch.equal(got, want)

@@ -33,26 +33,65 @@ __device__ __forceinline__ uint32_t blocks_of(int32_t length, const ForkArgs& a)
 // A sequence of before lives on if it is any sequence's parent.  A block is free again if it was held, and by none that lives on.
 // Every held block gets a mark, the highest of its holders': n_seq + 1 of one that lives on, n_seq - i of sequence i that does
 // not.  So the mark tells which blocks are free, and which of several holders gives one back.
-//   1. mark: the tables are put aside (they are rewritten in place), the marks made.
-//   2. count: how many blocks each sequence gives back; the last workgroup to be done has all the counts, adds them up, and
-//      knows who takes a block for a copy and where from.
+//   1. mark: the tables are put aside (they are rewritten in place), the marks made; a workgroup of its own finds who takes a block for a copy.
+//   2. count: how many blocks each sequence gives back; the last workgroup to be done has all the counts and adds them up.
 //   3. write: tables, lengths, the stack, copies; the marks go back to zero.
 // Whole numbers and maxima: the order of the atomics changes nothing.
 __global__ __launch_bounds__(THREADS) void fork_mark_kernel(ForkArgs a) {
   const uint32_t i = blockIdx.x, tid = threadIdx.x;
-  __shared__ uint32_t lives;
+  extern __shared__ int32_t first_child[];            // [n_seq], of the last workgroup
+  __shared__ uint32_t lives, flags, red[WAVES];
+  if (i == a.n_seq) {
+    // ---- beside the marks: which copy is a sequence's, what is wrong
+    for (uint32_t j = tid; j < a.n_seq; j += THREADS) first_child[j] = (int32_t)a.n_seq;
+    if (tid == 0) flags = 0;
+    __syncthreads();
+    const int64_t room = (int64_t)a.max_blocks << a.block_shift;
+    uint32_t wrong = 0;
+#pragma unroll 4
+    for (uint32_t j = tid; j < a.n_seq; j += THREADS) {
+      const int32_t p = a.parents[j], length = a.lengths[j];
+      if (p >= (int32_t)a.n_seq || length < 0) wrong |= 1u;
+      if (length > room) wrong |= 2u;
+      if (p >= 0 && p < (int32_t)a.n_seq) atomicMin(first_child + p, (int32_t)j);
+    }
+    if (wrong) atomicOr(&flags, wrong);
+    __syncthreads();
+    const uint32_t per = (a.n_seq + THREADS - 1) / THREADS, first = min(tid * per, a.n_seq), end = min(first + per, a.n_seq);
+    auto copies = [&](uint32_t j) {
+      const int32_t p = a.parents[j];
+      const bool known = p >= 0 && p < (int32_t)a.n_seq;
+      return known && (a.lengths[known ? p : 0] & ((1 << a.block_shift) - 1)) && first_child[known ? p : 0] != (int32_t)j;
+    };
+    uint32_t n_copy, copy = 0;
+#pragma unroll 4
+    for (uint32_t j = first; j < end; ++j) copy += copies(j);
+    copy = group_scan(copy, &n_copy, red) - copy;
+#pragma unroll 4
+    for (uint32_t j = first; j < end; ++j) {
+      const bool one = copies(j);
+      a.copy_of[j] = one ? (int32_t)copy : -1;
+      if (one) a.taker[copy] = (int32_t)j;
+      copy += one;
+    }
+    if (tid == 0) *a.plan = ForkPlan{a.state->n_free, 0, (int32_t)n_copy, (int32_t)flags};
+    return;
+  }
   if (tid == 0) lives = 0;
+  const int32_t length = a.lengths[i];
+  const int32_t* const row = a.tables + (uint64_t)i * a.max_blocks;
+  int32_t* const aside = a.aside + (uint64_t)i * a.max_blocks;
+  const int32_t id0 = row[min(tid, a.max_blocks - 1u)];          // on its way beside the parents
   __syncthreads();
   bool found = false;
+#pragma unroll 4
   for (uint32_t j = tid; j < a.n_seq; j += THREADS) found |= a.parents[j] == (int32_t)i;
   if (__any(found) && (tid & 63u) == 0) lives = 1;
   __syncthreads();
-  const uint32_t mark = lives ? a.n_seq + 1u : a.n_seq - i, n = blocks_of(a.lengths[i], a);
-  if (tid == 0) a.old_lengths[i] = a.lengths[i];
-  const int32_t* const row = a.tables + (uint64_t)i * a.max_blocks;
-  int32_t* const aside = a.aside + (uint64_t)i * a.max_blocks;
+  if (tid == 0) a.old_lengths[i] = length;
+  const uint32_t mark = lives ? a.n_seq + 1u : a.n_seq - i, n = blocks_of(length, a);
   for (uint32_t j = tid; j < n; j += THREADS) {
-    const int32_t id = row[j];
+    const int32_t id = j == tid ? id0 : row[j];
     aside[j] = id;
     if ((uint32_t)id < a.n_blocks) atomicMax(a.marks + id, mark);
   }
@@ -60,13 +99,15 @@ __global__ __launch_bounds__(THREADS) void fork_mark_kernel(ForkArgs a) {
 
 __global__ __launch_bounds__(THREADS) void fork_count_kernel(ForkArgs a) {
   const uint32_t i = blockIdx.x, tid = threadIdx.x;
-  __shared__ uint32_t red[WAVES], last, flags;
+  __shared__ uint32_t red[WAVES], last;
+  const ForkPlan plan = *a.plan;                     // of the last workgroup's use
   {
-    const uint32_t n = blocks_of(a.lengths[i], a);
+    const int32_t id0 = a.aside[(uint64_t)i * a.max_blocks + min(tid, a.max_blocks - 1u)];       // beside the length
+    const uint32_t n = blocks_of(a.old_lengths[i], a);
     const int32_t* const aside = a.aside + (uint64_t)i * a.max_blocks;
     uint32_t count = 0, all;
     for (uint32_t j = tid; j < n; j += THREADS) {
-      const int32_t id = aside[j];
+      const int32_t id = j == tid ? id0 : aside[j];
       count += (uint32_t)id < a.n_blocks && a.marks[id] == a.n_seq - i;
     }
     group_scan(count, &all, red);
@@ -74,60 +115,37 @@ __global__ __launch_bounds__(THREADS) void fork_count_kernel(ForkArgs a) {
       __hip_atomic_store(a.given + i, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       last = atomicAdd(a.arrived, 1u) + 1u == a.n_seq;
-      flags = 0;
     }
   }
   __syncthreads();
   if (!last) return;
   if (tid == 0) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  extern __shared__ int32_t first_child[];            // [n_seq]
-  for (uint32_t j = tid; j < a.n_seq; j += THREADS) first_child[j] = (int32_t)a.n_seq;
-  __syncthreads();
-  const int64_t room = (int64_t)a.max_blocks << a.block_shift;
-  uint32_t wrong = 0;
-  for (uint32_t j = tid; j < a.n_seq; j += THREADS) {
-    const int32_t p = a.parents[j], length = a.lengths[j];
-    if (p >= (int32_t)a.n_seq || length < 0) wrong |= 1u;
-    if (length > room) wrong |= 2u;
-    if (p >= 0 && p < (int32_t)a.n_seq) atomicMin(first_child + p, (int32_t)j);
+  // ---- what the sequences before give back, a few sequences a thread
+  constexpr uint32_t PER = CACHE_MAX_SEQ / THREADS;
+  const uint32_t per = (a.n_seq + THREADS - 1) / THREADS, j_first = tid * per;
+  uint32_t given[PER], back = 0, n_back;
+#pragma unroll
+  for (uint32_t x = 0; x < PER; ++x) {
+    if (x >= per) break;
+    given[x] = __hip_atomic_load(a.given + min(j_first + x, a.n_seq - 1u), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  if (wrong) atomicOr(&flags, wrong);
-  __syncthreads();
-  // a few sequences a thread: what those before give back, which copy is a sequence's
-  const uint32_t per = (a.n_seq + THREADS - 1) / THREADS, j_first = min(tid * per, a.n_seq), j_end = min(j_first + per, a.n_seq);
-  auto copies = [&](uint32_t j) {
-    const int32_t p = a.parents[j];
-    return p >= 0 && p < (int32_t)a.n_seq && (a.lengths[p] & ((1 << a.block_shift) - 1)) && first_child[p] != (int32_t)j;
-  };
-  uint32_t n_back, n_copy, back = 0, copy = 0;
-#pragma unroll 4
-  for (uint32_t j = j_first; j < j_end; ++j) {
-    back += __hip_atomic_load(a.given + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    copy += copies(j);
-  }
+#pragma unroll
+  for (uint32_t x = 0; x < PER; ++x)
+    if (x < per && j_first + x < a.n_seq) back += given[x];
   back = group_scan(back, &n_back, red) - back;
-  copy = group_scan(copy, &n_copy, red) - copy;
-#pragma unroll 4
-  for (uint32_t j = j_first; j < j_end; ++j) {
-    const uint32_t n = __hip_atomic_load(a.given + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool one = copies(j);
-    a.before[j] = back;
-    a.copy_of[j] = one ? (int32_t)copy : -1;
-    if (one) a.taker[copy] = (int32_t)j;
-    back += n;
-    copy += one;
-  }
-  __syncthreads();
-  const int32_t n_free = a.state->n_free;
+#pragma unroll
+  for (uint32_t x = 0; x < PER; ++x)
+    if (x < per && j_first + x < a.n_seq) { a.before[j_first + x] = back; back += given[x]; }
+  const int32_t n_free = plan.n_free, n_copy = plan.n_copy, flags = plan.status;
   int32_t status = QZO_OK;
-  if ((flags & 1u) || n_free < 0 || (uint32_t)n_free > a.n_blocks) status = QZO_ERR_ARG;
-  else if (flags & 2u) status = QZO_ERR_SHAPE;
+  if ((flags & 1) || n_free < 0 || (uint32_t)n_free > a.n_blocks) status = QZO_ERR_ARG;
+  else if (flags & 2) status = QZO_ERR_SHAPE;
   else if ((uint64_t)n_free + n_back > a.n_blocks) status = QZO_ERR_ARG;
-  else if (n_copy > (uint32_t)n_free + n_back) status = QZO_ERR_WORKSPACE;
+  else if ((uint32_t)n_copy > (uint32_t)n_free + n_back) status = QZO_ERR_WORKSPACE;
   if (tid == 0) {
     const bool ok = status == QZO_OK;
-    *a.plan = ForkPlan{n_free, ok ? (int32_t)n_back : 0, ok ? (int32_t)n_copy : 0, status};
-    *a.state = qzo_cache_state{ok ? n_free + (int32_t)n_back - (int32_t)n_copy : n_free, 0, status, ok ? (int32_t)n_copy : 0};
+    *a.plan = ForkPlan{n_free, ok ? (int32_t)n_back : 0, ok ? n_copy : 0, status};
+    *a.state = qzo_cache_state{ok ? n_free + (int32_t)n_back - n_copy : n_free, 0, status, ok ? n_copy : 0};
   }
 }
 
@@ -499,10 +517,10 @@ hipError_t launch_cache_fork(ForkArgs a, void* scratch, hipStream_t st) {
     return hipGetLastError();
   }
   carve_fork(&a, (unsigned char*)scratch, a.n_seq, a.n_blocks, a.max_blocks);
-  fork_mark_kernel<<<a.n_seq, THREADS, 0, st>>>(a);
+  fork_mark_kernel<<<a.n_seq + 1, THREADS, a.n_seq * 4, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  fork_count_kernel<<<a.n_seq, THREADS, a.n_seq * 4, st>>>(a);
+  fork_count_kernel<<<a.n_seq, THREADS, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   fork_write_kernel<<<a.n_seq + a.n_groups, THREADS, 0, st>>>(a);

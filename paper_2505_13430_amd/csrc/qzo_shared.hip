@@ -222,7 +222,7 @@ __global__ __launch_bounds__(CK_THREADS, 2) void common_keys_kernel(SharedArgs a
       }
     };
 
-    // ---- 32 keys
+    // ---- 32 keys; their values come out of the LDS while the weights are computed
     auto work = [&](const unsigned char* buffer, uint32_t sub, uint32_t there) {
       f32x16 s;
 #pragma unroll
@@ -230,6 +230,11 @@ __global__ __launch_bounds__(CK_THREADS, 2) void common_keys_kernel(SharedArgs a
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i)
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(buffer + k_place(sub * 32u + n, 2u * i + hi)), q[i], s, 0, 0, 0);
+      bf16x8 v[2][MT];
+#pragma unroll
+      for (uint32_t t = 0; t < 2; ++t)
+#pragma unroll
+        for (uint32_t i = 0; i < MT; ++i) v[t][i] = *reinterpret_cast<const bf16x8*>(buffer + K_BYTES + v_place(i * 32u + n, sub * 4u + 2u * t + hi));
       const bool first16 = there >> (2u * sub) & 1u, second16 = there >> (2u * sub + 1u) & 1u;
       if (!(first16 && second16)) {
 #pragma unroll
@@ -273,12 +278,12 @@ __global__ __launch_bounds__(CK_THREADS, 2) void common_keys_kernel(SharedArgs a
       for (uint32_t t = 0; t < 2; ++t)
 #pragma unroll
         for (uint32_t i = 0; i < MT; ++i)
-          o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(buffer + K_BYTES + v_place(i * 32u + n, sub * 4u + 2u * t + hi)), p[t], o[i], 0, 0, 0);
+          o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[t][i], p[t], o[i], 0, 0, 0);
     };
 
     __syncthreads();                              // what the last piece left in the LDS has been read
     Ids ids = ids_of(at);
-    uint32_t there = there_of(at, ids), there_next = 0;
+    uint32_t there = there_of(at, ids);
     Staged st = load(at, ids);
     ids = ids_of(min(at + 1u, u_end - 1u));
     store(lds, st, there);
@@ -286,18 +291,15 @@ __global__ __launch_bounds__(CK_THREADS, 2) void common_keys_kernel(SharedArgs a
     uint32_t buffer = 0;
 #pragma unroll 1
     for (uint32_t u = at; u < u_end; ++u) {
-      const bool more = u + 1u < u_end;
-      if (more) {
-        there_next = there_of(u + 1u, ids);
-        st = load(u + 1u, ids);
-        ids = ids_of(min(u + 2u, u_end - 1u));
-      }
+      const uint32_t next = min(u + 1u, u_end - 1u), there_next = there_of(next, ids);      // (the last step again: without a branch around the loads)
+      st = load(next, ids);
+      ids = ids_of(min(next + 1u, u_end - 1u));
       if (active) {
 #pragma unroll 1
         for (uint32_t sub = twice ? part : 0u; sub < (twice ? part + 1u : 2u); ++sub) work(lds + buffer * BUFFER, sub, there);
       }
       buffer ^= 1u;
-      if (more) store(lds + buffer * BUFFER, st, there_next);
+      store(lds + buffer * BUFFER, st, there_next);
       there = there_next;
       __syncthreads();
     }
@@ -429,9 +431,18 @@ __global__ __launch_bounds__(256) void join_shares_kernel(SharedArgs a, bool e4m
   j.add(head_common[0], head_common[1], o_common);
   if (parts) {                              // of common_keys_kernel: the pieces behind the first
     const uint32_t where = __float_as_uint(head_common[2]), c = __float_as_uint(head_common[3]), wg = where >> 16, pieces = where & 0xffffu;
-    for (uint32_t i = 1; i < pieces; ++i) {
-      const float* const from = parts + ((uint64_t)(wg + i) * CK_TILE + c) * STRIDE;
-      j.add(from[0], from[1], *reinterpret_cast<const f32x4*>(from + 4 + d));
+    for (uint32_t i = 1; i < pieces; i += 4) {
+      float2 ml[4];
+      f32x4 x[4];
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k) {
+        const float* const from = parts + ((uint64_t)(wg + min(i + k, pieces - 1u)) * CK_TILE + c) * STRIDE;
+        ml[k] = *reinterpret_cast<const float2*>(from);
+        x[k] = *reinterpret_cast<const f32x4*>(from + 4 + d);
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k)
+        if (i + k < pieces) j.add(ml[k].x, ml[k].y, x[k]);
     }
   }
   j.add(head_own[0], head_own[1], o_own);

@@ -8,15 +8,16 @@ namespace {
 
 constexpr uint32_t THREADS = 256, WAVES = THREADS / 64;
 
-// Inclusive sum over a workgroup's threads; total: of all of them.  red: [WAVES], read before the next call by way of its first barrier.
+// Inclusive sum over a workgroup's threads; total: of all of them.  N: its wavefronts; red: [N], read before the next call by way of its first barrier.
+template <uint32_t N = WAVES>
 __device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t* total, uint32_t* red) {
   const uint32_t upto = lane_scan(v);
   __syncthreads();
   if ((threadIdx.x & 63u) == 63u) red[threadIdx.x >> 6] = upto;
   __syncthreads();
   uint32_t before = 0, all = 0;
-  const uint32_t waves = blockDim.x >> 6;
-  for (uint32_t w = 0; w < waves; ++w) {
+#pragma unroll
+  for (uint32_t w = 0; w < N; ++w) {
     if (w < (threadIdx.x >> 6)) before += red[w];
     all += red[w];
   }
@@ -97,26 +98,27 @@ __global__ __launch_bounds__(THREADS) void fork_mark_kernel(ForkArgs a) {
   }
 }
 
+constexpr uint32_t COUNT_WGS = 128;
 __global__ __launch_bounds__(THREADS) void fork_count_kernel(ForkArgs a) {
-  const uint32_t i = blockIdx.x, tid = threadIdx.x;
+  const uint32_t tid = threadIdx.x, lane = tid & 63u;
   __shared__ uint32_t red[WAVES], last;
   const ForkPlan plan = *a.plan;                     // of the last workgroup's use
-  {
-    const int32_t id0 = a.aside[(uint64_t)i * a.max_blocks + min(tid, a.max_blocks - 1u)];       // beside the length
-    const uint32_t n = blocks_of(a.old_lengths[i], a);
+  // a wavefront a sequence; few workgroups, for all count at one place, 10 ns each (768 sequences with a workgroup each 14.4 us)
+  for (uint32_t i = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * WAVES + (tid >> 6))); i < a.n_seq; i += COUNT_WGS * WAVES) {
     const int32_t* const aside = a.aside + (uint64_t)i * a.max_blocks;
-    uint32_t count = 0, all;
-    for (uint32_t j = tid; j < n; j += THREADS) {
-      const int32_t id = j == tid ? id0 : aside[j];
-      count += (uint32_t)id < a.n_blocks && a.marks[id] == a.n_seq - i;
+    const uint32_t n = blocks_of(a.old_lengths[i], a);
+    uint32_t count = 0;
+#pragma unroll 4
+    for (uint32_t j = lane; j < n; j += 64) {
+      const int32_t id = aside[j];
+      count += (uint32_t)id < a.n_blocks && a.marks[(uint32_t)id < a.n_blocks ? id : 0] == a.n_seq - i;
     }
-    group_scan(count, &all, red);
-    if (tid == 0) {
-      __hip_atomic_store(a.given + i, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      last = atomicAdd(a.arrived, 1u) + 1u == a.n_seq;
-    }
+    count = (uint32_t)__builtin_amdgcn_readlane((int)lane_scan(count), 63);
+    if (lane == 0) __hip_atomic_store(a.given + i, count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) last = atomicAdd(a.arrived, 1u) + 1u == gridDim.x;
   __syncthreads();
   if (!last) return;
   if (tid == 0) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -289,7 +291,8 @@ __global__ __launch_bounds__(SMALL_THREADS) void fork_small_kernel(ForkArgs a) {
   const int32_t p0 = tid < a.n_seq ? parent[tid] : -1;
   const uint32_t copy = p0 >= 0 && p0 < (int32_t)a.n_seq && ((uint32_t)length[p0] & mask) && first_child[p0] != (int32_t)tid;
   uint32_t n_back, n_copy;
-  const uint32_t back_before = group_scan(back, &n_back, red) - back, copy_before = group_scan(copy, &n_copy, red) - copy;
+  const uint32_t back_before = group_scan<SMALL_THREADS / 64>(back, &n_back, red) - back;
+  const uint32_t copy_before = group_scan<SMALL_THREADS / 64>(copy, &n_copy, red) - copy;
   int32_t status = QZO_OK;
   if ((flags & 1u) || n_free < 0 || (uint32_t)n_free > a.n_blocks) status = QZO_ERR_ARG;
   else if (flags & 2u) status = QZO_ERR_SHAPE;
@@ -511,16 +514,19 @@ uint64_t cache_fork_scratch(uint32_t n_seq, uint32_t n_blocks, uint32_t max_bloc
 
 hipError_t launch_cache_fork(ForkArgs a, void* scratch, hipStream_t st) {
   if (a.n_seq <= SMALL_SEQ && (uint64_t)a.n_seq * a.max_blocks <= SMALL_ENTRIES && a.n_blocks <= SMALL_BLOCKS) {
-    hipError_t e = hipFuncSetAttribute((const void*)fork_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (SMALL_ENTRIES + SMALL_BLOCKS) * 4);
-    if (e != hipSuccess) return e;
-    fork_small_kernel<<<1, SMALL_THREADS, (a.n_seq * a.max_blocks + a.n_blocks) * 4, st>>>(a);
+    const uint32_t lds = (a.n_seq * a.max_blocks + a.n_blocks) * 4;
+    if (lds > 48u * 1024) {                       // the limit that all calls have in common
+      hipError_t e = hipFuncSetAttribute((const void*)fork_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (SMALL_ENTRIES + SMALL_BLOCKS) * 4);
+      if (e != hipSuccess) return e;
+    }
+    fork_small_kernel<<<1, SMALL_THREADS, lds, st>>>(a);
     return hipGetLastError();
   }
   carve_fork(&a, (unsigned char*)scratch, a.n_seq, a.n_blocks, a.max_blocks);
   fork_mark_kernel<<<a.n_seq + 1, THREADS, a.n_seq * 4, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  fork_count_kernel<<<a.n_seq, THREADS, 0, st>>>(a);
+  fork_count_kernel<<<std::min((a.n_seq + WAVES - 1) / WAVES, COUNT_WGS), THREADS, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   fork_write_kernel<<<a.n_seq + a.n_groups, THREADS, 0, st>>>(a);

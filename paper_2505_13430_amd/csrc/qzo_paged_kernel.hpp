@@ -153,7 +153,9 @@ __device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, const int
   }
   const uint64_t cols = (uint64_t)w.rows * a.group;
   w.wide = !TILED && wide && cols > 2 * D::TC;
-  w.quad = !TILED && quads && cols <= D::TC && w.len - w.from <= QUAD_LEN;
+  // own keys only, and half as many as without groups: 16 x 8 beams with up to 150 / 500 of their own 100 / 155 us, with QUAD_LEN 100 / 164, with none
+  // 106 / 155; common keys so, too, 100 / 172
+  w.quad = !TILED && quads && !w.all && cols <= D::TC && w.len - w.from <= QUAD_LEN / 2;
   w.units = max(1u, (w.len - w.from + D::unit(w) - 1) / D::unit(w));
   w.tiles = (uint32_t)((cols + D::cols(w) - 1) / D::cols(w));
   return w;

@@ -91,7 +91,7 @@ __device__ __forceinline__ bool last_of(uint32_t* counter, uint32_t all, uint32_
 //   A tile whose sum or maximum tells of a NaN, an infinity or a number beyond 1e30 is gone through again, logit by logit.
 //   The best tokens: the width-th highest of the lanes' maxima is a bound that no lane with a lower maximum reaches, which leaves `width`
 // lanes (more where there are ties), whose logits alone are read again and compared.  (Looked for in every tile, as the row goes by, they cost
-// twice the instructions of all the rest: 96 x 5 rows of 99991 65 us, so 30.)
+// twice the instructions of all the rest: 96 x 5 rows of 99991 65 us, so 41.)
 struct Part {
   uint32_t best = 0;            // lane i: the i-th best: the logit's order above, the place from behind below: no two are equal
   double sum = 0.0, ref = 0.0;  // sum of e^x = sum e^ref; ref the same in all lanes
@@ -278,6 +278,9 @@ __device__ __forceinline__ Candidate wave_first(const Candidate& c) {
   return r;
 }
 
+// 96 x 5 rows of 99991: 41 us.  The logits have been read after 22 (88 MB, 4 TB/s), then come the hand-over to a prompt's
+// last workgroup, its lists, rounds and states, 10 us from one to the next of which only the last prompt's show.  1 x 4 rows of 32000: 12 us, all latency:
+// a part 3.6, the hand-over 1.7, lists and sums 2.3, rounds 2.5, states 1.4.
 // One launch.  Every wavefront takes a part of a row; the last workgroup of a prompt to be done finds its beams among the parts' best, each list of
 // them in order; the last prompt's packs the tokens.
 constexpr uint32_t STAGED = 8192;                                        // best tokens of all parts that fit the LDS
@@ -321,7 +324,7 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
   uint32_t longest_old = 0;
   for (uint32_t b = 0; b < W; ++b)
     if (kind[b]) longest_old = max(longest_old, min((uint32_t)count[b], a.max_history));
-  const bool short_ones = longest_old * W <= THREADS * 4u;
+  const bool short_ones = longest_old <= THREADS * 4u / W;
   __shared__ int32_t histories[THREADS * 4];
   int32_t early[4];
 #pragma unroll
@@ -489,7 +492,7 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
       if (c < end || (c == end && kind[b] == 1u)) f(u, i, b, c, end);
     }
   };
-  if (short_ones && longest * W <= THREADS * HELD) {
+  if (short_ones && longest <= THREADS * HELD / W) {
     each(0, longest, [&](uint32_t, uint32_t i, uint32_t b, uint32_t c, uint32_t end) {
       if (c < end && b == i) return;
       a.history[(uint64_t)(r0 + i) * a.max_history + c] = c < end ? histories[b * longest_old + c] : token[i];

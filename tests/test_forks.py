@@ -928,3 +928,90 @@ def test_values_that_are_not_finite(n, dh, e4m3):
     assert got[n // 2, :dh].isnan().all()
     got[n // 2, :dh] = want[n // 2, :dh]
     assert torch.equal(got, want)
+
+
+# ------------------------------------------------------------------ captured, long, out of order ----
+@gpu
+@pytest.mark.parametrize("n,longest", [(300, 90), (12, 700), (40, 7000)])
+def test_captured_forks_replay(n, longest):
+    """Few and many sequences: a captured fork and its copies, replayed on other parents with the program's own work in between."""
+    rng = np.random.default_rng(n)
+    lengths = [int(x) for x in rng.integers(0, longest, n)]
+    starts = list(range(0, n, 4)) + [n]
+    tables, free, n_free = _forest(lengths, 16, -(-longest // 16) + 1, n, n, [(i, min(i + 3, n)) for i in range(0, n, 4)])
+    kept = [_i32(lengths), _i32(tables), _i32(free), _i32([n_free, 0, 0, 0]), torch.full((n, 4), -9, dtype=torch.int32, device=DEV)]
+    x, parents, shared = [t.clone() for t in kept], torch.zeros(n, dtype=torch.int32, device=DEV), torch.zeros(len(starts) - 1, dtype=torch.int32, device=DEV)
+    group_starts = _i32(starts)
+    pool = torch.zeros(2, len(free), 2, 16, 64, dtype=torch.bfloat16, device=DEV)
+    filled = torch.randint(0, 30000, pool.shape, dtype=torch.int16, device=DEV).view(torch.bfloat16)
+    cache = qb.make_cache(pool[0], pool[1])
+    room = torch.zeros(qb.qzo_cache_fork_scratch_bytes(n, len(free), tables.shape[1]), dtype=torch.uint8, device=DEV)
+
+    def step():
+        for t, k in zip(x, kept):
+            t.copy_(k)
+        pool.copy_(filled)
+        qb.qzo_cache_fork(parents, 16, *x, group_starts=group_starts, shared=shared, scratch=room)
+        qb.qzo_cache_copy(cache, x[4], count=x[3])
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for turn in range(4):
+        p = [int(i) for i in (rng.integers(-1, n, n) if turn % 2 else np.clip(np.arange(n) // 4 * 4 + rng.integers(0, 4, n), 0, n - 1))]
+        parents.copy_(_i32(p))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        want = fork_reference(p, lengths, tables, free, n_free, 16, starts)
+        assert isinstance(want, dict) and x[0].tolist() == list(want["lengths"]) and (x[1].cpu().numpy() == want["tables"]).all()
+        assert (x[2].cpu().numpy() == want["free"]).all() and x[3].tolist() == want["state"] and shared.tolist() == want["shared"]
+        assert x[4][:len(want["copies"])].tolist() == want["copies"]
+        moved = filled.view(torch.int16).clone()
+        for a, b, tokens, _ in want["copies"]:
+            moved[:, b, :, :tokens] = moved[:, a, :, :tokens]
+        assert torch.equal(pool.view(torch.int16), moved)
+        assert _fork(p, lengths, tables, free, n_free, 16, starts)["state"].tolist() == want["state"]         # eager, by scratch of its own
+
+
+@gpu
+@pytest.mark.parametrize("n,dh,e4m3", [(4, 128, False), (40, 64, True), (90, 128, False)])
+def test_captured_shared_attention_replays(n, dh, e4m3):
+    """Queries and lengths that change between replays."""
+    d, gen = _attend([n, n], [500, 90], [30] * (2 * n), 4, 2, dh, 16, e4m3=e4m3, seed=n), torch.Generator(device=DEV)
+    cache = qb.make_cache(d["k"], d["v"], *d["scales"])
+    room = torch.zeros(qb.qzo_paged_attention_shared_scratch_bytes(2 * n, 2 * n, 4, 2, dh), dtype=torch.uint8, device=DEV)
+    out, side = torch.zeros_like(d["q"]), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        qb.qzo_paged_attention_shared(d["q"], cache, d["tables"], d["lengths"], d["group_starts"], d["shared"], out, d["scale"], scratch=room)
+    for turn in range(4):
+        d["q"].copy_(torch.randn(d["q"].shape, generator=gen, device=DEV))
+        d["lengths"].sub_(turn * 2 + 1)
+        d["shared"].sub_(turn * 9)
+        torch.cuda.synchronize()
+        g.replay()
+        other = _check_shared(d)
+        torch.cuda.synchronize()
+        assert torch.equal(out, other)
+
+
+@gpu
+def test_select_with_a_history_of_many_columns():
+    """64 beams of 2^26 columns: columns times beams are beyond 32 bits."""
+    columns = 1 << 26
+    history = torch.empty(64, columns, dtype=torch.int32, device=DEV)
+    torch.arange(columns, dtype=torch.int32, device=DEV, out=history[5])
+    logits = torch.linspace(4.0, -4.0, 64, device=DEV).to(torch.bfloat16).repeat(64, 1)
+    scores, counts = torch.full((64,), -math.inf, device=DEV), torch.zeros(64, dtype=torch.int32, device=DEV)
+    scores[5], counts[5] = 0.0, columns - 1
+    rest = [torch.zeros(64, dtype=torch.int32, device=DEV) for _ in range(5)]
+    qb.qzo_beam_select(logits, 64, scores, counts, rest[0], history, *rest[1:])
+    torch.cuda.synchronize()
+    assert rest[1].tolist() == [5] * 64 and rest[2].tolist() == list(range(64)) and (counts == columns).all()
+    assert history[:, -1].tolist() == list(range(64))
+    for i in (0, 4, 5, 6, 63):
+        assert torch.equal(history[i, :-1], torch.arange(columns - 1, dtype=torch.int32, device=DEV))

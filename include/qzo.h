@@ -477,6 +477,7 @@ qzo_status qzo_cache_compact(uint32_t n_seq, uint32_t block, uint32_t n_blocks, 
  * Copies blocks within the pools of n_layers layers: cache describes those of layer 0, the others follow, as in qzo_answer.  copies_dev
  * [n_copies]; with count_dev (nullable: all) only its first *count_dev (at most n_copies; below 0: none).  An entry with a block outside the pool, with from = to
  * or without tokens is passed over, more tokens than a block has are a block's.  No block is copied to twice, or both copied from and to.
+ * n_layers * kv_heads below 2^24.
  */
 qzo_status qzo_cache_copy(const qzo_cache* cache, uint32_t n_layers, const qzo_block_copy* copies_dev, uint32_t n_copies,
                           const int32_t* count_dev, void* stream);
@@ -487,7 +488,8 @@ qzo_status qzo_cache_copy(const qzo_cache* cache, uint32_t n_layers, const qzo_b
  *   total = score + x_v - log sum_v e^x_v over the finite logits,  key = total / count^length_penalty with the new token counted (0: key = total);
  * one that has ended stays as it is: a single candidate, of its score and count, token end_token (0 if that is -1).  A score of
  * -infinity or NaN stands for no beam, and its logits are not read.  Row i of a prompt becomes the candidate with the i-th
- * highest key, ties to the lower beam, then the lower token (within a beam the logits decide, 0 and -0 being equal); sums in 64 bits.
+ * highest key, ties to the lower beam, then the lower token (within a beam the logits decide, 0 and -0 being equal).
+ * e^x and the sum of a lane's 16 logits in 32 bits, what they add up to, logarithm, total and key in 64.
  *   scores_dev fp32: total; counts_dev: tokens of the beam (one more, but for an ended one); ended_dev: 1 if the token is end_token or it had ended;
  *   history_dev int32 [rows, max_history] (null with max_history 0): the parent's first count tokens, then the new one; columns beyond
  *     are not written, tokens beyond max_history are not recorded;
@@ -513,7 +515,8 @@ qzo_status qzo_beam_select(const void* logits_dev, uint64_t ld_logits, uint32_t 
  * tokens have the same keys and values.  Those, down to a multiple of 16, are read once for all the group's rows, through the table of its first
  * sequence; every sequence's other positions through its own.  A sequence whose new tokens begin before the shared part ends reads all of
  * its positions itself; so do all where the first sequence is shorter than that.  Otherwise results, limits and roundings are
- * those of qzo_paged_attention (p meets v as two bf16 numbers where the columns of the group, or of the sequence, are as few as it says).
+ * those of qzo_paged_attention (p meets v as two bf16 numbers where the columns of the group, or of the sequence, are as few as it says; in
+ * groups of more than 64 columns a key head on average, new tokens times query heads of a key head, the common keys' p is rounded once).
  * scratch_dev: qzo_paged_attention_shared_scratch_bytes bytes, kept as qzo_paged_attention's (its first 2048 bytes zero).  n_groups 1 .. 2048.
  */
 qzo_status qzo_paged_attention_shared_scratch_bytes(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t kv_heads,

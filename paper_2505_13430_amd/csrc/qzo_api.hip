@@ -1892,7 +1892,7 @@ qzo_status qzo_cache_copy(const qzo_cache* cache, uint32_t n_layers, const qzo_b
   if (st != QZO_OK) return st;
   if (!n_layers || n_layers > 65535) return fail(QZO_ERR_SHAPE, "n_layers must be 1 .. 65535");
   if (n_copies >= (1u << 31)) return fail(QZO_ERR_SHAPE, "n_copies must be below 2^31");
-  if ((uint64_t)n_layers * cache->kv_heads * 2 >= (1ull << 32)) return fail(QZO_ERR_SHAPE, "n_layers * kv_heads must be below 2^31");
+  if ((uint64_t)n_layers * cache->kv_heads >= (1ull << 24)) return fail(QZO_ERR_SHAPE, "n_layers * kv_heads must be below 2^24");
   CopyArgs a = {cache->k_dev, cache->v_dev, n_layers, cache->n_blocks, (uint32_t)__builtin_ctz(cache->block), cache->kv_heads,
                 cache->head_dim * (cache->type ? 1u : 2u), copies_dev, n_copies, count_dev};
   QZO_HIP(launch_cache_copy(a, (hipStream_t)stream));

@@ -38,6 +38,7 @@ __device__ __forceinline__ uint32_t blocks_of(int32_t length, const ForkArgs& a)
 //   2. count: how many blocks each sequence gives back; the last workgroup to be done has all the counts and adds them up.
 //   3. write: tables, lengths, the stack, copies; the marks go back to zero.
 // Whole numbers and maxima: the order of the atomics changes nothing.
+// 128 x 6 sequences of up to 80 blocks: 21 us, of which 5, 11 and 6 are the three launches'; latency is what they consist of (the bytes take 0.2 us).
 __global__ __launch_bounds__(THREADS) void fork_mark_kernel(ForkArgs a) {
   const uint32_t i = blockIdx.x, tid = threadIdx.x;
   extern __shared__ int32_t first_child[];            // [n_seq], of the last workgroup
@@ -241,8 +242,8 @@ __global__ __launch_bounds__(THREADS) void fork_write_kernel(ForkArgs a) {
   }
 }
 
-// The same with few sequences and a small pool, in one workgroup: tables and marks in the LDS.  Latency is all there is to it (8 beams behind 2500
-// tokens, in three launches 13.8 us).
+// The same with few sequences and a small pool, in one workgroup: tables and marks in the LDS.  Latency is all there is to it: 8 beams behind 2500
+// tokens 8.6 us, in three launches 13.8.
 constexpr uint32_t SMALL_THREADS = 1024, SMALL_SEQ = 256, SMALL_ENTRIES = 16384, SMALL_BLOCKS = 16384;
 __global__ __launch_bounds__(SMALL_THREADS) void fork_small_kernel(ForkArgs a) {
   extern __shared__ int32_t small_lds[];
@@ -367,6 +368,8 @@ __global__ __launch_bounds__(SMALL_THREADS) void fork_small_kernel(ForkArgs a) {
 
 // ------------------------------------------------------------------ compact ----
 // Held blocks are marked; n of them: those from n on go to the places below n that none holds, in order.
+// Four launches that wait for one another, 2.7 + 4.7 + 4.2 + 2.9 us for 1400 blocks, 3.1 + 6.1 + 6.8 + 4.3 for 150001 (in a graph 13 and 19 us): each step
+// needs all of the one before.
 constexpr uint32_t CHUNK = 8 * THREADS;           // blocks that a workgroup counts
 __global__ __launch_bounds__(THREADS) void compact_mark_kernel(ForkArgs a) {
   const uint32_t i = blockIdx.x, n = blocks_of(a.lengths[i], a);
@@ -460,12 +463,12 @@ __global__ __launch_bounds__(THREADS) void compact_write_kernel(ForkArgs a) {
 
 // ------------------------------------------------------------------ copies ----
 // The first tokens of a block are consecutive for each layer, pool and head: such a run is a wavefront's, 16 bytes a lane, four times
-// on their way.  A row of the grid takes every gridDim.y-th entry.  An XCD sees to neighbouring layers, so that it has few pages' addresses to look up.
+// on their way.  A row of the grid takes every gridDim.y-th entry.  Bound by memory: 700 e4m3 blocks of 32 layers, 0.73 GB, 297 us, 4.9 TB/s read and
+// written, which is a large copy's rate; three blocks, 25 MB, 5.0 us.  (The four pieces in variables of their own: as an array they go to the LDS, by an
+// index for which every workgroup reads its launch packet in host memory: 18 us in place of 5.)
 __global__ __launch_bounds__(THREADS) void copy_blocks_kernel(CopyArgs a) {
   const uint32_t lane = threadIdx.x & 63u;
-  // workgroups of an XCD (every eighth) take neighbouring runs
-  const uint32_t wg = (blockIdx.x & 7u) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-  const uint32_t run = (uint32_t)__builtin_amdgcn_readfirstlane((int)(wg * WAVES + (threadIdx.x >> 6))), runs = a.layers * 2u * a.kv_heads;
+  const uint32_t run = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * WAVES + (threadIdx.x >> 6))), runs = a.layers * 2u * a.kv_heads;
   const uint32_t n = a.count ? (uint32_t)min(max(*a.count, 0), (int32_t)a.n_copies) : a.n_copies;
   if (run >= runs) return;
   const uint32_t pool = run / a.kv_heads, head = run - pool * a.kv_heads;             // layer by layer, k and v
@@ -552,7 +555,7 @@ hipError_t launch_cache_compact(ForkArgs a, void* scratch, hipStream_t st) {
 constexpr uint32_t COPY_WGS = 4096;
 hipError_t launch_cache_copy(const CopyArgs& a, hipStream_t st) {
   if (a.n_copies == 0) return hipSuccess;
-  const uint32_t wide = ((a.layers * 2 * a.kv_heads + WAVES - 1) / WAVES + 7) / 8 * 8, high = std::min(a.n_copies, std::max(1u, COPY_WGS / wide));
+  const uint32_t wide = (a.layers * 2 * a.kv_heads + WAVES - 1) / WAVES, high = std::min(a.n_copies, std::max(1u, COPY_WGS / wide));
   copy_blocks_kernel<<<dim3(wide, high), THREADS, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -284,6 +284,7 @@ class Answers:
 
     def fork(self, parents: torch.Tensor, stream=None):
         """parents int32 [n_seq]: sequence i goes on from what sequence parents[i] is (negative: it ends).  Full blocks are shared, open ones copied.
+        An `add` that was captured before the first fork does not know that blocks may be shared (with a width it does).
         Whether there were blocks for that is in state[2], as for `add` (not QZO_OK: nothing has changed)."""
         self._for_forks(stream)
         self.forked = True

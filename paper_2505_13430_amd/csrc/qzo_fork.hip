@@ -38,7 +38,7 @@ __device__ __forceinline__ uint32_t blocks_of(int32_t length, const ForkArgs& a)
 //   2. count: how many blocks each sequence gives back; the last workgroup to be done has all the counts and adds them up.
 //   3. write: tables, lengths, the stack, copies; the marks go back to zero.
 // Whole numbers and maxima: the order of the atomics changes nothing.
-// 128 x 6 sequences of up to 80 blocks: 21 us, of which 5, 11 and 6 are the three launches'; latency is what they consist of (the bytes take 0.2 us).
+// 128 x 6 sequences of up to 253 blocks: 21 us, of which 5, 11 and 6 are the three launches'; latency is what they consist of (the bytes take 0.2 us).
 __global__ __launch_bounds__(THREADS) void fork_mark_kernel(ForkArgs a) {
   const uint32_t i = blockIdx.x, tid = threadIdx.x;
   extern __shared__ int32_t first_child[];            // [n_seq], of the last workgroup
@@ -463,7 +463,7 @@ __global__ __launch_bounds__(THREADS) void compact_write_kernel(ForkArgs a) {
 
 // ------------------------------------------------------------------ copies ----
 // The first tokens of a block are consecutive for each layer, pool and head: such a run is a wavefront's, 16 bytes a lane, four times
-// on their way.  A row of the grid takes every gridDim.y-th entry.  Bound by memory: 700 e4m3 blocks of 32 layers, 0.73 GB, 297 us, 4.9 TB/s read and
+// on their way.  A row of the grid takes every gridDim.y-th entry.  Bound by memory: 700 e4m3 blocks of 8 layers, 0.73 GB, 298 us, 4.9 TB/s read and
 // written, which is a large copy's rate; three blocks, 25 MB, 5.0 us.  (The four pieces in variables of their own: as an array they go to the LDS, by an
 // index for which every workgroup reads its launch packet in host memory: 18 us in place of 5.)
 __global__ __launch_bounds__(THREADS) void copy_blocks_kernel(CopyArgs a) {

@@ -23,11 +23,11 @@ namespace {
 // The units of 64 keys of all groups, heads and tiles are dealt out in even shares; a tile's first piece leaves its share in place of its
 // columns, a later one, with which its workgroup begins, in that workgroup's place; join_shares_kernel adds them up.
 // An accumulator that is NaN, by a value whose weight is 0, say: the column is gone through again, one key a thread, without those.
-// 64 sequences behind 32768 tokens, 32 heads on 8 of 128 (256 columns a key head, 69 GFLOP): 90 to 107 us, 650 to 770 TFLOP/s; matrix pipe busy 29 %
+// 64 sequences behind 32768 tokens, 64 heads on 8 of 128 (512 columns a key head, 69 GFLOP): 90 to 107 us, 650 to 770 TFLOP/s; matrix pipe busy 29 %
 // of the SIMDs' time, vector pipe 37 %, no bank conflicts: two wavefronts a SIMD (128 accumulators and the values of a step leave no
 // registers for more), whose steps of loads from the LDS, products and weights overlap little.  The call 121 us, with paged_attention_kernel for this 217.
 // 64 columns a wavefront would halve the LDS reads and do not fit (spills, 278 us for the call); priorities, four wavefronts a workgroup and a second
-// step in registers gave nothing.  12 groups in e4m3, heads of 64: 49 us (the call 82, otherwise 103), 1.2 to 2 us a step of 64 keys, most of them pieces' beginnings and ends.
+// step in registers gave nothing.  6 x 12 candidates of 9 tokens in e4m3, 40 heads on 8 of 64: 49 us (the call 82, otherwise 103), 1.2 to 2 us a step of 64 keys, most of them pieces' beginnings and ends.
 // Weights meet the values rounded once to bf16: error against 64 bits as that of prompts.
 constexpr uint32_t CK_THREADS = 512, CK_WAVES = 8, CK_KEYS = 64, CK_COLS = 32, CK_TILE = CK_COLS * CK_WAVES, CK_WGS = 256, CK_LEAST = 4;
 typedef float f32x16 __attribute__((ext_vector_type(16)));

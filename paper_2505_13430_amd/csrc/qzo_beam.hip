@@ -90,16 +90,17 @@ __device__ __forceinline__ bool last_of(uint32_t* counter, uint32_t all, uint32_
 // less than what two candidates differ by.
 //   A tile whose sum or maximum tells of a NaN, an infinity or a number beyond 1e30 is gone through again, logit by logit.
 //   The best tokens: the width-th highest of the lanes' maxima is a bound that no lane with a lower maximum reaches, which leaves `width`
-// lanes (more where there are ties), whose logits alone are read again and compared.  (Looked for in every tile, as the row goes by, they cost
+// lanes (more where there are ties); the tiles of theirs whose maximum reaches it, too, are read again and compared.  (Looked for in every tile, as the row goes by, they cost
 // twice the instructions of all the rest: 96 x 5 rows of 99991 65 us, so 41.)
 struct Part {
   uint32_t best = 0;            // lane i: the i-th best: the logit's order above, the place from behind below: no two are equal
   double sum = 0.0, ref = 0.0;  // sum of e^x = sum e^ref; ref the same in all lanes
 };
 constexpr uint32_t WAITING = 768;      // a turn adds 512 at most
-struct PartSpace { uint32_t waiting[WAITING]; uint8_t lanes[64]; };
+constexpr uint32_t TOPS = 4;            // tiles' maxima at a time
+struct PartSpace { uint32_t waiting[WAITING], pieces[32 + TOPS * 64 + 32]; };
 template <class Counts>
-__device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v1, uint32_t width, PartSpace& space, Counts&& counts) {
+__device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v1, uint32_t width, PartSpace& space, uint16_t* tops, Counts&& counts) {
   uint32_t* const waiting = space.waiting;
   const uint32_t lane = threadIdx.x & 63u;
   // whole 16-byte pieces as they lie in memory; the up to seven logits before them and those behind them one a lane (0 .. 6, 8 .. 14)
@@ -174,6 +175,7 @@ __device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v
       p.sum += (double)s;
     }
     lane_top = fmaxf(lane_top, top);
+    return top;
   };
 #pragma unroll 1
   for (uint32_t i = 0; i < n_tiles; ++i) {
@@ -183,9 +185,8 @@ __device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v
 #pragma unroll
       for (uint32_t u = 0; u < LANE / 2; ++u) t.d[u] = i * (TILE / 8u) + u / 4 * 64u + lane < pieces ? t.d[u] : NONE;
     }
-    add(t.d, std::integral_constant<uint32_t, LANE / 2>{});
+    tops[i * 64u + lane] = (uint16_t)(__float_as_uint(add(t.d, std::integral_constant<uint32_t, LANE / 2>{})) >> 16);
   }
-  const float whole_top = lane_top;
   if (before + behind) add(&edge, std::integral_constant<uint32_t, 1>{});
   p.ref = huge ? (double)m : (double)m + ((double)c - (double)m * (double)LOG2E) * LN2;        // 2^(x LOG2E - c) stands for e^(x - m) 2^(m LOG2E - c)
   p.sum = wave_total(p.sum);
@@ -226,27 +227,42 @@ __device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v
     n_waiting += (uint32_t)__popcll(who);
   };
   if (before + behind) wait(edge & 0xffffu, edge_at);
-  // a lane's pieces are 64 apart; all pieces of those lanes, one a lane
-  const uint64_t who = __ballot(whole_top >= bound && whole_top > -INFINITY);
-  if (who >> lane & 1u) space.lanes[(uint32_t)__popcll(who & ((1ull << lane) - 1ull))] = (uint8_t)lane;
-  const uint32_t rows = 2u * n_tiles, all = (uint32_t)__popcll(who) * rows;
-  auto piece_of = [&](uint32_t i) {               // i: counted lane by lane
-    const uint32_t which = i / rows, at = (i - which * rows) * 64u + space.lanes[min(which, 63u)];
-    return i < all && at < pieces ? at : ~0u;
-  };
-  if (all) {
-    uint32_t at_next = piece_of(lane);
-    uint4 q = piece(min(at_next, pieces - 1u));
+  // a lane's two pieces of every tile in which it reaches the bound are read again, one a lane
+  const uint64_t lower = (1ull << lane) - 1ull;
+  uint32_t n_found = 0;
 #pragma unroll 1
-    for (uint32_t first = 0; first < all; first += 64u) {
-      const uint4 now = q;
-      const uint32_t at = at_next, d[4] = {now.x, now.y, now.z, now.w};
-      at_next = piece_of(first + 64u + lane);
-      q = piece(min(at_next, pieces - 1u));
+  for (uint32_t first = 0; first < n_tiles; first += TOPS) {
+    float top[TOPS];
+#pragma unroll
+    for (uint32_t u = 0; u < TOPS; ++u) {
+      top[u] = __uint_as_float((uint32_t)tops[min(first + u, n_tiles - 1u) * 64u + lane] << 16);
+      if (first + u >= n_tiles || !(top[u] >= bound)) top[u] = -INFINITY;
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < TOPS; ++u) {
+      const uint64_t found = __ballot(top[u] > -INFINITY);
+      if (!found) continue;
+      const uint32_t at = (first + u) * 128u + lane;
+      if (found >> lane & 1u) space.pieces[n_found / 2u + (uint32_t)__popcll(found & lower)] = at | (at + 64u) << 16;
+      n_found += 2u * (uint32_t)__popcll(found);
+    }
+    const bool last = first + TOPS >= n_tiles;
+    if (!n_found || (n_found < 64u && !last)) continue;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    uint32_t done = 0;
+    for (; done < n_found && (last || n_found - done >= 64u); done += 64u) {
+      const uint32_t k = min(done + lane, n_found - 1u), at = space.pieces[k / 2u] >> 16u * (k & 1u) & 0xffffu;
+      const bool there = done + lane < n_found && at < pieces;
+      const uint4 q = piece(min(at, pieces - 1u));
+      const uint32_t d[4] = {q.x, q.y, q.z, q.w};
       if (n_waiting > WAITING - 512u) sort_out();
 #pragma unroll
-      for (uint32_t u = 0; u < 8; ++u) wait(at != ~0u ? d[u / 2] >> 16 * (u & 1) & 0xffffu : 0xff80u, before + at * 8u + u);
+      for (uint32_t u = 0; u < 8; ++u) wait(there ? d[u / 2] >> 16 * (u & 1) & 0xffffu : 0xff80u, before + at * 8u + u);
     }
+    if (last) break;
+    const uint32_t left = n_found - done, x = space.pieces[done / 2u + (lane & 31u)];       // less than a wavefront's: for the next turn
+    if (2u * lane < left) space.pieces[lane] = x;
+    n_found = left;
   }
   sort_out();
   return p;
@@ -291,6 +307,7 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
   __shared__ double lse[BEAM_MAX_WIDTH], score[BEAM_MAX_WIDTH], factor[BEAM_MAX_WIDTH];        // factor: what a beam's totals are divided by
   __shared__ int32_t count[BEAM_MAX_WIDTH], parent[BEAM_MAX_WIDTH], token[BEAM_MAX_WIDTH];
   __shared__ uint32_t kind[BEAM_MAX_WIDTH];                                                     // 0: none, 1: goes on, 2: has ended
+  extern __shared__ uint32_t staged[];    // a part's tiles' maxima; then the parts' best tokens and a cursor for every list but a thread's first
   float old_score = -INFINITY;
   int32_t old_count = 0, old_ended = 0;
   if (tid < W) { old_score = a.scores[r0 + tid]; old_count = a.counts[r0 + tid]; old_ended = a.ended[r0 + tid]; }
@@ -300,7 +317,7 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
       const uint32_t v0 = part * a.span;
       __shared__ PartSpace space[WAVES];
       // (a beam that is none, or has ended: nobody asks for what is left here)
-      const Part p = part_of(a.logits + (uint64_t)row * a.ld, v0, min(v0 + a.span, a.vocab), W, space[wave], [&] { return !a.ended[row] && a.scores[row] > -INFINITY; });
+      const Part p = part_of(a.logits + (uint64_t)row * a.ld, v0, min(v0 + a.span, a.vocab), W, space[wave], (uint16_t*)staged + (uint64_t)wave * a.tiles * 64u, [&] { return !a.ended[row] && a.scores[row] > -INFINITY; });
       const uint64_t list = (uint64_t)group * lists + w;
       if (lane < W) share_out(a.best + list * W + lane, p.best);
       if (lane == 0) { share_out(a.sums + 2 * list, p.sum); share_out(a.sums + 2 * list + 1, p.ref); }
@@ -316,7 +333,6 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
 
   __shared__ uint64_t found_order[WAVES][BEAM_MAX_WIDTH];
   __shared__ uint32_t found_place[WAVES][BEAM_MAX_WIDTH], found_logit[WAVES][BEAM_MAX_WIDTH];
-  extern __shared__ uint32_t staged[];                                                          // the parts' best tokens, then a cursor for every list but a thread's first
   const bool stage = lists * W <= STAGED;
   uint8_t* const cursor = (uint8_t*)(staged + (stage ? lists * W : 0u));
   const uint32_t* const best = a.best + (uint64_t)group * lists * W;
@@ -554,7 +570,8 @@ hipError_t launch_beam_select(BeamArgs a, void* scratch, hipStream_t st) {
   a.sums = (double*)((char*)scratch + BEAM_COUNTERS * 4);
   a.best = (uint32_t*)((char*)a.sums + 16ull * a.n_rows * a.parts);
   a.wgs = (a.width * a.parts + WAVES - 1) / WAVES;
-  const uint32_t lists = a.width * a.parts, lds = (lists * a.width <= STAGED ? lists * a.width * 4 : 0) + lists;
+  a.tiles = (a.span / 8 + TILE / 8 - 1) / (TILE / 8);
+  const uint32_t lists = a.width * a.parts, lds = std::max(WAVES * a.tiles * 128, (lists * a.width <= STAGED ? lists * a.width * 4 : 0) + lists);
   beam_select_kernel<<<a.n_rows / a.width * a.wgs, THREADS, lds, st>>>(a);
   return hipGetLastError();
 }

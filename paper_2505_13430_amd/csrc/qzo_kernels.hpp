@@ -394,7 +394,7 @@ struct BeamArgs {
   // in the scratch, and how rows are cut
   uint32_t* counters;
   double* sums;                      // of every part: a sum, what its exponents are relative to
-  uint32_t *best, parts, span, wgs;  // wgs: workgroups of a prompt
+  uint32_t *best, parts, span, wgs, tiles;  // wgs: workgroups of a prompt; tiles: of a part, at most
 };
 uint64_t beam_select_scratch(uint32_t n_rows, uint32_t width, uint32_t vocab);
 hipError_t launch_beam_select(BeamArgs a, void* scratch, hipStream_t st);

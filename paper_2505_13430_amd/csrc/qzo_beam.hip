@@ -300,12 +300,13 @@ __device__ __forceinline__ Candidate wave_first(const Candidate& c) {
 // One launch.  Every wavefront takes a part of a row; the last workgroup of a prompt to be done finds its beams among the parts' best, each list of
 // them in order; the last prompt's packs the tokens.
 constexpr uint32_t STAGED = 8192;                                        // best tokens of all parts that fit the LDS
-constexpr uint32_t HELD = 16;
+constexpr uint32_t HELD = 16, EARLY = 8;
 __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
   const uint32_t W = a.width, lists = W * a.parts, group = blockIdx.x / a.wgs, r0 = group * W;
   __shared__ double lse[BEAM_MAX_WIDTH], score[BEAM_MAX_WIDTH], factor[BEAM_MAX_WIDTH];        // factor: what a beam's totals are divided by
   __shared__ int32_t count[BEAM_MAX_WIDTH], parent[BEAM_MAX_WIDTH], token[BEAM_MAX_WIDTH];
+  __shared__ PartSpace space[WAVES];
   __shared__ uint32_t kind[BEAM_MAX_WIDTH];                                                     // 0: none, 1: goes on, 2: has ended
   extern __shared__ uint32_t staged[];    // a part's tiles' maxima; then the parts' best tokens and a cursor for every list but a thread's first
   float old_score = -INFINITY;
@@ -315,7 +316,6 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
     const uint32_t w = (blockIdx.x % a.wgs) * WAVES + wave, b = w / a.parts, part = w % a.parts, row = r0 + b;
     if (w < lists) {
       const uint32_t v0 = part * a.span;
-      __shared__ PartSpace space[WAVES];
       // (a beam that is none, or has ended: nobody asks for what is left here)
       const Part p = part_of(a.logits + (uint64_t)row * a.ld, v0, min(v0 + a.span, a.vocab), W, space[wave], (uint16_t*)staged + (uint64_t)wave * a.tiles * 64u, [&] { return !a.ended[row] && a.scores[row] > -INFINITY; });
       const uint64_t list = (uint64_t)group * lists + w;
@@ -340,11 +340,12 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
   uint32_t longest_old = 0;
   for (uint32_t b = 0; b < W; ++b)
     if (kind[b]) longest_old = max(longest_old, min((uint32_t)count[b], a.max_history));
-  const bool short_ones = longest_old <= THREADS * 4u / W;
-  __shared__ int32_t histories[THREADS * 4];
-  int32_t early[4];
+  const bool short_ones = longest_old <= THREADS * EARLY / W;
+  int32_t* const histories = (int32_t*)space;                    // the parts are done
+  static_assert(sizeof(space) >= THREADS * EARLY * 4);
+  int32_t early[EARLY];
 #pragma unroll
-  for (uint32_t u = 0; u < 4; ++u) {
+  for (uint32_t u = 0; u < EARLY; ++u) {
     const uint32_t e = u * THREADS + tid;
     if (short_ones && e < longest_old * W) early[u] = a.history[(uint64_t)(r0 + e / longest_old) * a.max_history + e % longest_old];
   }
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
   if (stage && wave >= W)                       // (a wavefront without a beam)
     for (uint32_t i = tid; i < lists * W; i += THREADS) staged[i] = shared_in(best + i);
 #pragma unroll
-  for (uint32_t u = 0; u < 4; ++u)
+  for (uint32_t u = 0; u < EARLY; ++u)
     if (short_ones && u * THREADS + tid < longest_old * W) histories[u * THREADS + tid] = early[u];
   __syncthreads();
   auto total_of = [&](uint32_t b, float x) { return kind[b] == 2u ? score[b] : ((double)x - lse[b]) + score[b]; };

@@ -91,7 +91,7 @@ __device__ __forceinline__ bool last_of(uint32_t* counter, uint32_t all, uint32_
 //   A tile whose sum or maximum tells of a NaN, an infinity or a number beyond 1e30 is gone through again, logit by logit.
 //   The best tokens: the width-th highest of the lanes' maxima is a bound that no lane with a lower maximum reaches, which leaves `width`
 // lanes (more where there are ties); the tiles of theirs whose maximum reaches it, too, are read again and compared.  (Looked for in every tile, as the row goes by, they cost
-// twice the instructions of all the rest: 96 x 5 rows of 99991 65 us, so 41.)
+// twice the instructions of all the rest: 96 x 5 rows of 99991 65 us, so 41; all pieces of those lanes, 41, their best tiles' only, 38.)
 struct Part {
   uint32_t best = 0;            // lane i: the i-th best: the logit's order above, the place from behind below: no two are equal
   double sum = 0.0, ref = 0.0;  // sum of e^x = sum e^ref; ref the same in all lanes
@@ -294,9 +294,9 @@ __device__ __forceinline__ Candidate wave_first(const Candidate& c) {
   return r;
 }
 
-// 96 x 5 rows of 99991: 41 us.  The logits have been read after 22 (88 MB, 4 TB/s), then come the hand-over to a prompt's
-// last workgroup, its lists, rounds and states, 10 us from one to the next of which only the last prompt's show.  1 x 4 rows of 32000: 12 us, all latency:
-// a part 3.6, the hand-over 1.7, lists and sums 2.3, rounds 2.5, states 1.4.
+// 96 x 5 rows of 99991 (88 MB, 14.5 us of reading): 35.6 us; exponentials beside the loads, then the hand-over to a prompt's last workgroup, its lists,
+// rounds and states, some 10 us of which the last prompts' show.  1 x 4 rows of 32000: 12.6 us, all latency: a part 4, the hand-over 1.7, lists and
+// sums 2.3, rounds 2.5, states 1.4.
 // One launch.  Every wavefront takes a part of a row; the last workgroup of a prompt to be done finds its beams among the parts' best, each list of
 // them in order; the last prompt's packs the tokens.
 constexpr uint32_t STAGED = 8192;                                        // best tokens of all parts that fit the LDS
@@ -546,9 +546,9 @@ __global__ __launch_bounds__(THREADS) void beam_select_kernel(BeamArgs a) {
   }
 }
 
-// Parts of a row: enough wavefronts for the chip (96 x 5 rows of 99991 with 2048 / 4096 / 6144: 36 / 36 / 45 us), two tiles at least for each (4 rows of
-// 32000 in 32 parts of one: 1 us more, for the lists that there are then).
-constexpr uint32_t WANTED_WAVES = 4096;
+// Parts of a row: enough wavefronts for the chip (rows of 99991, five a prompt, with 1536 / 2048 / 3072 / 4096 wavefronts: 480 rows 38.5 / 35.6 / 36.3 / 37.3 us,
+// 80 rows 25.5 / 26.4 / 28.5 / 31.9), two tiles at least for each (4 rows of 32000 in 32 parts of one: 1 us more, for the lists that there are then).
+constexpr uint32_t WANTED_WAVES = 2048;
 void cut(uint32_t n_rows, uint32_t vocab, uint32_t* parts, uint32_t* span) {
   uint32_t p = std::min((vocab + 2 * TILE - 1) / (2 * TILE), std::max(1u, WANTED_WAVES / n_rows));
   p = std::min(std::max(p, (vocab + MAX_SPAN - 1) / MAX_SPAN), MAX_PARTS);

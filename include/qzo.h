@@ -512,9 +512,10 @@ qzo_status qzo_beam_select(const void* logits_dev, uint64_t ld_logits, uint32_t 
 /*
  * qzo_paged_attention for groups of sequences that begin alike: group g is sequences group_starts[g] .. group_starts[g + 1] - 1 (int32
  * [n_groups + 1], ascending, values cut off at 0 and n_seq; sequences in no group attend as in qzo_paged_attention), whose first shared_dev[g]
- * tokens have the same keys and values.  Those, down to a multiple of 16, are read once for all the group's rows, through the table of its first
- * sequence; every sequence's other positions through its own.  A sequence whose new tokens begin before the shared part ends reads all of
- * its positions itself; so do all where the first sequence is shorter than that.  Otherwise results, limits and roundings are
+ * tokens, down to a multiple of 16, have the same keys and values wherever they lie before a sequence's new tokens (a sequence that has ended, or
+ * whose new tokens begin before that, need not agree).  They are read once for all the group's rows, through the table of the first sequence that has
+ * them before its new tokens; every sequence's other positions through its own.  A sequence whose new tokens begin before the shared
+ * part ends reads all of its positions itself.  Otherwise results, limits and roundings are
  * those of qzo_paged_attention (p meets v as two bf16 numbers where the columns of the group, or of the sequence, are as few as it says; in
  * groups of more than 64 columns a key head on average, new tokens times query heads of a key head, the common keys' p is rounded once).
  * scratch_dev: qzo_paged_attention_shared_scratch_bytes bytes, kept as qzo_paged_attention's (its first 2048 bytes zero).  n_groups 1 .. 2048.

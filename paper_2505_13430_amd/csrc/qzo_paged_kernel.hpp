@@ -122,34 +122,74 @@ __device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, uint32_t i, bool
   return w;
 }
 
-// Item i of a launch.  In the LDS: starts [n_groups + 1], the groups' first sequences, and common [n_groups], how many positions each group
-// reads together.
+// First row of sequence s, and behind sequence s - 1.
+__device__ __forceinline__ uint32_t row_of(const SharedArgs& a, uint32_t s) { return (uint32_t)(a.starts ? min(max(a.starts[s], 0), (int32_t)a.n_rows) : (int32_t)min(s, a.n_rows)); }
+__device__ __forceinline__ uint32_t rows_of(const SharedArgs& a, uint32_t s) {
+  const uint32_t first = row_of(a, s), end = row_of(a, s + 1);
+  return end > first ? end - first : 0u;
+}
+__device__ __forceinline__ uint32_t length_of(const SharedArgs& a, uint32_t s) { return (uint32_t)min(max(a.lengths[s], 0), (int32_t)(a.max_blocks << a.block_shift)); }
+// The group that sequence s may be in: the last one that does not begin behind it.
+__device__ __forceinline__ uint32_t group_at(const int32_t* starts, uint32_t n_groups, uint32_t s) {
+  uint32_t lo = 0, hi = n_groups;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) >> 1;
+    if ((uint32_t)starts[mid] <= s) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+// What the groups are, by all N threads of a workgroup, into the LDS: starts [n_groups + 1], their first sequences; leader [n_groups], each one's first
+// sequence with the common keys behind its new tokens: its table names them (one that has ended, or that a new text has taken, names others); common
+// [n_groups], how many positions a group reads together, 0 where none leads.
+template <uint32_t N>
+__device__ __forceinline__ void find_groups(const SharedArgs& a, int32_t* starts, int32_t* common, int32_t* leader) {
+  const uint32_t tid = threadIdx.x, lane = tid & 63u;
+  for (uint32_t g = tid; g <= a.n_groups; g += N) {
+    const int32_t s0 = min(max(a.group_starts[g], 0), (int32_t)a.n_seq);
+    starts[g] = s0;
+    if (g == a.n_groups) break;
+    // (loads without branches around them, at once)
+    const uint32_t first = min((uint32_t)s0, a.n_seq - 1u), length = length_of(a, first), rows = rows_of(a, first);
+    const int32_t s1 = min(max(a.group_starts[g + 1], s0), (int32_t)a.n_seq), shared = max(0, a.shared[g]) & ~15, n = s1 - s0 < 2 ? 0 : shared;
+    common[g] = n;
+    leader[g] = n && length < rows + (uint32_t)n ? (int32_t)a.n_seq : (int32_t)first;
+  }
+  __syncthreads();
+  bool searched = false;
+  for (uint32_t g0 = 0; g0 < a.n_groups; g0 += 64) searched |= leader[min(g0 + lane, a.n_groups - 1u)] == (int32_t)a.n_seq;
+  if (!__any(searched)) return;
+  __syncthreads();
+  // a group whose first sequence does not lead: all sequences are looked at, one a thread
+  for (uint32_t s = tid; s < a.n_seq; s += N) {
+    const uint32_t g = group_at(starts, a.n_groups, s), n = (uint32_t)common[g];
+    if (n && (uint32_t)starts[g] <= s && s < (uint32_t)starts[g + 1] && length_of(a, s) >= rows_of(a, s) + n) atomicMin(leader + g, (int32_t)s);
+  }
+  __syncthreads();
+  for (uint32_t g = tid; g < a.n_groups; g += N)
+    if (leader[g] == (int32_t)a.n_seq) { leader[g] = 0; common[g] = 0; }
+  __syncthreads();
+}
+
+// Item i of a launch; the groups as find_groups leaves them.
 template <int CT, bool TILED>
-__device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, const int32_t* starts, const int32_t* common, uint32_t i, bool wide, bool quads) {
+__device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, const int32_t* starts, const int32_t* common, const int32_t* leader, uint32_t i, bool wide, bool quads) {
   typedef Dealing<CT, TILED> D;
   const uint32_t item = a.item_first + i;
   SharedWork w;
-  auto row_of = [&](uint32_t s) { return (uint32_t)(a.starts ? min(max(a.starts[s], 0), (int32_t)a.n_rows) : (int32_t)min(s, a.n_rows)); };
   if (item < a.n_groups) {
     const uint32_t s0 = (uint32_t)starts[item], s1 = max(s0, (uint32_t)starts[item + 1]);
-    w.all = 1; w.from = 0; w.table = s0;
+    w.all = 1; w.from = 0; w.table = (uint32_t)leader[item];
     w.len = (uint32_t)common[item];
-    w.row0 = row_of(s0);
-    const uint32_t end = row_of(s1);
+    w.row0 = row_of(a, s0);
+    const uint32_t end = row_of(a, s1);
     w.rows = w.len && end > w.row0 ? end - w.row0 : 0u;
   } else {
-    const uint32_t s = item - a.n_groups;
+    const uint32_t s = item - a.n_groups, g = group_at(starts, a.n_groups, s);
     w.all = 0; w.table = s;
-    w.row0 = row_of(s);
-    const uint32_t end = row_of(s + 1);
-    w.rows = end > w.row0 ? end - w.row0 : 0u;
-    w.len = (uint32_t)min(max(a.lengths[s], 0), (int32_t)(a.max_blocks << a.block_shift));
-    uint32_t lo = 0, hi = a.n_groups;
-    while (hi - lo > 1) {
-      const uint32_t mid = (lo + hi) >> 1;
-      if ((uint32_t)starts[mid] <= s) lo = mid; else hi = mid;
-    }
-    w.from = (uint32_t)starts[lo] <= s && s < (uint32_t)starts[lo + 1] && w.len >= w.rows + (uint32_t)common[lo] ? (uint32_t)common[lo] : 0u;
+    w.row0 = row_of(a, s);
+    w.rows = rows_of(a, s);
+    w.len = length_of(a, s);
+    w.from = (uint32_t)starts[g] <= s && s < (uint32_t)starts[g + 1] && w.len >= w.rows + (uint32_t)common[g] ? (uint32_t)common[g] : 0u;
   }
   const uint64_t cols = (uint64_t)w.rows * a.group;
   w.wide = !TILED && wide && cols > 2 * D::TC;
@@ -277,22 +317,16 @@ __global__ __launch_bounds__(THREADS, 8 / WAVES) void paged_attention_kernel(typ
 
   // ---- the sequences' units: up to 64 sequences in the lanes of every wavefront, more in the LDS
   uint32_t n_seq = a.n_seq;                         // SHARED: of items
-  int32_t *group_starts = nullptr, *common = nullptr;
+  int32_t *group_starts = nullptr, *common = nullptr, *leader = nullptr;
   if constexpr (SHARED) {
     n_seq = a.n_items;
     group_starts = (int32_t*)(first_unit + (few ? 0u : n_seq));       // [n_groups + 1]
     common = group_starts + a.n_groups + 1;                           // [n_groups]
-    for (uint32_t g = tid; g <= a.n_groups; g += THREADS) {
-      const int32_t s0 = min(max(a.group_starts[g], 0), (int32_t)a.n_seq);
-      group_starts[g] = s0;
-      if (g == a.n_groups) break;
-      const int32_t s1 = min(max(a.group_starts[g + 1], s0), (int32_t)a.n_seq);
-      common[g] = s1 - s0 < 2 ? 0 : max(0, min(min(a.shared[g], a.lengths[s0]), (int32_t)(a.max_blocks << a.block_shift))) & ~15;
-    }
-    __syncthreads();
+    leader = common + a.n_groups;                                     // [n_groups]
+    find_groups<THREADS>(a, group_starts, common, leader);
   }
   auto work_of = [&](uint32_t i, bool wide, bool quads) {
-    if constexpr (SHARED) return shared_work<CT, TILED>(a, group_starts, common, i, wide, quads);
+    if constexpr (SHARED) return shared_work<CT, TILED>(a, group_starts, common, leader, i, wide, quads);
     else return seq_work<CT, TILED>(a, i, wide, quads);
   };
   const uint32_t per = (n_seq + THREADS - 1) / THREADS, s_first = min(tid * per, n_seq), s_last = min(s_first + per, n_seq);

@@ -44,25 +44,18 @@ __global__ __launch_bounds__(CK_THREADS, 2) void common_keys_kernel(SharedArgs a
   uint64_t* const first_unit = (uint64_t*)(lds + ck_lds<DH>());         // [n_groups + 1]
   int32_t* const group_starts = (int32_t*)(first_unit + a.n_groups + 1);  // [n_groups + 1]
   int32_t* const common = group_starts + a.n_groups + 1;                // [n_groups]
+  int32_t* const leader = common + a.n_groups;                          // [n_groups]
   __shared__ uint64_t red[CK_WAVES];
   __shared__ uint32_t bad[CK_TILE];
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = scalar(tid >> 6), n = lane & 31u, hi = lane >> 5;
 
   // ---- the groups' units
-  for (uint32_t g = tid; g <= a.n_groups; g += CK_THREADS) {
-    const int32_t s0 = min(max(a.group_starts[g], 0), (int32_t)a.n_seq);
-    group_starts[g] = s0;
-    if (g == a.n_groups) break;
-    const int32_t s1 = min(max(a.group_starts[g + 1], s0), (int32_t)a.n_seq);
-    common[g] = s1 - s0 < 2 ? 0 : max(0, min(min(a.shared[g], a.lengths[s0]), (int32_t)(a.max_blocks << a.block_shift))) & ~15;
-  }
-  __syncthreads();
+  find_groups<CK_THREADS>(a, group_starts, common, leader);
   struct Group { uint32_t row0, cols, tiles, units; };
-  auto row_of = [&](uint32_t s) { return (uint32_t)(a.starts ? min(max(a.starts[s], 0), (int32_t)a.n_rows) : (int32_t)min(s, a.n_rows)); };
   auto group_of = [&](uint32_t g) {
     Group w;
-    const uint32_t s0 = (uint32_t)group_starts[g], s1 = max(s0, (uint32_t)group_starts[g + 1]), end = row_of(s1);
-    w.row0 = row_of(s0);
+    const uint32_t s0 = (uint32_t)group_starts[g], s1 = max(s0, (uint32_t)group_starts[g + 1]), end = row_of(a, s1);
+    w.row0 = row_of(a, s0);
     w.cols = end > w.row0 ? (end - w.row0) * a.group : 0u;
     w.tiles = (w.cols + CK_TILE - 1) / CK_TILE;
     w.units = w.cols ? ((uint32_t)common[g] + CK_KEYS - 1) / CK_KEYS : 0u;
@@ -109,7 +102,7 @@ __global__ __launch_bounds__(CK_THREADS, 2) void common_keys_kernel(SharedArgs a
     const uint64_t group_end = unit - at + w.units;
     const uint32_t pieces = scalar((uint32_t)((group_end - 1) / share)) + 1u - wg;     // of the first piece's, this workgroup included
     unit += u_end - at;
-    const uint32_t n_keys = scalar((uint32_t)common[g]), seq = scalar((uint32_t)group_starts[g]);
+    const uint32_t n_keys = scalar((uint32_t)common[g]), seq = scalar((uint32_t)leader[g]);
 
     // ---- this wavefront's columns
     const uint32_t col0 = tile * CK_TILE, n_cols = min(CK_TILE, w.cols - col0), blocks = (n_cols + CK_COLS - 1) / CK_COLS;
@@ -482,10 +475,10 @@ hipError_t launch_items(SharedArgs a, uint32_t rows, uint32_t first, uint32_t n_
   const uint64_t units = (((uint64_t)a.max_blocks << a.block_shift) + 31) / 32;
   const bool few = n_items <= 64 && (double)groups * (double)(2 * units + 2) < 4e9;      // 32 bits hold the sums, padding included
   const uint32_t sums = WAVES * TC * (DH + 4) * 4 + WAVES * TC * 8, row = DH * (E4M3 ? 1u : 2u), tiles = TILED ? 8u * tile_step(row) * row : 0u;
-  const uint32_t fixed = std::max(sums, tiles) + WAVES * 8, lds = fixed + (few ? 0 : n_items * 8) + (2 * a.n_groups + 1) * 4;
+  const uint32_t fixed = std::max(sums, tiles) + WAVES * 8, lds = fixed + (few ? 0 : n_items * 8) + (3 * a.n_groups + 1) * 4;
   if (lds > 60u * 1024) {                       // the limit that all calls have in common
     hipError_t e = hipFuncSetAttribute((const void*)paged_attention_kernel<DH, E4M3, CT, TILED, true>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)(fixed + CACHE_MAX_SEQ * 8 + (2 * SHARED_MAX_GROUPS + 1) * 4));
+                                       (int)(fixed + CACHE_MAX_SEQ * 8 + (3 * SHARED_MAX_GROUPS + 1) * 4));
     if (e != hipSuccess) return e;
   }
   const uint32_t wgs = (uint32_t)std::min<uint64_t>(MAX_WGS, (groups * ((units + MIN_PIECE - 1) / MIN_PIECE) + 7) / 8 * 8);
@@ -513,8 +506,8 @@ hipError_t launch_shared(SharedArgs a, void* scratch, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (many_columns(rows, a.group, a.n_groups)) {
     pieces = (float*)((char*)scratch + MAX_WGS * 4) + 2ull * MAX_WGS * shared_part_columns(a.n_rows, a.group) * (DH + 4);
-    const uint32_t lds = ck_lds<DH>() + (a.n_groups + 1) * 8 + (2 * a.n_groups + 1) * 4;
-    e = hipFuncSetAttribute((const void*)common_keys_kernel<DH, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(ck_lds<DH>() + (SHARED_MAX_GROUPS + 1) * 16));
+    const uint32_t lds = ck_lds<DH>() + (a.n_groups + 1) * 8 + (3 * a.n_groups + 1) * 4;
+    e = hipFuncSetAttribute((const void*)common_keys_kernel<DH, E4M3>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(ck_lds<DH>() + (SHARED_MAX_GROUPS + 1) * 20));
     if (e != hipSuccess) return e;
     common_keys_kernel<DH, E4M3><<<CK_WGS, CK_THREADS, lds, st>>>(a, pieces);
     e = hipGetLastError();

@@ -1015,3 +1015,82 @@ def test_select_with_a_history_of_many_columns():
     assert history[:, -1].tolist() == list(range(64))
     for i in (0, 4, 5, 6, 63):
         assert torch.equal(history[i, :-1], torch.arange(columns - 1, dtype=torch.int32, device=DEV))
+
+
+# ------------------------------------------------------------------ sequences that end and begin among those that share ----
+def _refill(d, i, length, seed=0):
+    """Sequence i of what _attend made, which has ended, begins again: `length` tokens, all of them new, in blocks that nobody holds."""
+    gen, block = torch.Generator(device=DEV).manual_seed(seed), d["k"].shape[2]
+    assert d["starts"] is not None and int(d["lengths"][i]) == 0
+    n = -(-length // block)
+    unused = sorted(set(range(d["k"].shape[0])) - set(d["tables"].flatten().tolist()))
+    d["tables"] = torch.nn.functional.pad(d["tables"], (0, max(0, n - d["tables"].shape[1])), value=-1)
+    d["tables"][i, :n] = _i32(unused[:n])
+    d["lengths"][i] = length
+    at, starts = d["starts_list"][i], d["starts_list"]
+    q = torch.randn(length, d["q"].shape[1], generator=gen, device=DEV).to(torch.bfloat16)
+    d["q"] = torch.cat([d["q"][:at], q, d["q"][at:]])
+    d["starts_list"] = starts[:i + 1] + [x + length for x in starts[i + 1:]]
+    d["starts"] = _i32(d["starts_list"])
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("length", [1, 16, 20, 63, 64, 65, 100])
+@pytest.mark.parametrize("n,H,Hk,dh", [(4, 4, 4, 128), (4, 4, 2, 64), (40, 4, 2, 128), (150, 1, 1, 64)])
+def test_a_sequence_that_begins_among_those_that_share(n, H, Hk, dh, length, e4m3):
+    """Its keys are not the group's, however many they are; first of its group, in the middle, and both."""
+    for dead in ((0,), (n // 2,), (0, 1, n - 1)):
+        d = _attend([n, 3], [64, 48], [12] * (n + 3), H, Hk, dh, 16, news=[1] * (n + 3), e4m3=e4m3, dead=dead, seed=n + length, extra=30)
+        for i in dead:
+            _refill(d, i, length, seed=i)
+        _check_shared(d)
+
+
+@gpu
+@pytest.mark.parametrize("news", [False, True])
+@pytest.mark.parametrize("n,H,Hk,dh", [(5, 4, 4, 128), (90, 4, 2, 64), (600, 1, 1, 64)])
+def test_who_has_the_common_keys(n, H, Hk, dh, news):
+    """They are read through the table of the first sequence that has them before its new tokens: what the others' tables name there does not matter."""
+    for dead in ((), (0,), (0, 1, 3), tuple(range(n - 2))):
+        d = _attend([n, 2], [64, 32], [12] * (n + 2), H, Hk, dh, 16, news=[1 + 2 * (i % 2) for i in range(n + 2)] if news else None, dead=dead, seed=n + len(dead))
+        want = _check_shared(d)
+        first = min(set(range(n)) - set(dead))
+        for i in range(first + 1, n):
+            d["tables"][i, :4] = -1
+        assert torch.equal(_shared_call(d), want)
+
+
+@gpu
+@pytest.mark.parametrize("name,e4m3", [("tiny", False), ("wide_heads", False), ("tiny", True)])
+@pytest.mark.parametrize("length", [20, 40, 100])
+def test_a_new_prompt_beside_candidates(name, e4m3, length):
+    """In the step in which the others go on, and in the steps behind it: the logits of the model over each text."""
+    m = _model(name, "int4")
+    rng = torch.Generator().manual_seed(7)
+    text = lambda k: torch.randint(0, m.shape["vocab"], (k,), generator=rng, dtype=torch.int32).to(DEV)
+    a = Answers(m, n_seq=6, n_blocks=60, block=16, max_blocks=12, width=4, e4m3=e4m3)
+    prompt = text(75)
+    a.add(prompt, _i32([75, 0, 0, 0, 0, 0]))
+    a.fork(_i32([0, 0, 0, 0, -1, -1]))
+    texts = [prompt] * 4 + [prompt[:0]] * 2
+    nothing = torch.zeros(0, dtype=torch.int32, device=DEV)
+
+    def step(added, where):
+        new = [text(k) if k > 0 else nothing for k in added]
+        for i, x in enumerate(new):
+            texts[i] = torch.cat([texts[i], x]) if added[i] >= 0 else nothing
+        got = a.add(torch.cat(new), _i32(added)).clone()
+        assert int(a.state[2]) == 0 and a.lengths.tolist() == [t.numel() for t in texts]
+        for i in where:
+            want = _logits(m, texts[i])
+            assert _far(got[i], want[-1]) <= max(0.1 if e4m3 else 2e-2, 2 * _apart(m, texts[i], want)), i
+        _check_cache(a)
+
+    step([1, 2, 1, 1, 0, 0], [0, 1, 2, 3])
+    step([-1, 0, 0, 0, 0, 0], [])
+    assert a.shared.tolist()[0] == 64
+    step([length, 1, 3, 1, 9, 0], [0, 1, 2, 3, 4])
+    step([1, 1, 1, 1, 1, 2], [0, 1, 2, 3, 4, 5])
+    step([0, 0, -1, 0, 0, 0], [])
+    step([1, 1, length, 1, 1, 1], [0, 1, 2, 3, 4, 5])

@@ -233,7 +233,8 @@ class Answers:
             self.group_starts = torch.arange(n_groups + 1, **i32).mul_(width).clamp_(max=n_seq)
             self.shared = torch.zeros(n_groups, **i32)
         self.forked = width is not None
-        self.copies, self._fork_room, self._own = None, None, torch.arange(n_seq, **i32)
+        self._own = torch.arange(n_seq, **i32)
+        self._make_fork_room()
 
     def rows(self, n_tokens: int, stream=None):
         """Slots, positions and workspace of steps of that many rows, from buffers that double as they are outgrown; the earlier ones
@@ -274,19 +275,17 @@ class Answers:
                           group_starts=self.group_starts, shared=self.shared)
         return self.logits
 
-    def _for_forks(self, stream):
-        """List of copies and scratch of forks and compactions, made on the stream that uses them first."""
-        if self.copies is None:
-            n, n_blocks = len(self.lengths), self.free.numel()
-            with torch.cuda.stream(stream):
-                self.copies = torch.zeros(max(n, n_blocks // 2), 4, dtype=torch.int32, device=self.free.device)
-                self._fork_room = torch.zeros(qb.qzo_cache_fork_scratch_bytes(n, n_blocks, self.tables.shape[1]), dtype=torch.uint8, device=self.free.device)
+    def _make_fork_room(self):
+        """List of copies and scratch of forks and compactions, made with the pools: were it made in the first call, and that one captured, the
+        scratch would be zero from the graph's first replay on only, and eager calls may come before it."""
+        n, n_blocks, dev = len(self.lengths), self.free.numel(), self.free.device
+        self.copies = torch.zeros(max(n, n_blocks // 2), 4, dtype=torch.int32, device=dev)
+        self._fork_room = torch.zeros(qb.qzo_cache_fork_scratch_bytes(n, n_blocks, self.tables.shape[1]), dtype=torch.uint8, device=dev)
 
     def fork(self, parents: torch.Tensor, stream=None):
         """parents int32 [n_seq]: sequence i goes on from what sequence parents[i] is (negative: it ends).  Full blocks are shared, open ones copied.
         An `add` that was captured before the first fork does not know that blocks may be shared (with a width it does).
         Whether there were blocks for that is in state[2], as for `add` (not QZO_OK: nothing has changed)."""
-        self._for_forks(stream)
         self.forked = True
         qb.qzo_cache_fork(parents, self.block, self.lengths, self.tables, self.free, self.state, self.copies, group_starts=self.group_starts,
                           shared=self.shared, scratch=self._fork_room, stream=stream)
@@ -294,7 +293,6 @@ class Answers:
 
     def compact(self, stream=None):
         """The blocks in use to the front of the pools: those from n_blocks - state[0] on are free."""
-        self._for_forks(stream)
         qb.qzo_cache_compact(self.block, self.lengths, self.tables, self.free, self.tables, self.state, self.copies, scratch=self._fork_room, stream=stream)
         qb.qzo_cache_copy(self.cache, self.copies, layers=self.k.shape[0], count=self.state, stream=stream)
 
@@ -320,7 +318,7 @@ class Answers:
         self.free = torch.full((n_blocks,), -1, **i32)
         self.free[:n_blocks - used] = torch.arange(n_blocks - 1, used - 1, -1, **i32)
         self.state[0] = n_blocks - used
-        self.copies = self._fork_room = None
+        self._make_fork_room()
 
 
 class Beams:

@@ -5,6 +5,7 @@ Tolerances are what the roundings add up to.  eps/2 of bf16 is 2^-8, of e4m3 2^-
 import ctypes as C
 import math
 import random
+import types
 
 import numpy as np
 import pytest
@@ -1094,3 +1095,75 @@ def test_a_new_prompt_beside_candidates(name, e4m3, length):
     step([1, 1, 1, 1, 1, 2], [0, 1, 2, 3, 4, 5])
     step([0, 0, -1, 0, 0, 0], [])
     step([1, 1, length, 1, 1, 1], [0, 1, 2, 3, 4, 5])
+
+
+# ------------------------------------------------------------------ what an Answers keeps, without a device ----
+def _on_the_host(monkeypatch, events):
+    """Answers over host tensors, its calls of the library only noted: (name, scratch)."""
+    note = lambda name: lambda *a, **k: events.append((name, k.get("scratch")))
+    for name in ("qzo_cache_fork", "qzo_cache_copy", "qzo_cache_compact", "qzo_cache_plan", "qzo_answer"):
+        monkeypatch.setattr(qb, name, note(name))
+    monkeypatch.setattr(qb, "make_cache", lambda *a: None)
+    monkeypatch.setattr(qb, "qzo_answer_workspace_bytes", lambda *a: 256)
+    monkeypatch.setattr(torch.cuda, "synchronize", note("synchronize"))
+    model = types.SimpleNamespace(shape=dict(d_model=128, n_heads=2, vocab=8, n_layers=1), scales=torch.zeros(1), handle=None)
+    return lambda **k: Answers(model, n_seq=8, n_blocks=2100, block=16, **k)
+
+
+@pytest.mark.parametrize("width", [None, 4])
+def test_scratch_of_forks_is_there_before_any_call(monkeypatch, width):
+    """A call that makes it may be captured: nothing has zeroed it then before the graph's first replay."""
+    events = []
+    a = _on_the_host(monkeypatch, events)(width=width)
+    for turn in range(2):
+        room = a._fork_room
+        assert room.numel() >= qb.qzo_cache_fork_scratch_bytes(8, a.free.numel(), 2100) and not room.any() and a.copies.shape[0] >= max(8, a.free.numel() // 2)
+        events.clear()
+        a.fork(torch.arange(8, dtype=torch.int32))
+        a.add(torch.zeros(3, dtype=torch.int32), torch.tensor([3] + [0] * 7, dtype=torch.int32))
+        a.compact()
+        assert all(s is room for name, s in events if name in ("qzo_cache_fork", "qzo_cache_compact")) and len(events) >= 5
+        a.state[0] = a.free.numel()
+        a.resize(3000)
+
+
+@gpu
+@pytest.mark.parametrize("first", ["add", "fork", "resize"])
+def test_a_captured_first_fork_before_eager_ones(first):
+    """A step is captured, the prompts are read by eager calls, then it is replayed: beyond the fork's small form, in memory that was not zero."""
+    m = _model("tiny", "int4")
+    text = torch.randint(0, 1024, (200,), generator=torch.Generator().manual_seed(8), dtype=torch.int32).to(DEV)
+    runs = []
+    for captured in (False, True):
+        torch.cuda.empty_cache()
+        filled = [torch.full((1 << n,), -1, dtype=torch.int32, device=DEV) for n in range(7, 24)]
+        del filled
+        a = Answers(m, n_seq=8, n_blocks=2100 if first != "resize" else 50, block=16, width=4 if first != "fork" else None)
+        if first == "resize":
+            a.resize(17000)                     # the table's columns stay: the small form's pool is what it is beyond
+        one, tokens, parents = _i32([1] * 4 + [0] * 4), text[:4].contiguous(), _i32([0, 1, 2, 3, -1, -1, -1, -1])
+
+        def step():
+            if first == "fork":
+                a.fork(parents)
+            a.add(tokens, one)
+
+        a.rows(200)
+        torch.cuda.synchronize()
+        if captured:
+            g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+            with torch.cuda.graph(g, stream=side):
+                step()
+        a.add(text[:90].contiguous(), _i32([30, 20, 25, 15, 0, 0, 0, 0]))
+        a.fork(_i32([0, 0, 2, 2, 1, -1, -1, -1]))
+        found = []
+        for _ in range(4):
+            g.replay() if captured else step()
+            torch.cuda.synchronize()
+            assert int(a.state[2]) == 0
+            _check_cache(a)
+            found += [a.logits.clone(), a.lengths.clone(), a.tables.clone()]
+            a.add(text[:5].contiguous(), _i32([2, 1, 1, 1, 0, 0, 0, 0]))
+            found.append(a.logits.clone())
+        runs.append(found)
+    assert all(torch.equal(x, y) for x, y in zip(*runs))

@@ -297,15 +297,16 @@ class Answers:
         qb.qzo_cache_copy(self.cache, self.copies, layers=self.k.shape[0], count=self.state, stream=stream)
 
     def resize(self, n_blocks: int):
-        """Pools of another number of blocks: memory given back to a training step between answers, or more of it.  Waits for the device; what
-        was captured with the old pools is no longer valid.  ValueError: the sequences hold more blocks than that (nothing has changed but their places)."""
+        """Pools of another number of blocks: memory given back to a training step between answers, or more of it.  Waits for the device, before (steps
+        may be under way on any stream) and behind what it does; what was captured with the old pools is no longer valid.  ValueError: the
+        sequences hold more blocks than that (nothing has changed but their places)."""
+        torch.cuda.synchronize(self.free.device)
         self.compact()
         free, had = int(self.state[0]), self.free.numel()
         used = had - free
         if n_blocks < max(1, used):
+            torch.cuda.synchronize(self.free.device)
             raise ValueError(f"{used} blocks are in use")
-        torch.cuda.synchronize()
-        pools = []
         for name in ("k", "v"):                 # one pool after the other: the old one's memory is free before the next is made
             old = getattr(self, name)
             new = torch.empty((old.shape[0], n_blocks, *old.shape[2:]), dtype=old.dtype, device=old.device)
@@ -319,6 +320,7 @@ class Answers:
         self.free[:n_blocks - used] = torch.arange(n_blocks - 1, used - 1, -1, **i32)
         self.state[0] = n_blocks - used
         self._make_fork_room()
+        torch.cuda.synchronize(self.free.device)
 
 
 class Beams:

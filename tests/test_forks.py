@@ -1167,3 +1167,47 @@ def test_a_captured_first_fork_before_eager_ones(first):
             found.append(a.logits.clone())
         runs.append(found)
     assert all(torch.equal(x, y) for x, y in zip(*runs))
+
+
+def test_a_resize_waits_before_it_begins(monkeypatch):
+    """Steps may be under way on any stream: the device is waited for before the pool is made compact, and behind whatever resize does."""
+    events = []
+    a = _on_the_host(monkeypatch, events)(width=4)
+    for n_blocks, held in ((3000, 5), (100, 100), (2, 3)):
+        a.state[0] = a.free.numel() - held
+        events.clear()
+        if n_blocks < held:
+            with pytest.raises(ValueError):
+                a.resize(n_blocks)
+        else:
+            a.resize(n_blocks)
+        names = [name for name, _ in events]
+        assert names[:2] == ["synchronize", "qzo_cache_compact"] and names[-1] == "synchronize"
+
+
+@gpu
+def test_a_resize_behind_steps_on_another_stream():
+    m = _model("tiny", "int4")
+    text = torch.randint(0, 1024, (400,), generator=torch.Generator().manual_seed(9), dtype=torch.int32).to(DEV)
+    runs, side, kept = [], torch.cuda.Stream(), []       # kept: what the side stream reads stays until it has been read
+
+    def counts(x):
+        kept.append(_i32(x))
+        return kept[-1]
+
+    for stream in (None, side):
+        a = Answers(m, n_seq=4, n_blocks=60, block=16, max_blocks=12, width=2)
+        torch.cuda.synchronize()
+        found = []
+        for n_blocks in (40, 80, 50):
+            for added in ([60, 0, 40, 0], [1, 0, 1, 0], [3, 0, 2, 0]):
+                a.add(text[:sum(added)].contiguous(), counts(added), stream)
+            a.fork(counts([0, 0, 2, 2]), stream)
+            a.resize(n_blocks)
+            _check_cache(a)
+            a.add(text[:8].contiguous(), counts([1, 3, 2, 2]), stream)
+            torch.cuda.synchronize()
+            found.append(a.logits.cpu())
+            a.add(text[:0], counts([-1] * 4), stream)
+        runs.append(found)
+    assert all(torch.equal(x, y) for x, y in zip(*runs))

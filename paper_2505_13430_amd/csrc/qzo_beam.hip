@@ -13,7 +13,7 @@ namespace {
 constexpr uint32_t THREADS = 256, WAVES = THREADS / 64, LANE = 16, TILE = 64 * LANE;      // logits of a lane and of a wavefront at a time
 constexpr uint32_t MAX_PARTS = 64, MAX_SPAN = 65536;          // a logit's place in a part is 16 bits
 constexpr double LN2 = 0.693147180559945309417;
-constexpr float LOG2E = 1.44269504088896f;
+constexpr float LOG2E = 1.44269504088896f, HIGHEST = 8.0f;
 
 // Highest and lowest value of the wavefront's lanes.
 template <int CTRL, int ROWS>
@@ -84,10 +84,11 @@ __device__ __forceinline__ bool last_of(uint32_t* counter, uint32_t all, uint32_
 
 // ---- a part of a row: its best tokens and its sum
 // A wavefront's part, TILE logits at a time, the next ones on their way.  Memory is what is to count, so a logit costs few instructions: half a
-// maximum, and 2^(x log2(e) - c) into the sum.  c stands for the part's maximum m; it is the first tile's (at most 60 less than any
-// later logit), a float that the sum is relative to exactly, so that its rounding is in no result.  What is off is log2(e) as a float (1.3e-8 of x - m), the
-// product's rounding (2^-24 of a few) and the exponential's (one ulp), which differ from logit to logit: some 1e-8 of a sum over many, far
-// less than what two candidates differ by.
+// maximum, and 2^(x log2(e) - c) into the sum.  c stands for the part's maximum m; it is the first tile's, or a later one's that is
+// 2^HIGHEST above it, a float that the sum is relative to exactly: the old sum is scaled by 2^(c - c2) in 64 bits, so that c's rounding is in
+// no result.  What is off, of a term near the maximum: log2(e) as a float (1.3e-8 of x - m), the product's rounding (2^-22 where the exponent is 4 to 8, 2.8 x
+// 2^-24 of the term), the exponential's (one ulp), a lane's sum of 16; at most some 16 x 2^-24, far less for a sum over many, whose
+// terms' roundings differ.  (With HIGHEST 60 the product's rounding is 2^-19 of a term, and 480 rows of 99991 or 4 of 32000 take as long.)
 //   A tile whose sum or maximum tells of a NaN, an infinity or a number beyond 1e30 is gone through again, logit by logit.
 //   The best tokens: the width-th highest of the lanes' maxima is a bound that no lane with a lower maximum reaches, which leaves `width`
 // lanes (more where there are ties); the tiles of theirs whose maximum reaches it, too, are read again and compared.  (Looked for in every tile, as the row goes by, they cost
@@ -137,12 +138,14 @@ __device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v
 #pragma unroll
     for (uint32_t u = 0; u < N; ++u) top = fmaxf(fmaxf(top, low_half(d[u])), high_half(d[u]));
     auto refer_to = [&](float tile_top) {          // a new reference, where these logits ask for one
-      if (!any(tile_top > -INFINITY && (!some || (tile_top - m) * LOG2E > 60.0f))) return;
+      if (!any(tile_top > -INFINITY && (!some || (tile_top - m) * LOG2E > HIGHEST))) return;
       float m2 = some ? fmaxf(m, tile_top) : tile_top;
       m2 = unordered(wave_top(ordered(m2)));
-      p.sum = some ? p.sum * (double)__builtin_amdgcn_exp2f((m - m2) * LOG2E) : 0.0;
-      m = m2; c = m * LOG2E; some = true;
-      huge = !(fabsf(m) < 1e30f);
+      const float c2 = m2 * LOG2E;
+      const bool huge2 = !(fabsf(m2) < 1e30f);
+      p.sum = some && !huge && !huge2 ? p.sum * exp2((double)c - (double)c2) : 0.0;      // (next to 1e30 a step of a logit is all there is)
+      m = m2; c = c2; some = true;
+      huge = huge2;
     };
     bool odd = huge || any(fabsf(top) > 1e30f && top != -INFINITY);
     if (!odd) {

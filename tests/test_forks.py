@@ -1211,3 +1211,29 @@ def test_a_resize_behind_steps_on_another_stream():
             a.add(text[:0], counts([-1] * 4), stream)
         runs.append(found)
     assert all(torch.equal(x, y) for x, y in zip(*runs))
+
+
+# ------------------------------------------------------------------ sums of rows that rise ----
+def _rising_rows(n, vocab, seed):
+    """Rows of tiles that lie higher than the ones before, by 2 to 120, anywhere from -3000 to 3000: few or many logits near the highest."""
+    rng = np.random.default_rng(seed)
+    off, rise = rng.choice([-3000, -400, -376, -100, -24.25, 0, 100, 400, 776, 3000], n), rng.choice([2, 5, 5.6, 8, 20, 40, 41, 41.5, 42, 44, 50, 60], n)
+    x = off[:, None] + rng.standard_normal((n, vocab)) * 0.1
+    x[:, 1024:2048] += rise[:, None]
+    for i in range(n):
+        k = (1, 17, 1000)[i % 3]
+        x[i, 2048:2048 + k] += rise[i] + rng.uniform(0, 6)
+        x[i, 3000] += rise[i] + rng.uniform(0, 8)
+        if i % 5 == 0:
+            x[i, 3500] += 2 * rise[i]
+    x[0] = -np.inf                              # 776, many at 816, the highest 820: the reference moves by 44 while the sum is all of the others'
+    x[0, :1024], x[0, 1024:2024], x[0, 2048] = 776, 816, 820
+    return torch.tensor(x, dtype=torch.float32, device=DEV).to(torch.bfloat16)
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab", [(1200, 4096), (1100, 8200), (20, 4096)])
+def test_select_sums_up_rows_that_rise(n, vocab):
+    """One beam a prompt, whose score tells its row's sum; more than 1024 rows: a row is one wavefront's, whose reference moves."""
+    logits = _rising_rows(n, vocab, n)
+    _check_select(logits, 1, [0.0] * n, [0] * n, [0] * n, np.zeros((n, 0), np.int32), -1, 0.0)

@@ -13,7 +13,7 @@ namespace {
 constexpr uint32_t THREADS = 256, WAVES = THREADS / 64, LANE = 16, TILE = 64 * LANE;      // logits of a lane and of a wavefront at a time
 constexpr uint32_t MAX_PARTS = 64, MAX_SPAN = 65536;          // a logit's place in a part is 16 bits
 constexpr double LN2 = 0.693147180559945309417;
-constexpr float LOG2E = 1.44269504088896f, HIGHEST = 8.0f;
+constexpr float LOG2E = 1.44269504088896f, HIGHEST = 8.0f, LARGE = 32768.0f;
 
 // Highest and lowest value of the wavefront's lanes.
 template <int CTRL, int ROWS>
@@ -89,7 +89,9 @@ __device__ __forceinline__ bool last_of(uint32_t* counter, uint32_t all, uint32_
 // no result.  What is off, of a term near the maximum: log2(e) as a float (1.3e-8 of x - m), the product's rounding (2^-22 where the exponent is 4 to 8, 2.8 x
 // 2^-24 of the term), the exponential's (one ulp), a lane's sum of 16; at most some 16 x 2^-24, far less for a sum over many, whose
 // terms' roundings differ.  (With HIGHEST 60 the product's rounding is 2^-19 of a term, and 480 rows of 99991 or 4 of 32000 take as long.)
-//   A tile whose sum or maximum tells of a NaN, an infinity or a number beyond 1e30 is gone through again, logit by logit.
+//   A tile whose sum or maximum tells of a NaN or an infinity is gone through again, logit by logit; so is every tile while the reference is LARGE:
+// x log2(e) and c are rounded to more than 2^-9 there (to more than the exponents that there are, from 2^31 on), but the next lower logit is 128 less, so that
+// a term is 2^((x - m) log2(e)), 1 or as good as 0, and a sum is forgotten at a new reference.
 //   The best tokens: the width-th highest of the lanes' maxima is a bound that no lane with a lower maximum reaches, which leaves `width`
 // lanes (more where there are ties); the tiles of theirs whose maximum reaches it, too, are read again and compared.  (Looked for in every tile, as the row goes by, they cost
 // twice the instructions of all the rest: 96 x 5 rows of 99991 65 us, so 41; all pieces of those lanes, 41, their best tiles' only, 38.)
@@ -129,7 +131,7 @@ __device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v
   Part p;
   if (!counts()) return p;
   float m = 0.0f, c = 0.0f, lane_top = -INFINITY;     // m: what c stands for
-  bool some = false, huge = false;
+  bool some = false, large = false;
   auto any = [](bool b) { return __ballot(b) != 0; };
   // Dwords d[0 .. n - 1] of two logits each.
   auto add = [&](const uint32_t* d, auto n) {
@@ -142,14 +144,14 @@ __device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v
       float m2 = some ? fmaxf(m, tile_top) : tile_top;
       m2 = unordered(wave_top(ordered(m2)));
       const float c2 = m2 * LOG2E;
-      const bool huge2 = !(fabsf(m2) < 1e30f);
-      p.sum = some && !huge && !huge2 ? p.sum * exp2((double)c - (double)c2) : 0.0;      // (next to 1e30 a step of a logit is all there is)
+      const bool large2 = !(fabsf(m2) < LARGE);
+      p.sum = some && !large && !large2 ? p.sum * exp2((double)c - (double)c2) : 0.0;
       m = m2; c = c2; some = true;
-      huge = huge2;
+      large = large2;
     };
-    bool odd = huge || any(fabsf(top) > 1e30f && top != -INFINITY);
+    bool odd = any(top == INFINITY);
+    if (!odd) { refer_to(top); odd = large; }
     if (!odd) {
-      refer_to(top);
       float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
       for (uint32_t u = 0; u < N; ++u) {
@@ -173,7 +175,7 @@ __device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v
       for (uint32_t u = 0; u < 2 * N; ++u) {
         const uint32_t o = order_of(d[u / 2] >> 16 * (u & 1) & 0xffffu);
         const float v = value_of(o);
-        s += o ? __builtin_amdgcn_exp2f(huge ? (v - m) * LOG2E : __builtin_fmaf(v, LOG2E, -c)) : 0.0f;
+        s += o ? __builtin_amdgcn_exp2f(large ? (v - m) * LOG2E : __builtin_fmaf(v, LOG2E, -c)) : 0.0f;
       }
       p.sum += (double)s;
     }
@@ -191,7 +193,7 @@ __device__ __forceinline__ Part part_of(const bf16_t* x, uint32_t v0, uint32_t v
     tops[i * 64u + lane] = (uint16_t)(__float_as_uint(add(t.d, std::integral_constant<uint32_t, LANE / 2>{})) >> 16);
   }
   if (before + behind) add(&edge, std::integral_constant<uint32_t, 1>{});
-  p.ref = huge ? (double)m : (double)m + ((double)c - (double)m * (double)LOG2E) * LN2;        // 2^(x LOG2E - c) stands for e^(x - m) 2^(m LOG2E - c)
+  p.ref = large ? (double)m : (double)m + ((double)c - (double)m * (double)LOG2E) * LN2;        // 2^(x LOG2E - c) stands for e^(x - m) 2^(m LOG2E - c)
   p.sum = wave_total(p.sum);
 
   // ---- the best

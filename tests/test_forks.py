@@ -1237,3 +1237,29 @@ def test_select_sums_up_rows_that_rise(n, vocab):
     """One beam a prompt, whose score tells its row's sum; more than 1024 rows: a row is one wavefront's, whose reference moves."""
     logits = _rising_rows(n, vocab, n)
     _check_select(logits, 1, [0.0] * n, [0] * n, [0] * n, np.zeros((n, 0), np.int32), -1, 0.0)
+
+
+@gpu
+@pytest.mark.parametrize("n,vocab", [(1100, 4096), (12, 40000), (1100, 9)])
+def test_select_of_large_logits(n, vocab):
+    """From 2^13 to the largest number, of either sign, at the beginning, late, everywhere, and as masks."""
+    rng = np.random.default_rng(n + vocab)
+    x = rng.standard_normal((n, vocab))
+    for i in range(n):
+        v = 2.0 ** rng.uniform(13, 127.9)
+        at = [0, vocab - 1, vocab // 2, rng.integers(0, vocab)][i % 4]
+        kind = i % 6
+        if kind == 0:
+            x[i, at] = v
+        elif kind == 1:
+            x[i, at:at + 3] = [v, v, v * 0.75][:len(x[i, at:at + 3])]
+        elif kind == 2:
+            x[i] = -v * (1 + rng.random(vocab))
+        elif kind == 3:
+            x[i, rng.random(vocab) < 0.5] = -v            # a mask
+        elif kind == 4:
+            x[i, :-1] = -3.3895e38                        # all but one
+        else:
+            x[i] *= v / 8
+    x = np.clip(x, -3.3895e38, 3.3895e38)
+    _check_select(torch.tensor(x, dtype=torch.float32, device=DEV).to(torch.bfloat16), 1, [0.0] * n, [0] * n, [0] * n, np.zeros((n, 0), np.int32), -1, 0.0)

@@ -223,15 +223,19 @@ class Answers:
         i32 = dict(dtype=torch.int32, device=dev)
         self.tables = torch.full((n_seq, max_blocks or n_blocks), -1, **i32)
         self.free = torch.arange(n_blocks, **i32)
-        self.state = torch.tensor([n_blocks, 0, 0, 0], **i32)
-        self.lengths, self.starts = torch.zeros(n_seq, **i32), torch.zeros(n_seq + 1, **i32)
+        n_groups = 0 if width is None else -(-n_seq // width)
+        # what a step that is refused leaves as it was, in one tensor: the state, lengths, what the groups share
+        at = 4 + (n_seq + 3) // 4 * 4
+        self._kept_whole = torch.zeros(at + n_groups, **i32)
+        self.state, self.lengths = self._kept_whole[:4], self._kept_whole[4:4 + n_seq]
+        self.state[0] = n_blocks
+        self.starts = torch.zeros(n_seq + 1, **i32)
         self.logits = torch.zeros(n_seq, self.vocab, dtype=torch.bfloat16, device=dev)
         self._kept = [(torch.zeros(0, **i32), torch.zeros(0, **i32), torch.zeros(0, dtype=torch.uint8, device=dev))]
         self.group_starts = self.shared = None
         if width is not None:
-            n_groups = -(-n_seq // width)
             self.group_starts = torch.arange(n_groups + 1, **i32).mul_(width).clamp_(max=n_seq)
-            self.shared = torch.zeros(n_groups, **i32)
+            self.shared = self._kept_whole[at:]
         self.forked = width is not None
         self._own = torch.arange(n_seq, **i32)
         self._make_fork_room()
@@ -254,13 +258,20 @@ class Answers:
         it ends and gives its blocks back).  A step without tokens ends sequences and runs no model.  Returns the logits bf16 [n_seq, vocab]
         of the last new tokens: `logits`, the same buffer every step, which the next one overwrites (a graph that holds the step writes it, too;
         keep a copy of what is to outlive a step).  Whether the step could be planned is in state[2], where the caller may look (not QZO_OK: nothing has
-        changed, the logits are zeros)."""
-        if self.forked:                         # what ends may share its blocks: they are given back by a fork
-            with torch.cuda.stream(stream):
-                parents = torch.where(added < 0, -1, self._own)
-                added = added.clamp(min=0)
-            self.fork(parents, stream)
-        return self._add(tokens, added, stream)
+        changed, no sequence has ended, the logits are zeros)."""
+        if not self.forked:
+            return self._add(tokens, added, stream)
+        with torch.cuda.stream(stream):         # what ends may share its blocks: they are given back by a fork
+            before = self._kept_whole.clone()
+            parents = torch.where(added < 0, -1, self._own)
+        self.fork(parents, stream)
+        with torch.cuda.stream(stream):         # none is negative; but where the fork was refused those that were still are, and the plan is refused as well
+            added = torch.maximum(added, self.state[2:3])
+        self._add(tokens, added, stream)
+        with torch.cuda.stream(stream):         # a plan that is refused takes the fork back: no more of the free list's valid part than its end was written
+            before[1:4] = self.state[1:4]
+            torch.where(self.state[2:3] == 0, self._kept_whole, before, out=self._kept_whole)
+        return self.logits
 
     def _add(self, tokens, added, stream=None):
         slots, positions, ws = self.rows(max(1, tokens.numel()), stream)

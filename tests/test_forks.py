@@ -1263,3 +1263,71 @@ def test_select_of_large_logits(n, vocab):
             x[i] *= v / 8
     x = np.clip(x, -3.3895e38, 3.3895e38)
     _check_select(torch.tensor(x, dtype=torch.float32, device=DEV).to(torch.bfloat16), 1, [0.0] * n, [0] * n, [0] * n, np.zeros((n, 0), np.int32), -1, 0.0)
+
+
+# ------------------------------------------------------------------ steps that cannot be made ----
+@gpu
+@pytest.mark.parametrize("width", [None, 2])
+def test_a_refused_step_ends_nobody(width):
+    """Sequences that share blocks are ended by a fork ahead of the plan: a plan that is refused takes that back, and a refused fork refuses the step."""
+    m = _model("tiny", "int4")
+    text = torch.randint(0, 1024, (400,), generator=torch.Generator().manual_seed(10), dtype=torch.int32).to(DEV)
+    runs = []
+    for refused in (False, True):
+        a = Answers(m, n_seq=5, n_blocks=14, block=16, max_blocks=10, width=width)
+        a.add(text[:70].contiguous(), _i32([40, 0, 30, 0, 0]))
+        a.fork(_i32([0, 0, 2, 2, 2]))
+        a.add(text[:5].contiguous(), _i32([1] * 5))
+        found = []
+        for turn in range(3):
+            if refused:
+                kept = lambda: [x.clone() for x in (a.lengths, a.free[:int(a.state[0])], a.tables, a.state[:1])] + ([] if width is None else [a.shared.clone()])
+                before = kept()
+                for added, rows, status in [([-1, 1, 200, 0, 0], 201, qb.QZO_ERR_SHAPE), ([0, 0, 118, -1, 1], 119, qb.QZO_ERR_WORKSPACE), ([-1, 0, 9, -2, 1], 9, qb.QZO_ERR_SHAPE),
+                                            ([-1, 0, 0, -1, 1], 0, qb.QZO_ERR_SHAPE)]:
+                    out = a.add(text[:rows].contiguous(), _i32(added))
+                    assert a.state.tolist()[1:] == [0, status, 0] and (out == 0).all()
+                    assert all(torch.equal(x, y) for x, y in zip(before, kept()))
+                n_free = int(a.state[0])
+                a.state[0] = 14                      # more than there can be, so that nothing can be given back
+                before[1], before[3] = a.free[:14].clone(), a.state[:1].clone()
+                a.add(text[:2].contiguous(), _i32([-1, -1, -1, 1, 1]))
+                assert a.state.tolist() == [14, 0, qb.QZO_ERR_ARG, 0] and all(torch.equal(x, y) for x, y in zip(before, kept()))
+                a.state[0] = n_free
+            found.append(a.add(text[:6].contiguous(), _i32([1, -1 if turn == 1 else 1, 1, 3 if turn == 1 else 2, 1 if turn < 2 else -1])).clone())
+            assert int(a.state[2]) == 0
+            found.append(a.lengths.clone())
+            _check_cache(a)
+        runs.append(found)
+    assert all(torch.equal(x, y) for x, y in zip(*runs))
+
+
+@gpu
+def test_captured_steps_of_which_some_are_refused():
+    """The step is the same graph, whatever it is given: replayed with counts that fit and that do not, eager work in between."""
+    m = _model("tiny", "int4")
+    text = torch.randint(0, 1024, (400,), generator=torch.Generator().manual_seed(11), dtype=torch.int32).to(DEV)
+    counts = [[1, 1, 1, 1], [-1, 1, 1, 5], [1, 2, -1, 1], [-1, -1, 4, 0], [0, 4, 0, 0], [-1, 1, 2, 1]]
+    runs = []
+    for captured in (False, True):
+        a = Answers(m, n_seq=4, n_blocks=12, block=16, max_blocks=6, width=4)
+        tokens, added = torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+        a.add(text[:60].contiguous(), _i32([60, 0, 0, 0]))
+        a.fork(_i32([0] * 4))
+        torch.cuda.synchronize()
+        if captured:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                a.add(tokens, added)
+        found = []
+        for i in range(12):
+            added.copy_(_i32(counts[i % 6]))
+            tokens.copy_(text[4 * i:4 * i + 4])
+            g.replay() if captured else a.add(tokens, added)
+            torch.cuda.synchronize()
+            m.forward_loss(text.view(1, -1)[:, :40].contiguous(), 1, 1e-3, 1)
+            found += [a.logits.clone(), a.lengths.clone(), a.state.clone(), a.shared.clone(), a.tables.clone()]
+            _check_cache(a)
+        assert {int(x[2]) for x in found[2::5]} >= {0, qb.QZO_ERR_SHAPE}
+        runs.append(found)
+    assert all(torch.equal(x, y) for x, y in zip(*runs))

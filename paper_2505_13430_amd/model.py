@@ -209,10 +209,13 @@ class DeviceModel:
 class Answers:
     """Sequences that a DeviceModel continues: the pools of all layers, block tables, the free list, the lengths.  One call of `add`
     per step; everything stays on the device.  width: sequences i * width .. (i + 1) * width - 1 are a group that may come to share what
-    they begin with (`fork`), and attend to that together; the last group may be smaller."""
+    they begin with (`fork`), and attend to that together; the last group may be smaller.  At most 2048 groups, but any number of one sequence each,
+    which attend by themselves."""
 
     def __init__(self, model: DeviceModel, n_seq: int, n_blocks: int, block: int = 32, max_blocks: int | None = None, e4m3: bool = False,
                  k_scale=None, v_scale=None, width: int | None = None):
+        if width is not None and width > 1 and -(-n_seq // width) > qb.MAX_GROUPS:
+            raise ValueError(f"groups of {width} of {n_seq} sequences are more than {qb.MAX_GROUPS}")
         sh, dev = model.shape, model.scales.device
         dh = sh["d_model"] // sh["n_heads"]
         self.model, self.block, self.vocab = model, block, sh["vocab"]
@@ -236,7 +239,7 @@ class Answers:
         if width is not None:
             self.group_starts = torch.arange(n_groups + 1, **i32).mul_(width).clamp_(max=n_seq)
             self.shared = self._kept_whole[at:]
-        self.forked = width is not None
+        self.forked, self.together = width is not None, width is not None and width > 1
         self._own = torch.arange(n_seq, **i32)
         self._make_fork_room()
 
@@ -244,7 +247,7 @@ class Answers:
         """Slots, positions and workspace of steps of that many rows, from buffers that double as they are outgrown; the earlier ones
         are kept for the graphs that were captured with them.  New ones are made on the stream that uses them."""
         slots, positions, ws = self._kept[-1]
-        need = qb.qzo_answer_workspace_bytes(self.model.handle, n_tokens, len(self.lengths), self.shared is not None)
+        need = qb.qzo_answer_workspace_bytes(self.model.handle, n_tokens, len(self.lengths), self.together)
         if slots.numel() < n_tokens or ws.numel() < need:
             dev, n = self.free.device, max(n_tokens, 2 * slots.numel())
             with torch.cuda.stream(stream):
@@ -283,7 +286,7 @@ class Answers:
                           self.state, stream)
         if tokens.numel():
             qb.qzo_answer(self.model.handle, tokens, self.cache, self.tables, self.lengths, self.starts, slots, positions, ws, self.logits, stream,
-                          group_starts=self.group_starts, shared=self.shared)
+                          group_starts=self.group_starts if self.together else None, shared=self.shared if self.together else None)
         return self.logits
 
     def _make_fork_room(self):

@@ -1107,7 +1107,7 @@ def _on_the_host(monkeypatch, events):
     monkeypatch.setattr(qb, "qzo_answer_workspace_bytes", lambda *a: 256)
     monkeypatch.setattr(torch.cuda, "synchronize", note("synchronize"))
     model = types.SimpleNamespace(shape=dict(d_model=128, n_heads=2, vocab=8, n_layers=1), scales=torch.zeros(1), handle=None)
-    return lambda **k: Answers(model, n_seq=8, n_blocks=2100, block=16, **k)
+    return lambda **k: Answers(model, **dict(dict(n_seq=8, n_blocks=2100, block=16), **k))
 
 
 @pytest.mark.parametrize("width", [None, 4])
@@ -1331,3 +1331,37 @@ def test_captured_steps_of_which_some_are_refused():
         assert {int(x[2]) for x in found[2::5]} >= {0, qb.QZO_ERR_SHAPE}
         runs.append(found)
     assert all(torch.equal(x, y) for x, y in zip(*runs))
+
+
+# ------------------------------------------------------------------ how many groups there may be ----
+def test_more_groups_than_attend_together_are_refused(monkeypatch):
+    """When the pools are made, not in a step that has planned already.  Groups of one attend by themselves."""
+    make = _on_the_host(monkeypatch, [])
+    for n, width in ((4097, 2), (8192, 3), (2049 * 3, 3)):
+        with pytest.raises(ValueError):
+            make(n_seq=n, n_blocks=4, width=width)
+    for n, width in ((4096, 2), (2048 * 3, 3), (8192, 4)):
+        assert make(n_seq=n, n_blocks=4, width=width).shared.numel() == -(-n // width) <= qb.MAX_GROUPS
+    seen = []
+    monkeypatch.setattr(qb, "qzo_answer", lambda *a, group_starts, shared: seen.append((group_starts, shared)))
+    for width in (1, 2):
+        a = make(n_seq=4096, n_blocks=4, width=width)
+        a.add(torch.zeros(3, dtype=torch.int32), torch.zeros(4096, dtype=torch.int32))
+        assert (a.group_starts.numel(), a.shared.numel()) == (4096 // width + 1, 4096 // width)
+    assert seen[0] == (None, None) and seen[1] == (a.group_starts, a.shared)
+
+
+@gpu
+def test_beams_of_more_prompts_than_groups():
+    """2100 prompts with one beam each: greedy continuations, every step's tokens those of the highest logits."""
+    m, n = _model("tiny", "int4"), 2100
+    b = Beams(m, n, 1, n_blocks=2 * n, max_new=4, block=16, max_blocks=2)
+    tokens = torch.randint(0, m.shape["vocab"], (3 * n,), generator=torch.Generator().manual_seed(12), dtype=torch.int32).to(DEV)
+    b.start(tokens, _i32([3] * n))
+    for i in range(3):
+        logits = b.answers.logits.float()
+        assert torch.equal(logits.gather(1, b.tokens.long()[:, None])[:, 0], logits.max(1).values) and int(b.failed) == 0
+        b.step()
+    _check_cache(b.answers)
+    with pytest.raises(ValueError):
+        Beams(m, n, 2, n_blocks=n, max_new=4, block=16, max_blocks=2)

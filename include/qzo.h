@@ -407,8 +407,8 @@ qzo_status qzo_qk_norm_rope(const void* qkv_dev, uint64_t ld_qkv, uint32_t n_tok
  * the one new token of sequence i.  A row sees the positions of its sequence up to its own:
  *   out[row, h] = sum_k p_k v_k / sum_k p_k,  p_k = exp(scale * q . k - max),  out_dev bf16, rows ld_out elements apart.
  * One pass over the cache with the running maximum and sum (fp32).  p meets v as two bf16 numbers, 2^-16 of it at most missing; but
- * for prompts, and for heads of 128 or an e4m3 cache with more than eight columns (new tokens of a sequence times the query
- * heads of a key head), it is rounded to one, 2^-8.  The sum is that of what meets v.  The sequences are cut into pieces that fill the chip and joined in
+ * for prompts, for heads of 128 or an e4m3 cache with more than eight columns (new tokens of a sequence times the query heads
+ * of a key head), and for heads of 64 in e4m3 where the sequences have 24 columns or more on average, it is rounded to one, 2^-8.  The sum is that of what meets v.  The sequences are cut into pieces that fill the chip and joined in
  * order: the same call gives the same bits.  A row that sees nothing (length 0) is set to zero; rows behind the last sequence's and not named by starts stay as they are.  Keys that a row does not see
  * reach its output in no way, NaN and infinities among them; nor do positions whose block id lies outside the pool (they
  * count as unseen), or positions beyond max_blocks * block.  A score of -infinity counts as unseen.
@@ -516,8 +516,9 @@ qzo_status qzo_beam_select(const void* logits_dev, uint64_t ld_logits, uint32_t 
  * whose new tokens begin before that, need not agree).  They are read once for all the group's rows, through the table of the first sequence that has
  * them before its new tokens; every sequence's other positions through its own.  A sequence whose new tokens begin before the shared
  * part ends reads all of its positions itself.  Otherwise results, limits and roundings are
- * those of qzo_paged_attention (p meets v as two bf16 numbers where the columns of the group, or of the sequence, are as few as it says; in
- * groups of more than 64 columns a key head on average, new tokens times query heads of a key head, the common keys' p is rounded once).
+ * those of qzo_paged_attention.  p meets v as two bf16 numbers or as one by the same rule, where the columns of the common keys are the group's, those of a
+ * sequence's own keys the sequence's, and the average is the groups'; in groups of more than 64 columns on average the common keys' p is always
+ * rounded to one, and the average of the own keys is the sequences'.  So a sequence whose p is two numbers by itself may have one in a group.
  * scratch_dev: qzo_paged_attention_shared_scratch_bytes bytes, kept as qzo_paged_attention's (its first 2048 bytes zero).  n_groups 1 .. 2048.
  */
 qzo_status qzo_paged_attention_shared_scratch_bytes(uint32_t n_rows, uint32_t n_seq, uint32_t q_heads, uint32_t kv_heads,

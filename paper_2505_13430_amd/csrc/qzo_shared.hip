@@ -24,8 +24,8 @@ namespace {
 // columns, a later one, with which its workgroup begins, in that workgroup's place; join_shares_kernel adds them up.
 // An accumulator that is NaN, by a value whose weight is 0, say: the column is gone through again, one key a thread, without those.
 // 64 sequences behind 32768 tokens, 64 heads on 8 of 128 (512 columns a key head, 69 GFLOP): 90 to 107 us, 650 to 770 TFLOP/s; matrix pipe busy 29 %
-// of the SIMDs' time, vector pipe 37 %, no bank conflicts: two wavefronts a SIMD (128 accumulators and the values of a step leave no
-// registers for more), whose steps of loads from the LDS, products and weights overlap little.  The call 121 us, with paged_attention_kernel for this 217.
+// of the SIMDs' time, vector pipe 37 %, no bank conflicts: two wavefronts a SIMD (64 accumulators, queries, scores, the values of a step and what is on
+// its way: up to 255 registers with heads of 128), whose steps of loads from the LDS, products and weights overlap little.  The call 121 us, with paged_attention_kernel for this 217.
 // 64 columns a wavefront would halve the LDS reads and do not fit (spills, 278 us for the call); priorities, four wavefronts a workgroup and a second
 // step in registers gave nothing.  6 x 12 candidates of 9 tokens in e4m3, 40 heads on 8 of 64: 49 us (the call 82, otherwise 103), 1.2 to 2 us a step of 64 keys, most of them pieces' beginnings and ends.
 // Weights meet the values rounded once to bf16: error against 64 bits as that of prompts.
@@ -452,7 +452,10 @@ __global__ __launch_bounds__(256) void join_shares_kernel(SharedArgs a, bool e4m
   *reinterpret_cast<uint2*>(to) = j.l == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(j.o[0] * inv, j.o[1] * inv), pack_bf16x2(j.o[2] * inv, j.o[3] * inv));
 }
 
-// Columns that a group has on average from which on its common keys are common_keys_kernel's.
+// Columns that a group has on average from which on its common keys are common_keys_kernel's.  The call with paged_attention_kernel for them / with
+// common_keys_kernel, us, 32 columns, 64, 96, 128; heads of 64: one group behind 1000 tokens 17 / 22, 17 / 23, 29 / 23, 32 / 24, one behind 32768 41 / 46, 41 / 47,
+// 84 / 48, 154 / 49, 40 behind 1000 50 / 62, 82 / 74, 129 / 84, 165 / 96; heads of 128: 19 / 24, 19 / 25, 50 / 27, 56 / 28, then 66 / 51, 84 / 53, 153 / 56, 296 / 59,
+// then 91 / 76, 152 / 96, 235 / 119, 242 / 141; in e4m3 much the same.  More than 64 columns always gain; fewer do where there are many keys, which the host does not know.
 constexpr uint32_t CK_FROM = 65;
 bool many_columns(uint32_t n_rows, uint32_t group, uint32_t n_groups) { return (uint64_t)n_rows * group >= (uint64_t)CK_FROM * n_groups; }
 uint32_t shared_part_columns(uint32_t n_rows, uint32_t group) {

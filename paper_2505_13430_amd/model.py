@@ -313,7 +313,7 @@ class Answers:
     def resize(self, n_blocks: int):
         """Pools of another number of blocks: memory given back to a training step between answers, or more of it.  Waits for the device, before (steps
         may be under way on any stream) and behind what it does; what was captured with the old pools is no longer valid.  ValueError: the
-        sequences hold more blocks than that (nothing has changed but their places)."""
+        sequences hold more blocks than that (nothing has changed but their places).  Where memory runs out for the new pools, the old ones are gone."""
         torch.cuda.synchronize(self.free.device)
         self.compact()
         free, had = int(self.state[0]), self.free.numel()
